@@ -50,7 +50,8 @@ enum {
   HSD_STATUS_POOL_EXHAUSTED = 1, /* not enough free KV blocks for the speculative append */
   HSD_STATUS_TABLE_OVERFLOW = 2, /* seq_len + q_len exceeds max_blocks_per_seq * 16       */
   HSD_STATUS_BAD_SLOT = 4,       /* a seq_slot entry lies outside [0, n_slots)           */
-  HSD_STATUS_BAD_TREE = 8        /* a tree_end / tree_depth entry was not a valid packed tree */
+  HSD_STATUS_BAD_TREE = 8,       /* a tree_end / tree_depth entry was not a valid packed tree */
+  HSD_STATUS_NOT_FINITE = 16     /* a NaN or an infinity went into an 8-bit cache (hsd_kv_quant_append) */
 };
 
 enum { HSD_KV_BLOCK_TOKENS = 16, HSD_HEAD_DIM = 64, HSD_MAX_SEQ = 4096 };
@@ -293,6 +294,73 @@ void hsd_drafts_destroy(hsd_drafts *drafts);
 int hsd_drafts_tree(const hsd_drafts *drafts, const int64_t *window, int32_t n_window, int64_t pending, int64_t max_packed,
                     int32_t capacity, int32_t *tokens, int32_t *tree_end, int32_t *tree_depth, int32_t *n_rows);
 int hsd_tree_path(const int32_t *tokens, const int32_t *tree_end, int32_t n_rows, int32_t stop, int32_t alpha, int32_t *path);
+
+/* ---------------------------------------------------------------------------------------------------------------
+ * Operators of a serving step around a cache that is held in 8 bits.  They need no context: a caller with a decoder of its
+ * own places rows, appends keys and values, attends and scores tokens with them.  The conventions at the top hold; nothing is
+ * kept between calls; the kernels run on the current device, which has to be the tensors' and the stream's. */
+
+/* Places new rows in pages.  Of `batch` are read: n_seq, total_q, max_blocks_per_seq, n_slots, cu_q (cu_q[n_seq] = total_q;
+ * a sequence may have no rows), seq_slot, seq_len, block_table, status; of `pool`: n_blocks, free_list, free_count (the page
+ * pointers may be NULL).  For every sequence in order, block-table entries that cover positions seq_len .. seq_len + q_len - 1
+ * and hold no block (-1) take one from the free stack; row_slot[r] = 16 * block + position % 16 is then the place of packed row
+ * r in every layer, -1 where there is none (see HSD_STATUS_*; with too few free blocks none is taken), and row_pos[r] its
+ * position.  row_slot, row_pos: dev [total_q]; row_pos may be NULL.  seq_len is not modified: see hsd_kv_commit_rows. */
+int hsd_kv_reserve(void *stream, const hsd_kv_pool *pool, const hsd_batch *batch, int32_t *row_slot, int32_t *row_pos);
+
+/* hsd_kv_commit_rollback for callers without a context: seq_len += 1 + accept_len[s] where accept_len[s] >= 0, nothing where it
+ * is negative, and every row if accept_len is NULL; blocks beyond the new length go back to the pool.  Of `batch` are read what
+ * hsd_kv_reserve reads (status excepted) and accept_len. */
+int hsd_kv_commit_rows(void *stream, const hsd_kv_pool *pool, const hsd_batch *batch);
+
+/* Pages of one layer in 8 bits: e4m3 codes, and for each block and kv head one power-of-two scale of its keys and one of its
+ * values, value = code * scale.  Block ids are those of a pool's free list.  A page's contents are written by
+ * hsd_kv_quant_append and read by the calls below; the first slot of a page has to be written before a later one counts, as
+ * sequences that grow from a block's start do.  k_codes and v_codes are 16-byte aligned. */
+typedef struct hsd_kv_quant {
+  void *k_codes, *v_codes;   /* dev [n_blocks][n_kv_heads][1024] bytes */
+  float *k_scale, *v_scale;  /* dev [n_blocks][n_kv_heads]             */
+  int32_t n_blocks, n_kv_heads;
+} hsd_kv_quant;
+
+/* Keys and values of n_rows rows into the pages at row_slot (as hsd_kv_reserve gives them; a row with a negative or too large
+ * slot is left out).  k, v: dev [n_rows][n_kv_heads][64] in dtype, rows k_stride / v_stride elements apart, aligned to their
+ * elements.  Rows that share a block have to follow one another in row_slot, in the order of their slots; a block
+ * may not be named twice apart from that.  Slots of a touched block before its first new row keep their values, slots behind
+ * its last one are cleared.  The scale is the smallest 2^e, -100 <= e <= 119, with 448 * 2^e >= every magnitude that the page
+ * then holds; values round to the nearest code, ties to even.  Infinities and magnitudes above 448 * 2^119 are held
+ * as that, NaN as 0; NaN and infinities set HSD_STATUS_NOT_FINITE in *status (dev [1], or NULL). */
+int hsd_kv_quant_append(void *stream, const hsd_kv_quant *kv, int32_t n_rows, const int32_t *row_slot, int32_t dtype,
+                        const void *k, const void *v, int64_t k_stride, int64_t v_stride, int32_t *status);
+
+/* The values that the pages hold for n_rows slots (any slots in any order; 0 for a negative or too large one), to k and v, laid
+ * out as for append.  Exact in both types. */
+int hsd_kv_quant_read(void *stream, const hsd_kv_quant *kv, int32_t n_rows, const int32_t *row_slot, int32_t dtype, void *k,
+                      void *v, int64_t k_stride, int64_t v_stride);
+
+/* Attention over the pages: row i of sequence s sees positions 0 .. seq_len + i through block_table (its own rows appended
+ * before); query head h reads kv head h / (n_q_heads / n_kv_heads).  Of `batch` are read what hsd_kv_reserve reads (status
+ * excepted).  q, out: dev [total_q][n_q_heads][64] in dtype, rows q_stride / out_stride elements apart, aligned to their
+ * elements; softmax_scale multiplies the products (0.125 for 64 dimensions).  A position whose table entry holds no valid block is left
+ * out; a row that sees none becomes 0.  Softmax and sums in fp32; bf16 models round the probabilities to bf16 for the product
+ * with the values (and divide by the sum of the rounded ones).  The same call gives the same bits; another batch around a row may
+ * change how its keys are split and with it the last bits.  workspace: hsd_kv_quant_attention_bytes(kv, batch, n_q_heads) bytes, 256-byte aligned. */
+size_t hsd_kv_quant_attention_bytes(const hsd_kv_quant *kv, const hsd_batch *batch, int32_t n_q_heads);
+int hsd_kv_quant_attention(void *stream, const hsd_kv_quant *kv, const hsd_batch *batch, int32_t n_q_heads, int32_t dtype,
+                           float softmax_scale, const void *q, int64_t q_stride, void *out, int64_t out_stride,
+                           void *workspace, size_t ws_bytes);
+
+/* Scores of given tokens.  Row r of logits (dev [n_rows][vocab] in dtype, row_stride elements apart) is a distribution
+ * softmax(logits[r]): logprob[r] = log p(tokens[r]) (-inf for an id outside the vocabulary), entropy[r] in nats, and the n_top
+ * most probable tokens, largest first, the lower id first among equal logits: top_ids, top_logprobs dev [n_rows][n_top].
+ * A logit of -inf is a probability of 0 and never an alternative (places left over hold id -1 and -inf); a row without any other
+ * logit has logprob -inf and entropy 0.  With a NaN or +inf among its logits a row's logprob (of a token inside the vocabulary), entropy and top_logprobs are NaN,
+ * and its alternatives are taken from the logits that are numbers.  0 <= n_top <= HSD_MAX_TOP.  workspace: hsd_token_logprobs_bytes bytes, 256-byte aligned. */
+enum { HSD_MAX_TOP = 32 };
+size_t hsd_token_logprobs_bytes(int32_t n_rows, int32_t vocab, int32_t n_top);
+int hsd_token_logprobs(void *stream, int32_t n_rows, int32_t vocab, int32_t dtype, const void *logits, int64_t row_stride,
+                       const int32_t *tokens, float *logprob, float *entropy, int32_t n_top, int32_t *top_ids,
+                       float *top_logprobs, void *workspace, size_t ws_bytes);
 
 #ifdef __cplusplus
 }

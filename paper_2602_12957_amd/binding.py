@@ -19,8 +19,8 @@ lib = C.CDLL(LIB_PATH)
 
 HSD_OK, HSD_EINVAL, HSD_ENOSPC, HSD_ERANGE, HSD_EARCH, HSD_ENODEV, HSD_EHIP = 0, -1, -2, -3, -4, -5, -6
 HSD_FP32, HSD_BF16 = 0, 1
-HSD_STATUS_POOL_EXHAUSTED, HSD_STATUS_TABLE_OVERFLOW, HSD_STATUS_BAD_SLOT, HSD_STATUS_BAD_TREE = 1, 2, 4, 8
-HSD_KV_BLOCK_TOKENS, HSD_HEAD_DIM, HSD_MAX_SEQ = 16, 64, 4096
+HSD_STATUS_POOL_EXHAUSTED, HSD_STATUS_TABLE_OVERFLOW, HSD_STATUS_BAD_SLOT, HSD_STATUS_BAD_TREE, HSD_STATUS_NOT_FINITE = 1, 2, 4, 8, 16
+HSD_KV_BLOCK_TOKENS, HSD_HEAD_DIM, HSD_MAX_SEQ, HSD_MAX_TOP = 16, 64, 4096, 32
 
 i32, f32, vp = C.c_int32, C.c_float, C.c_void_p
 
@@ -47,6 +47,10 @@ class hsd_batch(C.Structure):
                 ("block_table", vp), ("argmax", vp), ("top2_margin", vp), ("accept_len", vp), ("bonus", vp),
                 ("status", vp), ("logits_dump", vp), ("dump_rows", vp), ("n_dump", i32),
                 ("log_tau", f32), ("draft_gap", vp), ("tree_end", vp), ("tree_depth", vp), ("stop_row", vp)]
+
+
+class hsd_kv_quant(C.Structure):
+    _fields_ = [("k_codes", vp), ("v_codes", vp), ("k_scale", vp), ("v_scale", vp), ("n_blocks", i32), ("n_kv_heads", i32)]
 
 
 _P = C.POINTER
@@ -82,11 +86,22 @@ HSD_PROBE_MFMA, HSD_PROBE_LOAD_REG, HSD_PROBE_LOAD_LDS, HSD_PROBE_LDS_READ = ran
 
 EXPORTS = ["hsd_probe_launch", "hsd_verify_region_batch_noalloc", "hsd_noalloc_scratch_bytes", "hsd_debug_set", "hsd_profile_enable", "hsd_profile_read", "hsd_status_string", "hsd_validate_model", "hsd_validate_batch", "hsd_create", "hsd_destroy",
            "hsd_workspace_bytes", "hsd_kv_pool_init", "hsd_verify_region_batch", "hsd_verify_page",
-           "hsd_kv_commit_rollback", "hsd_prefill", "hsd_drafts_create", "hsd_drafts_destroy", "hsd_drafts_tree", "hsd_tree_path"]
+           "hsd_kv_commit_rollback", "hsd_prefill", "hsd_drafts_create", "hsd_drafts_destroy", "hsd_drafts_tree", "hsd_tree_path",
+           "hsd_kv_reserve", "hsd_kv_commit_rows", "hsd_kv_quant_append", "hsd_kv_quant_read", "hsd_kv_quant_attention_bytes",
+           "hsd_kv_quant_attention", "hsd_token_logprobs_bytes", "hsd_token_logprobs"]
 lib.hsd_drafts_create.argtypes = [vp, vp, i32, C.POINTER(vp)]
 lib.hsd_drafts_destroy.argtypes, lib.hsd_drafts_destroy.restype = [vp], None
 lib.hsd_drafts_tree.argtypes = [vp, vp, i32, C.c_int64, C.c_int64, i32, vp, vp, vp, C.POINTER(i32)]
 lib.hsd_tree_path.argtypes = [vp, vp, i32, i32, i32, vp]
+i64, szt = C.c_int64, C.c_size_t
+lib.hsd_kv_reserve.argtypes = [vp, _P(hsd_kv_pool), _P(hsd_batch), vp, vp]
+lib.hsd_kv_commit_rows.argtypes = [vp, _P(hsd_kv_pool), _P(hsd_batch)]
+lib.hsd_kv_quant_append.argtypes = [vp, _P(hsd_kv_quant), i32, vp, i32, vp, vp, i64, i64, vp]
+lib.hsd_kv_quant_read.argtypes = [vp, _P(hsd_kv_quant), i32, vp, i32, vp, vp, i64, i64]
+lib.hsd_kv_quant_attention_bytes.argtypes, lib.hsd_kv_quant_attention_bytes.restype = [_P(hsd_kv_quant), _P(hsd_batch), i32], szt
+lib.hsd_kv_quant_attention.argtypes = [vp, _P(hsd_kv_quant), _P(hsd_batch), i32, i32, f32, vp, i64, vp, i64, vp, szt]
+lib.hsd_token_logprobs_bytes.argtypes, lib.hsd_token_logprobs_bytes.restype = [i32, i32, i32], szt
+lib.hsd_token_logprobs.argtypes = [vp, i32, i32, i32, vp, i64, vp, vp, vp, i32, vp, vp, vp, szt]
 
 
 class HsdError(RuntimeError):
@@ -148,3 +163,21 @@ def hsd_drafts_tree(drafts, window, pending, max_packed, out):
     return rc, n.value
 def hsd_tree_path(tokens, tree_end, stop, alpha, path):
     check("hsd_tree_path", lib.hsd_tree_path(tokens.ctypes.data, tree_end.ctypes.data, len(tokens), stop, alpha, path.ctypes.data))
+
+def hsd_kv_reserve(stream, pool, batch, row_slot, row_pos):
+    check("hsd_kv_reserve", lib.hsd_kv_reserve(stream, C.byref(pool), C.byref(batch), row_slot, row_pos))
+def hsd_kv_commit_rows(stream, pool, batch):
+    check("hsd_kv_commit_rows", lib.hsd_kv_commit_rows(stream, C.byref(pool), C.byref(batch)))
+def hsd_kv_quant_append(stream, kv, n_rows, row_slot, dtype, k, v, k_stride, v_stride, status):
+    check("hsd_kv_quant_append", lib.hsd_kv_quant_append(stream, C.byref(kv), n_rows, row_slot, dtype, k, v, k_stride, v_stride, status))
+def hsd_kv_quant_read(stream, kv, n_rows, row_slot, dtype, k, v, k_stride, v_stride):
+    check("hsd_kv_quant_read", lib.hsd_kv_quant_read(stream, C.byref(kv), n_rows, row_slot, dtype, k, v, k_stride, v_stride))
+def hsd_kv_quant_attention_bytes(kv, batch, n_q_heads):
+    return lib.hsd_kv_quant_attention_bytes(C.byref(kv), C.byref(batch), n_q_heads)
+def hsd_kv_quant_attention(stream, kv, batch, n_q_heads, dtype, scale, q, q_stride, out, out_stride, ws, ws_bytes):
+    check("hsd_kv_quant_attention", lib.hsd_kv_quant_attention(stream, C.byref(kv), C.byref(batch), n_q_heads, dtype, scale, q, q_stride,
+                                                               out, out_stride, ws, ws_bytes))
+def hsd_token_logprobs_bytes(n_rows, vocab, n_top): return lib.hsd_token_logprobs_bytes(n_rows, vocab, n_top)
+def hsd_token_logprobs(stream, n_rows, vocab, dtype, logits, row_stride, tokens, logprob, entropy, n_top, top_ids, top_logprobs, ws, ws_bytes):
+    check("hsd_token_logprobs", lib.hsd_token_logprobs(stream, n_rows, vocab, dtype, logits, row_stride, tokens, logprob, entropy, n_top,
+                                                       top_ids, top_logprobs, ws, ws_bytes))

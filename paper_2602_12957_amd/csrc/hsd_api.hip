@@ -1170,3 +1170,5 @@ int hsd_tree_path(const int32_t *tokens, const int32_t *tree_end, int32_t n_rows
 }
 
 }  // extern "C"
+
+#include "ops_api.h"

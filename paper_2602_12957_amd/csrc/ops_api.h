@@ -1,0 +1,159 @@
+// C entries of the operators that run without a decoder context: rows placed in pages, the 8-bit cache, token scores.
+#pragma once
+
+#include "attn_quant.h"
+#include "kv_place.h"
+#include "kv_quant.h"
+#include "token_scores.h"
+
+namespace {
+
+int check_rows(const hsd_batch *b) {
+  if (b == nullptr || b->n_seq < 1 || b->total_q < 0 || b->max_blocks_per_seq < 1 || b->n_slots < 1) return HSD_EINVAL;
+  if (b->seq_slot == nullptr && b->n_slots < b->n_seq) return HSD_EINVAL;
+  if (b->n_seq > HSD_MAX_SEQ || b->max_blocks_per_seq > INT32_MAX / HSD_KV_BLOCK_TOKENS) return HSD_ERANGE;
+  if (b->cu_q == nullptr || b->seq_len == nullptr || b->block_table == nullptr) return HSD_EINVAL;
+  return b->tree_end != nullptr ? HSD_EINVAL : HSD_OK;   // chains only
+}
+
+int check_free_list(const hsd_kv_pool *p) {
+  return p == nullptr || p->free_list == nullptr || p->free_count == nullptr || p->n_blocks < 1 ? HSD_EINVAL : HSD_OK;
+}
+
+int check_quant(const hsd_kv_quant *kv) {
+  if (kv == nullptr || kv->k_codes == nullptr || kv->v_codes == nullptr || kv->k_scale == nullptr || kv->v_scale == nullptr) return HSD_EINVAL;
+  if (kv->n_blocks < 1 || kv->n_kv_heads < 1) return HSD_EINVAL;
+  if (((reinterpret_cast<uintptr_t>(kv->k_codes) | reinterpret_cast<uintptr_t>(kv->v_codes)) & 15) != 0) return HSD_EINVAL;
+  if (kv->n_kv_heads > 1024 || static_cast<int64_t>(kv->n_blocks) * kv->n_kv_heads > INT32_MAX || kv->n_blocks > INT32_MAX / HSD_KV_BLOCK_TOKENS)
+    return HSD_ERANGE;
+  return HSD_OK;
+}
+
+QuantKV quant_pages(const hsd_kv_quant *kv) {
+  return QuantKV{static_cast<uint8_t *>(kv->k_codes), static_cast<uint8_t *>(kv->v_codes), kv->k_scale, kv->v_scale, kv->n_blocks, kv->n_kv_heads};
+}
+
+// 256-byte aligned, as the callers of the workspaces are told
+bool is_workspace(const void *ws) { return ws != nullptr && (reinterpret_cast<uintptr_t>(ws) & 255) == 0; }
+
+bool is_type(int32_t dtype) { return dtype == HSD_BF16 || dtype == HSD_FP32; }
+
+}  // namespace
+
+extern "C" {
+
+int hsd_kv_reserve(void *stream, const hsd_kv_pool *pool, const hsd_batch *b, int32_t *row_slot, int32_t *row_pos) {
+  int rc = check_rows(b);
+  if (rc == HSD_OK) rc = check_free_list(pool);
+  if (rc != HSD_OK) return rc;
+  if (b->status == nullptr || (row_slot == nullptr && b->total_q > 0)) return HSD_EINVAL;
+  const KvPlace p{b->n_seq, b->total_q, b->n_slots, b->max_blocks_per_seq, pool->n_blocks, b->cu_q, b->seq_slot, b->seq_len,
+                  b->block_table, pool->free_list, pool->free_count, b->status, row_slot, row_pos};
+  hipLaunchKernelGGL(k_kv_place, dim3(1), dim3(1024), 0, static_cast<hipStream_t>(stream), p, 1);
+  HSD_LAUNCH_CHECK();
+  return HSD_OK;
+}
+
+int hsd_kv_commit_rows(void *stream, const hsd_kv_pool *pool, const hsd_batch *b) {
+  int rc = check_rows(b);
+  if (rc == HSD_OK) rc = check_free_list(pool);
+  if (rc != HSD_OK) return rc;
+  hipLaunchKernelGGL(k_kv_commit, dim3(1), dim3(1024), 0, static_cast<hipStream_t>(stream), b->n_seq, b->cu_q, b->seq_slot, b->n_slots,
+                     b->seq_len, b->block_table, b->max_blocks_per_seq, pool->n_blocks, pool->free_list, pool->free_count,
+                     b->accept_len, static_cast<const int32_t *>(nullptr), static_cast<int32_t *>(nullptr), b->accept_len == nullptr ? 1 : 0);
+  HSD_LAUNCH_CHECK();
+  return HSD_OK;
+}
+
+int hsd_kv_quant_append(void *stream, const hsd_kv_quant *kv, int32_t n_rows, const int32_t *row_slot, int32_t dtype, const void *k, const void *v,
+                        int64_t k_stride, int64_t v_stride, int32_t *status) {
+  const int rc = check_quant(kv);
+  if (rc != HSD_OK) return rc;
+  if (n_rows < 0 || !is_type(dtype)) return HSD_EINVAL;
+  if (n_rows == 0) return HSD_OK;
+  const int64_t width = static_cast<int64_t>(kv->n_kv_heads) * HSD_HEAD_DIM;
+  if (row_slot == nullptr || k == nullptr || v == nullptr || k_stride < width || v_stride < width) return HSD_EINVAL;
+  const dim3 grid((static_cast<unsigned>(n_rows) + 3) / 4, kv->n_kv_heads);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (dtype == HSD_BF16)
+    hipLaunchKernelGGL((k_quant_append<bf16>), grid, dim3(256), 0, st, quant_pages(kv), n_rows, row_slot, static_cast<const bf16 *>(k),
+                       static_cast<const bf16 *>(v), k_stride, v_stride, status);
+  else
+    hipLaunchKernelGGL((k_quant_append<float>), grid, dim3(256), 0, st, quant_pages(kv), n_rows, row_slot, static_cast<const float *>(k),
+                       static_cast<const float *>(v), k_stride, v_stride, status);
+  HSD_LAUNCH_CHECK();
+  return HSD_OK;
+}
+
+int hsd_kv_quant_read(void *stream, const hsd_kv_quant *kv, int32_t n_rows, const int32_t *row_slot, int32_t dtype, void *k, void *v,
+                      int64_t k_stride, int64_t v_stride) {
+  const int rc = check_quant(kv);
+  if (rc != HSD_OK) return rc;
+  if (n_rows < 0 || !is_type(dtype)) return HSD_EINVAL;
+  if (n_rows == 0) return HSD_OK;
+  const int64_t width = static_cast<int64_t>(kv->n_kv_heads) * HSD_HEAD_DIM;
+  if (row_slot == nullptr || k == nullptr || v == nullptr || k_stride < width || v_stride < width) return HSD_EINVAL;
+  const dim3 grid((static_cast<unsigned>(n_rows) + 3) / 4, kv->n_kv_heads);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (dtype == HSD_BF16)
+    hipLaunchKernelGGL((k_quant_read<bf16>), grid, dim3(256), 0, st, quant_pages(kv), n_rows, row_slot, static_cast<bf16 *>(k),
+                       static_cast<bf16 *>(v), k_stride, v_stride);
+  else
+    hipLaunchKernelGGL((k_quant_read<float>), grid, dim3(256), 0, st, quant_pages(kv), n_rows, row_slot, static_cast<float *>(k),
+                       static_cast<float *>(v), k_stride, v_stride);
+  HSD_LAUNCH_CHECK();
+  return HSD_OK;
+}
+
+size_t hsd_kv_quant_attention_bytes(const hsd_kv_quant *kv, const hsd_batch *b, int32_t n_q_heads) {
+  if (check_quant(kv) != HSD_OK || check_rows(b) != HSD_OK || n_q_heads < 1 || n_q_heads % kv->n_kv_heads != 0 || n_q_heads > 1024) return 0;
+  return 256;
+}
+
+int hsd_kv_quant_attention(void *stream, const hsd_kv_quant *kv, const hsd_batch *b, int32_t n_q_heads, int32_t dtype, float softmax_scale,
+                           const void *q, int64_t q_stride, void *out, int64_t out_stride, void *ws, size_t ws_bytes) {
+  int rc = check_quant(kv);
+  if (rc == HSD_OK) rc = check_rows(b);
+  if (rc != HSD_OK) return rc;
+  if (n_q_heads < 1 || n_q_heads % kv->n_kv_heads != 0 || !is_type(dtype) || !std::isfinite(softmax_scale)) return HSD_EINVAL;
+  if (n_q_heads > 1024) return HSD_ERANGE;
+  if (b->total_q == 0) return HSD_OK;
+  const int64_t width = static_cast<int64_t>(n_q_heads) * HSD_HEAD_DIM;
+  if (q == nullptr || out == nullptr || !is_workspace(ws) || q_stride < width || out_stride < width) return HSD_EINVAL;
+  if (ws_bytes < hsd_kv_quant_attention_bytes(kv, b, n_q_heads)) return HSD_ENOSPC;
+  const QuantAttn a{quant_pages(kv), b->n_seq, b->total_q, b->n_slots, b->max_blocks_per_seq, n_q_heads, b->cu_q, b->seq_slot, b->seq_len,
+                    b->block_table, q_stride, out_stride, softmax_scale * 1.4426950408889634f};
+  const dim3 grid(b->total_q, (n_q_heads + 3) / 4);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (dtype == HSD_BF16)
+    hipLaunchKernelGGL((k_attn_quant<bf16>), grid, dim3(256), 0, st, a, static_cast<const bf16 *>(q), static_cast<bf16 *>(out));
+  else
+    hipLaunchKernelGGL((k_attn_quant<float>), grid, dim3(256), 0, st, a, static_cast<const float *>(q), static_cast<float *>(out));
+  HSD_LAUNCH_CHECK();
+  return HSD_OK;
+}
+
+size_t hsd_token_logprobs_bytes(int32_t n_rows, int32_t vocab, int32_t n_top) {
+  if (n_rows < 0 || vocab < 1 || n_top < 0 || n_top > HSD_MAX_TOP) return 0;
+  return 256;
+}
+
+int hsd_token_logprobs(void *stream, int32_t n_rows, int32_t vocab, int32_t dtype, const void *logits, int64_t row_stride, const int32_t *tokens,
+                       float *logprob, float *entropy, int32_t n_top, int32_t *top_ids, float *top_logprobs, void *ws, size_t ws_bytes) {
+  if (n_rows < 0 || vocab < 1 || n_top < 0 || !is_type(dtype) || row_stride < vocab) return HSD_EINVAL;
+  if (n_top > HSD_MAX_TOP) return HSD_ERANGE;
+  if (n_rows == 0) return HSD_OK;
+  if (logits == nullptr || tokens == nullptr || logprob == nullptr || entropy == nullptr || !is_workspace(ws)) return HSD_EINVAL;
+  if (n_top > 0 && (top_ids == nullptr || top_logprobs == nullptr)) return HSD_EINVAL;
+  if (ws_bytes < hsd_token_logprobs_bytes(n_rows, vocab, n_top)) return HSD_ENOSPC;
+  const TokenScores a{n_rows, vocab, n_top, row_stride, tokens, logprob, entropy, top_logprobs, top_ids};
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (dtype == HSD_BF16)
+    hipLaunchKernelGGL((k_token_scores<bf16>), dim3(n_rows), dim3(256), 0, st, a, static_cast<const bf16 *>(logits));
+  else
+    hipLaunchKernelGGL((k_token_scores<float>), dim3(n_rows), dim3(256), 0, st, a, static_cast<const float *>(logits));
+  HSD_LAUNCH_CHECK();
+  return HSD_OK;
+}
+
+}  // extern "C"
