@@ -1,6 +1,19 @@
 // Attention over a cache held in 8 bits: row i of a sequence's block sees the cached tokens and rows 0 .. i of the block.
+//
+// One pass over the keys with a softmax reference that moves rarely.  A wave holds 16 * CT columns -- (row, query head of the kv
+// head) pairs, heads fastest -- and walks pairs of pages: a page of K and one of V are a 16-byte request a lane each, whose bytes are
+// the operands of 16x16x32 products once converted to bf16 (exact: code times a power of two).
+//   S^T = K Q^T: lane (g, c) receives tokens 4 g .. 4 g + 3 of a page for column c
+//   O^T += V^T P^T: the same lane's probabilities of two pages are the operand as they are; the rows of the product are dims
+//     (row 4 g + i of part t: dim 16 g + 4 i + t), so that a lane ends with 16 consecutive dims of its column
+// The row sums are a product with ones: sums of the rounded probabilities, whose rounding cancels in the quotient.
+// fp32 calls split queries and probabilities into three bf16 parts each (24 bits), three products in place of one.
+//
+// The waves of a workgroup share the columns and take every W-th pair of pages; the workgroups along grid.y take runs of
+// pairs of their own where few columns would leave the chip empty (k_attn_quant_join adds them up).
 #pragma once
 
+#include "attn_wide.h"
 #include "kv_quant.h"
 #include "misc_kernels.h"
 
@@ -8,53 +21,331 @@ namespace hsd {
 
 struct QuantAttn {
   QuantKV kv;
-  int n_seq, total_q, n_slots, max_blocks, n_q_heads;
+  int n_seq, total_q, n_slots, max_blocks, n_q_heads, group;   // group: query heads of a kv head
   const int32_t *cu_q, *seq_slot, *seq_len, *block_table;
   int64_t q_stride, o_stride;
-  float scale;   // log2(e) times the softmax scale
+  float scale;        // log2(e) times the softmax scale's magnitude
+  uint32_t q_sign;    // its sign, to be put on the queries
+  int n_tiles, n_splits;
+  float *part_o;      // [n_splits][n_tiles][n_kv_heads][columns][64]
+  float2 *part_ml;    // [n_splits][n_tiles][n_kv_heads][columns]: reference, sum
 };
 
-// grid: (total_q, ceil(n_q_heads / 4)), block 256: a wave per row and query head, a lane per key and per dimension
-template <typename T>
-__global__ void __launch_bounds__(256) k_attn_quant(QuantAttn a, const T *__restrict__ q, T *__restrict__ o) {
-  const int lane = threadIdx.x & 63, head = blockIdx.y * 4 + (threadIdx.x >> 6), r = blockIdx.x;
-  if (head >= a.n_q_heads) return;
-  const int h = head / (a.n_q_heads / a.kv.n_kv_heads), s = seq_of_row(a.cu_q, a.n_seq, r), sl = slot_of(a.seq_slot, s, a.n_slots);
-  const int n_keys = min(a.seq_len[sl] + (r - a.cu_q[s]) + 1, a.max_blocks * kBlk);
-  const T *qr = q + r * a.q_stride + head * kHd;
-  float m = -INFINITY, l = 0.f, acc = 0.f;
-  for (int j0 = 0; j0 < n_keys; j0 += kWave) {
-    const int j = j0 + lane;
-    int id = j < n_keys ? a.block_table[static_cast<size_t>(sl) * a.max_blocks + j / kBlk] : -1;
-    if (id >= a.kv.n_blocks) id = -1;
-    float score = -INFINITY;
-    if (id >= 0) {
-      const int page = id * a.kv.n_kv_heads + h;
-      const uint8_t *kp = a.kv.k_codes + static_cast<size_t>(page) * kPageCodes + j % kBlk * 16;
-      float dot = 0.f;
-      for (int d = 0; d < kHd; d += 4) {
-        float x[4], y[4];
-        dequant4(*reinterpret_cast<const uint32_t *>(kp + d / 16 * 256 + d % 16), 1.f, x);
-        quant_load4(qr + d, y);
-        for (int e = 0; e < 4; ++e) dot = fmaf(x[e], y[e], dot);
-      }
-      score = dot * a.kv.k_scale[page] * a.scale;
+constexpr float kRefSlack = 20.f;          // binary orders by which a score may exceed its column's reference before that moves
+constexpr int kSplitPairs = 16;            // a run of pairs for a workgroup of its own is no shorter
+
+// Tiles of `cols` columns of sequence s start at tile floor(cu_q[s] * group / cols) + s: as many as it needs, at most one too many.
+__device__ __forceinline__ int tile_start(int cu, int s, int group, int cols) { return cu * group / cols + s; }
+
+struct QuantTile {
+  int slot, S, n, base, j;   // state row, cached length, rows, first packed row, tile within the sequence
+};
+// Sequence and place of tile t; n = 0 where the tile has no columns
+__device__ __forceinline__ QuantTile find_tile(const QuantAttn &a, int t, int cols, int lane) {
+  int first = 0, stride = (a.n_seq + kWave - 1) / kWave;
+  QuantTile q;
+  for (;; stride = (stride + kWave - 1) / kWave) {
+    const int s = first + lane * stride;
+    const bool in = s < a.n_seq;
+    const int cu = in ? a.cu_q[s] : 0;
+    const unsigned long long m = __ballot(in && tile_start(cu, s, a.group, cols) <= t);
+    const int hit = 63 - __builtin_clzll(m);   // (tile 0 starts at sequence 0: m has bit 0)
+    if (stride == 1) {
+      const int end = in ? a.cu_q[s + 1] : 0, slot = in ? slot_of(a.seq_slot, s, a.n_slots) : 0, len = a.seq_len[slot];
+      q.base = __builtin_amdgcn_readlane(cu, hit);
+      q.n = __builtin_amdgcn_readlane(end, hit) - q.base;
+      q.slot = __builtin_amdgcn_readlane(slot, hit);
+      q.S = max(__builtin_amdgcn_readlane(len, hit), 0);
+      q.j = t - tile_start(q.base, first + hit, a.group, cols);
+      break;
     }
-    const float m_new = fmaxf(m, wave_max(score));
-    if (!__any(id >= 0)) continue;
-    const float p = id >= 0 ? exp2f(score - m_new) : 0.f, corr = m == -INFINITY ? 0.f : exp2f(m - m_new);
-    l = l * corr + wave_sum(p);
-    acc *= corr;
-    for (int i = 0; i < kWave; ++i) {
-      const int b = __builtin_amdgcn_readlane(id, i);
-      if (b < 0) continue;
-      const int page = b * a.kv.n_kv_heads + h, tok = i % kBlk;
-      const float x = __builtin_amdgcn_cvt_f32_fp8(a.kv.v_codes[static_cast<size_t>(page) * kPageCodes + (tok >> 2) * 256 + (lane >> 2) * 16 + (lane & 3) * 4 + (tok & 3)], 0);
-      acc = fmaf(__shfl(p, i, kWave) * a.kv.v_scale[page], x, acc);
-    }
-    m = m_new;
+    first += hit * stride;
   }
-  o[r * a.o_stride + head * kHd + lane] = from_f32<T>(l == 0.f ? 0.f : acc / l);
+  return q;
+}
+
+// Pairs of pages that the columns of a tile see, and those of run z
+__device__ __forceinline__ int tile_keys(const QuantAttn &a, const QuantTile &q, int cols) {
+  return min(q.S + min(((q.j + 1) * cols - 1) / a.group + 1, q.n), a.max_blocks * kBlk);
+}
+__device__ __forceinline__ int run_pairs(int n_pairs, int n_splits) { return max((n_pairs + n_splits - 1) / n_splits, kSplitPairs); }
+
+// Eight values, four a half, as NS bf16 parts
+template <int NS>
+__device__ __forceinline__ void split8(const float *x, bf16x8 (&part)[NS]) {
+  floatx8 f = {x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]};
+#pragma unroll
+  for (int n = 0; n < NS; ++n) {
+    part[n] = __builtin_convertvector(f, bf16x8);
+    if (n + 1 < NS) f -= __builtin_convertvector(part[n], floatx8);
+  }
+}
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ bf16x8 page_operand(uint32_t a, uint32_t b, float sa, float sb) {
+  const bf16x2 x = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, sa, false), y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, sa, true);
+  const bf16x2 z = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, sb, false), w = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, sb, true);
+  return bf16x8{x[0], x[1], y[0], y[1], z[0], z[1], w[0], w[1]};
+}
+
+__device__ __forceinline__ void load_q8(const bf16 *p, uint32_t sign, bf16x8 (&part)[1]) {
+  typedef uint32_t u4 __attribute__((ext_vector_type(4), aligned(2)));
+  u4 u = *reinterpret_cast<const u4 *>(p);
+  u ^= sign | (sign >> 16);
+  part[0] = *reinterpret_cast<bf16x8 *>(&u);
+}
+__device__ __forceinline__ void load_q8(const float *p, uint32_t sign, bf16x8 (&part)[3]) {
+  float x[8];
+  quant_load4(p, x), quant_load4(p + 4, x + 4);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(__float_as_uint(x[i]) ^ sign);
+  split8<3>(x, part);
+}
+
+__device__ __forceinline__ void store4(float *p, const floatx4 &v) { quant_store4(p, reinterpret_cast<const float *>(&v)); }
+__device__ __forceinline__ void store4(bf16 *p, const floatx4 &v) {
+  typedef uint32_t u2 __attribute__((ext_vector_type(2), aligned(2)));
+  bf16x4 b = __builtin_convertvector(v, bf16x4);
+  *reinterpret_cast<u2 *>(p) = *reinterpret_cast<u2 *>(&b);
+}
+
+// grid: (n_tiles * n_kv_heads, n_splits), block 64 * W, dynamic LDS quant_attn_lds(W, CT)
+inline int quant_attn_lds(int waves, int ct) { return waves > 1 ? waves * ct * (64 * 16 + 32) * static_cast<int>(sizeof(float)) : 0; }
+
+template <typename T, int CT>
+__global__ void __launch_bounds__(CT == 1 ? 1024 : 512) k_attn_quant(QuantAttn a, const T *__restrict__ q, T *__restrict__ out) {
+  constexpr int NS = std::is_same<T, float>::value ? 3 : 1, C = 16 * CT;
+  extern __shared__ __attribute__((aligned(16))) float lds[];
+  const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+  const int W = blockDim.x >> 6, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h = blockIdx.x / a.n_tiles, tile = a.n_tiles - 1 - blockIdx.x % a.n_tiles, z = blockIdx.y;
+  const QuantTile qt = find_tile(a, tile, C, lane);
+  const int n_cols = qt.n * a.group - qt.j * C;   // columns from this tile's first on
+  if (n_cols <= 0) return;
+  const int n_keys = tile_keys(a, qt, C), n_pages = (n_keys + kBlk - 1) / kBlk, n_pairs = (n_pages + 1) / 2;
+  const int run = run_pairs(n_pairs, a.n_splits), p0 = z * run, p1 = min(p0 + run, n_pairs);
+  if (z > 0 && p0 >= p1) return;
+  const bool whole = n_pairs <= run;
+  const int n_steps = p1 > p0 + w ? (p1 - p0 - w + W - 1) / W : 0;
+
+  // columns
+  bf16x8 qf[CT][2][NS];
+  int lim[CT];   // last position that the lane's column sees
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    const int f = qt.j * C + min(16 * ct + c, n_cols - 1), row = f / a.group, hd = f - row * a.group;
+    lim[ct] = qt.S + row;
+    const T *p = q + (qt.base + row) * a.q_stride + (h * a.group + hd) * kHd + 16 * g;
+    load_q8(p, a.q_sign, qf[ct][0]);
+    load_q8(p + 8, a.q_sign, qf[ct][1]);
+  }
+  const int lim_first = qt.S + qt.j * C / a.group;   // what every column sees
+
+  floatx4 o[CT][4], l[CT];
+  float ref[CT], thr[CT];   // thr: ref + slack, -inf while the column has seen nothing (its ref is then 0)
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) o[ct][t] = floatx4{0.f, 0.f, 0.f, 0.f};
+    l[ct] = floatx4{0.f, 0.f, 0.f, 0.f};
+    ref[ct] = 0.f, thr[ct] = -INFINITY;
+  }
+  bf16x8 ones;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) ones[e] = static_cast<__bf16>(1.0f);
+
+  // ids and scales of the pages of 32 steps: lane 2 i + p has page p of step i
+  const int32_t *table = a.block_table + static_cast<size_t>(qt.slot) * a.max_blocks;
+  int id = -1;
+  float ksc = 1.f, vsc = 1.f;
+  auto batch = [&](int i0) {
+    const int page = 2 * (p0 + w + W * (i0 + (lane >> 1))) + (lane & 1);
+    id = page < n_pages ? table[page] : -1;
+    if (id >= a.kv.n_blocks) id = -1;
+    const int at = max(id, 0) * a.kv.n_kv_heads + h;
+    ksc = a.kv.k_scale[at], vsc = a.kv.v_scale[at];
+  };
+  struct Step {
+    u32x4 k[2], v[2];
+    float ks[2], vs[2];
+    bool ok;
+  };
+  auto request = [&](int i, Step &s) {
+    if (i >= n_steps) return;
+    if ((i & 31) == 0) batch(i);
+    s.ok = true;
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const int src = 2 * (i & 31) + p, b = __builtin_amdgcn_readlane(id, src);
+      const size_t at = static_cast<size_t>(max(b, 0) * a.kv.n_kv_heads + h) * kPageCodes;
+      s.k[p] = reinterpret_cast<const u32x4 *>(a.kv.k_codes + at)[lane];
+      s.v[p] = reinterpret_cast<const u32x4 *>(a.kv.v_codes + at)[lane];
+      s.ks[p] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ksc), src));
+      s.vs[p] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vsc), src));
+      if (b < 0) {
+        s.ok = false;
+        s.ks[p] = __uint_as_float(0x7fc00000u);   // marks the page: its positions are left out
+        s.v[p] = u32x4{0, 0, 0, 0};
+        s.vs[p] = 1.f;
+      }
+    }
+  };
+  auto step = [&](int i, const Step &s) {
+    if (i >= n_steps) return;
+    const int pos0 = 32 * (p0 + w + W * i);
+    floatx4 sc[2][CT];
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const bf16x8 k0 = page_operand(s.k[p][0], s.k[p][1], s.ks[p], s.ks[p]), k1 = page_operand(s.k[p][2], s.k[p][3], s.ks[p], s.ks[p]);
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        floatx4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int n = NS - 1; n >= 0; --n) {
+          x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, qf[ct][0][n], x, 0, 0, 0);
+          x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, qf[ct][1][n], x, 0, 0, 0);
+        }
+        sc[p][ct] = x * a.scale;
+      }
+    }
+    if (!s.ok || pos0 + 31 > lim_first) {
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        const bool gone = s.ks[p] != s.ks[p];
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (gone || pos0 + 16 * p + 4 * g + e > lim[ct]) sc[p][ct][e] = -INFINITY;
+      }
+    }
+    float mx[CT];
+    bool move = false;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      mx[ct] = fmaxf(fmaxf(fmaxf(sc[0][ct][0], sc[0][ct][1]), fmaxf(sc[0][ct][2], sc[0][ct][3])),
+                     fmaxf(fmaxf(sc[1][ct][0], sc[1][ct][1]), fmaxf(sc[1][ct][2], sc[1][ct][3])));
+      move = move || mx[ct] > thr[ct];
+    }
+    if (__any(move)) {
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        const float m = half_max(quarter_max(mx[ct]));
+        if (m > thr[ct]) {
+          const float f = thr[ct] == -INFINITY ? 0.f : exp2f(ref[ct] - m);
+#pragma unroll
+          for (int t = 0; t < 4; ++t) o[ct][t] *= f;
+          l[ct] *= f;
+          ref[ct] = m, thr[ct] = m + kRefSlack;
+        }
+      }
+    }
+    bf16x8 v[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) v[t] = page_operand(s.v[0][t], s.v[1][t], s.vs[0], s.vs[1]);
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      float p[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(sc[e >> 2][ct][e & 3] - ref[ct]);
+      bf16x8 pf[NS];
+      split8<NS>(p, pf);
+#pragma unroll
+      for (int n = NS - 1; n >= 0; --n) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) o[ct][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[t], pf[n], o[ct][t], 0, 0, 0);
+        l[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[n], l[ct], 0, 0, 0);
+      }
+    }
+  };
+  Step s0, s1;
+  request(0, s0);
+  for (int i = 0; i < n_steps; i += 2) {
+    request(i + 1, s1);
+    step(i, s0);
+    request(i + 2, s0);
+    step(i + 1, s1);
+  }
+
+  // the waves' parts together; a column's 16 dims of a lane in pieces of four
+  auto put = [&](int ct, int i, int ln, floatx4 x, float m, float sum) {
+    const int col = 16 * ct + (ln & 15), dim = 16 * (ln >> 4) + 4 * i;
+    if (col >= n_cols) return;
+    if (whole) {
+      const int f = qt.j * C + col, row = f / a.group, hd = f - row * a.group;
+      if (sum == 0.f) x = floatx4{0.f, 0.f, 0.f, 0.f};
+      else x /= sum;
+      store4(out + (qt.base + row) * a.o_stride + (h * a.group + hd) * kHd + dim, x);
+    } else {
+      const size_t at = ((static_cast<size_t>(z) * a.n_tiles + tile) * a.kv.n_kv_heads + h) * C + col;
+      *reinterpret_cast<floatx4 *>(a.part_o + at * kHd + dim) = x;
+      if (dim == 0) a.part_ml[at] = float2{m, sum};
+    }
+  };
+  if (W == 1) {
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        put(ct, i, lane, floatx4{o[ct][0][i], o[ct][1][i], o[ct][2][i], o[ct][3][i]}, thr[ct] == -INFINITY ? -INFINITY : ref[ct], l[ct][0]);
+    return;
+  }
+  float *const ml = lds + W * CT * 1024;   // [wave][part of 16 columns][reference | sum][16]
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<floatx4 *>(lds + ((w * CT + ct) * 4 + i) * 256 + lane * 4) = floatx4{o[ct][0][i], o[ct][1][i], o[ct][2][i], o[ct][3][i]};
+    if (lane < 16) {
+      ml[(w * CT + ct) * 32 + lane] = thr[ct] == -INFINITY ? -INFINITY : ref[ct];
+      ml[(w * CT + ct) * 32 + 16 + lane] = l[ct][0];
+    }
+  }
+  __syncthreads();
+  for (int item = threadIdx.x; item < 256 * CT; item += blockDim.x) {
+    const int ln = item & 63, i = (item >> 6) & 3, ct = item >> 8;
+    float m = -INFINITY;
+    for (int u = 0; u < W; ++u) m = fmaxf(m, ml[(u * CT + ct) * 32 + (ln & 15)]);
+    const float base = m == -INFINITY ? 0.f : m;
+    floatx4 x = {0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f;
+    for (int u = 0; u < W; ++u) {
+      const float f = exp2f(ml[(u * CT + ct) * 32 + (ln & 15)] - base);
+      x += f * *reinterpret_cast<const floatx4 *>(lds + ((u * CT + ct) * 4 + i) * 256 + ln * 4);
+      sum += f * ml[(u * CT + ct) * 32 + 16 + (ln & 15)];
+    }
+    put(ct, i, ln, x, m, sum);
+  }
+}
+
+// The runs of a tile together, in order.  grid: n_tiles * n_kv_heads, block 256: 16 columns at a time, 16 lanes a column
+template <typename T>
+__global__ void __launch_bounds__(256) k_attn_quant_join(QuantAttn a, int cols, T *__restrict__ out) {
+  const int h = blockIdx.x / a.n_tiles, tile = blockIdx.x % a.n_tiles;
+  const QuantTile qt = find_tile(a, tile, cols, threadIdx.x & 63);
+  const int n_cols = qt.n * a.group - qt.j * cols;
+  if (n_cols <= 0) return;
+  const int n_pairs = ((tile_keys(a, qt, cols) + kBlk - 1) / kBlk + 1) / 2, run = run_pairs(n_pairs, a.n_splits);
+  if (n_pairs <= run) return;   // written already
+  const int n = (n_pairs + run - 1) / run, dim = 4 * (threadIdx.x & 15);
+  for (int col = threadIdx.x >> 4; col < min(cols, n_cols); col += 16) {
+    const size_t at0 = (static_cast<size_t>(tile) * a.kv.n_kv_heads + h) * cols + col, step = static_cast<size_t>(a.n_tiles) * a.kv.n_kv_heads * cols;
+    float m = -INFINITY;
+    for (int z = 0; z < n; ++z) m = fmaxf(m, a.part_ml[at0 + z * step].x);
+    const float base = m == -INFINITY ? 0.f : m;
+    floatx4 x = {0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f;
+    for (int z = 0; z < n; ++z) {
+      const float2 ml = a.part_ml[at0 + z * step];
+      const float f = exp2f(ml.x - base);
+      x += f * *reinterpret_cast<const floatx4 *>(a.part_o + (at0 + z * step) * kHd + dim);
+      sum += f * ml.y;
+    }
+    if (sum == 0.f) x = floatx4{0.f, 0.f, 0.f, 0.f};
+    else x /= sum;
+    const int f = qt.j * cols + col, row = f / a.group, hd = f - row * a.group;
+    store4(out + (qt.base + row) * a.o_stride + (h * a.group + hd) * kHd + dim, x);
+  }
 }
 
 }  // namespace hsd

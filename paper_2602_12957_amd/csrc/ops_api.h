@@ -36,6 +36,49 @@ QuantKV quant_pages(const hsd_kv_quant *kv) {
 // 256-byte aligned, as the callers of the workspaces are told
 bool is_workspace(const void *ws) { return ws != nullptr && (reinterpret_cast<uintptr_t>(ws) & 255) == 0; }
 
+int check_heads(const hsd_kv_quant *kv, const hsd_batch *b, int32_t n_q_heads) {
+  if (n_q_heads < 1 || n_q_heads % kv->n_kv_heads != 0) return HSD_EINVAL;
+  return n_q_heads > 1024 || static_cast<int64_t>(b->total_q) * n_q_heads > INT32_MAX / 2 ? HSD_ERANGE : HSD_OK;
+}
+
+// How an attention call is split.  Lengths are on the device: the plan goes by rows, heads and what the tables can hold.
+struct QuantPlan {
+  int ct, waves, n_tiles, n_splits;
+  size_t part_rows;   // rows of the workspace's parts
+};
+QuantPlan plan_quant_attention(const hsd_kv_quant *kv, const hsd_batch *b, int32_t n_q_heads, bool f32) {
+  const int64_t group = n_q_heads / kv->n_kv_heads, cols = b->total_q * group;
+  QuantPlan p;
+  auto tiles = [&](int ct) { return cols / (16 * ct) + b->n_seq; };
+  p.ct = cols <= 24 * b->n_seq ? 1 : (f32 || cols <= 48 * b->n_seq ? 2 : 4);
+  p.n_tiles = static_cast<int>(tiles(p.ct));
+  const int64_t groups = p.n_tiles * static_cast<int64_t>(kv->n_kv_heads), max_pairs = (b->max_blocks_per_seq + 1) / 2;
+  const int most = p.ct == 1 ? 16 : 8;
+  p.waves = 1;
+  while (p.waves < most && groups * p.waves < 2048 && p.waves < max_pairs) p.waves *= 2;
+  p.n_splits = 1;
+  if (groups < 512 && max_pairs > 64) p.n_splits = static_cast<int>(std::min<int64_t>({(1023 + groups) / groups, (max_pairs + 31) / 32, 256}));
+  p.part_rows = p.n_splits > 1 ? static_cast<size_t>(groups) * p.n_splits * 16 * p.ct : 0;
+  return p;
+}
+
+template <typename T, int CT>
+int launch_quant_attention(hipStream_t st, const QuantAttn &a, const QuantPlan &p, const T *q, T *out) {
+  auto kern = k_attn_quant<T, CT>;
+  const int lds = quant_attn_lds(p.waves, CT);
+  static const hipError_t attr_rc = hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                        quant_attn_lds(CT == 1 ? 16 : 8, CT));
+  if (attr_rc != hipSuccess) return HSD_EHIP;
+  const unsigned groups = static_cast<unsigned>(p.n_tiles) * a.kv.n_kv_heads;
+  hipLaunchKernelGGL(kern, dim3(groups, p.n_splits), dim3(64 * p.waves), lds, st, a, q, out);
+  HSD_LAUNCH_CHECK();
+  if (p.n_splits > 1) {
+    hipLaunchKernelGGL((k_attn_quant_join<T>), dim3(groups), dim3(256), 0, st, a, 16 * CT, out);
+    HSD_LAUNCH_CHECK();
+  }
+  return HSD_OK;
+}
+
 bool is_type(int32_t dtype) { return dtype == HSD_BF16 || dtype == HSD_FP32; }
 
 }  // namespace
@@ -106,8 +149,9 @@ int hsd_kv_quant_read(void *stream, const hsd_kv_quant *kv, int32_t n_rows, cons
 }
 
 size_t hsd_kv_quant_attention_bytes(const hsd_kv_quant *kv, const hsd_batch *b, int32_t n_q_heads) {
-  if (check_quant(kv) != HSD_OK || check_rows(b) != HSD_OK || n_q_heads < 1 || n_q_heads % kv->n_kv_heads != 0 || n_q_heads > 1024) return 0;
-  return 256;
+  if (check_quant(kv) != HSD_OK || check_rows(b) != HSD_OK || check_heads(kv, b, n_q_heads) != HSD_OK) return 0;
+  const QuantPlan bf = plan_quant_attention(kv, b, n_q_heads, false), f32 = plan_quant_attention(kv, b, n_q_heads, true);
+  return 256 + std::max(bf.part_rows, f32.part_rows) * (HSD_HEAD_DIM + 2) * sizeof(float);
 }
 
 int hsd_kv_quant_attention(void *stream, const hsd_kv_quant *kv, const hsd_batch *b, int32_t n_q_heads, int32_t dtype, float softmax_scale,
@@ -115,22 +159,27 @@ int hsd_kv_quant_attention(void *stream, const hsd_kv_quant *kv, const hsd_batch
   int rc = check_quant(kv);
   if (rc == HSD_OK) rc = check_rows(b);
   if (rc != HSD_OK) return rc;
-  if (n_q_heads < 1 || n_q_heads % kv->n_kv_heads != 0 || !is_type(dtype) || !std::isfinite(softmax_scale)) return HSD_EINVAL;
-  if (n_q_heads > 1024) return HSD_ERANGE;
+  if (!is_type(dtype) || !std::isfinite(softmax_scale)) return HSD_EINVAL;
+  if ((rc = check_heads(kv, b, n_q_heads)) != HSD_OK) return rc;
   if (b->total_q == 0) return HSD_OK;
   const int64_t width = static_cast<int64_t>(n_q_heads) * HSD_HEAD_DIM;
   if (q == nullptr || out == nullptr || !is_workspace(ws) || q_stride < width || out_stride < width) return HSD_EINVAL;
   if (ws_bytes < hsd_kv_quant_attention_bytes(kv, b, n_q_heads)) return HSD_ENOSPC;
-  const QuantAttn a{quant_pages(kv), b->n_seq, b->total_q, b->n_slots, b->max_blocks_per_seq, n_q_heads, b->cu_q, b->seq_slot, b->seq_len,
-                    b->block_table, q_stride, out_stride, softmax_scale * 1.4426950408889634f};
-  const dim3 grid(b->total_q, (n_q_heads + 3) / 4);
+  const QuantPlan p = plan_quant_attention(kv, b, n_q_heads, dtype == HSD_FP32);
+  float *part = static_cast<float *>(ws);
+  const QuantAttn a{quant_pages(kv), b->n_seq, b->total_q, b->n_slots, b->max_blocks_per_seq, n_q_heads, n_q_heads / kv->n_kv_heads, b->cu_q,
+                    b->seq_slot, b->seq_len, b->block_table, q_stride, out_stride, std::fabs(softmax_scale) * 1.4426950408889634f,
+                    std::signbit(softmax_scale) ? 0x80000000u : 0u, p.n_tiles, p.n_splits, part, reinterpret_cast<float2 *>(part + p.part_rows * HSD_HEAD_DIM)};
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if (dtype == HSD_BF16)
-    hipLaunchKernelGGL((k_attn_quant<bf16>), grid, dim3(256), 0, st, a, static_cast<const bf16 *>(q), static_cast<bf16 *>(out));
-  else
-    hipLaunchKernelGGL((k_attn_quant<float>), grid, dim3(256), 0, st, a, static_cast<const float *>(q), static_cast<float *>(out));
-  HSD_LAUNCH_CHECK();
-  return HSD_OK;
+  if (dtype == HSD_BF16) {
+    const bf16 *x = static_cast<const bf16 *>(q);
+    bf16 *y = static_cast<bf16 *>(out);
+    return p.ct == 1 ? launch_quant_attention<bf16, 1>(st, a, p, x, y)
+                     : (p.ct == 2 ? launch_quant_attention<bf16, 2>(st, a, p, x, y) : launch_quant_attention<bf16, 4>(st, a, p, x, y));
+  }
+  const float *x = static_cast<const float *>(q);
+  float *y = static_cast<float *>(out);
+  return p.ct == 1 ? launch_quant_attention<float, 1>(st, a, p, x, y) : launch_quant_attention<float, 2>(st, a, p, x, y);
 }
 
 size_t hsd_token_logprobs_bytes(int32_t n_rows, int32_t vocab, int32_t n_top) {
