@@ -110,10 +110,12 @@ __device__ __forceinline__ void store4(bf16 *p, const floatx4 &v) {
 }
 
 // grid: (n_tiles * n_kv_heads, n_splits), block 64 * W, dynamic LDS quant_attn_lds(W, CT)
+// (16 waves leave 128 registers each, which one part of 16 bf16 columns fits)
+constexpr int quant_attn_waves(bool f32, int ct) { return ct == 1 && !f32 ? 16 : 8; }
 inline int quant_attn_lds(int waves, int ct) { return waves > 1 ? waves * ct * (64 * 16 + 32) * static_cast<int>(sizeof(float)) : 0; }
 
 template <typename T, int CT>
-__global__ void __launch_bounds__(CT == 1 ? 1024 : 512) k_attn_quant(QuantAttn a, const T *__restrict__ q, T *__restrict__ out) {
+__global__ void __launch_bounds__(64 * quant_attn_waves(std::is_same<T, float>::value, CT)) k_attn_quant(QuantAttn a, const T *__restrict__ q, T *__restrict__ out) {
   constexpr int NS = std::is_same<T, float>::value ? 3 : 1, C = 16 * CT;
   extern __shared__ __attribute__((aligned(16))) float lds[];
   const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;

@@ -53,7 +53,7 @@ QuantPlan plan_quant_attention(const hsd_kv_quant *kv, const hsd_batch *b, int32
   p.ct = cols <= 24 * b->n_seq ? 1 : (f32 || cols <= 48 * b->n_seq ? 2 : 4);
   p.n_tiles = static_cast<int>(tiles(p.ct));
   const int64_t groups = p.n_tiles * static_cast<int64_t>(kv->n_kv_heads), max_pairs = (b->max_blocks_per_seq + 1) / 2;
-  const int most = p.ct == 1 ? 16 : 8;
+  const int most = quant_attn_waves(f32, p.ct);
   p.waves = 1;
   while (p.waves < most && groups * p.waves < 2048 && p.waves < max_pairs) p.waves *= 2;
   p.n_splits = 1;
@@ -67,13 +67,44 @@ int launch_quant_attention(hipStream_t st, const QuantAttn &a, const QuantPlan &
   auto kern = k_attn_quant<T, CT>;
   const int lds = quant_attn_lds(p.waves, CT);
   static const hipError_t attr_rc = hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                                        quant_attn_lds(CT == 1 ? 16 : 8, CT));
+                                                        quant_attn_lds(quant_attn_waves(std::is_same<T, float>::value, CT), CT));
   if (attr_rc != hipSuccess) return HSD_EHIP;
   const unsigned groups = static_cast<unsigned>(p.n_tiles) * a.kv.n_kv_heads;
   hipLaunchKernelGGL(kern, dim3(groups, p.n_splits), dim3(64 * p.waves), lds, st, a, q, out);
   HSD_LAUNCH_CHECK();
   if (p.n_splits > 1) {
     hipLaunchKernelGGL((k_attn_quant_join<T>), dim3(groups), dim3(256), 0, st, a, 16 * CT, out);
+    HSD_LAUNCH_CHECK();
+  }
+  return HSD_OK;
+}
+
+// How rows of logits are dealt out: in parts where few rows would leave the chip empty, to large workgroups where there are
+// fewer than the chip has units.
+struct ScorePlan {
+  int n_parts, part_len, waves;
+};
+ScorePlan plan_scores(int64_t n_rows, int64_t vocab, int piece) {
+  ScorePlan p;
+  p.n_parts = static_cast<int>(std::max<int64_t>(std::min<int64_t>({kScoreParts, 512 / std::max<int64_t>(n_rows, 1), vocab / 16384}), 1));
+  p.part_len = static_cast<int>(vocab);
+  if (p.n_parts > 1) {
+    const int64_t unit = 64 * piece;   // (no part is empty: 64 * 8 * 16 is less than a part)
+    p.part_len = static_cast<int>((vocab + p.n_parts * unit - 1) / (p.n_parts * unit) * unit);
+    p.n_parts = static_cast<int>((vocab + p.part_len - 1) / p.part_len);
+  }
+  p.waves = n_rows * p.n_parts <= 512 ? 16 : 4;
+  return p;
+}
+
+template <typename T>
+int launch_scores(hipStream_t st, const TokenScores &a, const ScorePlan &p, const T *logits) {
+  const dim3 grid(static_cast<unsigned>(a.n_rows) * p.n_parts);
+  if (p.waves == 16) hipLaunchKernelGGL((k_token_scores<T, 16>), grid, dim3(1024), 0, st, a, logits);
+  else hipLaunchKernelGGL((k_token_scores<T, 4>), grid, dim3(256), 0, st, a, logits);
+  HSD_LAUNCH_CHECK();
+  if (p.n_parts > 1) {
+    hipLaunchKernelGGL((k_token_scores_join<T>), dim3(a.n_rows), dim3(256), 0, st, a, logits);
     HSD_LAUNCH_CHECK();
   }
   return HSD_OK;
@@ -184,25 +215,24 @@ int hsd_kv_quant_attention(void *stream, const hsd_kv_quant *kv, const hsd_batch
 
 size_t hsd_token_logprobs_bytes(int32_t n_rows, int32_t vocab, int32_t n_top) {
   if (n_rows < 0 || vocab < 1 || n_top < 0 || n_top > HSD_MAX_TOP) return 0;
-  return 256;
+  const int parts = plan_scores(n_rows, vocab, 4).n_parts;
+  return 256 + (parts > 1 ? static_cast<size_t>(n_rows) * parts * (sizeof(float4) + n_top * sizeof(uint64_t)) : 0);
 }
 
 int hsd_token_logprobs(void *stream, int32_t n_rows, int32_t vocab, int32_t dtype, const void *logits, int64_t row_stride, const int32_t *tokens,
                        float *logprob, float *entropy, int32_t n_top, int32_t *top_ids, float *top_logprobs, void *ws, size_t ws_bytes) {
   if (n_rows < 0 || vocab < 1 || n_top < 0 || !is_type(dtype) || row_stride < vocab) return HSD_EINVAL;
-  if (n_top > HSD_MAX_TOP) return HSD_ERANGE;
+  if (n_top > HSD_MAX_TOP || vocab > (1 << 30)) return HSD_ERANGE;
   if (n_rows == 0) return HSD_OK;
   if (logits == nullptr || tokens == nullptr || logprob == nullptr || entropy == nullptr || !is_workspace(ws)) return HSD_EINVAL;
   if (n_top > 0 && (top_ids == nullptr || top_logprobs == nullptr)) return HSD_EINVAL;
   if (ws_bytes < hsd_token_logprobs_bytes(n_rows, vocab, n_top)) return HSD_ENOSPC;
-  const TokenScores a{n_rows, vocab, n_top, row_stride, tokens, logprob, entropy, top_logprobs, top_ids};
+  const ScorePlan p = plan_scores(n_rows, vocab, dtype == HSD_BF16 ? 8 : 4);
+  float4 *sums = static_cast<float4 *>(ws);
+  const TokenScores a{n_rows, vocab, n_top, p.n_parts, p.part_len, row_stride, tokens, logprob, entropy, top_logprobs, top_ids, sums,
+                      reinterpret_cast<uint64_t *>(sums + static_cast<size_t>(n_rows) * p.n_parts)};
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if (dtype == HSD_BF16)
-    hipLaunchKernelGGL((k_token_scores<bf16>), dim3(n_rows), dim3(256), 0, st, a, static_cast<const bf16 *>(logits));
-  else
-    hipLaunchKernelGGL((k_token_scores<float>), dim3(n_rows), dim3(256), 0, st, a, static_cast<const float *>(logits));
-  HSD_LAUNCH_CHECK();
-  return HSD_OK;
+  return dtype == HSD_BF16 ? launch_scores(st, a, p, static_cast<const bf16 *>(logits)) : launch_scores(st, a, p, static_cast<const float *>(logits));
 }
 
 }  // extern "C"

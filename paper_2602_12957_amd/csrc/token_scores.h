@@ -1,4 +1,14 @@
 // Scores of given tokens under rows of logits: log probability, entropy of the row, its most probable tokens.
+//
+// The row is read once.  A thread keeps a reference m that is one of its logits, within kScoreSlack of the largest so far, and
+//   Z = sum e^(x - m),   W = sum (x - m) e^(x - m)      (fp32; a -inf logit adds nothing)
+// which two threads with references m, m' join as Z + Z' e^(m' - m), W + (W' + (m' - m) Z') e^(m' - m); in the end
+// log p(t) = x_t - m - ln Z and the entropy is ln Z - W / Z.
+//
+// Alternatives.  A lane (the same lane of all waves) keeps the largest value it has seen and the 16-byte piece of the row in which
+// it saw it first.  The k-th largest of these 64 (value, piece) pairs bounds the k-th largest logit from below, and what
+// reaches it lies with the k lanes that have such a pair: only their pieces are read again, k / 64 of the row, from the cache.
+// What reaches the bound is listed in LDS (little more than k entries unless large logits lie 64 pieces apart) and ranked.
 #pragma once
 
 #include "common.h"
@@ -6,77 +16,259 @@
 namespace hsd {
 
 struct TokenScores {
-  int n_rows, vocab, n_top;
+  int n_rows, vocab, n_top, n_parts, part_len;   // a row in n_parts parts of part_len logits (a multiple of 64 pieces), the last shorter
   int64_t stride;
   const int32_t *tokens;
   float *logprob, *entropy, *top_logprob;
   int32_t *top_id;
+  float4 *part_sums;     // [n_rows][n_parts]: m (-inf: no logit), Z, W
+  uint64_t *part_top;    // [n_rows][n_parts][n_top]
 };
 
-// (value, index) order of the alternatives: larger value first, lower index among equals
-__device__ __forceinline__ bool score_before(float va, int ia, float vb, int ib) { return va > vb || (va == vb && ia < ib); }
+constexpr float kScoreSlack = 8.f;   // natural orders by which a logit may exceed the reference before that moves
+constexpr int kScoreList = 512;      // entries of the list in LDS
 
-// One workgroup a row.  m = max x, Z = sum e^(x - m), W = sum (x - m) e^(x - m): log p = x - m - ln Z, entropy = ln Z - W / Z.
-// grid: n_rows, block 256
-template <typename T>
-__global__ void __launch_bounds__(256) k_token_scores(TokenScores a, const T *__restrict__ logits) {
-  __shared__ float s_v[4], s_w[4];
-  __shared__ int s_i[4];
-  const int r = blockIdx.x, t = threadIdx.x, wave = t >> 6, lane = t & 63;
-  const T *x = logits + r * a.stride;
-  float m = -INFINITY;
-  for (int i = t; i < a.vocab; i += 256) m = fmaxf(m, to_f32(x[i]));
-  m = wave_max(m);
-  if (lane == 0) s_v[wave] = m;
-  __syncthreads();
-  m = fmaxf(fmaxf(s_v[0], s_v[1]), fmaxf(s_v[2], s_v[3]));
-  __syncthreads();
-  float z = 0.f, w = 0.f;
-  for (int i = t; i < a.vocab; i += 256) {
-    const float v = to_f32(x[i]);
-    if (v == -INFINITY) continue;
-    const float d = v - m, e = expf(d);
-    z += e;
-    if (!(e <= 0.f)) w = fmaf(d, e, w);
+// Keys whose order is that of the alternatives: larger value first, the lower index among equals.  0: none.
+__device__ __forceinline__ uint64_t score_key(float v, int i) {
+  const uint32_t u = __float_as_uint(v + 0.f);   // (-0 and 0 are equal)
+  const uint32_t o = (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+  return (static_cast<uint64_t>(o) << 32) | (0xffffffffu - static_cast<uint32_t>(i));
+}
+__device__ __forceinline__ float key_value(uint64_t k) {
+  const uint32_t o = static_cast<uint32_t>(k >> 32);
+  return __uint_as_float((o & 0x80000000u) ? (o & 0x7fffffffu) : ~o);
+}
+__device__ __forceinline__ int key_index(uint64_t k) { return static_cast<int>(0xffffffffu - static_cast<uint32_t>(k)); }
+
+// A piece: 16 bytes of a row, aligned to its elements
+__device__ __forceinline__ void load_piece(const float *p, float (&x)[4]) {
+  typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
+  const f4 v = *reinterpret_cast<const f4 *>(p);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = v[i];
+}
+__device__ __forceinline__ void load_piece(const bf16 *p, float (&x)[8]) {
+  typedef uint32_t u4 __attribute__((ext_vector_type(4), aligned(2)));
+  const u4 v = *reinterpret_cast<const u4 *>(p);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(v[i] << 16), x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+}
+template <typename T, int E>
+__device__ __forceinline__ void piece_at(const T *x, int piece, int len, float (&v)[E]) {
+  const int i0 = piece * E;
+  if (i0 + E <= len) {
+    load_piece(x + i0, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = i0 + e < len ? to_f32(x[i0 + e]) : -INFINITY;
   }
-  z = wave_sum(z), w = wave_sum(w);
-  if (lane == 0) s_v[wave] = z, s_w[wave] = w;
+}
+
+struct ScoreSum {
+  float m, z, w;
+};
+__device__ __forceinline__ ScoreSum score_join(const ScoreSum &a, const ScoreSum &b) {
+  const float m = fmaxf(a.m, b.m);
+  ScoreSum r{m, 0.f, 0.f};
+  auto add = [&](const ScoreSum &s) {
+    if (s.m == -INFINITY) {   // no logit: 0, or NaN where there was a NaN
+      r.z += s.z;
+      return;
+    }
+    const float d = s.m - m, f = expf(d);
+    r.z += s.z * f;
+    if (f != 0.f) r.w += (s.w + d * s.z) * f;
+  };
+  add(a), add(b);
+  return r;
+}
+
+// What a row's sums give; v: the token's logit, -inf for none
+__device__ __forceinline__ void score_write(const TokenScores &a, int r, const ScoreSum &s, bool inside, float v) {
+  const float lz = logf(s.z);
+  a.logprob[r] = inside && s.z != s.z ? s.z : (v == -INFINITY ? v : v - s.m - lz);
+  a.entropy[r] = s.m == -INFINITY && s.z == 0.f ? 0.f : lz - s.w / s.z;
+}
+__device__ __forceinline__ void score_write_top(const TokenScores &a, int r, const ScoreSum &s, int rank, uint64_t key) {
+  const size_t at = static_cast<size_t>(r) * a.n_top + rank;
+  a.top_id[at] = key == 0 ? -1 : key_index(key);
+  a.top_logprob[at] = key == 0 ? -INFINITY : key_value(key) - s.m - logf(s.z);
+}
+
+// grid: n_rows * n_parts, block 64 * NW
+template <typename T, int NW>
+__global__ void __launch_bounds__(64 * NW) k_token_scores(TokenScores a, const T *__restrict__ logits) {
+  constexpr int E = 16 / sizeof(T), U = 4;
+  __shared__ ScoreSum s_sum[NW];
+  __shared__ uint64_t s_best[NW][64], s_list[kScoreList], s_bound, s_next[NW];
+  __shared__ int s_win[64], s_n, s_winners;
+  const int r = blockIdx.x / a.n_parts, part = blockIdx.x - r * a.n_parts, t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63;
+  const int first = part * a.part_len, len = min(a.part_len, a.vocab - first);
+  const T *x = logits + r * a.stride + first;
+  const int n_pieces = (len + E - 1) / E;
+  // the token's logit, ahead of everything else
+  const int tok = a.tokens[r];
+  const bool inside = tok >= 0 && tok < a.vocab;
+  const float tv = inside && a.n_parts == 1 ? to_f32(x[tok]) : -INFINITY;
+
+  ScoreSum s{0.f, 0.f, 0.f};   // (m: 0 while nothing was seen, thr then -inf)
+  float thr = -INFINITY, best = -INFINITY;
+  int best_piece = 0;
+  for (int p0 = t; p0 < n_pieces; p0 += 64 * NW * U) {
+    float v[U][E], top[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int p = p0 + u * 64 * NW;
+      if (p < n_pieces) {
+        piece_at(x, p, len, v[u]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[u][e] = -INFINITY;
+      }
+    }
+    float all = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      top[u] = v[u][0];
+#pragma unroll
+      for (int e = 1; e < E; ++e) top[u] = fmaxf(top[u], v[u][e]);
+      if (top[u] > best) best = top[u], best_piece = p0 + u * 64 * NW;
+      all = fmaxf(all, top[u]);
+    }
+    if (all > thr) {
+      const float d = s.m - all, f = thr == -INFINITY ? 0.f : expf(d);
+      s.w = f != 0.f ? (s.w + d * s.z) * f : 0.f;
+      s.z = thr == -INFINITY ? s.z : s.z * f;
+      s.m = all, thr = all + kScoreSlack;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float d = v[u][e] - s.m, p = __builtin_amdgcn_exp2f(d * 1.4426950408889634f);
+        s.z += p;                                   // NaN where the logit is
+        s.w = fmaf(fmaxf(d, -200.f), p, s.w);       // (below -200 p is 0)
+      }
+  }
+  if (thr == -INFINITY) s.m = -INFINITY;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) s = score_join(s, ScoreSum{__shfl_xor(s.m, o, kWave), __shfl_xor(s.z, o, kWave), __shfl_xor(s.w, o, kWave)});
+  if (lane == 0) s_sum[wave] = s;
+  s_best[wave][lane] = best == -INFINITY ? 0 : score_key(best, best_piece);
+  if (t == 0) s_n = 0;
   __syncthreads();
-  z = s_v[0] + s_v[1] + s_v[2] + s_v[3], w = s_w[0] + s_w[1] + s_w[2] + s_w[3];
-  const float lz = logf(z);
+  s = s_sum[0];
+#pragma unroll
+  for (int w = 1; w < NW; ++w) s = score_join(s, s_sum[w]);
+  const bool whole = a.n_parts == 1;
+  const size_t at = static_cast<size_t>(r) * a.n_parts + part;
+  if (t == 0) {
+    if (whole) score_write(a, r, s, inside, tv);
+    else a.part_sums[at] = float4{s.m, s.z, s.w, 0.f};
+  }
+  if (a.n_top == 0) return;
+
+  // the bound and the lanes that reach it
+  if (wave == 0) {
+    uint64_t key = s_best[0][lane];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) key = max(key, s_best[w][lane]);
+    int rank = 0;
+#pragma unroll 8
+    for (int j = 0; j < 64; ++j) {
+      const uint64_t o = (static_cast<uint64_t>(__builtin_amdgcn_readlane(static_cast<uint32_t>(key >> 32), j)) << 32) |
+                         static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<uint32_t>(key), j));
+      rank += o > key;
+    }
+    const int n = min(__popcll(__ballot(key != 0)), a.n_top);
+    if (key != 0 && rank < n) {
+      s_win[rank] = lane;
+      if (rank == n - 1) s_bound = key;
+    }
+    if (lane == 0) s_winners = n;
+  }
   __syncthreads();
+  const int winners = s_winners;
+  const uint64_t bound = winners < a.n_top ? 0 : s_bound;   // fewer lanes than alternatives: all their logits are listed
+  // listed: keys by value and piece not behind the bound (a piece's logits have its index there, so this errs on the safe side)
+  auto walk = [&](auto &&take) {
+    for (int i = wave; i < winners; i += NW) {
+      const int l = s_win[i];
+      for (int p = l + 64 * lane; p < n_pieces; p += 64 * 64) {
+        float v[E];
+        piece_at(x, p, len, v);
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (v[e] > -INFINITY && score_key(v[e], p) >= bound) take(score_key(v[e], first + p * E + e));
+      }
+    }
+  };
+  walk([&](uint64_t key) {
+    const int i = atomicAdd(&s_n, 1);
+    if (i < kScoreList) s_list[i] = key;
+  });
+  __syncthreads();
+  const int n = s_n;
+  auto emit = [&](int rank, uint64_t key) {
+    if (whole) score_write_top(a, r, s, rank, key);
+    else a.part_top[at * a.n_top + rank] = key;
+  };
+  if (n <= kScoreList) {
+    for (int i = t; i < n; i += 64 * NW) {
+      const uint64_t key = s_list[i];
+      int rank = 0;
+      for (int j = 0; j < n; ++j) rank += s_list[j] > key;
+      if (rank < a.n_top) emit(rank, key);
+    }
+    for (int i = n + t; i < a.n_top; i += 64 * NW) emit(i, 0);
+    return;
+  }
+  // more than the list holds: one alternative after the other
+  uint64_t last = ~0ull;
+  for (int k = 0; k < a.n_top; ++k) {
+    uint64_t mine = 0;
+    walk([&](uint64_t key) {
+      if (key < last && key > mine) mine = key;
+    });
+    for (int o = 32; o > 0; o >>= 1) {
+      const uint64_t u = (static_cast<uint64_t>(__shfl_xor(static_cast<uint32_t>(mine >> 32), o, kWave)) << 32) |
+                         static_cast<uint32_t>(__shfl_xor(static_cast<uint32_t>(mine), o, kWave));
+      mine = max(mine, u);
+    }
+    if (lane == 0) s_next[wave] = mine;
+    __syncthreads();
+    last = s_next[0];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) last = max(last, s_next[w]);
+    __syncthreads();
+    if (t == 0) emit(k, last);
+  }
+}
+
+// The parts of a row together.  grid: n_rows, block 256
+constexpr int kScoreParts = 16;
+template <typename T>
+__global__ void __launch_bounds__(256) k_token_scores_join(TokenScores a, const T *__restrict__ logits) {
+  __shared__ uint64_t s_key[kScoreParts * HSD_MAX_TOP];
+  const int r = blockIdx.x, t = threadIdx.x;
+  ScoreSum s{-INFINITY, 0.f, 0.f};
+  for (int p = 0; p < a.n_parts; ++p) {
+    const float4 v = a.part_sums[static_cast<size_t>(r) * a.n_parts + p];
+    s = score_join(s, ScoreSum{v.x, v.y, v.z});
+  }
   if (t == 0) {
     const int tok = a.tokens[r];
     const bool inside = tok >= 0 && tok < a.vocab;
-    const float v = inside ? to_f32(x[tok]) : -INFINITY;
-    a.logprob[r] = inside && z != z ? z : (v == -INFINITY ? v : v - m - lz);
-    a.entropy[r] = m == -INFINITY && z == 0.f ? 0.f : lz - w / z;
+    score_write(a, r, s, inside, inside ? to_f32(logits[r * a.stride + tok]) : -INFINITY);
   }
-  float pv = INFINITY;
-  int pi = -1;
-  for (int j = 0; j < a.n_top; ++j) {
-    float bv = -INFINITY;
-    int bi = 0x7fffffff;
-    for (int i = t; i < a.vocab; i += 256) {
-      const float v = to_f32(x[i]);
-      if (score_before(pv, pi, v, i) && score_before(v, i, bv, bi)) bv = v, bi = i;
-    }
-    for (int o = 32; o > 0; o >>= 1) {
-      const float ov = __shfl_xor(bv, o, kWave);
-      const int oi = __shfl_xor(bi, o, kWave);
-      if (score_before(ov, oi, bv, bi)) bv = ov, bi = oi;
-    }
-    if (lane == 0) s_v[wave] = bv, s_i[wave] = bi;
-    __syncthreads();
-    for (int u = 0; u < 4; ++u)
-      if (score_before(s_v[u], s_i[u], bv, bi)) bv = s_v[u], bi = s_i[u];
-    __syncthreads();
-    const bool none = bv == -INFINITY;
-    if (t == 0) {
-      a.top_id[static_cast<size_t>(r) * a.n_top + j] = none ? -1 : bi;
-      a.top_logprob[static_cast<size_t>(r) * a.n_top + j] = none ? -INFINITY : bv - m - lz;
-    }
-    pv = bv, pi = none ? 0x7fffffff : bi;
+  const int n = a.n_parts * a.n_top;
+  for (int i = t; i < n; i += 256) s_key[i] = a.part_top[static_cast<size_t>(r) * n + i];
+  __syncthreads();
+  for (int i = t; i < n; i += 256) {
+    const uint64_t key = s_key[i];
+    int rank = 0;
+    for (int j = 0; j < n; ++j) rank += s_key[j] > key || (key == 0 && s_key[j] == 0 && j < i);   // (empty places in order)
+    if (rank < a.n_top) score_write_top(a, r, s, rank, key);
   }
 }
 

@@ -151,3 +151,25 @@ def test_a_captured_call_replays_and_two_streams_agree():
         torch.cuda.synchronize()
         for o in outs:
             assert all(torch.equal(a, b) for a, b in zip(o, have)), rep
+
+
+@pytest.mark.parametrize("dtype,step", [(torch.bfloat16, 512), (torch.float32, 256)])
+@pytest.mark.parametrize("rows", [2, 700])
+def test_large_logits_64_pieces_apart(dtype, step, rows):
+    """The largest logits at one lane's places: more of them reach the bound than the list holds."""
+    rng = np.random.default_rng(6)
+    vocab = 40 * step + 3
+    x = rng.standard_normal((rows, vocab))
+    for e in range(step // 64):
+        for lane in range(32):
+            x[:, lane * (step // 64) + e::step] += 30.0 + 0.001 * lane
+    logits = torch.from_numpy(x).to(dtype).cuda()
+    check(logits, torch.zeros(rows, dtype=torch.int32, device="cuda"), 32)
+    check(logits, torch.zeros(rows, dtype=torch.int32, device="cuda"), 5)
+
+
+def test_many_rows():
+    """More rows than a grid's second dimension takes."""
+    rng = np.random.default_rng(7)
+    logits, tokens = make(rng, 70000, 40, torch.float32)
+    check(logits, tokens, 3)
