@@ -344,7 +344,8 @@ int hsd_kv_quant_read(void *stream, const hsd_kv_quant *kv, int32_t n_rows, cons
  * elements; softmax_scale multiplies the products (0.125 for 64 dimensions).  A position whose table entry holds no valid block is left
  * out; a row that sees none becomes 0.  Softmax and sums in fp32; bf16 models round the probabilities to bf16 for the product
  * with the values (and divide by the sum of the rounded ones).  The same call gives the same bits; another batch around a row may
- * change how its keys are split and with it the last bits.  workspace: hsd_kv_quant_attention_bytes(kv, batch, n_q_heads) bytes, 256-byte aligned. */
+ * change how its keys are split and with it the last bits.  workspace: hsd_kv_quant_attention_bytes(kv, batch, n_q_heads)
+ * bytes, 256-byte aligned; NULL if that is 0 (which it also is where the call would refuse its arguments). */
 size_t hsd_kv_quant_attention_bytes(const hsd_kv_quant *kv, const hsd_batch *batch, int32_t n_q_heads);
 int hsd_kv_quant_attention(void *stream, const hsd_kv_quant *kv, const hsd_batch *batch, int32_t n_q_heads, int32_t dtype,
                            float softmax_scale, const void *q, int64_t q_stride, void *out, int64_t out_stride,
@@ -355,7 +356,8 @@ int hsd_kv_quant_attention(void *stream, const hsd_kv_quant *kv, const hsd_batch
  * most probable tokens, largest first, the lower id first among equal logits: top_ids, top_logprobs dev [n_rows][n_top].
  * A logit of -inf is a probability of 0 and never an alternative (places left over hold id -1 and -inf); a row without any other
  * logit has logprob -inf and entropy 0.  With a NaN or +inf among its logits a row's logprob (of a token inside the vocabulary), entropy and top_logprobs are NaN,
- * and its alternatives are taken from the logits that are numbers.  0 <= n_top <= HSD_MAX_TOP.  workspace: hsd_token_logprobs_bytes bytes, 256-byte aligned. */
+ * and its alternatives are taken from the logits that are numbers.  0 <= n_top <= HSD_MAX_TOP.  workspace: hsd_token_logprobs_bytes bytes, 256-byte
+ * aligned; NULL if that is 0. */
 enum { HSD_MAX_TOP = 32 };
 size_t hsd_token_logprobs_bytes(int32_t n_rows, int32_t vocab, int32_t n_top);
 int hsd_token_logprobs(void *stream, int32_t n_rows, int32_t vocab, int32_t dtype, const void *logits, int64_t row_stride,

@@ -49,6 +49,24 @@ class hsd_batch(C.Structure):
                 ("log_tau", f32), ("draft_gap", vp), ("tree_end", vp), ("tree_depth", vp), ("stop_row", vp)]
 
 
+class _NoSwitch:
+    def __enter__(self): pass
+    def __exit__(self, *exc): pass
+
+
+_no_switch = _NoSwitch()
+
+
+def current_stream(index):
+    """Handle of torch's current stream on GPU `index`, as the calls take it."""
+    return torch._C._cuda_getCurrentRawStream(index)
+
+
+def on_device(index):
+    """GPU `index` as the current one, for the calls that launch on it (nothing to do where it is that already)."""
+    return _no_switch if torch._C._cuda_getDevice() == index else torch.cuda.device(index)
+
+
 class hsd_kv_quant(C.Structure):
     _fields_ = [("k_codes", vp), ("v_codes", vp), ("k_scale", vp), ("v_scale", vp), ("n_blocks", i32), ("n_kv_heads", i32)]
 
@@ -165,19 +183,24 @@ def hsd_tree_path(tokens, tree_end, stop, alpha, path):
     check("hsd_tree_path", lib.hsd_tree_path(tokens.ctypes.data, tree_end.ctypes.data, len(tokens), stop, alpha, path.ctypes.data))
 
 def hsd_kv_reserve(stream, pool, batch, row_slot, row_pos):
-    check("hsd_kv_reserve", lib.hsd_kv_reserve(stream, C.byref(pool), C.byref(batch), row_slot, row_pos))
+    rc = lib.hsd_kv_reserve(stream, pool, batch, row_slot, row_pos)
+    if rc: check("hsd_kv_reserve", rc)
 def hsd_kv_commit_rows(stream, pool, batch):
-    check("hsd_kv_commit_rows", lib.hsd_kv_commit_rows(stream, C.byref(pool), C.byref(batch)))
+    rc = lib.hsd_kv_commit_rows(stream, pool, batch)
+    if rc: check("hsd_kv_commit_rows", rc)
 def hsd_kv_quant_append(stream, kv, n_rows, row_slot, dtype, k, v, k_stride, v_stride, status):
-    check("hsd_kv_quant_append", lib.hsd_kv_quant_append(stream, C.byref(kv), n_rows, row_slot, dtype, k, v, k_stride, v_stride, status))
+    rc = lib.hsd_kv_quant_append(stream, kv, n_rows, row_slot, dtype, k, v, k_stride, v_stride, status)
+    if rc: check("hsd_kv_quant_append", rc)
 def hsd_kv_quant_read(stream, kv, n_rows, row_slot, dtype, k, v, k_stride, v_stride):
-    check("hsd_kv_quant_read", lib.hsd_kv_quant_read(stream, C.byref(kv), n_rows, row_slot, dtype, k, v, k_stride, v_stride))
+    rc = lib.hsd_kv_quant_read(stream, kv, n_rows, row_slot, dtype, k, v, k_stride, v_stride)
+    if rc: check("hsd_kv_quant_read", rc)
 def hsd_kv_quant_attention_bytes(kv, batch, n_q_heads):
-    return lib.hsd_kv_quant_attention_bytes(C.byref(kv), C.byref(batch), n_q_heads)
+    return lib.hsd_kv_quant_attention_bytes(kv, batch, n_q_heads)
 def hsd_kv_quant_attention(stream, kv, batch, n_q_heads, dtype, scale, q, q_stride, out, out_stride, ws, ws_bytes):
-    check("hsd_kv_quant_attention", lib.hsd_kv_quant_attention(stream, C.byref(kv), C.byref(batch), n_q_heads, dtype, scale, q, q_stride,
-                                                               out, out_stride, ws, ws_bytes))
+    rc = lib.hsd_kv_quant_attention(stream, kv, batch, n_q_heads, dtype, scale, q, q_stride, out, out_stride, ws, ws_bytes)
+    if rc: check("hsd_kv_quant_attention", rc)
 def hsd_token_logprobs_bytes(n_rows, vocab, n_top): return lib.hsd_token_logprobs_bytes(n_rows, vocab, n_top)
 def hsd_token_logprobs(stream, n_rows, vocab, dtype, logits, row_stride, tokens, logprob, entropy, n_top, top_ids, top_logprobs, ws, ws_bytes):
-    check("hsd_token_logprobs", lib.hsd_token_logprobs(stream, n_rows, vocab, dtype, logits, row_stride, tokens, logprob, entropy, n_top,
-                                                       top_ids, top_logprobs, ws, ws_bytes))
+    rc = lib.hsd_token_logprobs(stream, n_rows, vocab, dtype, logits, row_stride, tokens, logprob, entropy, n_top, top_ids, top_logprobs, ws,
+                                ws_bytes)
+    if rc: check("hsd_token_logprobs", rc)

@@ -40,27 +40,22 @@ __device__ __forceinline__ int tile_start(int cu, int s, int group, int cols) { 
 struct QuantTile {
   int slot, S, n, base, j;   // state row, cached length, rows, first packed row, tile within the sequence
 };
-// Sequence and place of tile t; n = 0 where the tile has no columns
+// Sequence and place of tile t: a search by 64 lanes at a time (one round up to 64 sequences, two up to 4096)
 __device__ __forceinline__ QuantTile find_tile(const QuantAttn &a, int t, int cols, int lane) {
-  int first = 0, stride = (a.n_seq + kWave - 1) / kWave;
-  QuantTile q;
-  for (;; stride = (stride + kWave - 1) / kWave) {
-    const int s = first + lane * stride;
-    const bool in = s < a.n_seq;
-    const int cu = in ? a.cu_q[s] : 0;
-    const unsigned long long m = __ballot(in && tile_start(cu, s, a.group, cols) <= t);
-    const int hit = 63 - __builtin_clzll(m);   // (tile 0 starts at sequence 0: m has bit 0)
-    if (stride == 1) {
-      const int end = in ? a.cu_q[s + 1] : 0, slot = in ? slot_of(a.seq_slot, s, a.n_slots) : 0, len = a.seq_len[slot];
-      q.base = __builtin_amdgcn_readlane(cu, hit);
-      q.n = __builtin_amdgcn_readlane(end, hit) - q.base;
-      q.slot = __builtin_amdgcn_readlane(slot, hit);
-      q.S = max(__builtin_amdgcn_readlane(len, hit), 0);
-      q.j = t - tile_start(q.base, first + hit, a.group, cols);
-      break;
-    }
-    first += hit * stride;
+  int first = 0;
+  if (a.n_seq > kWave) {
+    const int stride = (a.n_seq + kWave - 1) / kWave, s = lane * stride;
+    first = (63 - __builtin_clzll(__ballot(s < a.n_seq && tile_start(a.cu_q[min(s, a.n_seq)], s, a.group, cols) <= t))) * stride;
   }
+  const int s = min(first + lane, a.n_seq - 1);
+  const int cu = a.cu_q[s], end = a.cu_q[s + 1], slot = slot_of(a.seq_slot, s, a.n_slots), len = a.seq_len[slot];
+  const int hit = 63 - __builtin_clzll(__ballot(first + lane < a.n_seq && tile_start(cu, s, a.group, cols) <= t));   // (lane 0 always does)
+  QuantTile q;
+  q.base = __builtin_amdgcn_readlane(cu, hit);
+  q.n = __builtin_amdgcn_readlane(end, hit) - q.base;
+  q.slot = __builtin_amdgcn_readlane(slot, hit);
+  q.S = max(__builtin_amdgcn_readlane(len, hit), 0);
+  q.j = t - tile_start(q.base, first + hit, a.group, cols);
   return q;
 }
 
@@ -122,6 +117,11 @@ __global__ void __launch_bounds__(64 * quant_attn_waves(std::is_same<T, float>::
   const int W = blockDim.x >> 6, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = blockIdx.x / a.n_tiles, tile = a.n_tiles - 1 - blockIdx.x % a.n_tiles, z = blockIdx.y;
   const QuantTile qt = find_tile(a, tile, C, lane);
+  const int32_t *table = a.block_table + static_cast<size_t>(qt.slot) * a.max_blocks;
+  // ids of the pages of 32 steps from pair p0 on: lane 2 i + p has page p of step i
+  auto page_of = [&](int pair0, int i0) { return 2 * (pair0 + w + W * (i0 + (lane >> 1))) + (lane & 1); };
+  auto fetch = [&](int page) { return table[min(page, a.max_blocks - 1)]; };
+  int id0 = fetch(page_of(0, 0));   // (the first ones ahead of the length where the walk starts at the first page)
   const int n_cols = qt.n * a.group - qt.j * C;   // columns from this tile's first on
   if (n_cols <= 0) return;
   const int n_keys = tile_keys(a, qt, C), n_pages = (n_keys + kBlk - 1) / kBlk, n_pairs = (n_pages + 1) / 2;
@@ -143,104 +143,115 @@ __global__ void __launch_bounds__(64 * quant_attn_waves(std::is_same<T, float>::
   }
   const int lim_first = qt.S + qt.j * C / a.group;   // what every column sees
 
+  // Probabilities are 2^(scale s - ref).  ref is one of the column's scores, moved when one exceeds it by more than kRefSlack orders
+  // (fp32 sums and bf16 probabilities have room for that), and 0 as long as the column has seen nothing.
   floatx4 o[CT][4], l[CT];
-  float ref[CT], thr[CT];   // thr: ref + slack, -inf while the column has seen nothing (its ref is then 0)
+  float ref[CT];
+  bool seen[CT];
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) {
 #pragma unroll
     for (int t = 0; t < 4; ++t) o[ct][t] = floatx4{0.f, 0.f, 0.f, 0.f};
     l[ct] = floatx4{0.f, 0.f, 0.f, 0.f};
-    ref[ct] = 0.f, thr[ct] = -INFINITY;
+    ref[ct] = 0.f, seen[ct] = false;
   }
+  bool all_seen = false;   // every column of the wave has
   bf16x8 ones;
 #pragma unroll
   for (int e = 0; e < 8; ++e) ones[e] = static_cast<__bf16>(1.0f);
 
-  // ids and scales of the pages of 32 steps: lane 2 i + p has page p of step i
-  const int32_t *table = a.block_table + static_cast<size_t>(qt.slot) * a.max_blocks;
-  int id = -1;
+  int id = 0;
   float ksc = 1.f, vsc = 1.f;
+  unsigned long long bad = 0;   // bit l: the page of lane l has no valid block
   auto batch = [&](int i0) {
-    const int page = 2 * (p0 + w + W * (i0 + (lane >> 1))) + (lane & 1);
-    id = page < n_pages ? table[page] : -1;
-    if (id >= a.kv.n_blocks) id = -1;
-    const int at = max(id, 0) * a.kv.n_kv_heads + h;
-    ksc = a.kv.k_scale[at], vsc = a.kv.v_scale[at];
+    const int page = page_of(p0, i0);
+    id = i0 == 0 && p0 == 0 ? id0 : fetch(page);
+    const bool ok = page < n_pages && id >= 0 && id < a.kv.n_blocks;
+    bad = __ballot(!ok);
+    id = (ok ? id : 0) * a.kv.n_kv_heads + h;
+    ksc = a.kv.k_scale[id], vsc = a.kv.v_scale[id];
   };
   struct Step {
     u32x4 k[2], v[2];
     float ks[2], vs[2];
-    bool ok;
+    int bad;   // bit p: page p is left out
   };
   auto request = [&](int i, Step &s) {
     if (i >= n_steps) return;
     if ((i & 31) == 0) batch(i);
-    s.ok = true;
+    const int src = 2 * (i & 31);
+    s.bad = static_cast<int>(bad >> src) & 3;
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
-      const int src = 2 * (i & 31) + p, b = __builtin_amdgcn_readlane(id, src);
-      const size_t at = static_cast<size_t>(max(b, 0) * a.kv.n_kv_heads + h) * kPageCodes;
+      const size_t at = static_cast<size_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(id, src + p))) * kPageCodes;
       s.k[p] = reinterpret_cast<const u32x4 *>(a.kv.k_codes + at)[lane];
       s.v[p] = reinterpret_cast<const u32x4 *>(a.kv.v_codes + at)[lane];
-      s.ks[p] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ksc), src));
-      s.vs[p] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vsc), src));
-      if (b < 0) {
-        s.ok = false;
-        s.ks[p] = __uint_as_float(0x7fc00000u);   // marks the page: its positions are left out
-        s.v[p] = u32x4{0, 0, 0, 0};
-        s.vs[p] = 1.f;
-      }
+      s.ks[p] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ksc), src + p));
+      s.vs[p] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vsc), src + p));
     }
   };
-  auto step = [&](int i, const Step &s) {
+  auto step = [&](int i, Step &s) {
     if (i >= n_steps) return;
     const int pos0 = 32 * (p0 + w + W * i);
-    floatx4 sc[2][CT];
+    float x[CT][8];   // the exponents: tokens 4 g + e of the first page, then of the second
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
       const bf16x8 k0 = page_operand(s.k[p][0], s.k[p][1], s.ks[p], s.ks[p]), k1 = page_operand(s.k[p][2], s.k[p][3], s.ks[p], s.ks[p]);
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) {
-        floatx4 x = {0.f, 0.f, 0.f, 0.f};
+        floatx4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int n = NS - 1; n >= 0; --n) {
-          x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, qf[ct][0][n], x, 0, 0, 0);
-          x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, qf[ct][1][n], x, 0, 0, 0);
+          y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, qf[ct][0][n], y, 0, 0, 0);
+          y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, qf[ct][1][n], y, 0, 0, 0);
         }
-        sc[p][ct] = x * a.scale;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[ct][4 * p + e] = fmaf(y[e], a.scale, -ref[ct]);
       }
     }
-    if (!s.ok || pos0 + 31 > lim_first) {
-#pragma unroll
-      for (int p = 0; p < 2; ++p) {
-        const bool gone = s.ks[p] != s.ks[p];
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (gone || pos0 + 16 * p + 4 * g + e > lim[ct]) sc[p][ct][e] = -INFINITY;
-      }
-    }
-    float mx[CT];
-    bool move = false;
+    const bool masked = s.bad != 0 || pos0 + 31 > lim_first;
+    bool move = false;   // (as integers, positive floats keep their order and negative ones lie below them)
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
-      mx[ct] = fmaxf(fmaxf(fmaxf(sc[0][ct][0], sc[0][ct][1]), fmaxf(sc[0][ct][2], sc[0][ct][3])),
-                     fmaxf(fmaxf(sc[1][ct][0], sc[1][ct][1]), fmaxf(sc[1][ct][2], sc[1][ct][3])));
-      move = move || mx[ct] > thr[ct];
+      int m = __float_as_int(x[ct][0]);
+#pragma unroll
+      for (int e = 1; e < 8; ++e) m = max(m, __float_as_int(x[ct][e]));
+      move = move || m > __float_as_int(kRefSlack);
     }
-    if (__any(move)) {
+    if (masked || !all_seen || __any(move)) {
+      if (masked) {
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct) {
-        const float m = half_max(quarter_max(mx[ct]));
-        if (m > thr[ct]) {
-          const float f = thr[ct] == -INFINITY ? 0.f : exp2f(ref[ct] - m);
+        for (int p = 0; p < 2; ++p) {
+          const bool gone = (s.bad >> p) & 1;
+          if (gone) s.v[p] = u32x4{0, 0, 0, 0}, s.vs[p] = 1.f;
 #pragma unroll
-          for (int t = 0; t < 4; ++t) o[ct][t] *= f;
-          l[ct] *= f;
-          ref[ct] = m, thr[ct] = m + kRefSlack;
+          for (int ct = 0; ct < CT; ++ct) {
+            const int left = gone ? -1 : lim[ct] - (pos0 + 16 * p + 4 * g);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (e > left) x[ct][4 * p + e] = -INFINITY;
+          }
         }
       }
+      bool all = true;
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        float m = x[ct][0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) m = fmaxf(m, x[ct][e]);
+        m = half_max(quarter_max(m));
+        if (m > (seen[ct] ? kRefSlack : -INFINITY)) {
+          const float f = __builtin_amdgcn_exp2f(-m);   // (nothing seen: o and l are 0 or NaN, whatever f is, unless it is inf)
+#pragma unroll
+          for (int t = 0; t < 4; ++t) o[ct][t] = seen[ct] ? o[ct][t] * f : o[ct][t];
+          l[ct] = seen[ct] ? l[ct] * f : l[ct];
+          ref[ct] += m, seen[ct] = true;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[ct][e] -= m;
+        }
+        all = all && seen[ct];
+      }
+      all_seen = __all(all);
     }
     bf16x8 v[4];
 #pragma unroll
@@ -249,7 +260,7 @@ __global__ void __launch_bounds__(64 * quant_attn_waves(std::is_same<T, float>::
     for (int ct = 0; ct < CT; ++ct) {
       float p[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(sc[e >> 2][ct][e & 3] - ref[ct]);
+      for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(x[ct][e]);
       bf16x8 pf[NS];
       split8<NS>(p, pf);
 #pragma unroll
@@ -289,7 +300,7 @@ __global__ void __launch_bounds__(64 * quant_attn_waves(std::is_same<T, float>::
     for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        put(ct, i, lane, floatx4{o[ct][0][i], o[ct][1][i], o[ct][2][i], o[ct][3][i]}, thr[ct] == -INFINITY ? -INFINITY : ref[ct], l[ct][0]);
+        put(ct, i, lane, floatx4{o[ct][0][i], o[ct][1][i], o[ct][2][i], o[ct][3][i]}, seen[ct] ? ref[ct] : -INFINITY, l[ct][0]);
     return;
   }
   float *const ml = lds + W * CT * 1024;   // [wave][part of 16 columns][reference | sum][16]
@@ -299,7 +310,7 @@ __global__ void __launch_bounds__(64 * quant_attn_waves(std::is_same<T, float>::
     for (int i = 0; i < 4; ++i)
       *reinterpret_cast<floatx4 *>(lds + ((w * CT + ct) * 4 + i) * 256 + lane * 4) = floatx4{o[ct][0][i], o[ct][1][i], o[ct][2][i], o[ct][3][i]};
     if (lane < 16) {
-      ml[(w * CT + ct) * 32 + lane] = thr[ct] == -INFINITY ? -INFINITY : ref[ct];
+      ml[(w * CT + ct) * 32 + lane] = seen[ct] ? ref[ct] : -INFINITY;
       ml[(w * CT + ct) * 32 + 16 + lane] = l[ct][0];
     }
   }
@@ -320,34 +331,43 @@ __global__ void __launch_bounds__(64 * quant_attn_waves(std::is_same<T, float>::
   }
 }
 
-// The runs of a tile together, in order.  grid: n_tiles * n_kv_heads, block 256: 16 columns at a time, 16 lanes a column
+// The runs of a tile together, in order.  grid: (n_tiles * n_kv_heads, columns / 4), block 64: 16 lanes a column
+constexpr int kMaxSplits = 256;
 template <typename T>
-__global__ void __launch_bounds__(256) k_attn_quant_join(QuantAttn a, int cols, T *__restrict__ out) {
-  const int h = blockIdx.x / a.n_tiles, tile = blockIdx.x % a.n_tiles;
-  const QuantTile qt = find_tile(a, tile, cols, threadIdx.x & 63);
-  const int n_cols = qt.n * a.group - qt.j * cols;
-  if (n_cols <= 0) return;
+__global__ void __launch_bounds__(64) k_attn_quant_join(QuantAttn a, int cols, T *__restrict__ out) {
+  __shared__ float s_f[4][kMaxSplits];
+  const int h = blockIdx.x / a.n_tiles, tile = blockIdx.x % a.n_tiles, lane = threadIdx.x, i = lane & 15, lc = lane >> 4;
+  const QuantTile qt = find_tile(a, tile, cols, lane);
+  const int n_cols = qt.n * a.group - qt.j * cols, col = blockIdx.y * 4 + lc;
+  if (static_cast<int>(blockIdx.y) * 4 >= n_cols) return;
   const int n_pairs = ((tile_keys(a, qt, cols) + kBlk - 1) / kBlk + 1) / 2, run = run_pairs(n_pairs, a.n_splits);
   if (n_pairs <= run) return;   // written already
-  const int n = (n_pairs + run - 1) / run, dim = 4 * (threadIdx.x & 15);
-  for (int col = threadIdx.x >> 4; col < min(cols, n_cols); col += 16) {
-    const size_t at0 = (static_cast<size_t>(tile) * a.kv.n_kv_heads + h) * cols + col, step = static_cast<size_t>(a.n_tiles) * a.kv.n_kv_heads * cols;
-    float m = -INFINITY;
-    for (int z = 0; z < n; ++z) m = fmaxf(m, a.part_ml[at0 + z * step].x);
-    const float base = m == -INFINITY ? 0.f : m;
-    floatx4 x = {0.f, 0.f, 0.f, 0.f};
-    float sum = 0.f;
-    for (int z = 0; z < n; ++z) {
-      const float2 ml = a.part_ml[at0 + z * step];
-      const float f = exp2f(ml.x - base);
-      x += f * *reinterpret_cast<const floatx4 *>(a.part_o + (at0 + z * step) * kHd + dim);
-      sum += f * ml.y;
-    }
-    if (sum == 0.f) x = floatx4{0.f, 0.f, 0.f, 0.f};
-    else x /= sum;
-    const int f = qt.j * cols + col, row = f / a.group, hd = f - row * a.group;
-    store4(out + (qt.base + row) * a.o_stride + (h * a.group + hd) * kHd + dim, x);
+  const int n = (n_pairs + run - 1) / run;
+  const size_t step = static_cast<size_t>(a.n_tiles) * a.kv.n_kv_heads * cols;
+  const size_t at = (static_cast<size_t>(tile) * a.kv.n_kv_heads + h) * cols + min(col, n_cols - 1);
+  // a lane looks at every 16th run
+  float m = -INFINITY, sum = 0.f;
+  for (int z = i; z < n; z += 16) m = fmaxf(m, a.part_ml[at + z * step].x);
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, kWave));
+  const float base = m == -INFINITY ? 0.f : m;
+  for (int z = i; z < n; z += 16) {
+    const float2 ml = a.part_ml[at + z * step];
+    const float f = exp2f(ml.x - base);
+    s_f[lc][z] = f;
+    sum += f * ml.y;
   }
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) sum += __shfl_xor(sum, o, kWave);
+  __syncthreads();
+  floatx4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+  for (int z = 0; z < n; ++z) x += s_f[lc][z] * *reinterpret_cast<const floatx4 *>(a.part_o + (at + z * step) * kHd + 4 * i);
+  if (col >= n_cols) return;
+  if (sum == 0.f) x = floatx4{0.f, 0.f, 0.f, 0.f};
+  else x /= sum;
+  const int f = qt.j * cols + col, row = f / a.group, hd = f - row * a.group;
+  store4(out + (qt.base + row) * a.o_stride + (h * a.group + hd) * kHd + 4 * i, x);
 }
 
 }  // namespace hsd

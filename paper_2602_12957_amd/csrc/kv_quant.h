@@ -74,104 +74,158 @@ __device__ __forceinline__ void quant_store4(bf16 *p, const float *v) {   // (a 
                                   (__float_as_uint(v[2]) >> 16) | (__float_as_uint(v[3]) & 0xffff0000u)};
 }
 
-// A run: rows r, r + 1, .. whose places are consecutive slots of one block.  Returns the number of rows of the run that starts at
-// row r, or 0 where none starts (no place, or row r - 1 is part of the same run).  All lanes of a wave alike.
-__device__ __forceinline__ int run_at(const int32_t *row_slot, int n_rows, int r, int n_slots, int lane, int &slot) {
-  const int i = r - 1 + lane;
-  const int v = lane <= kBlk && i >= 0 && i < n_rows ? row_slot[i] : -1;
-  slot = __builtin_amdgcn_readlane(v, 1);
-  const int before = __builtin_amdgcn_readlane(v, 0);
-  if (slot < 0 || slot >= n_slots) return 0;
-  const int off = slot % kBlk;
-  if (off > 0 && before == slot - 1) return 0;
-  const bool ok = lane >= 1 && lane <= kBlk - off && v == slot + lane - 1;
-  return __ffsll(static_cast<long long>(~(__ballot(ok) >> 1))) - 1;
+// Eight consecutive elements
+__device__ __forceinline__ void quant_load8(const float *p, float *v) { quant_load4(p, v), quant_load4(p + 4, v + 4); }
+__device__ __forceinline__ void quant_load8(const bf16 *p, float *v) {
+  typedef uint32_t u4 __attribute__((ext_vector_type(4), aligned(2)));
+  const u4 x = *reinterpret_cast<const u4 *>(p);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(x[i] << 16), v[2 * i + 1] = __uint_as_float(x[i] & 0xffff0000u);
 }
+__device__ __forceinline__ void quant_store8(float *p, const float *v) { quant_store4(p, v), quant_store4(p + 4, v + 4); }
+__device__ __forceinline__ void quant_store8(bf16 *p, const float *v) {
+  typedef uint32_t u4 __attribute__((ext_vector_type(4), aligned(2)));
+  u4 x;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = (__float_as_uint(v[2 * i]) >> 16) | (__float_as_uint(v[2 * i + 1]) & 0xffff0000u);
+  *reinterpret_cast<u4 *>(p) = x;
+}
+
+// Runs: rows whose places are consecutive slots of one block.  A wave looks at rows r0 .. r0 + span - 1 (span <= 16) and takes
+// the runs that start there; one may reach 15 rows further.
+struct RowRuns {
+  int slot;                 // lane l: place of row r0 - 1 + l, l <= 32; -1 without one
+  unsigned long long start; // bit l: a run starts at row r0 - 1 + l
+  unsigned long long more;  // bit l: row r0 - 1 + l continues the run of the row before it
+  __device__ __forceinline__ RowRuns(const int32_t *row_slot, int n_rows, int r0, int span, int n_slots, int lane) {
+    const int r = r0 - 1 + lane;
+    slot = lane <= 32 && r >= 0 && r < n_rows ? row_slot[r] : -1;
+    if (slot >= n_slots) slot = -1;
+    const int before = __shfl_up(slot, 1, kWave);
+    const bool go = lane > 0 && slot >= 0 && slot % kBlk != 0 && before == slot - 1;
+    more = __ballot(go);
+    start = __ballot(lane >= 1 && lane <= span && slot >= 0 && !go);
+  }
+  // the first run that is left: its row, place and number of rows; removes it
+  __device__ __forceinline__ void take(int r0, int &row, int &place, int &n) {
+    const int l = __builtin_ctzll(start);
+    start &= start - 1;
+    row = r0 - 1 + l, place = __builtin_amdgcn_readlane(slot, l);
+    n = 1 + __builtin_ctzll(~(more >> (l + 1)));
+  }
+};
+// Rows of a wave: one where that gives no more waves than the chip holds in a few rounds (a run's loads wait for one another,
+// 16 runs in a row of 64 sequences' single tokens take 4 times as long), 16 beyond (a wave a row that finds no run costs its launch: 32772 rows
+// of 4 heads 22.5 us against 13).
+inline int run_span(int64_t n_rows, int heads) { return n_rows * heads <= 32768 ? 1 : 16; }
 
 // New rows into the pages.  One wave a run and kv head: what the page keeps of earlier tokens (slots before the run's first) and
 // the new rows make up the page; slots behind them become 0.
-// grid: (ceil(n_rows / 4), n_kv_heads), block 256
+// grid: (ceil(n_rows / (4 * span)), n_kv_heads), block 256
 template <typename T>
-__global__ void __launch_bounds__(256) k_quant_append(QuantKV kv, int n_rows, const int32_t *__restrict__ row_slot, const T *__restrict__ k,
+__global__ void __launch_bounds__(256) k_quant_append(QuantKV kv, int n_rows, int span, const int32_t *__restrict__ row_slot, const T *__restrict__ k,
                                                       const T *__restrict__ v, int64_t k_stride, int64_t v_stride, int32_t *status) {
   const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, h = blockIdx.y;
-  const int r = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (r >= n_rows) return;
-  int slot;
-  const int n = run_at(row_slot, n_rows, r, kv.n_blocks * kBlk, lane, slot);
-  if (n == 0) return;
-  const int off = slot % kBlk, page = slot / kBlk * kv.n_kv_heads + h;
-  uint4 *kp = reinterpret_cast<uint4 *>(kv.k_codes + static_cast<size_t>(page) * kPageCodes) + lane;
-  uint4 *vp = reinterpret_cast<uint4 *>(kv.v_codes + static_cast<size_t>(page) * kPageCodes) + lane;
-  uint4 kc{0, 0, 0, 0}, vc{0, 0, 0, 0};
-  float ks = 0.f, vs = 0.f;
-  if (off > 0) kc = *kp, vc = *vp, ks = kv.k_scale[page], vs = kv.v_scale[page];
-  float kx[16], vx[16];   // vx: [token][dim]
+  const int r0 = (blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * span;
+  if (r0 >= n_rows) return;
+  RowRuns runs(row_slot, n_rows, r0, span, kv.n_blocks * kBlk, lane);
   bool odd = false;
+  while (runs.start != 0) {
+    int r, place, n;
+    runs.take(r0, r, place, n);
+    const int off = place % kBlk, page = place / kBlk * kv.n_kv_heads + h;
+    u32x4 *kp = reinterpret_cast<u32x4 *>(kv.k_codes + static_cast<size_t>(page) * kPageCodes) + lane;
+    u32x4 *vp = reinterpret_cast<u32x4 *>(kv.v_codes + static_cast<size_t>(page) * kPageCodes) + lane;
+    float kx[16], vx[4][4];   // K: dims 16 g .. of token c; V: [token 4 g + j][dim 4 c + e]
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    // K: dims 16 g + 4 j .. of token c
-    const int i = c - off;
-    float x[4] = {0.f, 0.f, 0.f, 0.f};
-    if (i >= 0 && i < n) {
-      quant_load4(k + (r + i) * k_stride + h * kHd + 16 * g + 4 * j, x);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = quant_input(x[e], odd);
-    } else if (i < 0) {
-      dequant4((&kc.x)[j], ks, x);
+    for (int e = 0; e < 16; ++e) kx[e] = vx[e >> 2][e & 3] = 0.f;
+    const int ik = c - off;
+    if (ik >= 0 && ik < n) {
+      const T *p = k + (r + ik) * k_stride + h * kHd + 16 * g;
+      quant_load8(p, kx), quant_load8(p + 8, kx + 8);
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) kx[4 * j + e] = x[e];
-    // V: token 4 g + j, dims 4 c ..
-    const int iv = 4 * g + j - off;
-    float y[4] = {0.f, 0.f, 0.f, 0.f};
-    if (iv >= 0 && iv < n) {
-      quant_load4(v + (r + iv) * v_stride + h * kHd + 4 * c, y);
+    for (int j = 0; j < 4; ++j) {
+      const int iv = 4 * g + j - off;
+      if (iv >= 0 && iv < n) quant_load4(v + (r + iv) * v_stride + h * kHd + 4 * c, vx[j]);
+    }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] = quant_input(y[e], odd);
-    } else if (iv < 0) {
+    for (int e = 0; e < 16; ++e) {
+      kx[e] = quant_input(kx[e], odd);
+      vx[e >> 2][e & 3] = quant_input(vx[e >> 2][e & 3], odd);
+    }
+    if (off > 0) {
+      const u32x4 kc = *kp, vc = *vp;
+      const float ks = kv.k_scale[page], vs = kv.v_scale[page];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float z[4];
-        dequant4((&vc.x)[e], vs, z);
-        y[e] = z[j];
+      for (int j = 0; j < 4; ++j) {
+        float x[4], y[4];
+        dequant4(kc[j], ks, x), dequant4(vc[j], vs, y);   // (y: dim 4 c + j of tokens 4 g ..)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (c < off) kx[4 * j + e] = x[e];
+          if (4 * g + e < off) vx[e][j] = y[e];
+        }
       }
     }
+    float ka = 0.f, va = 0.f;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) vx[4 * j + e] = y[e];
+    for (int e = 0; e < 16; ++e) ka = fmaxf(ka, fabsf(kx[e])), va = fmaxf(va, fabsf(vx[e >> 2][e & 3]));
+    const int ke = scale_exp(wave_max(ka)), ve = scale_exp(wave_max(va));
+    const float ki = exp2_int(-ke), vi = exp2_int(-ve);
+    u32x4 kc, vc;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      kc[j] = quant4(kx[4 * j] * ki, kx[4 * j + 1] * ki, kx[4 * j + 2] * ki, kx[4 * j + 3] * ki);
+      vc[j] = quant4(vx[0][j] * vi, vx[1][j] * vi, vx[2][j] * vi, vx[3][j] * vi);
+    }
+    *kp = kc, *vp = vc;
+    if (lane == 0) kv.k_scale[page] = exp2_int(ke), kv.v_scale[page] = exp2_int(ve);
   }
-  float ka = 0.f, va = 0.f;
-#pragma unroll
-  for (int j = 0; j < 16; ++j) ka = fmaxf(ka, fabsf(kx[j])), va = fmaxf(va, fabsf(vx[j]));
-  const int ke = scale_exp(wave_max(ka)), ve = scale_exp(wave_max(va));
-  const float ki = exp2_int(-ke), vi = exp2_int(-ve);
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    (&kc.x)[j] = quant4(kx[4 * j] * ki, kx[4 * j + 1] * ki, kx[4 * j + 2] * ki, kx[4 * j + 3] * ki);
-    (&vc.x)[j] = quant4(vx[j] * vi, vx[4 + j] * vi, vx[8 + j] * vi, vx[12 + j] * vi);
-  }
-  *kp = kc, *vp = vc;
-  if (lane == 0) kv.k_scale[page] = exp2_int(ke), kv.v_scale[page] = exp2_int(ve);
   if (status != nullptr && __any(odd) && lane == 0) atomicOr(status, HSD_STATUS_NOT_FINITE);
 }
 
-// The values of rows back out of the pages; rows without a place become 0.  Grid and block as k_quant_append.
+// The values of rows back out of the pages; rows without a place become 0.  Runs, grid and block as for k_quant_append.
 template <typename T>
-__global__ void __launch_bounds__(256) k_quant_read(QuantKV kv, int n_rows, const int32_t *__restrict__ row_slot, T *__restrict__ k,
+__global__ void __launch_bounds__(256) k_quant_read(QuantKV kv, int n_rows, int span, const int32_t *__restrict__ row_slot, T *__restrict__ k,
                                                     T *__restrict__ v, int64_t k_stride, int64_t v_stride) {
-  const int lane = threadIdx.x & 63, h = blockIdx.y;
-  const int r = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (r >= n_rows) return;
-  const int slot = row_slot[r];
-  float kx = 0.f, vx = 0.f;
-  if (slot >= 0 && slot / kBlk < kv.n_blocks) {
-    const int tok = slot % kBlk, page = slot / kBlk * kv.n_kv_heads + h;
-    const size_t o = static_cast<size_t>(page) * kPageCodes;
-    kx = __builtin_amdgcn_cvt_f32_fp8(kv.k_codes[o + (lane >> 4) * 256 + tok * 16 + (lane & 15)], 0) * kv.k_scale[page];
-    vx = __builtin_amdgcn_cvt_f32_fp8(kv.v_codes[o + (tok >> 2) * 256 + (lane >> 2) * 16 + (lane & 3) * 4 + (tok & 3)], 0) * kv.v_scale[page];
+  const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, h = blockIdx.y;
+  const int r0 = (blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * span;
+  if (r0 >= n_rows) return;
+  RowRuns runs(row_slot, n_rows, r0, span, kv.n_blocks * kBlk, lane);
+  unsigned long long none = __ballot(lane >= 1 && lane <= span && r0 - 1 + lane < n_rows && runs.slot < 0);
+  while (none != 0) {
+    const int r = r0 - 1 + __builtin_ctzll(none);
+    none &= none - 1;
+    k[r * k_stride + h * kHd + lane] = from_f32<T>(0.f);
+    v[r * v_stride + h * kHd + lane] = from_f32<T>(0.f);
   }
-  k[r * k_stride + h * kHd + lane] = from_f32<T>(kx);
-  v[r * v_stride + h * kHd + lane] = from_f32<T>(vx);
+  while (runs.start != 0) {
+    int r, place, n;
+    runs.take(r0, r, place, n);
+    const int off = place % kBlk, page = place / kBlk * kv.n_kv_heads + h;
+    const u32x4 kc = reinterpret_cast<const u32x4 *>(kv.k_codes + static_cast<size_t>(page) * kPageCodes)[lane];
+    const u32x4 vc = reinterpret_cast<const u32x4 *>(kv.v_codes + static_cast<size_t>(page) * kPageCodes)[lane];
+    const float ks = kv.k_scale[page], vs = kv.v_scale[page];
+    float kx[16], vx[4][4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float y[4];
+      dequant4(kc[j], ks, kx + 4 * j), dequant4(vc[j], vs, y);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) vx[e][j] = y[e];
+    }
+    const int ik = c - off;
+    if (ik >= 0 && ik < n) {
+      T *p = k + (r + ik) * k_stride + h * kHd + 16 * g;
+      quant_store8(p, kx), quant_store8(p + 8, kx + 8);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int iv = 4 * g + j - off;
+      if (iv >= 0 && iv < n) quant_store4(v + (r + iv) * v_stride + h * kHd + 4 * c, vx[j]);
+    }
+  }
 }
 
 }  // namespace hsd

@@ -33,8 +33,12 @@ QuantKV quant_pages(const hsd_kv_quant *kv) {
   return QuantKV{static_cast<uint8_t *>(kv->k_codes), static_cast<uint8_t *>(kv->v_codes), kv->k_scale, kv->v_scale, kv->n_blocks, kv->n_kv_heads};
 }
 
-// 256-byte aligned, as the callers of the workspaces are told
-bool is_workspace(const void *ws) { return ws != nullptr && (reinterpret_cast<uintptr_t>(ws) & 255) == 0; }
+// Whether `ws` will do as a workspace of `need` bytes (aligned to 256, as the callers are told; NULL if nothing is needed)
+int check_workspace(const void *ws, size_t ws_bytes, size_t need) {
+  if (need == 0) return HSD_OK;
+  if (ws == nullptr || (reinterpret_cast<uintptr_t>(ws) & 255) != 0) return HSD_EINVAL;
+  return ws_bytes < need ? HSD_ENOSPC : HSD_OK;
+}
 
 int check_heads(const hsd_kv_quant *kv, const hsd_batch *b, int32_t n_q_heads) {
   if (n_q_heads < 1 || n_q_heads % kv->n_kv_heads != 0) return HSD_EINVAL;
@@ -53,11 +57,16 @@ QuantPlan plan_quant_attention(const hsd_kv_quant *kv, const hsd_batch *b, int32
   p.ct = cols <= 24 * b->n_seq ? 1 : (f32 || cols <= 48 * b->n_seq ? 2 : 4);
   p.n_tiles = static_cast<int>(tiles(p.ct));
   const int64_t groups = p.n_tiles * static_cast<int64_t>(kv->n_kv_heads), max_pairs = (b->max_blocks_per_seq + 1) / 2;
+  // tiles that have columns, about (each sequence may have an empty one more)
+  const int64_t real = (cols <= 16 * p.ct * b->n_seq ? b->n_seq : cols / (16 * p.ct) + b->n_seq / 2) * kv->n_kv_heads;
+  // keys over the workgroups where a wave of a full workgroup would take more than eight steps and the chip is not full
+  p.n_splits = 1;
+  if (max_pairs > 128 && real < 512) p.n_splits = static_cast<int>(std::min<int64_t>({(1023 + real) / real, (max_pairs + 63) / 64, kMaxSplits}));
+  // keys over the waves: as many as fit the chip at once
+  const int64_t fit = p.ct == 1 && !f32 ? 4096 : 2048;
   const int most = quant_attn_waves(f32, p.ct);
   p.waves = 1;
-  while (p.waves < most && groups * p.waves < 2048 && p.waves < max_pairs) p.waves *= 2;
-  p.n_splits = 1;
-  if (groups < 512 && max_pairs > 64) p.n_splits = static_cast<int>(std::min<int64_t>({(1023 + groups) / groups, (max_pairs + 31) / 32, 256}));
+  while (p.waves < most && real * p.n_splits * p.waves * 2 <= fit && p.waves < max_pairs) p.waves *= 2;
   p.part_rows = p.n_splits > 1 ? static_cast<size_t>(groups) * p.n_splits * 16 * p.ct : 0;
   return p;
 }
@@ -73,7 +82,7 @@ int launch_quant_attention(hipStream_t st, const QuantAttn &a, const QuantPlan &
   hipLaunchKernelGGL(kern, dim3(groups, p.n_splits), dim3(64 * p.waves), lds, st, a, q, out);
   HSD_LAUNCH_CHECK();
   if (p.n_splits > 1) {
-    hipLaunchKernelGGL((k_attn_quant_join<T>), dim3(groups), dim3(256), 0, st, a, 16 * CT, out);
+    hipLaunchKernelGGL((k_attn_quant_join<T>), dim3(groups, 4 * CT), dim3(64), 0, st, a, 16 * CT, out);
     HSD_LAUNCH_CHECK();
   }
   return HSD_OK;
@@ -123,8 +132,14 @@ int hsd_kv_reserve(void *stream, const hsd_kv_pool *pool, const hsd_batch *b, in
   if (b->status == nullptr || (row_slot == nullptr && b->total_q > 0)) return HSD_EINVAL;
   const KvPlace p{b->n_seq, b->total_q, b->n_slots, b->max_blocks_per_seq, pool->n_blocks, b->cu_q, b->seq_slot, b->seq_len,
                   b->block_table, pool->free_list, pool->free_count, b->status, row_slot, row_pos};
-  hipLaunchKernelGGL(k_kv_place, dim3(1), dim3(1024), 0, static_cast<hipStream_t>(stream), p, 1);
+  // one workgroup places up to 16384 rows in the time that a second launch takes
+  const bool rows = b->total_q <= 16384;
+  hipLaunchKernelGGL(k_kv_place, dim3(1), dim3(1024), 0, static_cast<hipStream_t>(stream), p, rows ? 1 : 0);
   HSD_LAUNCH_CHECK();
+  if (!rows) {
+    hipLaunchKernelGGL(k_kv_place_rows, dim3((b->total_q + 2047) / 2048), dim3(256), 0, static_cast<hipStream_t>(stream), p);
+    HSD_LAUNCH_CHECK();
+  }
   return HSD_OK;
 }
 
@@ -147,13 +162,14 @@ int hsd_kv_quant_append(void *stream, const hsd_kv_quant *kv, int32_t n_rows, co
   if (n_rows == 0) return HSD_OK;
   const int64_t width = static_cast<int64_t>(kv->n_kv_heads) * HSD_HEAD_DIM;
   if (row_slot == nullptr || k == nullptr || v == nullptr || k_stride < width || v_stride < width) return HSD_EINVAL;
-  const dim3 grid((static_cast<unsigned>(n_rows) + 3) / 4, kv->n_kv_heads);
+  const int span = run_span(n_rows, kv->n_kv_heads);
+  const dim3 grid((static_cast<unsigned>(n_rows) + 4 * span - 1) / (4 * span), kv->n_kv_heads);
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (dtype == HSD_BF16)
-    hipLaunchKernelGGL((k_quant_append<bf16>), grid, dim3(256), 0, st, quant_pages(kv), n_rows, row_slot, static_cast<const bf16 *>(k),
+    hipLaunchKernelGGL((k_quant_append<bf16>), grid, dim3(256), 0, st, quant_pages(kv), n_rows, span, row_slot, static_cast<const bf16 *>(k),
                        static_cast<const bf16 *>(v), k_stride, v_stride, status);
   else
-    hipLaunchKernelGGL((k_quant_append<float>), grid, dim3(256), 0, st, quant_pages(kv), n_rows, row_slot, static_cast<const float *>(k),
+    hipLaunchKernelGGL((k_quant_append<float>), grid, dim3(256), 0, st, quant_pages(kv), n_rows, span, row_slot, static_cast<const float *>(k),
                        static_cast<const float *>(v), k_stride, v_stride, status);
   HSD_LAUNCH_CHECK();
   return HSD_OK;
@@ -167,13 +183,14 @@ int hsd_kv_quant_read(void *stream, const hsd_kv_quant *kv, int32_t n_rows, cons
   if (n_rows == 0) return HSD_OK;
   const int64_t width = static_cast<int64_t>(kv->n_kv_heads) * HSD_HEAD_DIM;
   if (row_slot == nullptr || k == nullptr || v == nullptr || k_stride < width || v_stride < width) return HSD_EINVAL;
-  const dim3 grid((static_cast<unsigned>(n_rows) + 3) / 4, kv->n_kv_heads);
+  const int span = run_span(n_rows, kv->n_kv_heads);
+  const dim3 grid((static_cast<unsigned>(n_rows) + 4 * span - 1) / (4 * span), kv->n_kv_heads);
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (dtype == HSD_BF16)
-    hipLaunchKernelGGL((k_quant_read<bf16>), grid, dim3(256), 0, st, quant_pages(kv), n_rows, row_slot, static_cast<bf16 *>(k),
+    hipLaunchKernelGGL((k_quant_read<bf16>), grid, dim3(256), 0, st, quant_pages(kv), n_rows, span, row_slot, static_cast<bf16 *>(k),
                        static_cast<bf16 *>(v), k_stride, v_stride);
   else
-    hipLaunchKernelGGL((k_quant_read<float>), grid, dim3(256), 0, st, quant_pages(kv), n_rows, row_slot, static_cast<float *>(k),
+    hipLaunchKernelGGL((k_quant_read<float>), grid, dim3(256), 0, st, quant_pages(kv), n_rows, span, row_slot, static_cast<float *>(k),
                        static_cast<float *>(v), k_stride, v_stride);
   HSD_LAUNCH_CHECK();
   return HSD_OK;
@@ -182,7 +199,7 @@ int hsd_kv_quant_read(void *stream, const hsd_kv_quant *kv, int32_t n_rows, cons
 size_t hsd_kv_quant_attention_bytes(const hsd_kv_quant *kv, const hsd_batch *b, int32_t n_q_heads) {
   if (check_quant(kv) != HSD_OK || check_rows(b) != HSD_OK || check_heads(kv, b, n_q_heads) != HSD_OK) return 0;
   const QuantPlan bf = plan_quant_attention(kv, b, n_q_heads, false), f32 = plan_quant_attention(kv, b, n_q_heads, true);
-  return 256 + std::max(bf.part_rows, f32.part_rows) * (HSD_HEAD_DIM + 2) * sizeof(float);
+  return std::max(bf.part_rows, f32.part_rows) * (HSD_HEAD_DIM + 2) * sizeof(float);
 }
 
 int hsd_kv_quant_attention(void *stream, const hsd_kv_quant *kv, const hsd_batch *b, int32_t n_q_heads, int32_t dtype, float softmax_scale,
@@ -194,12 +211,12 @@ int hsd_kv_quant_attention(void *stream, const hsd_kv_quant *kv, const hsd_batch
   if ((rc = check_heads(kv, b, n_q_heads)) != HSD_OK) return rc;
   if (b->total_q == 0) return HSD_OK;
   const int64_t width = static_cast<int64_t>(n_q_heads) * HSD_HEAD_DIM;
-  if (q == nullptr || out == nullptr || !is_workspace(ws) || q_stride < width || out_stride < width) return HSD_EINVAL;
-  if (ws_bytes < hsd_kv_quant_attention_bytes(kv, b, n_q_heads)) return HSD_ENOSPC;
+  if (q == nullptr || out == nullptr || q_stride < width || out_stride < width) return HSD_EINVAL;
   const QuantPlan p = plan_quant_attention(kv, b, n_q_heads, dtype == HSD_FP32);
+  if ((rc = check_workspace(ws, ws_bytes, p.part_rows * (HSD_HEAD_DIM + 2) * sizeof(float))) != HSD_OK) return rc;
   float *part = static_cast<float *>(ws);
   const QuantAttn a{quant_pages(kv), b->n_seq, b->total_q, b->n_slots, b->max_blocks_per_seq, n_q_heads, n_q_heads / kv->n_kv_heads, b->cu_q,
-                    b->seq_slot, b->seq_len, b->block_table, q_stride, out_stride, std::fabs(softmax_scale) * 1.4426950408889634f,
+                    b->seq_slot, b->seq_len, b->block_table, q_stride, out_stride, std::max(std::fabs(softmax_scale) * 1.4426950408889634f, 1.2e-38f),
                     std::signbit(softmax_scale) ? 0x80000000u : 0u, p.n_tiles, p.n_splits, part, reinterpret_cast<float2 *>(part + p.part_rows * HSD_HEAD_DIM)};
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (dtype == HSD_BF16) {
@@ -216,7 +233,7 @@ int hsd_kv_quant_attention(void *stream, const hsd_kv_quant *kv, const hsd_batch
 size_t hsd_token_logprobs_bytes(int32_t n_rows, int32_t vocab, int32_t n_top) {
   if (n_rows < 0 || vocab < 1 || n_top < 0 || n_top > HSD_MAX_TOP) return 0;
   const int parts = plan_scores(n_rows, vocab, 4).n_parts;
-  return 256 + (parts > 1 ? static_cast<size_t>(n_rows) * parts * (sizeof(float4) + n_top * sizeof(uint64_t)) : 0);
+  return parts > 1 ? static_cast<size_t>(n_rows) * parts * (sizeof(float4) + n_top * sizeof(uint64_t)) : 0;
 }
 
 int hsd_token_logprobs(void *stream, int32_t n_rows, int32_t vocab, int32_t dtype, const void *logits, int64_t row_stride, const int32_t *tokens,
@@ -224,9 +241,10 @@ int hsd_token_logprobs(void *stream, int32_t n_rows, int32_t vocab, int32_t dtyp
   if (n_rows < 0 || vocab < 1 || n_top < 0 || !is_type(dtype) || row_stride < vocab) return HSD_EINVAL;
   if (n_top > HSD_MAX_TOP || vocab > (1 << 30)) return HSD_ERANGE;
   if (n_rows == 0) return HSD_OK;
-  if (logits == nullptr || tokens == nullptr || logprob == nullptr || entropy == nullptr || !is_workspace(ws)) return HSD_EINVAL;
+  if (logits == nullptr || tokens == nullptr || logprob == nullptr || entropy == nullptr) return HSD_EINVAL;
   if (n_top > 0 && (top_ids == nullptr || top_logprobs == nullptr)) return HSD_EINVAL;
-  if (ws_bytes < hsd_token_logprobs_bytes(n_rows, vocab, n_top)) return HSD_ENOSPC;
+  const int rc = check_workspace(ws, ws_bytes, hsd_token_logprobs_bytes(n_rows, vocab, n_top));
+  if (rc != HSD_OK) return rc;
   const ScorePlan p = plan_scores(n_rows, vocab, dtype == HSD_BF16 ? 8 : 4);
   float4 *sums = static_cast<float4 *>(ws);
   const TokenScores a{n_rows, vocab, n_top, p.n_parts, p.part_len, row_stride, tokens, logprob, entropy, top_logprobs, top_ids, sums,

@@ -13,7 +13,6 @@ cache's device and returns; nothing waits.  A step of a decoder on it:
 """
 from __future__ import annotations
 
-import ctypes as C
 import math
 from typing import Optional, Tuple
 
@@ -22,28 +21,31 @@ import torch
 from . import binding as B
 
 _TYPES = {torch.bfloat16: B.HSD_BF16, torch.float32: B.HSD_FP32}
-_PAGE = B.HSD_KV_BLOCK_TOKENS * B.HSD_HEAD_DIM
+_HD = B.HSD_HEAD_DIM
+_PAGE = B.HSD_KV_BLOCK_TOKENS * _HD
 
 
-def _rows3(name: str, t: torch.Tensor, rows: int, heads: int, dev: torch.device, dtype=None):
+def _rows3(name: str, t: torch.Tensor, rows: int, heads: int, index: int, dtype=None) -> int:
     """A [rows, heads, 64] tensor whose rows may lie apart; returns the distance of its rows in elements."""
-    if not isinstance(t, torch.Tensor) or t.device != dev:
-        raise ValueError(f"{name} must be a tensor on {dev}")
+    if not isinstance(t, torch.Tensor) or t.get_device() != index:
+        raise ValueError(f"{name} must be a tensor on cuda:{index}")
     if t.dtype not in _TYPES or (dtype is not None and t.dtype != dtype):
         raise ValueError(f"{name}: bfloat16 or float32, the same for all tensors of a call; got {t.dtype}")
-    if t.shape != (rows, heads, B.HSD_HEAD_DIM):
-        raise ValueError(f"{name} must be [{rows}, {heads}, {B.HSD_HEAD_DIM}], got {tuple(t.shape)}")
+    if t.shape != (rows, heads, _HD):
+        raise ValueError(f"{name} must be [{rows}, {heads}, {_HD}], got {tuple(t.shape)}")
+    if t.is_contiguous():
+        return heads * _HD
     s = t.stride()
-    if rows and (s[2] != 1 or (heads > 1 and s[1] != B.HSD_HEAD_DIM) or (rows > 1 and s[0] < heads * B.HSD_HEAD_DIM)):
+    if s[2] != 1 or (heads > 1 and s[1] != _HD) or (rows > 1 and s[0] < heads * _HD):
         raise ValueError(f"{name}: the heads of a row must lie one after the other and rows must not overlap")
-    return s[0] if rows > 1 else heads * B.HSD_HEAD_DIM
+    return s[0] if rows > 1 else heads * _HD
 
 
-def _ints(name: str, t: torch.Tensor, n: int, dev: torch.device):
-    if not isinstance(t, torch.Tensor) or t.device != dev or t.dtype != torch.int32 or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous int32 tensor on {dev}")
+def _ints(name: str, t: torch.Tensor, n: int, index: int) -> int:
+    if not isinstance(t, torch.Tensor) or t.get_device() != index or t.dtype != torch.int32 or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor on cuda:{index}")
     if t.dim() != 1 or (n >= 0 and t.shape[0] != n):
-        raise ValueError(f"{name} must be [{n}], got {tuple(t.shape)}")
+        raise ValueError(f"{name} must be [{n if n >= 0 else 'n_seq + 1'}], got {tuple(t.shape)}")
     return t.data_ptr()
 
 
@@ -55,8 +57,11 @@ class QuantKV:
         if not torch.cuda.is_available():
             raise RuntimeError("the 8-bit cache needs a GPU (MI355X); there is no CPU fallback")
         self.dev = torch.device(device)
+        if self.dev.type != "cuda":
+            raise ValueError(f"the cache lives on a GPU, not on {device}")
         if self.dev.index is None:
-            self.dev = torch.device(self.dev.type, torch.cuda.current_device())
+            self.dev = torch.device("cuda", torch.cuda.current_device())
+        self._index = self.dev.index
         self.n_blocks, self.n_kv_heads, self.n_slots, self.maxb, self.n_layers = n_blocks, n_kv_heads, n_slots, max_blocks_per_seq, n_layers
         shape = (n_layers, n_blocks, n_kv_heads)
         self.k_codes = torch.zeros(shape + (_PAGE,), dtype=torch.uint8, device=self.dev)
@@ -71,17 +76,23 @@ class QuantKV:
             [n_blocks, 1, n_slots, n_slots * max_blocks_per_seq, 1])
         self.block_table = table.view(n_slots, max_blocks_per_seq)
         self.cpool = B.hsd_kv_pool(None, None, n_blocks, self.free_list.data_ptr(), self.free_count.data_ptr())
+        # what every call's batch has in common: calls copy it, so that two threads do not share one
+        rows = B.hsd_batch()
+        rows.max_blocks_per_seq, rows.n_slots = max_blocks_per_seq, n_slots
+        rows.seq_len, rows.block_table, rows.status = self.seq_len.data_ptr(), self.block_table.data_ptr(), self.status.data_ptr()
+        self._rows = bytes(rows)
+        self._ws_bytes = {}
         self._layers = [B.hsd_kv_quant(self.k_codes[l].data_ptr(), self.v_codes[l].data_ptr(), self.k_scale[l].data_ptr(),
                                        self.v_scale[l].data_ptr(), n_blocks, n_kv_heads) for l in range(n_layers)]
         self.reset()
 
     @property
-    def stream(self):
-        return C.c_void_p(torch.cuda.current_stream(self.dev).cuda_stream)
+    def stream(self) -> int:
+        return B.current_stream(self._index)
 
     def reset(self):
         """Every block free, every sequence empty (the pages keep their bytes)."""
-        with torch.cuda.device(self.dev):
+        with B.on_device(self._index):
             self.seq_len.zero_()
             self.block_table.fill_(-1)
             self.status.zero_()
@@ -95,18 +106,17 @@ class QuantKV:
         """Returns the bookkeeping to the last snapshot (one copy on the current stream)."""
         self._state.copy_(self._snapshot)
 
-    def _batch(self, cu_q, total_q, seq_slot, accept_len=None) -> B.hsd_batch:
-        b = B.hsd_batch()
-        b.cu_q = _ints("cu_q", cu_q, -1, self.dev)
+    def _batch(self, cu_q, total_q, seq_slot=None, accept_len=None) -> B.hsd_batch:
+        b = B.hsd_batch.from_buffer_copy(self._rows)
+        b.cu_q = _ints("cu_q", cu_q, -1, self._index)
         n = cu_q.shape[0] - 1
         if n < 1 or total_q < 0 or (seq_slot is None and n > self.n_slots):
             raise ValueError(f"bad rows: n_seq={n}, total_q={total_q}, slots={self.n_slots}")
-        b.n_seq, b.total_q, b.max_blocks_per_seq, b.n_slots = n, total_q, self.maxb, self.n_slots
+        b.n_seq, b.total_q = n, total_q
         if seq_slot is not None:
-            b.seq_slot = _ints("seq_slot", seq_slot, n, self.dev)
+            b.seq_slot = _ints("seq_slot", seq_slot, n, self._index)
         if accept_len is not None:
-            b.accept_len = _ints("accept_len", accept_len, n, self.dev)
-        b.seq_len, b.block_table, b.status = self.seq_len.data_ptr(), self.block_table.data_ptr(), self.status.data_ptr()
+            b.accept_len = _ints("accept_len", accept_len, n, self._index)
         return b
 
     def _layer(self, layer: int) -> B.hsd_kv_quant:
@@ -118,53 +128,59 @@ class QuantKV:
         """Blocks for total_q new rows, sequence s owning rows cu_q[s] .. cu_q[s + 1] - 1 behind its seq_len tokens.
         Returns (row_slot, row_pos), int32 [total_q]; row_slot is -1 where the pool or the table is too small (see status)."""
         b = self._batch(cu_q, total_q, seq_slot)
-        with torch.cuda.device(self.dev):
-            out = torch.empty((2, total_q), dtype=torch.int32, device=self.dev)
-            B.hsd_kv_reserve(self.stream, self.cpool, b, out[0].data_ptr(), out[1].data_ptr())
-        return out[0], out[1]
+        slot = torch.empty(total_q, dtype=torch.int32, device=self.dev)
+        pos = torch.empty(total_q, dtype=torch.int32, device=self.dev)
+        with B.on_device(self._index):
+            B.hsd_kv_reserve(self.stream, self.cpool, b, slot.data_ptr(), pos.data_ptr())
+        return slot, pos
 
     def commit(self, cu_q: torch.Tensor, total_q: int, accept_len: Optional[torch.Tensor] = None,
                seq_slot: Optional[torch.Tensor] = None):
         """seq_len grows by all rows of a sequence, or by 1 + accept_len[s] (not at all where it is negative); blocks that
         are wholly beyond return to the pool."""
         b = self._batch(cu_q, total_q, seq_slot, accept_len)
-        with torch.cuda.device(self.dev):
+        with B.on_device(self._index):
             B.hsd_kv_commit_rows(self.stream, self.cpool, b)
 
     def append(self, k: torch.Tensor, v: torch.Tensor, row_slot: torch.Tensor, layer: int = 0):
         """Keys and values [rows, n_kv_heads, 64] into the pages at row_slot (as reserve returned it)."""
-        n, kv = row_slot.shape[0], self._layer(layer)
-        ks, vs = _rows3("k", k, n, self.n_kv_heads, self.dev), _rows3("v", v, n, self.n_kv_heads, self.dev, k.dtype)
-        with torch.cuda.device(self.dev):
-            B.hsd_kv_quant_append(self.stream, kv, n, _ints("row_slot", row_slot, n, self.dev), _TYPES[k.dtype], k.data_ptr(), v.data_ptr(),
-                                  ks, vs, self.status.data_ptr())
+        slots, n, kv = _ints("row_slot", row_slot, -1, self._index), row_slot.shape[0], self._layer(layer)
+        ks, vs = _rows3("k", k, n, self.n_kv_heads, self._index), _rows3("v", v, n, self.n_kv_heads, self._index, k.dtype)
+        with B.on_device(self._index):
+            B.hsd_kv_quant_append(self.stream, kv, n, slots, _TYPES[k.dtype], k.data_ptr(), v.data_ptr(), ks, vs, self.status.data_ptr())
 
     def read(self, row_slot: torch.Tensor, dtype: torch.dtype = torch.bfloat16, layer: int = 0) -> Tuple[torch.Tensor, torch.Tensor]:
         """The values that the cache holds at the given slots: (k, v) [rows, n_kv_heads, 64], exact in both types."""
         if dtype not in _TYPES:
             raise ValueError(f"bfloat16 or float32, got {dtype}")
-        n, kv = row_slot.shape[0], self._layer(layer)
-        with torch.cuda.device(self.dev):
-            out = torch.empty((2, n, self.n_kv_heads, B.HSD_HEAD_DIM), dtype=dtype, device=self.dev)
-            w = self.n_kv_heads * B.HSD_HEAD_DIM
-            B.hsd_kv_quant_read(self.stream, kv, n, _ints("row_slot", row_slot, n, self.dev), _TYPES[dtype], out[0].data_ptr(), out[1].data_ptr(), w, w)
-        return out[0], out[1]
+        slots, n, kv, w = _ints("row_slot", row_slot, -1, self._index), row_slot.shape[0], self._layer(layer), self.n_kv_heads * _HD
+        k = torch.empty((n, self.n_kv_heads, _HD), dtype=dtype, device=self.dev)
+        v = torch.empty((n, self.n_kv_heads, _HD), dtype=dtype, device=self.dev)
+        with B.on_device(self._index):
+            B.hsd_kv_quant_read(self.stream, kv, n, slots, _TYPES[dtype], k.data_ptr(), v.data_ptr(), w, w)
+        return k, v
 
     def attend(self, q: torch.Tensor, cu_q: torch.Tensor, seq_slot: Optional[torch.Tensor] = None, layer: int = 0,
                scale: Optional[float] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Causal attention of the rows q [rows, n_q_heads, 64] over their sequences: row i of a sequence sees its seq_len
         tokens and rows 0 .. i, whose keys and values have been appended.  scale: 1 / sqrt(64) by default."""
-        if q.dim() != 3 or q.shape[1] < 1 or q.shape[1] % self.n_kv_heads:
-            raise ValueError(f"q must be [rows, n_q_heads, 64] with a multiple of {self.n_kv_heads} heads, got {tuple(q.shape)}")
-        n, heads = q.shape[0], q.shape[1]
+        if not isinstance(q, torch.Tensor) or q.dim() != 3 or q.shape[1] < 1 or q.shape[1] % self.n_kv_heads:
+            raise ValueError(f"q must be [rows, n_q_heads, 64] with a multiple of {self.n_kv_heads} heads")
+        n, heads, _ = q.shape
         kv, b = self._layer(layer), self._batch(cu_q, n, seq_slot)
-        qs = _rows3("q", q, n, heads, self.dev)
-        scale = 1.0 / math.sqrt(B.HSD_HEAD_DIM) if scale is None else float(scale)
-        with torch.cuda.device(self.dev):
-            if out is None:
-                out = torch.empty((n, heads, B.HSD_HEAD_DIM), dtype=q.dtype, device=self.dev)
-            os = _rows3("out", out, n, heads, self.dev, q.dtype)
-            nb = B.hsd_kv_quant_attention_bytes(kv, b, heads)
-            ws = torch.empty(nb, dtype=torch.uint8, device=self.dev)
-            B.hsd_kv_quant_attention(self.stream, kv, b, heads, _TYPES[q.dtype], scale, q.data_ptr(), qs, out.data_ptr(), os, ws.data_ptr(), nb)
+        qs = _rows3("q", q, n, heads, self._index)
+        if out is None:
+            out, os = torch.empty((n, heads, _HD), dtype=q.dtype, device=self.dev), heads * _HD
+        else:
+            os = _rows3("out", out, n, heads, self._index, q.dtype)
+        key = (n, b.n_seq, heads)
+        nb = self._ws_bytes.get(key)
+        if nb is None:
+            if len(self._ws_bytes) > 4096:
+                self._ws_bytes.clear()
+            nb = self._ws_bytes[key] = B.hsd_kv_quant_attention_bytes(kv, b, heads)
+        ws = torch.empty(nb, dtype=torch.uint8, device=self.dev) if nb else None
+        with B.on_device(self._index):
+            B.hsd_kv_quant_attention(self.stream, kv, b, heads, _TYPES[q.dtype], 1.0 / math.sqrt(_HD) if scale is None else float(scale),
+                                     q.data_ptr(), qs, out.data_ptr(), os, ws.data_ptr() if nb else None, nb)
         return out

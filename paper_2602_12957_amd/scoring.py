@@ -1,7 +1,6 @@
 """Scores of tokens under rows of logits (include/hsd.h: hsd_token_logprobs)."""
 from __future__ import annotations
 
-import ctypes as C
 from typing import NamedTuple
 
 import torch
@@ -33,20 +32,21 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, n_top: int = 0) -
     stride = logits.stride(0) if n > 1 else vocab
     if (vocab > 1 and n > 0 and logits.stride(1) != 1) or stride < vocab:
         raise ValueError("logits: a row's values must lie one after the other and rows must not overlap")
-    if not isinstance(tokens, torch.Tensor) or tokens.device != logits.device or tokens.dtype != torch.int32 or not tokens.is_contiguous():
+    index = logits.get_device()
+    if not isinstance(tokens, torch.Tensor) or tokens.get_device() != index or tokens.dtype != torch.int32 or not tokens.is_contiguous():
         raise ValueError("tokens must be a contiguous int32 tensor on the logits' device")
     if tokens.shape != (n,):
         raise ValueError(f"tokens must be [{n}], got {tuple(tokens.shape)}")
     if not 0 <= n_top <= B.HSD_MAX_TOP:
         raise ValueError(f"n_top must lie in 0 .. {B.HSD_MAX_TOP}, got {n_top}")
     dev = logits.device
-    with torch.cuda.device(dev):
-        res = torch.empty((2, n), dtype=torch.float32, device=dev)
-        ids = torch.empty((n, n_top), dtype=torch.int32, device=dev)
-        top = torch.empty((n, n_top), dtype=torch.float32, device=dev)
-        nb = B.hsd_token_logprobs_bytes(n, vocab, n_top)
-        ws = torch.empty(nb, dtype=torch.uint8, device=dev)
-        B.hsd_token_logprobs(C.c_void_p(torch.cuda.current_stream(dev).cuda_stream), n, vocab, _TYPES[logits.dtype], logits.data_ptr(),
-                             stride, tokens.data_ptr(), res[0].data_ptr(), res[1].data_ptr(), n_top, ids.data_ptr(), top.data_ptr(),
-                             ws.data_ptr(), nb)
-    return TokenScores(res[0], res[1], ids, top)
+    logprob = torch.empty(n, dtype=torch.float32, device=dev)
+    entropy = torch.empty(n, dtype=torch.float32, device=dev)
+    ids = torch.empty((n, n_top), dtype=torch.int32, device=dev)
+    top = torch.empty((n, n_top), dtype=torch.float32, device=dev)
+    nb = B.hsd_token_logprobs_bytes(n, vocab, n_top)
+    ws = torch.empty(nb, dtype=torch.uint8, device=dev) if nb else None
+    with B.on_device(index):
+        B.hsd_token_logprobs(B.current_stream(index), n, vocab, _TYPES[logits.dtype], logits.data_ptr(), stride, tokens.data_ptr(),
+                             logprob.data_ptr(), entropy.data_ptr(), n_top, ids.data_ptr(), top.data_ptr(), ws.data_ptr() if nb else None, nb)
+    return TokenScores(logprob, entropy, ids, top)

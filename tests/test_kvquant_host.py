@@ -85,7 +85,7 @@ def test_append_and_read_arguments():
 
 
 def test_attention_arguments():
-    b, kv = _rows(), _kv()
+    b, kv = _rows(max_blocks_per_seq=4096), _kv()     # long tables: the keys are split over workgroups, which takes a workspace
     need = B.hsd_kv_quant_attention_bytes(kv, b, 16)
     assert need > 0
     ok = dict(heads=16, dtype=B.HSD_BF16, scale=0.125, q=FAKE, qs=1024, o=FAKE, os=1024, ws=FAKE, nb=need)
@@ -100,11 +100,11 @@ def test_attention_arguments():
 
 
 def test_token_logprobs_arguments():
-    need = B.hsd_token_logprobs_bytes(4, 1000, 5)
+    need = B.hsd_token_logprobs_bytes(4, 200000, 5)
     assert need > 0 and B.hsd_token_logprobs_bytes(4, 0, 5) == 0 and B.hsd_token_logprobs_bytes(4, 10, 33) == 0 and B.hsd_token_logprobs_bytes(-1, 10, 3) == 0
-    ok = dict(n=4, vocab=1000, dtype=B.HSD_FP32, x=FAKE, stride=1000, tok=FAKE, lp=FAKE, ent=FAKE, top=5, ids=FAKE, tlp=FAKE, ws=FAKE, nb=need)
+    ok = dict(n=4, vocab=200000, dtype=B.HSD_FP32, x=FAKE, stride=200000, tok=FAKE, lp=FAKE, ent=FAKE, top=5, ids=FAKE, tlp=FAKE, ws=FAKE, nb=need)
     for kw, code in ((dict(n=-1), B.HSD_EINVAL), (dict(vocab=0), B.HSD_EINVAL), (dict(dtype=9), B.HSD_EINVAL), (dict(x=None), B.HSD_EINVAL),
-                     (dict(stride=999), B.HSD_EINVAL), (dict(tok=None), B.HSD_EINVAL), (dict(lp=None), B.HSD_EINVAL), (dict(ent=None), B.HSD_EINVAL),
+                     (dict(stride=199999), B.HSD_EINVAL), (dict(tok=None), B.HSD_EINVAL), (dict(lp=None), B.HSD_EINVAL), (dict(ent=None), B.HSD_EINVAL),
                      (dict(top=-1), B.HSD_EINVAL), (dict(top=33), B.HSD_ERANGE), (dict(ids=None), B.HSD_EINVAL), (dict(tlp=None), B.HSD_EINVAL),
                      (dict(ws=None), B.HSD_EINVAL), (dict(nb=need - 1), B.HSD_ENOSPC), (dict(ws=FAKE + 64), B.HSD_EINVAL)):
         a = {**ok, **kw}
