@@ -34,29 +34,68 @@ struct QuantAttn {
 constexpr float kRefSlack = 20.f;          // binary orders by which a score may exceed its column's reference before that moves
 constexpr int kSplitPairs = 16;            // a run of pairs for a workgroup of its own is no shorter
 
-// Tiles of `cols` columns of sequence s start at tile floor(cu_q[s] * group / cols) + s: as many as it needs, at most one too many.
+// Tiles of `cols` columns.  Up to 64 sequences are numbered without gaps.  More: those of sequence s start at
+// floor(cu_q[s] * group / cols) + s, which leaves each as many as it needs and at most one too many.
 __device__ __forceinline__ int tile_start(int cu, int s, int group, int cols) { return cu * group / cols + s; }
+
+// Sum over the lanes up to and with this one
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);    // from 1, 2, 4 and 8 lanes below in a row of 16
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);   // a row's last lane to the next row, rows 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);   // lane 31 to rows 2 and 3
+  return v;
+}
 
 struct QuantTile {
   int slot, S, n, base, j;   // state row, cached length, rows, first packed row, tile within the sequence
 };
-// Sequence and place of tile t: a search by 64 lanes at a time (one round up to 64 sequences, two up to 4096)
+// Sequence and place of tile t, n = 0 where there is none; by 64 lanes at a time (one round up to 64 sequences, two up to 4096)
 __device__ __forceinline__ QuantTile find_tile(const QuantAttn &a, int t, int cols, int lane) {
+  const bool many = a.n_seq > kWave;
   int first = 0;
-  if (a.n_seq > kWave) {
+  if (many) {
     const int stride = (a.n_seq + kWave - 1) / kWave, s = lane * stride;
     first = (63 - __builtin_clzll(__ballot(s < a.n_seq && tile_start(a.cu_q[min(s, a.n_seq)], s, a.group, cols) <= t))) * stride;
   }
   const int s = min(first + lane, a.n_seq - 1);
   const int cu = a.cu_q[s], end = a.cu_q[s + 1], slot = slot_of(a.seq_slot, s, a.n_slots), len = a.seq_len[slot];
-  const int hit = 63 - __builtin_clzll(__ballot(first + lane < a.n_seq && tile_start(cu, s, a.group, cols) <= t));   // (lane 0 always does)
+  const bool in = first + lane < a.n_seq;
+  const int need = in ? ((end - cu) * a.group + cols - 1) / cols : 0;
+  const int start = many ? tile_start(cu, s, a.group, cols) : wave_scan(need) - need;
+  // the last sequence that starts at t or before; one without rows starts where the next one does
+  const unsigned long long m = __ballot(in && start <= t && (many || need > 0));
+  const int hit = m != 0 ? 63 - __builtin_clzll(m) : 0;
   QuantTile q;
   q.base = __builtin_amdgcn_readlane(cu, hit);
-  q.n = __builtin_amdgcn_readlane(end, hit) - q.base;
+  q.n = m != 0 ? __builtin_amdgcn_readlane(end, hit) - q.base : 0;
   q.slot = __builtin_amdgcn_readlane(slot, hit);
   q.S = max(__builtin_amdgcn_readlane(len, hit), 0);
-  q.j = t - tile_start(q.base, first + hit, a.group, cols);
+  q.j = t - __builtin_amdgcn_readlane(start, hit);
   return q;
+}
+
+// Workgroup b to (tile, kv head): workgroup b runs on XCD b % 8, and the tiles of one head go to as few XCDs as the heads leave it,
+// so that a sequence's pages enter one or two L2s; where there are several, they take the tiles in turns (late rows see
+// more keys).  Later tiles come first.  Head numbers that do not divide 8, or 8 them, keep the plain order.
+__device__ __forceinline__ bool tile_of_block(const QuantAttn &a, int b, int &tile, int &h) {
+  const int heads = a.kv.n_kv_heads, x = b & 7, u = b >> 3;
+  int t;
+  if (heads <= 8 && 8 % heads == 0) {
+    h = x % heads, t = u * (8 / heads) + x / heads;
+  } else if (heads % 8 == 0) {
+    h = x + 8 * (u / a.n_tiles), t = u % a.n_tiles;
+  } else {
+    h = b / a.n_tiles, t = b % a.n_tiles;
+  }
+  tile = a.n_tiles - 1 - t;
+  return t < a.n_tiles && h < heads;
+}
+inline unsigned tile_blocks(int64_t n_tiles, int64_t heads) {
+  if (heads <= 8 && 8 % heads == 0) return static_cast<unsigned>((n_tiles + 8 / heads - 1) / (8 / heads) * 8);
+  return static_cast<unsigned>(n_tiles * heads);
 }
 
 // Pairs of pages that the columns of a tile see, and those of run z
@@ -104,7 +143,7 @@ __device__ __forceinline__ void store4(bf16 *p, const floatx4 &v) {
   *reinterpret_cast<u2 *>(p) = *reinterpret_cast<u2 *>(&b);
 }
 
-// grid: (n_tiles * n_kv_heads, n_splits), block 64 * W, dynamic LDS quant_attn_lds(W, CT)
+// grid: (tile_blocks, n_splits), block 64 * W, dynamic LDS quant_attn_lds(W, CT)
 // (16 waves leave 128 registers each, which one part of 16 bf16 columns fits)
 constexpr int quant_attn_waves(bool f32, int ct) { return ct == 1 && !f32 ? 16 : 8; }
 inline int quant_attn_lds(int waves, int ct) { return waves > 1 ? waves * ct * (64 * 16 + 32) * static_cast<int>(sizeof(float)) : 0; }
@@ -115,7 +154,9 @@ __global__ void __launch_bounds__(64 * quant_attn_waves(std::is_same<T, float>::
   extern __shared__ __attribute__((aligned(16))) float lds[];
   const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
   const int W = blockDim.x >> 6, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int h = blockIdx.x / a.n_tiles, tile = a.n_tiles - 1 - blockIdx.x % a.n_tiles, z = blockIdx.y;
+  const int z = blockIdx.y;
+  int tile, h;
+  if (!tile_of_block(a, blockIdx.x, tile, h)) return;
   const QuantTile qt = find_tile(a, tile, C, lane);
   const int32_t *table = a.block_table + static_cast<size_t>(qt.slot) * a.max_blocks;
   // ids of the pages of 32 steps from pair p0 on: lane 2 i + p has page p of step i
@@ -331,12 +372,15 @@ __global__ void __launch_bounds__(64 * quant_attn_waves(std::is_same<T, float>::
   }
 }
 
-// The runs of a tile together, in order.  grid: (n_tiles * n_kv_heads, columns / 4), block 64: 16 lanes a column
+// The runs of a tile together, in a fixed order.  grid: (n_tiles * n_kv_heads, columns / 4), block 256: each wave takes four
+// columns, 16 lanes a column, and every fourth run.
 constexpr int kMaxSplits = 256;
 template <typename T>
-__global__ void __launch_bounds__(64) k_attn_quant_join(QuantAttn a, int cols, T *__restrict__ out) {
+__global__ void __launch_bounds__(256) k_attn_quant_join(QuantAttn a, int cols, T *__restrict__ out) {
   __shared__ float s_f[4][kMaxSplits];
-  const int h = blockIdx.x / a.n_tiles, tile = blockIdx.x % a.n_tiles, lane = threadIdx.x, i = lane & 15, lc = lane >> 4;
+  __shared__ floatx4 s_o[4][64];
+  const int h = blockIdx.x / a.n_tiles, tile = blockIdx.x % a.n_tiles, lane = threadIdx.x & 63, i = lane & 15, lc = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const QuantTile qt = find_tile(a, tile, cols, lane);
   const int n_cols = qt.n * a.group - qt.j * cols, col = blockIdx.y * 4 + lc;
   if (static_cast<int>(blockIdx.y) * 4 >= n_cols) return;
@@ -345,7 +389,7 @@ __global__ void __launch_bounds__(64) k_attn_quant_join(QuantAttn a, int cols, T
   const int n = (n_pairs + run - 1) / run;
   const size_t step = static_cast<size_t>(a.n_tiles) * a.kv.n_kv_heads * cols;
   const size_t at = (static_cast<size_t>(tile) * a.kv.n_kv_heads + h) * cols + min(col, n_cols - 1);
-  // a lane looks at every 16th run
+  // a lane looks at every 16th run; every wave for itself, the factors written by all alike
   float m = -INFINITY, sum = 0.f;
   for (int z = i; z < n; z += 16) m = fmaxf(m, a.part_ml[at + z * step].x);
 #pragma unroll
@@ -362,8 +406,11 @@ __global__ void __launch_bounds__(64) k_attn_quant_join(QuantAttn a, int cols, T
   __syncthreads();
   floatx4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
-  for (int z = 0; z < n; ++z) x += s_f[lc][z] * *reinterpret_cast<const floatx4 *>(a.part_o + (at + z * step) * kHd + 4 * i);
-  if (col >= n_cols) return;
+  for (int z = w; z < n; z += 4) x += s_f[lc][z] * *reinterpret_cast<const floatx4 *>(a.part_o + (at + z * step) * kHd + 4 * i);
+  s_o[w][lane] = x;
+  __syncthreads();
+  if (w != 0 || col >= n_cols) return;
+  x = (s_o[0][lane] + s_o[1][lane]) + (s_o[2][lane] + s_o[3][lane]);
   if (sum == 0.f) x = floatx4{0.f, 0.f, 0.f, 0.f};
   else x /= sum;
   const int f = qt.j * cols + col, row = f / a.group, hd = f - row * a.group;

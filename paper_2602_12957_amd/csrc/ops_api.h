@@ -61,7 +61,7 @@ QuantPlan plan_quant_attention(const hsd_kv_quant *kv, const hsd_batch *b, int32
   const int64_t real = (cols <= 16 * p.ct * b->n_seq ? b->n_seq : cols / (16 * p.ct) + b->n_seq / 2) * kv->n_kv_heads;
   // keys over the workgroups where a wave of a full workgroup would take more than eight steps and the chip is not full
   p.n_splits = 1;
-  if (max_pairs > 128 && real < 512) p.n_splits = static_cast<int>(std::min<int64_t>({(1023 + real) / real, (max_pairs + 63) / 64, kMaxSplits}));
+  if (max_pairs > 128 && real < 512) p.n_splits = static_cast<int>(std::min<int64_t>({(511 + real) / real, (max_pairs + 63) / 64, kMaxSplits}));
   // keys over the waves: as many as fit the chip at once
   const int64_t fit = p.ct == 1 && !f32 ? 4096 : 2048;
   const int most = quant_attn_waves(f32, p.ct);
@@ -79,10 +79,10 @@ int launch_quant_attention(hipStream_t st, const QuantAttn &a, const QuantPlan &
                                                         quant_attn_lds(quant_attn_waves(std::is_same<T, float>::value, CT), CT));
   if (attr_rc != hipSuccess) return HSD_EHIP;
   const unsigned groups = static_cast<unsigned>(p.n_tiles) * a.kv.n_kv_heads;
-  hipLaunchKernelGGL(kern, dim3(groups, p.n_splits), dim3(64 * p.waves), lds, st, a, q, out);
+  hipLaunchKernelGGL(kern, dim3(tile_blocks(p.n_tiles, a.kv.n_kv_heads), p.n_splits), dim3(64 * p.waves), lds, st, a, q, out);
   HSD_LAUNCH_CHECK();
   if (p.n_splits > 1) {
-    hipLaunchKernelGGL((k_attn_quant_join<T>), dim3(groups, 4 * CT), dim3(64), 0, st, a, 16 * CT, out);
+    hipLaunchKernelGGL((k_attn_quant_join<T>), dim3(groups, 4 * CT), dim3(256), 0, st, a, 16 * CT, out);
     HSD_LAUNCH_CHECK();
   }
   return HSD_OK;
