@@ -1,13 +1,18 @@
 // Attention over a cache held in 8 bits: row i of a sequence's block sees the cached tokens and rows 0 .. i of the block.
 //
-// One pass over the keys with a softmax reference that moves rarely.  A wave holds 16 * CT columns -- (row, query head of the kv
-// head) pairs, heads fastest -- and walks pairs of pages: a page of K and one of V are a 16-byte request a lane each, whose bytes are
-// the operands of 16x16x32 products once converted to bf16 (exact: code times a power of two).
-//   S^T = K Q^T: lane (g, c) receives tokens 4 g .. 4 g + 3 of a page for column c
-//   O^T += V^T P^T: the same lane's probabilities of two pages are the operand as they are; the rows of the product are dims
-//     (row 4 g + i of part t: dim 16 g + 4 i + t), so that a lane ends with 16 consecutive dims of its column
-// The row sums are a product with ones: sums of the rounded probabilities, whose rounding cancels in the quotient.
+// One pass over the keys with a softmax reference that moves rarely.  A wave holds 32 * CT columns -- (row, query head of the kv
+// head) pairs, heads fastest -- and walks pairs of pages, whose bytes are the operands of 32x32x16 products once converted to bf16
+// (exact: a code times a power of two).
+//   S^T = K Q^T: lane (h, c), h = lane / 32, receives keys 8 b + 4 h + e, b, e < 4, of the pair for column c
+//   O^T += V^T P^T: the same lane's probabilities of a page are the operand as they are (the V pages' token order); row r of part T is
+//     dim 2 r + T, so that a lane ends with dims 16 b + 8 h .. + 7, b < 4, of its column
+// The row sums are 16x16x32 products with ones in half of the places, which sum both halves of each column at once: sums of the
+// rounded probabilities, whose rounding cancels in the quotient.
 // fp32 calls split queries and probabilities into three bf16 parts each (24 bits), three products in place of one.
+//
+// 32x32x16 and not 16x16x32, which takes as long per product and fits 16-column decoding better: beside the short instruction the
+// other wave's exponentials hardly run.  ns a wave for 36 short / 18 long ones 322 / 278, for the exponentials and what goes with
+// them 271, for both, two waves a SIMD: 542 / 400.
 //
 // The waves of a workgroup share the columns and take every W-th pair of pages; the workgroups along grid.y take runs of
 // pairs of their own where few columns would leave the chip empty (k_attn_quant_join adds them up).
@@ -31,6 +36,13 @@ struct QuantAttn {
   float2 *part_ml;    // [n_splits][n_tiles][n_kv_heads][columns]: reference, sum
 };
 
+// Queries below 2^30, keys whose page's scale is below 2^30 (448 * 2^30 at most) and a scale below 2^50 give exponents that are
+// finite.  Where one of them is not, every step looks for columns that are not: such a column's probabilities would spoil another one's row
+// sum, so they are left out and the column ends as NaN.
+constexpr float kCalmQuery = 0x1p30f, kCalmPage = 0x1p30f, kCalmScale = 0x1p50f;
+// Common steps look at the row sums alone: above kSumMost the column's reference moves, and above kSumLost, where the products with values
+// may have left the range, the walk starts again with every step a general one.
+constexpr float kSumMost = 0x1p40f, kSumLost = 0x1p80f;
 constexpr float kRefSlack = 20.f;          // binary orders by which a score may exceed its column's reference before that moves
 constexpr int kSplitPairs = 16;            // a run of pairs for a workgroup of its own is no shorter
 
@@ -48,6 +60,8 @@ __device__ __forceinline__ int wave_scan(int v) {
   v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);   // lane 31 to rows 2 and 3
   return v;
 }
+
+__device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 struct QuantTile {
   int slot, S, n, base, j;   // state row, cached length, rows, first packed row, tile within the sequence
@@ -116,10 +130,19 @@ __device__ __forceinline__ void split8(const float *x, bf16x8 (&part)[NS]) {
 }
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ bf16x8 page_operand(uint32_t a, uint32_t b, float sa, float sb) {
-  const bf16x2 x = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, sa, false), y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, sa, true);
-  const bf16x2 z = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, sb, false), w = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, sb, true);
+__device__ __forceinline__ bf16x8 page_operand(uint32_t a, uint32_t b, float scale) {
+  const bf16x2 x = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false), y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true);
+  const bf16x2 z = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false), w = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true);
   return bf16x8{x[0], x[1], y[0], y[1], z[0], z[1], w[0], w[1]};
+}
+
+// The largest magnitude by its bits (infinities and NaN above all numbers) of m and eight bf16 values, to the bf16 below
+__device__ __forceinline__ float most_bits(float m, bf16x8 v) {
+  u32x4 u = *reinterpret_cast<u32x4 *>(&v);
+  uint32_t r = __float_as_uint(m);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r = max(r, max(u[i] & 0x7fff0000u, (u[i] << 16) & 0x7fff0000u));
+  return __uint_as_float(r);
 }
 
 __device__ __forceinline__ void load_q8(const bf16 *p, uint32_t sign, bf16x8 (&part)[1]) {
@@ -144,17 +167,18 @@ __device__ __forceinline__ void store4(bf16 *p, const floatx4 &v) {
 }
 
 // grid: (tile_blocks, n_splits), block 64 * W, dynamic LDS quant_attn_lds(W, CT)
-// (16 waves leave 128 registers each, which one part of 16 bf16 columns fits)
+// (16 waves leave 128 registers each, which 32 bf16 columns fit)
 constexpr int quant_attn_waves(bool f32, int ct) { return ct == 1 && !f32 ? 16 : 8; }
-inline int quant_attn_lds(int waves, int ct) { return waves > 1 ? waves * ct * (64 * 16 + 32) * static_cast<int>(sizeof(float)) : 0; }
+inline int quant_attn_lds(int waves, int ct) { return waves > 1 ? waves * ct * (64 * 32 + 64) * static_cast<int>(sizeof(float)) : 0; }
 
 template <typename T, int CT>
 __global__ void __launch_bounds__(64 * quant_attn_waves(std::is_same<T, float>::value, CT)) k_attn_quant(QuantAttn a, const T *__restrict__ q, T *__restrict__ out) {
-  constexpr int NS = std::is_same<T, float>::value ? 3 : 1, C = 16 * CT;
+  constexpr int NS = std::is_same<T, float>::value ? 3 : 1, C = 32 * CT;
   extern __shared__ __attribute__((aligned(16))) float lds[];
-  const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
-  const int W = blockDim.x >> 6, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int z = blockIdx.y;
+  const int lane = threadIdx.x & 63, hf = lane >> 5, c = lane & 31;
+  const int W = blockDim.x >> 6, z = blockIdx.y;
+  int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  asm volatile("" : "+s"(w));   // (kept, and not made again at each use)
   int tile, h;
   if (!tile_of_block(a, blockIdx.x, tile, h)) return;
   const QuantTile qt = find_tile(a, tile, C, lane);
@@ -165,41 +189,54 @@ __global__ void __launch_bounds__(64 * quant_attn_waves(std::is_same<T, float>::
   int id0 = fetch(page_of(0, 0));   // (the first ones ahead of the length where the walk starts at the first page)
   const int n_cols = qt.n * a.group - qt.j * C;   // columns from this tile's first on
   if (n_cols <= 0) return;
-  const int n_keys = tile_keys(a, qt, C), n_pages = (n_keys + kBlk - 1) / kBlk, n_pairs = (n_pages + 1) / 2;
-  const int run = run_pairs(n_pairs, a.n_splits), p0 = z * run, p1 = min(p0 + run, n_pairs);
+  // (quotients are formed in vector registers: back to scalar ones)
+  const int n_keys = scalar(tile_keys(a, qt, C)), n_pages = (n_keys + kBlk - 1) / kBlk, n_pairs = (n_pages + 1) / 2;
+  const int run = scalar(run_pairs(n_pairs, a.n_splits)), p0 = z * run, p1 = min(p0 + run, n_pairs);
   if (z > 0 && p0 >= p1) return;
   const bool whole = n_pairs <= run;
-  const int n_steps = p1 > p0 + w ? (p1 - p0 - w + W - 1) / W : 0;
+  const int n_steps = p1 > p0 + w ? scalar((p1 - p0 - w + W - 1) / W) : 0;
 
   // columns
-  bf16x8 qf[CT][2][NS];
+  bf16x8 qf[CT][4][NS];
   int lim[CT];   // last position that the lane's column sees
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) {
-    const int f = qt.j * C + min(16 * ct + c, n_cols - 1), row = f / a.group, hd = f - row * a.group;
+    const int f = qt.j * C + min(32 * ct + c, n_cols - 1), row = f / a.group, hd = f - row * a.group;
     lim[ct] = qt.S + row;
-    const T *p = q + (qt.base + row) * a.q_stride + (h * a.group + hd) * kHd + 16 * g;
-    load_q8(p, a.q_sign, qf[ct][0]);
-    load_q8(p + 8, a.q_sign, qf[ct][1]);
+    const T *p = q + (qt.base + row) * a.q_stride + (h * a.group + hd) * kHd + 32 * hf;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) load_q8(p + 8 * s, a.q_sign, qf[ct][s]);
   }
-  const int lim_first = qt.S + qt.j * C / a.group;   // what every column sees
+  const int lim_first = qt.S + scalar(qt.j * C / a.group);   // what every column sees
+  float q_most = 0.f;   // (of what is no number too: the largest bits)
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+    for (int s = 0; s < 4; ++s) q_most = most_bits(q_most, qf[ct][s][0]);
+  const bool calm = a.scale < kCalmScale && !__any(__float_as_uint(q_most) >= __float_as_uint(kCalmQuery));
 
   // Probabilities are 2^(scale s - ref).  ref is one of the column's scores, moved when one exceeds it by more than kRefSlack orders
   // (fp32 sums and bf16 probabilities have room for that), and 0 as long as the column has seen nothing.
-  floatx4 o[CT][4], l[CT];
+  floatx16 o[CT][2];
+  floatx4 l[CT];
   float ref[CT];
-  bool seen[CT];
+  bool seen[CT], spoilt[CT];
+  bool all_seen;   // every column of the wave has
+  auto clear = [&]() {
 #pragma unroll
-  for (int ct = 0; ct < CT; ++ct) {
+    for (int ct = 0; ct < CT; ++ct) {
 #pragma unroll
-    for (int t = 0; t < 4; ++t) o[ct][t] = floatx4{0.f, 0.f, 0.f, 0.f};
-    l[ct] = floatx4{0.f, 0.f, 0.f, 0.f};
-    ref[ct] = 0.f, seen[ct] = false;
-  }
-  bool all_seen = false;   // every column of the wave has
+      for (int e = 0; e < 16; ++e) o[ct][0][e] = o[ct][1][e] = 0.f;
+      l[ct] = floatx4{0.f, 0.f, 0.f, 0.f};
+      ref[ct] = 0.f, seen[ct] = spoilt[ct] = false;
+    }
+    all_seen = false;
+  };
+  clear();
+  // As a 16x16x32 operand the lanes of columns 16 .. 31 are k groups 1 and 3 of columns 0 .. 15: rows 4 u + i sum the groups of u's parity
   bf16x8 ones;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) ones[e] = static_cast<__bf16>(1.0f);
+  for (int e = 0; e < 8; ++e) ones[e] = static_cast<__bf16>(((lane >> 2) & 1) == ((lane >> 4) & 1) ? 1.0f : 0.0f);
 
   int id = 0;
   float ksc = 1.f, vsc = 1.f;
@@ -211,119 +248,180 @@ __global__ void __launch_bounds__(64 * quant_attn_waves(std::is_same<T, float>::
     bad = __ballot(!ok);
     id = (ok ? id : 0) * a.kv.n_kv_heads + h;
     ksc = a.kv.k_scale[id], vsc = a.kv.v_scale[id];
+    // they are waited for here: behind the branch around this the wait would be for every load in flight, at each step
+    asm volatile("" : "+v"(id), "+v"(ksc), "+v"(vsc));
   };
-  struct Step {
-    u32x4 k[2], v[2];
-    float ks[2], vs[2];
-    int bad;   // bit p: page p is left out
-  };
-  auto request = [&](int i, Step &s) {
-    if (i >= n_steps) return;
+  // What is in flight: the pages of the step, requested while the step before it works on its own
+  u32x4 kc[2], vc[2];    // K: 32 dims of the lane's key
+  struct Pages {
+    uint32_t id[2];
+    float ks, vs[2];
+    int bad;             // bit p: page p is left out
+    bool calm;
+  } now, next;
+  const uint8_t *k_lane = a.kv.k_codes + 512 * hf + 16 * (c & 15);
+  const bool second = (c & 16) != 0;   // the lane's key is in the pair's second page
+  auto request_k = [&](int i, Pages &s) {
     if ((i & 31) == 0) batch(i);
     const int src = 2 * (i & 31);
     s.bad = static_cast<int>(bad >> src) & 3;
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
-      const size_t at = static_cast<size_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(id, src + p))) * kPageCodes;
-      s.k[p] = reinterpret_cast<const u32x4 *>(a.kv.k_codes + at)[lane];
-      s.v[p] = reinterpret_cast<const u32x4 *>(a.kv.v_codes + at)[lane];
-      s.ks[p] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ksc), src + p));
+      s.id[p] = __builtin_amdgcn_readlane(id, src + p);
       s.vs[p] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vsc), src + p));
     }
+    const float ks0 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ksc), src));
+    const float ks1 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ksc), src + 1));
+    s.ks = second ? ks1 : ks0;
+    s.calm = calm && max(__float_as_uint(ks0), __float_as_uint(ks1)) < __float_as_uint(kCalmPage);
+    const uint32_t id_0 = s.id[0], id_1 = s.id[1];   // (values: a choice between the members would put them into memory)
+    const uint8_t *kp = k_lane + static_cast<size_t>(second ? id_1 : id_0) * kPageCodes;
+    kc[0] = *reinterpret_cast<const u32x4 *>(kp), kc[1] = *reinterpret_cast<const u32x4 *>(kp + 256);
   };
-  auto step = [&](int i, Step &s) {
-    if (i >= n_steps) return;
-    const int pos0 = 32 * (p0 + w + W * i);
-    float x[CT][8];   // the exponents: tokens 4 g + e of the first page, then of the second
+  auto request_v = [&](const Pages &s) {
 #pragma unroll
-    for (int p = 0; p < 2; ++p) {
-      const bf16x8 k0 = page_operand(s.k[p][0], s.k[p][1], s.ks[p], s.ks[p]), k1 = page_operand(s.k[p][2], s.k[p][3], s.ks[p], s.ks[p]);
+    for (int p = 0; p < 2; ++p) vc[p] = reinterpret_cast<const u32x4 *>(a.kv.v_codes + static_cast<size_t>(s.id[p]) * kPageCodes)[lane];
+  };
+  // the exponents of a step: x[ct][e] of key 8 (e / 4) + 4 hf + e % 4
+  auto scores = [&](int i_next, float (&x)[CT][16]) {
+    bf16x8 k[4];
+#pragma unroll
+    for (int d = 0; d < 4; ++d) k[d] = page_operand(kc[d >> 1][2 * (d & 1)], kc[d >> 1][2 * (d & 1) + 1], now.ks);
+    request_k(i_next, next);
+    floatx16 y[CT];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) y[ct][e] = 0.f;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int n = NS - 1; n >= 0; --n) y[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[d], qf[ct][d][n], y[ct], 0, 0, 0);
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[ct][e] = fmaf(y[ct][e], a.scale, -ref[ct]);
+  };
+  auto accumulate = [&](const float (&x)[CT][16]) {
+    bf16x8 pf[CT][2][NS];
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) {
-        floatx4 y = {0.f, 0.f, 0.f, 0.f};
+        float y[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = __builtin_amdgcn_exp2f(x[ct][8 * p + e]);
+        split8<NS>(y, pf[ct][p]);
+      }
+    bf16x8 v[2][2];
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) v[p][t] = page_operand(vc[p][2 * t], vc[p][2 * t + 1], now.vs[p]);
+    request_v(next);
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
         for (int n = NS - 1; n >= 0; --n) {
-          y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, qf[ct][0][n], y, 0, 0, 0);
-          y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, qf[ct][1][n], y, 0, 0, 0);
+          l[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[ct][p][n], l[ct], 0, 0, 0);
+          o[ct][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[p][0], pf[ct][p][n], o[ct][0], 0, 0, 0);
+          o[ct][1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[p][1], pf[ct][p][n], o[ct][1], 0, 0, 0);
         }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[ct][4 * p + e] = fmaf(y[e], a.scale, -ref[ct]);
-      }
-    }
-    const bool masked = s.bad != 0 || pos0 + 31 > lim_first;
-    bool move = false;   // (as integers, positive floats keep their order and negative ones lie below them)
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct) {
-      int m = __float_as_int(x[ct][0]);
-#pragma unroll
-      for (int e = 1; e < 8; ++e) m = max(m, __float_as_int(x[ct][e]));
-      move = move || m > __float_as_int(kRefSlack);
-    }
-    if (masked || !all_seen || __any(move)) {
-      if (masked) {
-#pragma unroll
-        for (int p = 0; p < 2; ++p) {
-          const bool gone = (s.bad >> p) & 1;
-          if (gone) s.v[p] = u32x4{0, 0, 0, 0}, s.vs[p] = 1.f;
-#pragma unroll
-          for (int ct = 0; ct < CT; ++ct) {
-            const int left = gone ? -1 : lim[ct] - (pos0 + 16 * p + 4 * g);
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (e > left) x[ct][4 * p + e] = -INFINITY;
-          }
-        }
-      }
-      bool all = true;
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct) {
-        float m = x[ct][0];
-#pragma unroll
-        for (int e = 1; e < 8; ++e) m = fmaxf(m, x[ct][e]);
-        m = half_max(quarter_max(m));
-        if (m > (seen[ct] ? kRefSlack : -INFINITY)) {
-          const float f = __builtin_amdgcn_exp2f(-m);   // (nothing seen: o and l are 0 or NaN, whatever f is, unless it is inf)
-#pragma unroll
-          for (int t = 0; t < 4; ++t) o[ct][t] = seen[ct] ? o[ct][t] * f : o[ct][t];
-          l[ct] = seen[ct] ? l[ct] * f : l[ct];
-          ref[ct] += m, seen[ct] = true;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[ct][e] -= m;
-        }
-        all = all && seen[ct];
-      }
-      all_seen = __all(all);
-    }
-    bf16x8 v[4];
-#pragma unroll
-    for (int t = 0; t < 4; ++t) v[t] = page_operand(s.v[0][t], s.v[1][t], s.vs[0], s.vs[1]);
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct) {
-      float p[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(x[ct][e]);
-      bf16x8 pf[NS];
-      split8<NS>(p, pf);
-#pragma unroll
-      for (int n = NS - 1; n >= 0; --n) {
-#pragma unroll
-        for (int t = 0; t < 4; ++t) o[ct][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[t], pf[n], o[ct][t], 0, 0, 0);
-        l[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[n], l[ct], 0, 0, 0);
-      }
-    }
+    now = next;
   };
-  Step s0, s1;
-  request(0, s0);
-  for (int i = 0; i < n_steps; i += 2) {
-    request(i + 1, s1);
-    step(i, s0);
-    request(i + 2, s0);
-    step(i + 1, s1);
+  // A step in which keys may be hidden, references may move or columns be no numbers
+  auto general = [&](int i, int i_next) {
+    const int pos0 = 32 * (p0 + w + W * i);
+    float x[CT][16];
+    scores(i_next, x);
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+      if ((now.bad >> p) & 1) vc[p] = u32x4{0, 0, 0, 0}, now.vs[p] = 1.f;
+    bool all = true;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      const int left = lim[ct] - (pos0 + 4 * hf);
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (8 * (e >> 2) + (e & 3) > left || ((now.bad >> (e >> 3)) & 1) != 0) x[ct][e] = -INFINITY;
+      if (!now.calm) {
+        bool fine = true;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) fine = fine && x[ct][e] < INFINITY;
+        spoilt[ct] = spoilt[ct] || __shfl_xor(fine ? 0 : 1, 32, kWave) != 0 || !fine;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[ct][e] = spoilt[ct] ? -INFINITY : x[ct][e];
+      }
+      float m = x[ct][0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) m = fmaxf(m, x[ct][e]);
+      m = half_max(m);
+      const bool move = m > (seen[ct] ? kRefSlack : -INFINITY);
+      const float by = move ? m : 0.f, f = move && seen[ct] ? __builtin_amdgcn_exp2f(-m) : 1.f;   // (nothing seen: o and l are 0)
+      o[ct][0] *= f, o[ct][1] *= f, l[ct] *= f;
+      ref[ct] += by, seen[ct] = seen[ct] || move;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[ct][e] -= by;
+      all = all && seen[ct];
+    }
+    all_seen = __all(all);
+    accumulate(x);
+  };
+  // Whether step i may be a common one: every column sees its keys and has seen some, and all is finite
+  bool careful = false;
+  auto common = [&](int i) { return now.bad == 0 && 32 * (p0 + w + W * i) + 31 <= lim_first && all_seen && now.calm && !careful; };
+  // Whether the sums so far stand: 0, or 1 if references have to move, 2 if the walk has to start again
+  auto sums = [&]() {
+    float m = l[0][0];
+#pragma unroll
+    for (int ct = 1; ct < CT; ++ct) m = fmaxf(m, l[ct][0]);
+    return !__any(!(m <= kSumMost)) ? 0 : (__any(!(m <= kSumLost)) ? 2 : 1);
+  };
+  // The walk: a general step, then common ones as long as they are.  (The general one stands outside the loop over the common
+  // ones: joined in one loop, their registers cost 34 moves a step.)  Pages are requested without a condition, so that no wait is
+  // for more than the step's own loads.
+  if (n_steps > 0) {
+    const int last = n_steps - 1;
+    for (int i = 0; i < n_steps;) {
+      if (i == 0) {
+        request_k(0, now);
+        request_v(now);
+      }
+      general(i, min(i + 1, last));
+      ++i;
+      int how = 0;
+      while (i < n_steps && common(i) && how == 0) {
+        float x[CT][16];
+        scores(min(i + 1, last), x);
+        accumulate(x);
+        ++i;
+        how = sums();
+      }
+      if (how == 2 && !careful) {
+        careful = true, i = 0;
+        clear();
+      } else if (how == 1) {
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+          if (l[ct][0] > kSumMost) o[ct][0] *= 1.f / kSumMost, o[ct][1] *= 1.f / kSumMost, l[ct] *= 1.f / kSumMost, ref[ct] += 40.f;
+      }
+    }
   }
 
-  // the waves' parts together; a column's 16 dims of a lane in pieces of four
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct)
+    if (spoilt[ct]) l[ct][0] = __uint_as_float(0x7fc00000u);
+  // the waves' parts together, four dims of a column at a time: piece i of a lane is dims 16 (i / 2) + 8 hf + 4 (i % 2) ..
+  auto piece = [&](int ct, int i) {
+    const int e = 4 * (i >> 1) + 2 * (i & 1);
+    return floatx4{o[ct][0][e], o[ct][1][e], o[ct][0][e + 1], o[ct][1][e + 1]};
+  };
   auto put = [&](int ct, int i, int ln, floatx4 x, float m, float sum) {
-    const int col = 16 * ct + (ln & 15), dim = 16 * (ln >> 4) + 4 * i;
+    const int col = 32 * ct + (ln & 31), dim = 16 * (i >> 1) + 8 * (ln >> 5) + 4 * (i & 1);
     if (col >= n_cols) return;
     if (whole) {
       const int f = qt.j * C + col, row = f / a.group, hd = f - row * a.group;
@@ -340,33 +438,32 @@ __global__ void __launch_bounds__(64 * quant_attn_waves(std::is_same<T, float>::
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        put(ct, i, lane, floatx4{o[ct][0][i], o[ct][1][i], o[ct][2][i], o[ct][3][i]}, seen[ct] ? ref[ct] : -INFINITY, l[ct][0]);
+      for (int i = 0; i < 8; ++i) put(ct, i, lane, piece(ct, i), seen[ct] ? ref[ct] : -INFINITY, l[ct][0]);
     return;
   }
-  float *const ml = lds + W * CT * 1024;   // [wave][part of 16 columns][reference | sum][16]
+  float *const ml = lds + W * CT * 2048;   // [wave][part of 32 columns][reference | sum][32]
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      *reinterpret_cast<floatx4 *>(lds + ((w * CT + ct) * 4 + i) * 256 + lane * 4) = floatx4{o[ct][0][i], o[ct][1][i], o[ct][2][i], o[ct][3][i]};
-    if (lane < 16) {
-      ml[(w * CT + ct) * 32 + lane] = seen[ct] ? ref[ct] : -INFINITY;
-      ml[(w * CT + ct) * 32 + 16 + lane] = l[ct][0];
+    for (int i = 0; i < 8; ++i) *reinterpret_cast<floatx4 *>(lds + ((w * CT + ct) * 8 + i) * 256 + lane * 4) = piece(ct, i);
+    if (lane < 32) {
+      ml[(w * CT + ct) * 64 + lane] = seen[ct] ? ref[ct] : -INFINITY;
+      ml[(w * CT + ct) * 64 + 32 + lane] = l[ct][0];
     }
   }
   __syncthreads();
-  for (int item = threadIdx.x; item < 256 * CT; item += blockDim.x) {
-    const int ln = item & 63, i = (item >> 6) & 3, ct = item >> 8;
+  for (int item = threadIdx.x; item < 512 * CT; item += blockDim.x) {
+    const int ln = item & 63, i = (item >> 6) & 7, ct = item >> 9, col = ln & 31;
+    if (32 * ct + col >= n_cols) continue;
     float m = -INFINITY;
-    for (int u = 0; u < W; ++u) m = fmaxf(m, ml[(u * CT + ct) * 32 + (ln & 15)]);
+    for (int u = 0; u < W; ++u) m = fmaxf(m, ml[(u * CT + ct) * 64 + col]);
     const float base = m == -INFINITY ? 0.f : m;
     floatx4 x = {0.f, 0.f, 0.f, 0.f};
     float sum = 0.f;
     for (int u = 0; u < W; ++u) {
-      const float f = exp2f(ml[(u * CT + ct) * 32 + (ln & 15)] - base);
-      x += f * *reinterpret_cast<const floatx4 *>(lds + ((u * CT + ct) * 4 + i) * 256 + ln * 4);
-      sum += f * ml[(u * CT + ct) * 32 + 16 + (ln & 15)];
+      const float f = __builtin_amdgcn_exp2f(ml[(u * CT + ct) * 64 + col] - base);
+      x += f * *reinterpret_cast<const floatx4 *>(lds + ((u * CT + ct) * 8 + i) * 256 + ln * 4);
+      sum += f * ml[(u * CT + ct) * 64 + 32 + col];
     }
     put(ct, i, ln, x, m, sum);
   }

@@ -5,9 +5,9 @@
 // 2^-6 * 2^e), a code's value is exact in bf16, and a page whose scale has to grow (a larger token joins it) keeps the values of
 // its earlier tokens but for those below 2^-6 of the new scale.  A page never holds a NaN or an infinity.
 //
-// Page layouts, in the order in which a wave of the attention reads them (16 bytes a lane, lane l = 16 g + c, one request a page):
-//   K  lane (g, c): token c, dims 16 g .. 16 g + 15
-//   V  lane (g, c): tokens 4 g .. 4 g + 3 of dim 4 c, then of dim 4 c + 1, 4 c + 2, 4 c + 3
+// Page layouts, in the order in which the attention's 32x32x16 products take their operands:
+//   K  [4 sixteenths of the dims][16 tokens][16 dims]
+//   V  [2 halves h][32 rows r][2 dims][8 tokens]: dims 2 r and 2 r + 1 of tokens 4 h .. 4 h + 3 and 8 + 4 h .. 8 + 4 h + 3
 #pragma once
 
 #include "common.h"
@@ -74,7 +74,18 @@ __device__ __forceinline__ void quant_store4(bf16 *p, const float *v) {   // (a 
                                   (__float_as_uint(v[2]) >> 16) | (__float_as_uint(v[3]) & 0xffff0000u)};
 }
 
-// Eight consecutive elements
+// Two and eight consecutive elements
+__device__ __forceinline__ void quant_load2(const float *p, float *v) { v[0] = p[0], v[1] = p[1]; }
+__device__ __forceinline__ void quant_load2(const bf16 *p, float *v) {
+  typedef uint32_t u1 __attribute__((aligned(2)));
+  const uint32_t x = *reinterpret_cast<const u1 *>(p);
+  v[0] = __uint_as_float(x << 16), v[1] = __uint_as_float(x & 0xffff0000u);
+}
+__device__ __forceinline__ void quant_store2(float *p, const float *v) { p[0] = v[0], p[1] = v[1]; }
+__device__ __forceinline__ void quant_store2(bf16 *p, const float *v) {
+  typedef uint32_t u1 __attribute__((aligned(2)));
+  *reinterpret_cast<u1 *>(p) = (__float_as_uint(v[0]) >> 16) | (__float_as_uint(v[1]) & 0xffff0000u);
+}
 __device__ __forceinline__ void quant_load8(const float *p, float *v) { quant_load4(p, v), quant_load4(p + 4, v + 4); }
 __device__ __forceinline__ void quant_load8(const bf16 *p, float *v) {
   typedef uint32_t u4 __attribute__((ext_vector_type(4), aligned(2)));
@@ -90,6 +101,9 @@ __device__ __forceinline__ void quant_store8(bf16 *p, const float *v) {
   for (int i = 0; i < 4; ++i) x[i] = (__float_as_uint(v[2 * i]) >> 16) | (__float_as_uint(v[2 * i + 1]) & 0xffff0000u);
   *reinterpret_cast<u4 *>(p) = x;
 }
+
+// Token of the j-th byte of half vh in a V page
+__device__ __forceinline__ int v_token(int j, int vh) { return 8 * (j >> 2) + 4 * vh + (j & 3); }
 
 // Runs: rows whose places are consecutive slots of one block.  A wave looks at rows r0 .. r0 + span - 1 (span <= 16) and takes
 // the runs that start there; one may reach 15 rows further.
@@ -125,7 +139,7 @@ inline int run_span(int64_t n_rows, int heads) { return n_rows * heads <= 32768 
 template <typename T>
 __global__ void __launch_bounds__(256) k_quant_append(QuantKV kv, int n_rows, int span, const int32_t *__restrict__ row_slot, const T *__restrict__ k,
                                                       const T *__restrict__ v, int64_t k_stride, int64_t v_stride, int32_t *status) {
-  const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, h = blockIdx.y;
+  const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, vh = lane >> 5, vr = lane & 31, h = blockIdx.y;
   const int r0 = (blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * span;
   if (r0 >= n_rows) return;
   RowRuns runs(row_slot, n_rows, r0, span, kv.n_blocks * kBlk, lane);
@@ -136,23 +150,23 @@ __global__ void __launch_bounds__(256) k_quant_append(QuantKV kv, int n_rows, in
     const int off = place % kBlk, page = place / kBlk * kv.n_kv_heads + h;
     u32x4 *kp = reinterpret_cast<u32x4 *>(kv.k_codes + static_cast<size_t>(page) * kPageCodes) + lane;
     u32x4 *vp = reinterpret_cast<u32x4 *>(kv.v_codes + static_cast<size_t>(page) * kPageCodes) + lane;
-    float kx[16], vx[4][4];   // K: dims 16 g .. of token c; V: [token 4 g + j][dim 4 c + e]
+    float kx[16], vx[8][2];   // K: dims 16 g .. of token c; V: [token v_token(j)][dim 2 vr + e]
 #pragma unroll
-    for (int e = 0; e < 16; ++e) kx[e] = vx[e >> 2][e & 3] = 0.f;
+    for (int e = 0; e < 16; ++e) kx[e] = vx[e >> 1][e & 1] = 0.f;
     const int ik = c - off;
     if (ik >= 0 && ik < n) {
       const T *p = k + (r + ik) * k_stride + h * kHd + 16 * g;
       quant_load8(p, kx), quant_load8(p + 8, kx + 8);
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int iv = 4 * g + j - off;
-      if (iv >= 0 && iv < n) quant_load4(v + (r + iv) * v_stride + h * kHd + 4 * c, vx[j]);
+    for (int j = 0; j < 8; ++j) {
+      const int iv = v_token(j, vh) - off;
+      if (iv >= 0 && iv < n) quant_load2(v + (r + iv) * v_stride + h * kHd + 2 * vr, vx[j]);
     }
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
       kx[e] = quant_input(kx[e], odd);
-      vx[e >> 2][e & 3] = quant_input(vx[e >> 2][e & 3], odd);
+      vx[e >> 1][e & 1] = quant_input(vx[e >> 1][e & 1], odd);
     }
     if (off > 0) {
       const u32x4 kc = *kp, vc = *vp;
@@ -160,24 +174,26 @@ __global__ void __launch_bounds__(256) k_quant_append(QuantKV kv, int n_rows, in
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         float x[4], y[4];
-        dequant4(kc[j], ks, x), dequant4(vc[j], vs, y);   // (y: dim 4 c + j of tokens 4 g ..)
+        dequant4(kc[j], ks, x), dequant4(vc[j], vs, y);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           if (c < off) kx[4 * j + e] = x[e];
-          if (4 * g + e < off) vx[e][j] = y[e];
+          const int t = 4 * (j & 1) + e;
+          if (v_token(t, vh) < off) vx[t][j >> 1] = y[e];
         }
       }
     }
     float ka = 0.f, va = 0.f;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) ka = fmaxf(ka, fabsf(kx[e])), va = fmaxf(va, fabsf(vx[e >> 2][e & 3]));
+    for (int e = 0; e < 16; ++e) ka = fmaxf(ka, fabsf(kx[e])), va = fmaxf(va, fabsf(vx[e >> 1][e & 1]));
     const int ke = scale_exp(wave_max(ka)), ve = scale_exp(wave_max(va));
     const float ki = exp2_int(-ke), vi = exp2_int(-ve);
     u32x4 kc, vc;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       kc[j] = quant4(kx[4 * j] * ki, kx[4 * j + 1] * ki, kx[4 * j + 2] * ki, kx[4 * j + 3] * ki);
-      vc[j] = quant4(vx[0][j] * vi, vx[1][j] * vi, vx[2][j] * vi, vx[3][j] * vi);
+      const int t = 4 * (j & 1), d = j >> 1;
+      vc[j] = quant4(vx[t][d] * vi, vx[t + 1][d] * vi, vx[t + 2][d] * vi, vx[t + 3][d] * vi);
     }
     *kp = kc, *vp = vc;
     if (lane == 0) kv.k_scale[page] = exp2_int(ke), kv.v_scale[page] = exp2_int(ve);
@@ -189,7 +205,7 @@ __global__ void __launch_bounds__(256) k_quant_append(QuantKV kv, int n_rows, in
 template <typename T>
 __global__ void __launch_bounds__(256) k_quant_read(QuantKV kv, int n_rows, int span, const int32_t *__restrict__ row_slot, T *__restrict__ k,
                                                     T *__restrict__ v, int64_t k_stride, int64_t v_stride) {
-  const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, h = blockIdx.y;
+  const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, vh = lane >> 5, vr = lane & 31, h = blockIdx.y;
   const int r0 = (blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * span;
   if (r0 >= n_rows) return;
   RowRuns runs(row_slot, n_rows, r0, span, kv.n_blocks * kBlk, lane);
@@ -207,13 +223,13 @@ __global__ void __launch_bounds__(256) k_quant_read(QuantKV kv, int n_rows, int 
     const u32x4 kc = reinterpret_cast<const u32x4 *>(kv.k_codes + static_cast<size_t>(page) * kPageCodes)[lane];
     const u32x4 vc = reinterpret_cast<const u32x4 *>(kv.v_codes + static_cast<size_t>(page) * kPageCodes)[lane];
     const float ks = kv.k_scale[page], vs = kv.v_scale[page];
-    float kx[16], vx[4][4];
+    float kx[16], vx[8][2];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       float y[4];
       dequant4(kc[j], ks, kx + 4 * j), dequant4(vc[j], vs, y);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) vx[e][j] = y[e];
+      for (int e = 0; e < 4; ++e) vx[4 * (j & 1) + e][j >> 1] = y[e];
     }
     const int ik = c - off;
     if (ik >= 0 && ik < n) {
@@ -221,9 +237,9 @@ __global__ void __launch_bounds__(256) k_quant_read(QuantKV kv, int n_rows, int 
       quant_store8(p, kx), quant_store8(p + 8, kx + 8);
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int iv = 4 * g + j - off;
-      if (iv >= 0 && iv < n) quant_store4(v + (r + iv) * v_stride + h * kHd + 4 * c, vx[j]);
+    for (int j = 0; j < 8; ++j) {
+      const int iv = v_token(j, vh) - off;
+      if (iv >= 0 && iv < n) quant_store2(v + (r + iv) * v_stride + h * kHd + 2 * vr, vx[j]);
     }
   }
 }

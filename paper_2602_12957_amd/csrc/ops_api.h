@@ -53,21 +53,18 @@ struct QuantPlan {
 QuantPlan plan_quant_attention(const hsd_kv_quant *kv, const hsd_batch *b, int32_t n_q_heads, bool f32) {
   const int64_t group = n_q_heads / kv->n_kv_heads, cols = b->total_q * group;
   QuantPlan p;
-  auto tiles = [&](int ct) { return cols / (16 * ct) + b->n_seq; };
-  p.ct = cols <= 24 * b->n_seq ? 1 : (f32 || cols <= 48 * b->n_seq ? 2 : 4);
-  p.n_tiles = static_cast<int>(tiles(p.ct));
+    p.ct = f32 || cols <= 40 * b->n_seq ? 1 : 2;
+  p.n_tiles = static_cast<int>(cols / (32 * p.ct) + b->n_seq);
   const int64_t groups = p.n_tiles * static_cast<int64_t>(kv->n_kv_heads), max_pairs = (b->max_blocks_per_seq + 1) / 2;
   // tiles that have columns, about (each sequence may have an empty one more)
-  const int64_t real = (cols <= 16 * p.ct * b->n_seq ? b->n_seq : cols / (16 * p.ct) + b->n_seq / 2) * kv->n_kv_heads;
+  const int64_t real = (cols <= 32 * p.ct * b->n_seq ? b->n_seq : cols / (32 * p.ct) + b->n_seq / 2) * kv->n_kv_heads;
   // keys over the workgroups where a wave of a full workgroup would take more than eight steps and the chip is not full
   p.n_splits = 1;
   if (max_pairs > 128 && real < 512) p.n_splits = static_cast<int>(std::min<int64_t>({(511 + real) / real, (max_pairs + 63) / 64, kMaxSplits}));
   // keys over the waves: as many as fit the chip at once
-  const int64_t fit = p.ct == 1 && !f32 ? 4096 : 2048;
   const int most = quant_attn_waves(f32, p.ct);
-  p.waves = 1;
-  while (p.waves < most && real * p.n_splits * p.waves * 2 <= fit && p.waves < max_pairs) p.waves *= 2;
-  p.part_rows = p.n_splits > 1 ? static_cast<size_t>(groups) * p.n_splits * 16 * p.ct : 0;
+  p.waves = static_cast<int>(std::max<int64_t>(std::min<int64_t>({most, 256 * most / (real * p.n_splits), max_pairs}), 1));
+  p.part_rows = p.n_splits > 1 ? static_cast<size_t>(groups) * p.n_splits * 32 * p.ct : 0;
   return p;
 }
 
@@ -82,7 +79,7 @@ int launch_quant_attention(hipStream_t st, const QuantAttn &a, const QuantPlan &
   hipLaunchKernelGGL(kern, dim3(tile_blocks(p.n_tiles, a.kv.n_kv_heads), p.n_splits), dim3(64 * p.waves), lds, st, a, q, out);
   HSD_LAUNCH_CHECK();
   if (p.n_splits > 1) {
-    hipLaunchKernelGGL((k_attn_quant_join<T>), dim3(groups, 4 * CT), dim3(256), 0, st, a, 16 * CT, out);
+    hipLaunchKernelGGL((k_attn_quant_join<T>), dim3(groups, 8 * CT), dim3(256), 0, st, a, 32 * CT, out);
     HSD_LAUNCH_CHECK();
   }
   return HSD_OK;
@@ -222,12 +219,11 @@ int hsd_kv_quant_attention(void *stream, const hsd_kv_quant *kv, const hsd_batch
   if (dtype == HSD_BF16) {
     const bf16 *x = static_cast<const bf16 *>(q);
     bf16 *y = static_cast<bf16 *>(out);
-    return p.ct == 1 ? launch_quant_attention<bf16, 1>(st, a, p, x, y)
-                     : (p.ct == 2 ? launch_quant_attention<bf16, 2>(st, a, p, x, y) : launch_quant_attention<bf16, 4>(st, a, p, x, y));
+    return p.ct == 1 ? launch_quant_attention<bf16, 1>(st, a, p, x, y) : launch_quant_attention<bf16, 2>(st, a, p, x, y);
   }
   const float *x = static_cast<const float *>(q);
   float *y = static_cast<float *>(out);
-  return p.ct == 1 ? launch_quant_attention<float, 1>(st, a, p, x, y) : launch_quant_attention<float, 2>(st, a, p, x, y);
+  return launch_quant_attention<float, 1>(st, a, p, x, y);
 }
 
 size_t hsd_token_logprobs_bytes(int32_t n_rows, int32_t vocab, int32_t n_top) {
