@@ -444,8 +444,9 @@ __global__ void __launch_bounds__(64 * quant_attn_waves(std::is_same<T, float>::
   float *const ml = lds + W * CT * 2048;   // [wave][part of 32 columns][reference | sum][32]
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) {
+    if (32 * ct + c < n_cols)   // (a token of 4 heads: 4 of the 32)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) *reinterpret_cast<floatx4 *>(lds + ((w * CT + ct) * 8 + i) * 256 + lane * 4) = piece(ct, i);
+      for (int i = 0; i < 8; ++i) *reinterpret_cast<floatx4 *>(lds + ((w * CT + ct) * 8 + i) * 256 + lane * 4) = piece(ct, i);
     if (lane < 32) {
       ml[(w * CT + ct) * 64 + lane] = seen[ct] ? ref[ct] : -INFINITY;
       ml[(w * CT + ct) * 64 + 32 + lane] = l[ct][0];

@@ -53,17 +53,24 @@ struct QuantPlan {
 QuantPlan plan_quant_attention(const hsd_kv_quant *kv, const hsd_batch *b, int32_t n_q_heads, bool f32) {
   const int64_t group = n_q_heads / kv->n_kv_heads, cols = b->total_q * group;
   QuantPlan p;
-    p.ct = f32 || cols <= 40 * b->n_seq ? 1 : 2;
+    // tiles that have columns, about (each sequence may have an empty one more)
+  auto real_tiles = [&](int64_t c) { return (cols <= c * b->n_seq ? b->n_seq : cols / c + b->n_seq / 2) * kv->n_kv_heads; };
+  // 64 columns a wave where that still gives every SIMD its two waves: they share what making operands of pages costs.  Below,
+  // 32, of which a unit holds 16 waves.  us a call, 64 / 32 columns, by tiles of 64 (16 heads on 4): 576 (16 blocks of up to 257 rows
+  // on 1055 keys) 34.0 / 29.7, 1024 (4 of 2000 rows) 77.7 / 71.2, 2112 (64 of up to 256 rows on 1280) 95.4 / 96.6.
+  const int64_t tiles64 = real_tiles(64);
+  p.ct = f32 || tiles64 < 2048 ? 1 : 2;
   p.n_tiles = static_cast<int>(cols / (32 * p.ct) + b->n_seq);
   const int64_t groups = p.n_tiles * static_cast<int64_t>(kv->n_kv_heads), max_pairs = (b->max_blocks_per_seq + 1) / 2;
-  // tiles that have columns, about (each sequence may have an empty one more)
-  const int64_t real = (cols <= 32 * p.ct * b->n_seq ? b->n_seq : cols / (32 * p.ct) + b->n_seq / 2) * kv->n_kv_heads;
+  const int64_t real = p.ct == 2 ? tiles64 : real_tiles(32);
   // keys over the workgroups where a wave of a full workgroup would take more than eight steps and the chip is not full
   p.n_splits = 1;
   if (max_pairs > 128 && real < 512) p.n_splits = static_cast<int>(std::min<int64_t>({(511 + real) / real, (max_pairs + 63) / 64, kMaxSplits}));
-  // keys over the waves: as many as fit the chip at once
+  // keys over the waves: as many as fit the chip at once, and two at least (late tiles of a block see more keys than early ones:
+  // 4 blocks of 2000 rows 89 us with one wave a tile, 71 with two)
   const int most = quant_attn_waves(f32, p.ct);
-  p.waves = static_cast<int>(std::max<int64_t>(std::min<int64_t>({most, 256 * most / (real * p.n_splits), max_pairs}), 1));
+  const int64_t fit = 256 * (f32 ? 8 : most) / (real * p.n_splits);
+  p.waves = static_cast<int>(std::max<int64_t>(std::min<int64_t>({most, std::max<int64_t>(fit, p.ct == 2 ? 1 : 2), max_pairs}), 1));
   p.part_rows = p.n_splits > 1 ? static_cast<size_t>(groups) * p.n_splits * 32 * p.ct : 0;
   return p;
 }
