@@ -99,7 +99,8 @@ struct ScorePlan {
 };
 ScorePlan plan_scores(int64_t n_rows, int64_t vocab, int piece) {
   ScorePlan p;
-  p.n_parts = static_cast<int>(std::max<int64_t>(std::min<int64_t>({kScoreParts, 512 / std::max<int64_t>(n_rows, 1), vocab / 16384}), 1));
+  // (16 rows of 32768: 7 us in one part, 6 and 4 to join them in two)
+  p.n_parts = static_cast<int>(std::max<int64_t>(std::min<int64_t>({kScoreParts, 512 / std::max<int64_t>(n_rows, 1), vocab / 32768}), 1));
   p.part_len = static_cast<int>(vocab);
   if (p.n_parts > 1) {
     const int64_t unit = 64 * piece;   // (no part is empty: 64 * 8 * 16 is less than a part)

@@ -65,22 +65,24 @@ __device__ __forceinline__ void piece_at(const T *x, int piece, int len, float (
 }
 
 struct ScoreSum {
-  float m, z, w;
+  float m, z, w;   // m: -inf where no logit was seen; z is then 0, or NaN where there was a NaN
 };
-__device__ __forceinline__ ScoreSum score_join(const ScoreSum &a, const ScoreSum &b) {
-  const float m = fmaxf(a.m, b.m);
-  ScoreSum r{m, 0.f, 0.f};
-  auto add = [&](const ScoreSum &s) {
-    if (s.m == -INFINITY) {   // no logit: 0, or NaN where there was a NaN
-      r.z += s.z;
-      return;
-    }
-    const float d = s.m - m, f = expf(d);
-    r.z += s.z * f;
-    if (f != 0.f) r.w += (s.w + d * s.z) * f;
-  };
-  add(a), add(b);
-  return r;
+// The sums of `s` with reference m (not below its own)
+__device__ __forceinline__ ScoreSum score_at(const ScoreSum &s, float m) {
+  if (s.m == -INFINITY) return ScoreSum{m, s.z, 0.f};
+  const float d = s.m - m, f = __builtin_amdgcn_exp2f(d * 1.4426950408889634f);
+  return ScoreSum{m, s.z * f, f != 0.f ? (s.w + d * s.z) * f : 0.f};
+}
+// The sums of 2^n lanes together, in all of them
+template <int N>
+__device__ __forceinline__ ScoreSum score_lanes(ScoreSum s) {
+  float m = s.m;
+#pragma unroll
+  for (int o = N / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, kWave));
+  s = score_at(s, m);
+#pragma unroll
+  for (int o = N / 2; o > 0; o >>= 1) s.z += __shfl_xor(s.z, o, kWave), s.w += __shfl_xor(s.w, o, kWave);
+  return s;
 }
 
 // What a row's sums give; v: the token's logit, -inf for none
@@ -151,15 +153,12 @@ __global__ void __launch_bounds__(64 * NW) k_token_scores(TokenScores a, const T
       }
   }
   if (thr == -INFINITY) s.m = -INFINITY;
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) s = score_join(s, ScoreSum{__shfl_xor(s.m, o, kWave), __shfl_xor(s.z, o, kWave), __shfl_xor(s.w, o, kWave)});
+  s = score_lanes<64>(s);
   if (lane == 0) s_sum[wave] = s;
   s_best[wave][lane] = best == -INFINITY ? 0 : score_key(best, best_piece);
   if (t == 0) s_n = 0;
   __syncthreads();
-  s = s_sum[0];
-#pragma unroll
-  for (int w = 1; w < NW; ++w) s = score_join(s, s_sum[w]);
+  s = score_lanes<NW>(s_sum[lane & (NW - 1)]);
   const bool whole = a.n_parts == 1;
   const size_t at = static_cast<size_t>(r) * a.n_parts + part;
   if (t == 0) {
@@ -168,24 +167,24 @@ __global__ void __launch_bounds__(64 * NW) k_token_scores(TokenScores a, const T
   }
   if (a.n_top == 0) return;
 
-  // the bound and the lanes that reach it
-  if (wave == 0) {
+  // the bound and the lanes that reach it: each wave ranks 64 / NW of the lanes
+  {
     uint64_t key = s_best[0][lane];
 #pragma unroll
     for (int w = 1; w < NW; ++w) key = max(key, s_best[w][lane]);
-    int rank = 0;
-#pragma unroll 8
-    for (int j = 0; j < 64; ++j) {
-      const uint64_t o = (static_cast<uint64_t>(__builtin_amdgcn_readlane(static_cast<uint32_t>(key >> 32), j)) << 32) |
-                         static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<uint32_t>(key), j));
-      rank += o > key;
-    }
     const int n = min(__popcll(__ballot(key != 0)), a.n_top);
-    if (key != 0 && rank < n) {
-      s_win[rank] = lane;
-      if (rank == n - 1) s_bound = key;
+#pragma unroll
+    for (int i = 0; i < 64 / NW; ++i) {
+      const int j = wave * (64 / NW) + i;
+      const uint64_t mine = (static_cast<uint64_t>(__builtin_amdgcn_readlane(static_cast<uint32_t>(key >> 32), j)) << 32) |
+                            static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<uint32_t>(key), j));
+      const int rank = __popcll(__ballot(key > mine));
+      if (mine != 0 && rank < n) {
+        s_win[rank] = j;
+        if (rank == n - 1) s_bound = mine;
+      }
     }
-    if (lane == 0) s_winners = n;
+    if (t == 0) s_winners = n;
   }
   __syncthreads();
   const int winners = s_winners;
@@ -252,10 +251,11 @@ __global__ void __launch_bounds__(256) k_token_scores_join(TokenScores a, const 
   __shared__ uint64_t s_key[kScoreParts * HSD_MAX_TOP];
   const int r = blockIdx.x, t = threadIdx.x;
   ScoreSum s{-INFINITY, 0.f, 0.f};
-  for (int p = 0; p < a.n_parts; ++p) {
-    const float4 v = a.part_sums[static_cast<size_t>(r) * a.n_parts + p];
-    s = score_join(s, ScoreSum{v.x, v.y, v.z});
+  if ((t & 15) < a.n_parts) {
+    const float4 v = a.part_sums[static_cast<size_t>(r) * a.n_parts + (t & 15)];
+    s = ScoreSum{v.x, v.y, v.z};
   }
+  s = score_lanes<kScoreParts>(s);
   if (t == 0) {
     const int tok = a.tokens[r];
     const bool inside = tok >= 0 && tok < a.vocab;

@@ -8,6 +8,7 @@ import torch
 from . import binding as B
 
 _TYPES = {torch.bfloat16: B.HSD_BF16, torch.float32: B.HSD_FP32}
+_SPLIT = 65536     # a row of fewer logits is not split over workgroups and takes no workspace
 
 
 class TokenScores(NamedTuple):
@@ -44,7 +45,7 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, n_top: int = 0) -
     entropy = torch.empty(n, dtype=torch.float32, device=dev)
     ids = torch.empty((n, n_top), dtype=torch.int32, device=dev)
     top = torch.empty((n, n_top), dtype=torch.float32, device=dev)
-    nb = B.hsd_token_logprobs_bytes(n, vocab, n_top)
+    nb = B.hsd_token_logprobs_bytes(n, vocab, n_top) if vocab >= _SPLIT else 0
     ws = torch.empty(nb, dtype=torch.uint8, device=dev) if nb else None
     with B.on_device(index):
         B.hsd_token_logprobs(B.current_stream(index), n, vocab, _TYPES[logits.dtype], logits.data_ptr(), stride, tokens.data_ptr(),
