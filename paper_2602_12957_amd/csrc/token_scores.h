@@ -5,10 +5,11 @@
 // which two threads with references m, m' join as Z + Z' e^(m' - m), W + (W' + (m' - m) Z') e^(m' - m); in the end
 // log p(t) = x_t - m - ln Z and the entropy is ln Z - W / Z.
 //
-// Alternatives.  A lane (the same lane of all waves) keeps the largest value it has seen and the 16-byte piece of the row in which
-// it saw it first.  The k-th largest of these 64 (value, piece) pairs bounds the k-th largest logit from below, and what
-// reaches it lies with the k lanes that have such a pair: only their pieces are read again, k / 64 of the row, from the cache.
-// What reaches the bound is listed in LDS (little more than k entries unless large logits lie 64 pieces apart) and ranked.
+// Alternatives.  The row's lines of 128 bytes are dealt to 64 groups in turns, and each keeps the largest value and the 16-byte piece
+// in which it stands first.  The k-th largest of these 64 (value, piece) pairs bounds the k-th largest logit from below, and what
+// reaches it lies in the k groups that have such a pair: only their lines are read again, k / 64 of the row.
+// (Groups of single pieces read a line for each: 1856 rows of 32749 bf16 logits with eight alternatives fetched 203 MB where the
+// logits are 122.)  What reaches the bound is listed in LDS (little more than k entries unless large logits lie 64 lines apart) and ranked.
 #pragma once
 
 #include "common.h"
@@ -41,23 +42,23 @@ __device__ __forceinline__ float key_value(uint64_t k) {
 __device__ __forceinline__ int key_index(uint64_t k) { return static_cast<int>(0xffffffffu - static_cast<uint32_t>(k)); }
 
 // A piece: 16 bytes of a row, aligned to its elements
-__device__ __forceinline__ void load_piece(const float *p, float (&x)[4]) {
-  typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
-  const f4 v = *reinterpret_cast<const f4 *>(p);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) x[i] = v[i];
-}
-__device__ __forceinline__ void load_piece(const bf16 *p, float (&x)[8]) {
+__device__ __forceinline__ u32x4 load_piece(const void *p) {
   typedef uint32_t u4 __attribute__((ext_vector_type(4), aligned(2)));
-  const u4 v = *reinterpret_cast<const u4 *>(p);
+  return *reinterpret_cast<const u4 *>(p);
+}
+__device__ __forceinline__ void piece_values(u32x4 u, float (&x)[4]) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(v[i] << 16), x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+  for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(u[i]);
+}
+__device__ __forceinline__ void piece_values(u32x4 u, float (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(u[i] << 16), x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
 }
 template <typename T, int E>
 __device__ __forceinline__ void piece_at(const T *x, int piece, int len, float (&v)[E]) {
   const int i0 = piece * E;
   if (i0 + E <= len) {
-    load_piece(x + i0, v);
+    piece_values(load_piece(x + i0), v);
   } else {
 #pragma unroll
     for (int e = 0; e < E; ++e) v[e] = i0 + e < len ? to_f32(x[i0 + e]) : -INFINITY;
@@ -101,8 +102,11 @@ __device__ __forceinline__ void score_write_top(const TokenScores &a, int r, con
 template <typename T, int NW>
 __global__ void __launch_bounds__(64 * NW) k_token_scores(TokenScores a, const T *__restrict__ logits) {
   constexpr int E = 16 / sizeof(T), U = 4;
+  // a wave's 64 pieces are 8 lines: a thread's pieces belong to NB groups, and NC waves share one
+  constexpr int NB = NW < 8 ? 8 / NW : 1, NC = NW > 8 ? NW / 8 : 1;
+  static_assert(U % NB == 0 && (NW % 8 == 0 || 8 % NW == 0), "a round's lines are whole turns of the groups");
   __shared__ ScoreSum s_sum[NW];
-  __shared__ uint64_t s_best[NW][64], s_list[kScoreList], s_bound, s_next[NW];
+  __shared__ uint64_t s_best[NC][64], s_list[kScoreList], s_bound, s_next[NW];
   __shared__ int s_win[64], s_n, s_winners;
   const int r = blockIdx.x / a.n_parts, part = blockIdx.x - r * a.n_parts, t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63;
   const int first = part * a.part_len, len = min(a.part_len, a.vocab - first);
@@ -114,28 +118,23 @@ __global__ void __launch_bounds__(64 * NW) k_token_scores(TokenScores a, const T
   const float tv = inside && a.n_parts == 1 ? to_f32(x[tok]) : -INFINITY;
 
   ScoreSum s{0.f, 0.f, 0.f};   // (m: 0 while nothing was seen, thr then -inf)
-  float thr = -INFINITY, best = -INFINITY;
-  int best_piece = 0;
-  for (int p0 = t; p0 < n_pieces; p0 += 64 * NW * U) {
-    float v[U][E], top[U];
+  float thr = -INFINITY, best[NB];
+  int best_piece[NB];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int p = p0 + u * 64 * NW;
-      if (p < n_pieces) {
-        piece_at(x, p, len, v[u]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) v[u][e] = -INFINITY;
-      }
-    }
+  for (int b = 0; b < NB; ++b) best[b] = -INFINITY, best_piece[b] = 0;
+  // N pieces, the first of them piece p0, the others 64 * NW apart; the first belongs to the thread's group b0
+  auto take = [&](auto &v, int p0, int b0) {
+    constexpr int N = sizeof(v) / sizeof(v[0]);
     float all = -INFINITY;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      top[u] = v[u][0];
+    for (int u = 0; u < N; ++u) {
+      float top = v[u][0];
 #pragma unroll
-      for (int e = 1; e < E; ++e) top[u] = fmaxf(top[u], v[u][e]);
-      if (top[u] > best) best = top[u], best_piece = p0 + u * 64 * NW;
-      all = fmaxf(all, top[u]);
+      for (int e = 1; e < E; ++e) top = fmaxf(top, v[u][e]);
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+        if (top > best[b] && (b0 + u) % NB == b) best[b] = top, best_piece[b] = p0 + u * 64 * NW;
+      all = fmaxf(all, top);
     }
     if (all > thr) {
       const float d = s.m - all, f = thr == -INFINITY ? 0.f : expf(d);
@@ -144,18 +143,47 @@ __global__ void __launch_bounds__(64 * NW) k_token_scores(TokenScores a, const T
       s.m = all, thr = all + kScoreSlack;
     }
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int u = 0; u < N; ++u)
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const float d = v[u][e] - s.m, p = __builtin_amdgcn_exp2f(d * 1.4426950408889634f);
         s.z += p;                                   // NaN where the logit is
         s.w = fmaf(fmaxf(d, -200.f), p, s.w);       // (below -200 p is 0)
       }
+  };
+  // U pieces a thread at a time, the next ones requested while these are worked on; then the pieces that are left one by one
+  constexpr int kStep = 64 * NW * U;
+  const int n_rounds = (len / E) / kStep;
+  u32x4 raw[U];
+  auto request = [&](int i) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) raw[u] = load_piece(x + static_cast<size_t>(i * kStep + u * 64 * NW + t) * E);
+  };
+  if (n_rounds > 0) request(0);
+  for (int i = 0; i < n_rounds; ++i) {
+    float v[U][E];
+#pragma unroll
+    for (int u = 0; u < U; ++u) piece_values(raw[u], v[u]);
+    request(min(i + 1, n_rounds - 1));
+    take(v, i * kStep + t, 0);
+  }
+  for (int p0 = n_rounds * kStep + t, b0 = 0; p0 < n_pieces; p0 += 64 * NW, ++b0) {
+    float v[1][E];
+    piece_at(x, p0, len, v[0]);
+    take(v, p0, b0);
   }
   if (thr == -INFINITY) s.m = -INFINITY;
   s = score_lanes<64>(s);
   if (lane == 0) s_sum[wave] = s;
-  s_best[wave][lane] = best == -INFINITY ? 0 : score_key(best, best_piece);
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {   // the eight lanes of a line
+    uint64_t key = best[b] == -INFINITY ? 0 : score_key(best[b], best_piece[b]);
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1)
+      key = max(key, (static_cast<uint64_t>(__shfl_xor(static_cast<uint32_t>(key >> 32), o, kWave)) << 32) |
+                         static_cast<uint32_t>(__shfl_xor(static_cast<uint32_t>(key), o, kWave)));
+    if ((lane & 7) == 0) s_best[wave / 8][(b * NW + wave) % 8 * 8 + (lane >> 3)] = key;
+  }
   if (t == 0) s_n = 0;
   __syncthreads();
   s = score_lanes<NW>(s_sum[lane & (NW - 1)]);
@@ -167,11 +195,11 @@ __global__ void __launch_bounds__(64 * NW) k_token_scores(TokenScores a, const T
   }
   if (a.n_top == 0) return;
 
-  // the bound and the lanes that reach it: each wave ranks 64 / NW of the lanes
+  // the bound and the groups that reach it: each wave ranks 64 / NW of them
   {
     uint64_t key = s_best[0][lane];
 #pragma unroll
-    for (int w = 1; w < NW; ++w) key = max(key, s_best[w][lane]);
+    for (int w = 1; w < NC; ++w) key = max(key, s_best[w][lane]);
     const int n = min(__popcll(__ballot(key != 0)), a.n_top);
 #pragma unroll
     for (int i = 0; i < 64 / NW; ++i) {
@@ -188,12 +216,11 @@ __global__ void __launch_bounds__(64 * NW) k_token_scores(TokenScores a, const T
   }
   __syncthreads();
   const int winners = s_winners;
-  const uint64_t bound = winners < a.n_top ? 0 : s_bound;   // fewer lanes than alternatives: all their logits are listed
+  const uint64_t bound = winners < a.n_top ? 0 : s_bound;   // fewer groups than alternatives: all their logits are listed
   // listed: keys by value and piece not behind the bound (a piece's logits have its index there, so this errs on the safe side)
   auto walk = [&](auto &&take) {
     for (int i = wave; i < winners; i += NW) {
-      const int l = s_win[i];
-      for (int p = l + 64 * lane; p < n_pieces; p += 64 * 64) {
+      for (int p = 8 * (s_win[i] + 64 * (lane >> 3)) + (lane & 7); p < n_pieces; p += 8 * 64 * 8) {
         float v[E];
         piece_at(x, p, len, v);
 #pragma unroll

@@ -168,6 +168,21 @@ def test_large_logits_64_pieces_apart(dtype, step, rows):
     check(logits, torch.zeros(rows, dtype=torch.int32, device="cuda"), 5)
 
 
+@pytest.mark.parametrize("dtype,line", [(torch.bfloat16, 64), (torch.float32, 32)])
+@pytest.mark.parametrize("rows,turns", [(3, 12), (600, 5), (1100, 5)])
+def test_large_logits_64_lines_apart(dtype, line, rows, turns):
+    """The largest logits in the lines of half of the groups: more of them reach the bound than the list holds."""
+    rng = np.random.default_rng(8)
+    vocab = turns * 64 * line + 5
+    x = rng.standard_normal((rows, vocab))
+    where = (np.arange(vocab) // line) % 2 == 0
+    x[:, where] += 40.0
+    logits = torch.from_numpy(x).to(dtype).cuda()
+    tokens = torch.from_numpy(rng.integers(0, vocab, rows).astype(np.int32)).cuda()
+    check(logits, tokens, 32)
+    check(logits, tokens, 5)
+
+
 def test_many_rows():
     """More rows than a grid's second dimension takes."""
     rng = np.random.default_rng(7)
