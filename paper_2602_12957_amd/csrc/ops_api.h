@@ -138,12 +138,10 @@ int hsd_kv_reserve(void *stream, const hsd_kv_pool *pool, const hsd_batch *b, in
   if (b->status == nullptr || (row_slot == nullptr && b->total_q > 0)) return HSD_EINVAL;
   const KvPlace p{b->n_seq, b->total_q, b->n_slots, b->max_blocks_per_seq, pool->n_blocks, b->cu_q, b->seq_slot, b->seq_len,
                   b->block_table, pool->free_list, pool->free_count, b->status, row_slot, row_pos};
-  // one workgroup places up to 16384 rows in the time that a second launch takes
-  const bool rows = b->total_q <= 16384;
-  hipLaunchKernelGGL(k_kv_place, dim3(1), dim3(1024), 0, static_cast<hipStream_t>(stream), p, rows ? 1 : 0);
+  hipLaunchKernelGGL(k_kv_place, dim3(1), dim3(1024), 0, static_cast<hipStream_t>(stream), p);
   HSD_LAUNCH_CHECK();
-  if (!rows) {
-    hipLaunchKernelGGL(k_kv_place_rows, dim3((b->total_q + 2047) / 2048), dim3(256), 0, static_cast<hipStream_t>(stream), p);
+  if (b->total_q > kPlaceRows) {
+    hipLaunchKernelGGL(k_kv_place_rows, dim3((b->total_q + 1023) / 1024), dim3(256), 0, static_cast<hipStream_t>(stream), p);
     HSD_LAUNCH_CHECK();
   }
   return HSD_OK;
