@@ -34,11 +34,10 @@ __device__ __forceinline__ int scale_exp(float amax) {
 
 // Largest magnitude the cache can hold: 448 * 2^119
 __device__ __forceinline__ float quant_limit() { return 448.f * exp2_int(kScaleExpMax); }
-// what is stored of x: finite, within the limit
+// what is stored of x: finite, within the limit; `odd`: x was not finite
 __device__ __forceinline__ float quant_input(float x, bool &odd) {
-  const bool nan = x != x;
-  odd = odd || !(fabsf(x) <= 3.402823466e38f);
-  return nan ? 0.f : fminf(fmaxf(x, -quant_limit()), quant_limit());
+  odd = odd || !(fabsf(x) < INFINITY);
+  return x == x ? __builtin_amdgcn_fmed3f(x, -quant_limit(), quant_limit()) : 0.f;
 }
 // four values of magnitude <= 448 to four e4m3 codes, nearest, ties to even
 __device__ __forceinline__ uint32_t quant4(float a, float b, float c, float d) {
@@ -151,22 +150,22 @@ __global__ void __launch_bounds__(256) k_quant_append(QuantKV kv, int n_rows, in
     u32x4 *kp = reinterpret_cast<u32x4 *>(kv.k_codes + static_cast<size_t>(page) * kPageCodes) + lane;
     u32x4 *vp = reinterpret_cast<u32x4 *>(kv.v_codes + static_cast<size_t>(page) * kPageCodes) + lane;
     float kx[16], vx[8][2];   // K: dims 16 g .. of token c; V: [token v_token(j)][dim 2 vr + e]
-#pragma unroll
-    for (int e = 0; e < 16; ++e) kx[e] = vx[e >> 1][e & 1] = 0.f;
+    // (loads without a condition, of the run's nearest row where a slot is not one of its: all are in flight at once)
     const int ik = c - off;
-    if (ik >= 0 && ik < n) {
-      const T *p = k + (r + ik) * k_stride + h * kHd + 16 * g;
+    {
+      const T *p = k + (r + min(max(ik, 0), n - 1)) * k_stride + h * kHd + 16 * g;
       quant_load8(p, kx), quant_load8(p + 8, kx + 8);
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const int iv = v_token(j, vh) - off;
-      if (iv >= 0 && iv < n) quant_load2(v + (r + iv) * v_stride + h * kHd + 2 * vr, vx[j]);
+      quant_load2(v + (r + min(max(iv, 0), n - 1)) * v_stride + h * kHd + 2 * vr, vx[j]);
     }
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      kx[e] = quant_input(kx[e], odd);
-      vx[e >> 1][e & 1] = quant_input(vx[e >> 1][e & 1], odd);
+      const int iv = v_token(e >> 1, vh) - off;
+      kx[e] = ik >= 0 && ik < n ? quant_input(kx[e], odd) : 0.f;
+      vx[e >> 1][e & 1] = iv >= 0 && iv < n ? quant_input(vx[e >> 1][e & 1], odd) : 0.f;
     }
     if (off > 0) {
       const u32x4 kc = *kp, vc = *vp;
