@@ -351,6 +351,19 @@ int hsd_kv_quant_attention(void *stream, const hsd_kv_quant *kv, const hsd_batch
                            float softmax_scale, const void *q, int64_t q_stride, void *out, int64_t out_stride,
                            void *workspace, size_t ws_bytes);
 
+/* Decoder passes on an 8-bit cache: hsd_verify_region_batch and hsd_prefill with the keys and values of layer l in layers[l]
+ * (a HOST array of n_layers; each with pool's n_blocks and the model's n_kv_heads).  Of `pool` n_blocks, free_list and free_count are
+ * used, its page pointers are not looked at.  A row's keys and values are rounded to the model's type as always and then to the page's codes,
+ * its own included: it attends to what the cache holds.  Chains only: HSD_EINVAL with batch.tree_end.  The scale of a page follows from the rows in it,
+ * rejected ones included until they are overwritten, so that a row's last bits depend on the block that it came in (by the values below 2^-6 of a scale).
+ * Commit with hsd_kv_commit_rollback (the page pointers of its pool have to be set, to anything) or hsd_kv_commit_rows.
+ * workspace: hsd_workspace_quant_bytes(desc, total_q, n_seq, max_blocks_per_seq) bytes at least, 256-byte aligned. */
+size_t hsd_workspace_quant_bytes(const hsd_model_desc *desc, int32_t max_total_q, int32_t max_n_seq, int32_t max_blocks_per_seq);
+int hsd_verify_quant(hsd_ctx *ctx, void *stream, const hsd_kv_pool *pool, const hsd_kv_quant *layers, const hsd_batch *batch,
+                     void *workspace, size_t ws_bytes);
+int hsd_prefill_quant(hsd_ctx *ctx, void *stream, const hsd_kv_pool *pool, const hsd_kv_quant *layers, const hsd_batch *batch,
+                      void *workspace, size_t ws_bytes);
+
 /* Scores of given tokens.  Row r of logits (dev [n_rows][vocab] in dtype, row_stride elements apart) is a distribution
  * softmax(logits[r]): logprob[r] = log p(tokens[r]) (-inf for an id outside the vocabulary), entropy[r] in nats, and the n_top
  * most probable tokens, largest first, the lower id first among equal logits: top_ids, top_logprobs dev [n_rows][n_top].

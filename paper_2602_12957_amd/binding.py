@@ -106,7 +106,7 @@ EXPORTS = ["hsd_probe_launch", "hsd_verify_region_batch_noalloc", "hsd_noalloc_s
            "hsd_workspace_bytes", "hsd_kv_pool_init", "hsd_verify_region_batch", "hsd_verify_page",
            "hsd_kv_commit_rollback", "hsd_prefill", "hsd_drafts_create", "hsd_drafts_destroy", "hsd_drafts_tree", "hsd_tree_path",
            "hsd_kv_reserve", "hsd_kv_commit_rows", "hsd_kv_quant_append", "hsd_kv_quant_read", "hsd_kv_quant_attention_bytes",
-           "hsd_kv_quant_attention", "hsd_token_logprobs_bytes", "hsd_token_logprobs"]
+           "hsd_kv_quant_attention", "hsd_workspace_quant_bytes", "hsd_verify_quant", "hsd_prefill_quant", "hsd_token_logprobs_bytes", "hsd_token_logprobs"]
 lib.hsd_drafts_create.argtypes = [vp, vp, i32, C.POINTER(vp)]
 lib.hsd_drafts_destroy.argtypes, lib.hsd_drafts_destroy.restype = [vp], None
 lib.hsd_drafts_tree.argtypes = [vp, vp, i32, C.c_int64, C.c_int64, i32, vp, vp, vp, C.POINTER(i32)]
@@ -118,6 +118,9 @@ lib.hsd_kv_quant_append.argtypes = [vp, _P(hsd_kv_quant), i32, vp, i32, vp, vp, 
 lib.hsd_kv_quant_read.argtypes = [vp, _P(hsd_kv_quant), i32, vp, i32, vp, vp, i64, i64]
 lib.hsd_kv_quant_attention_bytes.argtypes, lib.hsd_kv_quant_attention_bytes.restype = [_P(hsd_kv_quant), _P(hsd_batch), i32], szt
 lib.hsd_kv_quant_attention.argtypes = [vp, _P(hsd_kv_quant), _P(hsd_batch), i32, i32, f32, vp, i64, vp, i64, vp, szt]
+lib.hsd_workspace_quant_bytes.argtypes, lib.hsd_workspace_quant_bytes.restype = [_P(hsd_model_desc), i32, i32, i32], szt
+for _n in ("hsd_verify_quant", "hsd_prefill_quant"):
+    getattr(lib, _n).argtypes = [vp, vp, _P(hsd_kv_pool), _P(hsd_kv_quant), _P(hsd_batch), vp, szt]
 lib.hsd_token_logprobs_bytes.argtypes, lib.hsd_token_logprobs_bytes.restype = [i32, i32, i32], szt
 lib.hsd_token_logprobs.argtypes = [vp, i32, i32, i32, vp, i64, vp, vp, vp, i32, vp, vp, vp, szt]
 
@@ -204,3 +207,10 @@ def hsd_token_logprobs(stream, n_rows, vocab, dtype, logits, row_stride, tokens,
     rc = lib.hsd_token_logprobs(stream, n_rows, vocab, dtype, logits, row_stride, tokens, logprob, entropy, n_top, top_ids, top_logprobs, ws,
                                 ws_bytes)
     if rc: check("hsd_token_logprobs", rc)
+def hsd_workspace_quant_bytes(desc, max_total_q, max_n_seq, max_blocks_per_seq):
+    return lib.hsd_workspace_quant_bytes(C.byref(desc), max_total_q, max_n_seq, max_blocks_per_seq)
+def hsd_verify_quant(ctx, stream, pool, layers, batch, ws, ws_bytes):
+    """layers: ctypes array of hsd_kv_quant, one a layer"""
+    check("hsd_verify_quant", lib.hsd_verify_quant(ctx, stream, C.byref(pool), layers, C.byref(batch), ws, ws_bytes))
+def hsd_prefill_quant(ctx, stream, pool, layers, batch, ws, ws_bytes):
+    check("hsd_prefill_quant", lib.hsd_prefill_quant(ctx, stream, C.byref(pool), layers, C.byref(batch), ws, ws_bytes))

@@ -13,6 +13,7 @@
 #include "../../include/hsd.h"
 #include "attn_mfma.h"
 #include "attn_simple.h"
+#include "attn_quant.h"
 #include "attn_wide.h"
 #include "common.h"
 #include "draft_trees.h"
@@ -26,8 +27,11 @@
 #include "probes.h"
 #include "gemm_f32.h"
 #include "gemm_simple.h"
+#include "kv_place.h"
+#include "kv_quant.h"
 #include "misc_kernels.h"
 #include "pass_setup.h"
+#include "token_scores.h"
 
 using namespace hsd;
 
@@ -545,6 +549,8 @@ int launch_attn_wide(hipStream_t st, int n_wg, int n_q_heads, int g4, const Attn
   return HSD_OK;
 }
 
+#include "ops_launch.h"
+
 // How a pass's attention is split into tasks; decided once per pass, the task table is built accordingly.
 struct AttnPlan {
   bool mfma = false;   // bf16 with a grouping of query heads that fits the kernels; otherwise the plain kernel
@@ -668,9 +674,10 @@ bool weights_pass_by(const hsd_model_desc &d, const hsd_kv_pool *pool, const hsd
   return layers > kCacheBytes && kept <= kCacheBytes;
 }
 
+// layers: the 8-bit pages of every layer, or NULL: pool's pages in the model's type
 template <typename T>
 int forward(hsd_ctx *ctx, hipStream_t st, const hsd_kv_pool *pool, const hsd_batch *b, void *ws_base, bool page_mode,
-            bool with_head) {
+            bool with_head, const hsd_kv_quant *layers = nullptr) {
   const hsd_model_desc &d = ctx->desc;
   const int Tq = b->total_q;
   Workspace ws = carve(d, Tq, b->n_seq, ws_base);
@@ -678,7 +685,15 @@ int forward(hsd_ctx *ctx, hipStream_t st, const hsd_kv_pool *pool, const hsd_bat
   const bool relaxed = with_head && b->log_tau < 0.f;   // Eq. 11 with tau < 1: needs the draft tokens' own logits
   int rc;
 
-  const AttnPlan plan = plan_attention<T>(ctx, pool, b, page_mode);
+  const AttnPlan plan = layers == nullptr ? plan_attention<T>(ctx, pool, b, page_mode) : AttnPlan{};
+  QuantWorkspace qws{};
+  QuantPlan qplan{};
+  if (layers != nullptr) {
+    qws = carve_quant(d, Tq, b->n_seq, b->max_blocks_per_seq, ws_base);
+    qplan = plan_quant_attention(layers, b, d.n_q_heads, d.dtype == HSD_FP32);
+    hipLaunchKernelGGL(k_own_rows, dim3((Tq + 255) / 256), dim3(256), 0, st, Tq, qws.row);
+    HSD_LAUNCH_CHECK();
+  }
   const bool pass_by = weights_pass_by(d, pool, b);
   const bool dump = with_head && b->n_dump > 0 && b->logits_dump != nullptr;
   {
@@ -753,6 +768,10 @@ int forward(hsd_ctx *ctx, hipStream_t st, const hsd_kv_pool *pool, const hsd_bat
 
   for (int l = 0; l < d.n_layers; ++l) {
     PagedKV kv{pool->k_pool, pool->v_pool, b->block_table, b->max_blocks_per_seq, pool->n_blocks, d.n_kv_heads, l};
+    if (layers != nullptr) {   // the projection leaves the rows in order in pages of the workspace
+      kv = PagedKV{qws.k, qws.v, b->block_table, b->max_blocks_per_seq, (Tq + kBlk - 1) / kBlk, d.n_kv_heads, 0};
+      meta.row_kv = qws.row;
+    }
     // layer 0 reads the operand the set-up launch normalised; later layers the one the previous down projection left
     EpiQKV<T> eq{d.n_q_heads, d.n_kv_heads, meta, kv, static_cast<T *>(ws.q), l == 0 ? rs_none : rs_down};
     {
@@ -762,7 +781,17 @@ int forward(hsd_ctx *ctx, hipStream_t st, const hsd_kv_pool *pool, const hsd_bat
     }
     {
       ProfScope ps(ctx, st, HSD_PROF_ATTENTION);
-      if ((rc = launch_attention<T>(ctx, st, b, meta, kv, ws, plan))) return rc;
+      if (layers != nullptr) {
+        const int64_t stride = qdim;
+        if ((rc = launch_append(st, quant_pages(layers + l), Tq, ws.row_kv, QuantStaged<T>{static_cast<const T *>(qws.k), static_cast<const T *>(qws.v), d.n_kv_heads}, b->status)))
+          return rc;
+        // (bf16 query rows carry the scale, see EpiQKV::kQScale)
+        const float scale2 = std::is_same<T, bf16>::value ? 1.0f : 0.125f * kLog2e;
+        rc = run_quant_attention(st, layers + l, b, d.n_q_heads, d.dtype, scale2, ws.q, stride, ws.a, stride, qws.parts, qplan);
+      } else {
+        rc = launch_attention<T>(ctx, st, b, meta, kv, ws, plan);
+      }
+      if (rc != HSD_OK) return rc;
     }
     if ((rc = residual_proj(kSiteO, HSD_PROF_GEMM_O, ws.a, ctx->wo[l], qdim, ctx->ffn_norm[l], o_ss2))) return rc;
     EpiSwiGLU<T> es{static_cast<T *>(ws.u), d.d_ffn, rs_o};
@@ -811,18 +840,18 @@ int forward(hsd_ctx *ctx, hipStream_t st, const hsd_kv_pool *pool, const hsd_bat
 }
 
 int verify_common(hsd_ctx *ctx, void *stream, const hsd_kv_pool *pool, const hsd_batch *b, void *ws, size_t ws_bytes,
-                  bool page_mode, bool prefill) {
+                  bool page_mode, bool prefill, const hsd_kv_quant *layers = nullptr) {
   if (ctx == nullptr || ws == nullptr) return HSD_EINVAL;
-  int rc = hsd_validate_batch(&ctx->desc, pool, b, ws_bytes);
+  int rc = hsd_validate_batch(&ctx->desc, layers == nullptr ? pool : nullptr, b, ws_bytes);
   if (rc != HSD_OK) return rc;
   if (pool == nullptr) return HSD_EINVAL;
   if (!prefill && (b->argmax == nullptr || b->accept_len == nullptr || b->bonus == nullptr)) return HSD_EINVAL;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const bool with_head = !prefill;
   if (ctx->desc.dtype == HSD_BF16)
-    rc = forward<bf16>(ctx, st, pool, b, ws, page_mode, with_head);
+    rc = forward<bf16>(ctx, st, pool, b, ws, page_mode, with_head, layers);
   else
-    rc = forward<float>(ctx, st, pool, b, ws, page_mode, with_head);
+    rc = forward<float>(ctx, st, pool, b, ws, page_mode, with_head, layers);
   if (rc != HSD_OK) return rc;
   if (prefill) {
     hipLaunchKernelGGL(k_kv_commit, dim3(1), dim3(1024), 0, st, b->n_seq, b->cu_q, b->seq_slot, b->n_slots,
@@ -832,6 +861,24 @@ int verify_common(hsd_ctx *ctx, void *stream, const hsd_kv_pool *pool, const hsd
     HSD_LAUNCH_CHECK();
   }
   return HSD_OK;
+}
+
+// A pass on an 8-bit cache: chains only, every layer's pages numbered by the same pool
+int quant_pass(hsd_ctx *ctx, void *stream, const hsd_kv_pool *pool, const hsd_kv_quant *layers, const hsd_batch *b, void *ws, size_t ws_bytes,
+               bool prefill) {
+  if (ctx == nullptr || layers == nullptr || b == nullptr) return HSD_EINVAL;
+  const hsd_model_desc &d = ctx->desc;
+  int rc = check_free_list(pool);
+  if (rc == HSD_OK) rc = check_rows(b);   // (refuses trees)
+  for (int l = 0; rc == HSD_OK && l < d.n_layers; ++l) {
+    rc = check_quant(layers + l);
+    if (rc == HSD_OK && (layers[l].n_blocks != pool->n_blocks || layers[l].n_kv_heads != d.n_kv_heads)) rc = HSD_EINVAL;
+  }
+  if (rc == HSD_OK) rc = check_heads(layers, b, d.n_q_heads);
+  if (rc != HSD_OK) return rc;
+  if (ws == nullptr || (reinterpret_cast<uintptr_t>(ws) & 255) != 0 || b->total_q < b->n_seq) return HSD_EINVAL;
+  if (ws_bytes < carve_quant(d, b->total_q, b->n_seq, b->max_blocks_per_seq, nullptr).total) return HSD_ENOSPC;
+  return verify_common(ctx, stream, pool, b, ws, ws_bytes, /*page_mode=*/false, prefill, layers);
 }
 
 }  // namespace

@@ -132,12 +132,39 @@ struct RowRuns {
 // of 4 heads 22.5 us against 13).
 inline int run_span(int64_t n_rows, int heads) { return n_rows * heads <= 32768 ? 1 : 16; }
 
+// Where rows come from.  Rows of a caller, apart by strides; or a decoder pass's own, left by the projection in pages of the model's
+// type (row r in page r / 16, see kv_v_elem)
+template <typename T>
+struct QuantRows {
+  const T *k, *v;
+  int64_t k_stride, v_stride;
+  __device__ __forceinline__ void keys16(int r, int h, int g, float *x) const {
+    const T *p = k + r * k_stride + h * kHd + 16 * g;
+    quant_load8(p, x), quant_load8(p + 8, x + 8);
+  }
+  __device__ __forceinline__ void values2(int r, int h, int vr, float *x) const { quant_load2(v + r * v_stride + h * kHd + 2 * vr, x); }
+};
+template <typename T>
+struct QuantStaged {
+  const T *k, *v;
+  int n_kv_heads;
+  __device__ __forceinline__ size_t page(int r, int h) const { return (static_cast<size_t>(r / kBlk) * n_kv_heads + h) * kPageCodes; }
+  __device__ __forceinline__ void keys16(int r, int h, int g, float *x) const {
+    const T *p = k + page(r, h) + r % kBlk * kHd + 16 * g;
+    quant_load8(p, x), quant_load8(p + 8, x + 8);
+  }
+  __device__ __forceinline__ void values2(int r, int h, int vr, float *x) const {
+    const T *p = v + page(r, h);
+    x[0] = to_f32(p[kv_v_elem(r % kBlk, 2 * vr)]), x[1] = to_f32(p[kv_v_elem(r % kBlk, 2 * vr + 1)]);
+  }
+};
+
 // New rows into the pages.  One wave a run and kv head: what the page keeps of earlier tokens (slots before the run's first) and
 // the new rows make up the page; slots behind them become 0.
 // grid: (ceil(n_rows / (4 * span)), n_kv_heads), block 256
-template <typename T>
-__global__ void __launch_bounds__(256) k_quant_append(QuantKV kv, int n_rows, int span, const int32_t *__restrict__ row_slot, const T *__restrict__ k,
-                                                      const T *__restrict__ v, int64_t k_stride, int64_t v_stride, int32_t *status) {
+template <typename Src>
+__global__ void __launch_bounds__(256) k_quant_append(QuantKV kv, int n_rows, int span, const int32_t *__restrict__ row_slot, Src src,
+                                                      int32_t *status) {
   const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, vh = lane >> 5, vr = lane & 31, h = blockIdx.y;
   const int r0 = (blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * span;
   if (r0 >= n_rows) return;
@@ -152,14 +179,11 @@ __global__ void __launch_bounds__(256) k_quant_append(QuantKV kv, int n_rows, in
     float kx[16], vx[8][2];   // K: dims 16 g .. of token c; V: [token v_token(j)][dim 2 vr + e]
     // (loads without a condition, of the run's nearest row where a slot is not one of its: all are in flight at once)
     const int ik = c - off;
-    {
-      const T *p = k + (r + min(max(ik, 0), n - 1)) * k_stride + h * kHd + 16 * g;
-      quant_load8(p, kx), quant_load8(p + 8, kx + 8);
-    }
+    src.keys16(r + min(max(ik, 0), n - 1), h, g, kx);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const int iv = v_token(j, vh) - off;
-      quant_load2(v + (r + min(max(iv, 0), n - 1)) * v_stride + h * kHd + 2 * vr, vx[j]);
+      src.values2(r + min(max(iv, 0), n - 1), h, vr, vx[j]);
     }
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
@@ -198,6 +222,12 @@ __global__ void __launch_bounds__(256) k_quant_append(QuantKV kv, int n_rows, in
     if (lane == 0) kv.k_scale[page] = exp2_int(ke), kv.v_scale[page] = exp2_int(ve);
   }
   if (status != nullptr && __any(odd) && lane == 0) atomicOr(status, HSD_STATUS_NOT_FINITE);
+}
+
+// row r's place among a pass's own rows: itself
+__global__ void __launch_bounds__(256) k_own_rows(int n, int32_t *__restrict__ row) {
+  const int r = blockIdx.x * 256 + threadIdx.x;
+  if (r < n) row[r] = r;
 }
 
 // The values of rows back out of the pages; rows without a place become 0.  Runs, grid and block as for k_quant_append.

@@ -15,6 +15,7 @@ import numpy as np
 import torch
 
 from . import binding as B
+from .scoring import TokenScores, token_logprobs
 
 
 def _pack_bf16(a: np.ndarray) -> np.ndarray:
@@ -86,11 +87,15 @@ class VerifyOutput:
 class Engine:
     def __init__(self, desc, weights: dict, n_blocks: int, n_slots: int, max_blocks_per_seq: int,
                  max_total_q: int, max_dump: int = 0, device: str = "cuda:0", attn_key_chunk: int = 0,
-                 debug: Optional[dict] = None):
+                 debug: Optional[dict] = None, kv_cache: str = "model"):
         """debug: {"sync_layers" | "force_simple": int, "gemm_cfg": (qkv, o, gate_up, down, lm_head)} ->
-        hsd_debug_set (experiments and cross-checks only)."""
+        hsd_debug_set (experiments and cross-checks only).
+        kv_cache: "model" holds keys and values in the model's type, "fp8" in e4m3 codes with a power-of-two scale for each block
+        and kv head (half of a bf16 cache's bytes; chains only, no packed trees, no noalloc)."""
         if not torch.cuda.is_available():
             raise RuntimeError("the HSD verification path needs a GPU (MI355X); there is no CPU fallback")
+        if kv_cache not in ("model", "fp8"):
+            raise ValueError(f'kv_cache is "model" or "fp8", got {kv_cache!r}')
         self.dev = torch.device(device)
         torch.cuda.set_device(self.dev)
         self.bf16 = desc.dtype == "bf16"
@@ -131,9 +136,21 @@ class Engine:
 
         # ---- paged KV pools + per-sequence state
         es = torch.int16 if self.bf16 else torch.float32
-        pool_elems = L * n_blocks * desc.n_kv_heads * B.HSD_KV_BLOCK_TOKENS * B.HSD_HEAD_DIM
+        page = B.HSD_KV_BLOCK_TOKENS * B.HSD_HEAD_DIM
+        pool_elems = L * n_blocks * desc.n_kv_heads * page
+        if kv_cache == "fp8":
+            es = torch.uint8
         self.k_pool = torch.zeros(pool_elems, dtype=es, device=self.dev)
         self.v_pool = torch.zeros(pool_elems, dtype=es, device=self.dev)
+        self.layers8 = None                                      # 8-bit cache: every layer's pages
+        if kv_cache == "fp8":
+            self.k_scale = torch.ones((L, n_blocks, desc.n_kv_heads), dtype=torch.float32, device=self.dev)
+            self.v_scale = torch.ones_like(self.k_scale)
+            per = n_blocks * desc.n_kv_heads
+            self.layers8 = (B.hsd_kv_quant * L)(*[
+                B.hsd_kv_quant(self.k_pool.data_ptr() + l * per * page, self.v_pool.data_ptr() + l * per * page,
+                               self.k_scale.data_ptr() + 4 * l * per, self.v_scale.data_ptr() + 4 * l * per, n_blocks, desc.n_kv_heads)
+                for l in range(L)])
         # all KV bookkeeping lives in one int32 buffer so that a snapshot/restore is a single device copy
         # (the outputs the host reads back every round -- status, alpha, bonus, stop rows -- sit together at its end: one copy;
         # the stop rows come last and are not restored: a pass's stay readable until the next pass over trees)
@@ -156,7 +173,8 @@ class Engine:
                                    _ptr(self.free_count))
 
         # ---- workspace and batch staging
-        self.ws_bytes = B.hsd_workspace_bytes(self.cdesc, max_total_q, n_slots)
+        self.ws_bytes = (B.hsd_workspace_bytes(self.cdesc, max_total_q, n_slots) if self.layers8 is None else
+                         B.hsd_workspace_quant_bytes(self.cdesc, max_total_q, n_slots, max_blocks_per_seq))
         self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.dev)
         n_meta = (n_slots + 1) + n_slots + 3 * max_total_q + max(max_dump, 1)
         self._h_meta = torch.empty(n_meta, dtype=torch.int32).pin_memory()
@@ -208,7 +226,8 @@ class Engine:
         B.hsd_kv_pool_init(self.stream, self.cpool)
 
     def snapshot(self):
-        """Remembers the KV bookkeeping (free stack, lengths, block tables); cached K/V data is not copied."""
+        """Remembers the KV bookkeeping (free stack, lengths, block tables); cached K/V data is not copied (with an 8-bit cache a
+        later pass may round earlier tokens of a page that it adds to once more)."""
         self._snapshot.copy_(self._restored)
 
     def restore(self):
@@ -278,6 +297,18 @@ class Engine:
         return b
 
     # ------------------------------------------------------------------ library calls
+    def _pass(self, b: B.hsd_batch, mode: str, noalloc: bool = False):
+        """One verification pass over the batch, by the cache's type and the mode."""
+        if self.layers8 is not None:
+            if noalloc:
+                raise ValueError("an 8-bit cache takes this engine's workspace")
+            B.hsd_verify_quant(self.ctx, self.stream, self.cpool, self.layers8, b, _ptr(self.ws), self.ws_bytes)
+        elif noalloc:     # the library's own fixed scratch array instead of this engine's workspace
+            B.hsd_verify_region_batch_noalloc(self.ctx, self.stream, self.cpool, b)
+        else:
+            fn = B.hsd_verify_region_batch if mode == "region" else B.hsd_verify_page
+            fn(self.ctx, self.stream, self.cpool, b, _ptr(self.ws), self.ws_bytes)
+
     def prefill(self, slots: Sequence[int], tokens: Sequence[np.ndarray], embeds: Optional[Sequence] = None,
                 chunk: Optional[int] = None):
         """Appends rows to the sequences' caches.  tokens[i][r] < 0 takes row r of embeds[i] (fp32 [n, d]): a numpy
@@ -306,7 +337,10 @@ class Engine:
                         em.append(torch.from_numpy(np.ascontiguousarray(e[c0:c0 + per], dtype=np.float32)).to(self.dev))
                 dev_emb = torch.cat(em, dim=0).contiguous()
             b = self._make_batch(sl, tk, with_outputs=False, embeds=dev_emb)
-            B.hsd_prefill(self.ctx, self.stream, self.cpool, b, _ptr(self.ws), self.ws_bytes)
+            if self.layers8 is not None:
+                B.hsd_prefill_quant(self.ctx, self.stream, self.cpool, self.layers8, b, _ptr(self.ws), self.ws_bytes)
+            else:
+                B.hsd_prefill(self.ctx, self.stream, self.cpool, b, _ptr(self.ws), self.ws_bytes)
             if dev_emb is not None:
                 torch.cuda.current_stream(self.dev).synchronize()   # dev_emb must outlive the pass
 
@@ -316,17 +350,23 @@ class Engine:
         log_tau = 0 is the exact-match rule; log_tau < 0 the relaxed acceptance test with threshold tau.
         With trees[i] = (tree_end, tree_depth), blocks[i] holds the tokens of a packed prefix tree
         (see pack_prefix_tree) instead of a chain."""
+        if trees is not None and self.layers8 is not None:
+            raise ValueError("an 8-bit cache verifies chains, not packed trees")
         b = self._make_batch(slots, blocks, dump_rows, log_tau=log_tau, trees=trees)
-        if noalloc:       # the library's own fixed scratch array instead of this engine's workspace
-            B.hsd_verify_region_batch_noalloc(self.ctx, self.stream, self.cpool, b)
-        else:
-            fn = B.hsd_verify_region_batch if mode == "region" else B.hsd_verify_page
-            fn(self.ctx, self.stream, self.cpool, b, _ptr(self.ws), self.ws_bytes)
+        self._pass(b, mode, noalloc)
         self._batch = b
         n, T = b.n_seq, b.total_q
         return VerifyOutput(n, T, self._cu.copy(), self.argmax[:T], self.margin[:T], self.accept_len[:n],
                             self.bonus[:n], self.logits_dump[:b.n_dump] if b.n_dump else None,
                             self.gap[:T] if log_tau < 0 else None, self.stop_row[:n] if trees is not None else None)
+
+    def score(self, out: VerifyOutput, tokens: Sequence[int], n_top: int = 0) -> TokenScores:
+        """Log probabilities of tokens[i] under the i-th dumped row's logits of a verify (dump_rows), the rows' entropies and their
+        n_top most probable tokens.  On the logits of that pass: call it before the next one.  Asynchronous."""
+        if out.logits is None or len(tokens) != out.logits.shape[0]:
+            raise ValueError("score takes one token for each dumped row of the verify")
+        t = torch.as_tensor(np.asarray(tokens, dtype=np.int32)).to(self.dev)
+        return token_logprobs(out.logits, t, n_top)
 
     def prepare(self, slots: Sequence[int], blocks: Sequence[np.ndarray], log_tau: float = 0.0) -> B.hsd_batch:
         """Uploads a batch description once; verify_prepared/commit can then be replayed on it."""
@@ -335,8 +375,7 @@ class Engine:
         return b
 
     def verify_prepared(self, b: B.hsd_batch, mode: str = "region"):
-        fn = B.hsd_verify_region_batch if mode == "region" else B.hsd_verify_page
-        fn(self.ctx, self.stream, self.cpool, b, _ptr(self.ws), self.ws_bytes)
+        self._pass(b, mode)
         self._batch = b
 
     def override_acceptance(self, accept_len: np.ndarray, bonus: np.ndarray, stop_row: Optional[np.ndarray] = None):
@@ -370,9 +409,8 @@ class Engine:
         hist = torch.zeros((n_tokens, n), dtype=torch.int32, device=self.dev)
         b = self._make_batch(slots, [np.asarray([p], dtype=np.int32) for p in pending])
         tok_view = self._d_meta[2 * n + 1: 3 * n + 1]
-        fn = B.hsd_verify_region_batch if mode == "region" else B.hsd_verify_page
         for step in range(n_tokens):
-            fn(self.ctx, self.stream, self.cpool, b, _ptr(self.ws), self.ws_bytes)
+            self._pass(b, mode)
             B.hsd_kv_commit_rollback(self.ctx, self.stream, self.cpool, b, _ptr(tok_view))
             hist[step].copy_(self.bonus[:n])
         torch.cuda.current_stream(self.dev).synchronize()
