@@ -303,7 +303,7 @@ int hsd_tree_path(const int32_t *tokens, const int32_t *tree_end, int32_t n_rows
 /* Places new rows in pages.  Of `batch` are read: n_seq, total_q, max_blocks_per_seq, n_slots, cu_q (cu_q[n_seq] = total_q;
  * a sequence may have no rows), seq_slot, seq_len, block_table, status; of `pool`: n_blocks, free_list, free_count (the page
  * pointers may be NULL).  For every sequence in order, block-table entries that cover positions seq_len .. seq_len + q_len - 1
- * and hold no block (-1) take one from the free stack; row_slot[r] = 16 * block + position % 16 is then the place of packed row
+ * and hold no block (-1) take one from the free stack (a slot is not named by two sequences of a batch); row_slot[r] = 16 * block + position % 16 is then the place of packed row
  * r in every layer, -1 where there is none (see HSD_STATUS_*; with too few free blocks none is taken), and row_pos[r] its
  * position.  row_slot, row_pos: dev [total_q]; row_pos may be NULL.  seq_len is not modified: see hsd_kv_commit_rows. */
 int hsd_kv_reserve(void *stream, const hsd_kv_pool *pool, const hsd_batch *batch, int32_t *row_slot, int32_t *row_pos);
@@ -329,7 +329,8 @@ typedef struct hsd_kv_quant {
  * may not be named twice apart from that.  Slots of a touched block before its first new row keep their values, slots behind
  * its last one are cleared.  The scale is the smallest 2^e, -100 <= e <= 119, with 448 * 2^e >= every magnitude that the page
  * then holds; values round to the nearest code, ties to even.  Infinities and magnitudes above 448 * 2^119 are held
- * as that, NaN as 0; NaN and infinities set HSD_STATUS_NOT_FINITE in *status (dev [1], or NULL). */
+ * as that, NaN as 0; NaN and infinities set HSD_STATUS_NOT_FINITE in *status (dev [1], or NULL).  HSD_ERANGE: more than 2^29
+ * rows, here and in hsd_kv_quant_read. */
 int hsd_kv_quant_append(void *stream, const hsd_kv_quant *kv, int32_t n_rows, const int32_t *row_slot, int32_t dtype,
                         const void *k, const void *v, int64_t k_stride, int64_t v_stride, int32_t *status);
 
@@ -339,38 +340,40 @@ int hsd_kv_quant_read(void *stream, const hsd_kv_quant *kv, int32_t n_rows, cons
                       void *v, int64_t k_stride, int64_t v_stride);
 
 /* Attention over the pages: row i of sequence s sees positions 0 .. seq_len + i through block_table (its own rows appended
- * before); query head h reads kv head h / (n_q_heads / n_kv_heads).  Of `batch` are read what hsd_kv_reserve reads (status
- * excepted).  q, out: dev [total_q][n_q_heads][64] in dtype, rows q_stride / out_stride elements apart, aligned to their
- * elements; softmax_scale multiplies the products (0.125 for 64 dimensions).  A position whose table entry holds no valid block is left
- * out; a row that sees none becomes 0.  Softmax and sums in fp32; bf16 models round the probabilities to bf16 for the product
- * with the values (and divide by the sum of the rounded ones).  The same call gives the same bits; another batch around a row may
- * change how its keys are split and with it the last bits.  workspace: hsd_kv_quant_attention_bytes(kv, batch, n_q_heads)
- * bytes, 256-byte aligned; NULL if that is 0 (which it also is where the call would refuse its arguments). */
+ * before); query head h reads kv head h / (n_q_heads / n_kv_heads). Of `batch` are read what hsd_kv_reserve reads (status
+ * excepted). q, out: dev [total_q][n_q_heads][64] in dtype, rows q_stride / out_stride elements apart, aligned to their
+ * elements; softmax_scale multiplies the products (0.125 for 64 dimensions; finite, also times log2(e)). HSD_ERANGE: more than
+ * 2^29 rows times query heads, more than 1024 query heads. A position whose table entry holds no valid block is left out; a row
+ * that sees none becomes 0. Softmax and sums in fp32; bf16 models round the probabilities to bf16 for the product with the
+ * values (and divide by the sum of the rounded ones). The same call gives the same bits; another batch around a row may change
+ * how its keys are split and with it the last bits. workspace: hsd_kv_quant_attention_bytes(kv, batch, n_q_heads) bytes,
+ * 256-byte aligned; NULL if that is 0 (which it also is where the call would refuse its arguments). */
 size_t hsd_kv_quant_attention_bytes(const hsd_kv_quant *kv, const hsd_batch *batch, int32_t n_q_heads);
 int hsd_kv_quant_attention(void *stream, const hsd_kv_quant *kv, const hsd_batch *batch, int32_t n_q_heads, int32_t dtype,
                            float softmax_scale, const void *q, int64_t q_stride, void *out, int64_t out_stride,
                            void *workspace, size_t ws_bytes);
 
-/* Decoder passes on an 8-bit cache: hsd_verify_region_batch and hsd_prefill with the keys and values of layer l in layers[l]
- * (a HOST array of n_layers; each with pool's n_blocks and the model's n_kv_heads).  Of `pool` n_blocks, free_list and free_count are
- * used, its page pointers are not looked at.  A row's keys and values are rounded to the model's type as always and then to the page's codes,
- * its own included: it attends to what the cache holds.  Chains only: HSD_EINVAL with batch.tree_end.  The scale of a page follows from the rows in it,
- * rejected ones included until they are overwritten, so that a row's last bits depend on the block that it came in (by the values below 2^-6 of a scale).
- * Commit with hsd_kv_commit_rollback (the page pointers of its pool have to be set, to anything) or hsd_kv_commit_rows.
- * workspace: hsd_workspace_quant_bytes(desc, total_q, n_seq, max_blocks_per_seq) bytes at least, 256-byte aligned. */
+/* Decoder passes on an 8-bit cache: hsd_verify_region_batch and hsd_prefill with the keys and values of layer l in layers[l] (a
+ * HOST array of n_layers; each with pool's n_blocks and the model's n_kv_heads). Of `pool` n_blocks, free_list and free_count
+ * are used, its page pointers are not looked at. A row's keys and values are rounded to the model's type as always and then to
+ * the page's codes, its own included: it attends to what the cache holds. Chains only: HSD_EINVAL with batch.tree_end;
+ * attn_key_chunk is not looked at. The scale of a page follows from the rows in it, rejected ones included until they are
+ * overwritten, so that a row's last bits depend on the block that it came in (by the values below 2^-6 of a scale). Commit with
+ * hsd_kv_commit_rollback (the page pointers of its pool have to be set, to anything) or hsd_kv_commit_rows. workspace:
+ * hsd_workspace_quant_bytes(desc, total_q, n_seq, max_blocks_per_seq) bytes at least, 256-byte aligned. */
 size_t hsd_workspace_quant_bytes(const hsd_model_desc *desc, int32_t max_total_q, int32_t max_n_seq, int32_t max_blocks_per_seq);
 int hsd_verify_quant(hsd_ctx *ctx, void *stream, const hsd_kv_pool *pool, const hsd_kv_quant *layers, const hsd_batch *batch,
                      void *workspace, size_t ws_bytes);
 int hsd_prefill_quant(hsd_ctx *ctx, void *stream, const hsd_kv_pool *pool, const hsd_kv_quant *layers, const hsd_batch *batch,
                       void *workspace, size_t ws_bytes);
 
-/* Scores of given tokens.  Row r of logits (dev [n_rows][vocab] in dtype, row_stride elements apart) is a distribution
+/* Scores of given tokens. Row r of logits (dev [n_rows][vocab] in dtype, row_stride elements apart) is a distribution
  * softmax(logits[r]): logprob[r] = log p(tokens[r]) (-inf for an id outside the vocabulary), entropy[r] in nats, and the n_top
- * most probable tokens, largest first, the lower id first among equal logits: top_ids, top_logprobs dev [n_rows][n_top].
- * A logit of -inf is a probability of 0 and never an alternative (places left over hold id -1 and -inf); a row without any other
- * logit has logprob -inf and entropy 0.  With a NaN or +inf among its logits a row's logprob (of a token inside the vocabulary), entropy and top_logprobs are NaN,
- * and its alternatives are taken from the logits that are numbers.  0 <= n_top <= HSD_MAX_TOP.  workspace: hsd_token_logprobs_bytes bytes, 256-byte
- * aligned; NULL if that is 0. */
+ * most probable tokens, largest first, the lower id first among equal logits: top_ids, top_logprobs dev [n_rows][n_top]. A
+ * logit of -inf is a probability of 0 and never an alternative (places left over hold id -1 and -inf); a row without any other
+ * logit has logprob -inf and entropy 0. With a NaN or +inf among its logits a row's logprob (of a token inside the vocabulary),
+ * entropy and top_logprobs are NaN, and its alternatives are taken from the logits that are numbers. 0 <= n_top <= HSD_MAX_TOP,
+ * n_rows < 2^24. workspace: hsd_token_logprobs_bytes bytes, 256-byte aligned; NULL if that is 0. */
 enum { HSD_MAX_TOP = 32 };
 size_t hsd_token_logprobs_bytes(int32_t n_rows, int32_t vocab, int32_t n_top);
 int hsd_token_logprobs(void *stream, int32_t n_rows, int32_t vocab, int32_t dtype, const void *logits, int64_t row_stride,

@@ -37,6 +37,7 @@ int hsd_kv_quant_append(void *stream, const hsd_kv_quant *kv, int32_t n_rows, co
   const int rc = check_quant(kv);
   if (rc != HSD_OK) return rc;
   if (n_rows < 0 || !is_type(dtype)) return HSD_EINVAL;
+  if (n_rows > kMostPlacedRows) return HSD_ERANGE;
   if (n_rows == 0) return HSD_OK;
   const int64_t width = static_cast<int64_t>(kv->n_kv_heads) * HSD_HEAD_DIM;
   if (row_slot == nullptr || k == nullptr || v == nullptr || k_stride < width || v_stride < width) return HSD_EINVAL;
@@ -51,6 +52,7 @@ int hsd_kv_quant_read(void *stream, const hsd_kv_quant *kv, int32_t n_rows, cons
   const int rc = check_quant(kv);
   if (rc != HSD_OK) return rc;
   if (n_rows < 0 || !is_type(dtype)) return HSD_EINVAL;
+  if (n_rows > kMostPlacedRows) return HSD_ERANGE;
   if (n_rows == 0) return HSD_OK;
   const int64_t width = static_cast<int64_t>(kv->n_kv_heads) * HSD_HEAD_DIM;
   if (row_slot == nullptr || k == nullptr || v == nullptr || k_stride < width || v_stride < width) return HSD_EINVAL;
@@ -78,7 +80,7 @@ int hsd_kv_quant_attention(void *stream, const hsd_kv_quant *kv, const hsd_batch
   int rc = check_quant(kv);
   if (rc == HSD_OK) rc = check_rows(b);
   if (rc != HSD_OK) return rc;
-  if (!is_type(dtype) || !std::isfinite(softmax_scale)) return HSD_EINVAL;
+  if (!is_type(dtype) || !std::isfinite(softmax_scale * kLog2e)) return HSD_EINVAL;
   if ((rc = check_heads(kv, b, n_q_heads)) != HSD_OK) return rc;
   if (b->total_q == 0) return HSD_OK;
   const int64_t width = static_cast<int64_t>(n_q_heads) * HSD_HEAD_DIM;
@@ -97,7 +99,7 @@ size_t hsd_token_logprobs_bytes(int32_t n_rows, int32_t vocab, int32_t n_top) {
 int hsd_token_logprobs(void *stream, int32_t n_rows, int32_t vocab, int32_t dtype, const void *logits, int64_t row_stride, const int32_t *tokens,
                        float *logprob, float *entropy, int32_t n_top, int32_t *top_ids, float *top_logprobs, void *ws, size_t ws_bytes) {
   if (n_rows < 0 || vocab < 1 || n_top < 0 || !is_type(dtype) || row_stride < vocab) return HSD_EINVAL;
-  if (n_top > HSD_MAX_TOP || vocab > (1 << 30)) return HSD_ERANGE;
+  if (n_top > HSD_MAX_TOP || vocab > (1 << 30) || n_rows > kMostScoredRows) return HSD_ERANGE;
   if (n_rows == 0) return HSD_OK;
   if (logits == nullptr || tokens == nullptr || logprob == nullptr || entropy == nullptr) return HSD_EINVAL;
   if (n_top > 0 && (top_ids == nullptr || top_logprobs == nullptr)) return HSD_EINVAL;

@@ -35,9 +35,12 @@ int check_workspace(const void *ws, size_t ws_bytes, size_t need) {
   return ws_bytes < need ? HSD_ENOSPC : HSD_OK;
 }
 
+// A launch has fewer than 2^32 threads: rows that take 4 and 256 of them each
+constexpr int kMostPlacedRows = 1 << 29, kMostScoredRows = (1 << 24) - 1;
+
 int check_heads(const hsd_kv_quant *kv, const hsd_batch *b, int32_t n_q_heads) {
   if (n_q_heads < 1 || n_q_heads % kv->n_kv_heads != 0) return HSD_EINVAL;
-  return n_q_heads > 1024 || static_cast<int64_t>(b->total_q) * n_q_heads > INT32_MAX / 2 ? HSD_ERANGE : HSD_OK;
+  return n_q_heads > 1024 || static_cast<int64_t>(b->total_q) * n_q_heads > INT32_MAX / 4 ? HSD_ERANGE : HSD_OK;
 }
 
 constexpr int kSplitBlocks = 256;   // keys are split over workgroups where tables hold more

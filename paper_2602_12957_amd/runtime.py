@@ -416,5 +416,5 @@ class Engine:
         torch.cuda.current_stream(self.dev).synchronize()
         status = int(self.status.item())
         if status:
-            raise RuntimeError(f"greedy_decode: device status {status} (KV pool exhausted or block table too short)")
+            raise RuntimeError(f"greedy_decode: device status {status} (KV pool exhausted, block table too short, or keys and values that are no numbers)")
         return hist.cpu().numpy().T.copy()

@@ -22,7 +22,7 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, n_top: int = 0) -
     """Log probability of tokens[r] under softmax(logits[r]), the entropy of that distribution and its n_top most probable
     tokens (the lower id first among equals).  logits: [rows, vocab] bfloat16 or float32, rows may lie apart; tokens: int32
     [rows], an id outside the vocabulary has log probability -inf.  A logit of -inf is a probability of 0.  Enqueues on
-    torch's current stream of the tensors' device."""
+    torch's current stream of the tensors' device; no gradient."""
     if not isinstance(logits, torch.Tensor) or not logits.is_cuda:
         raise ValueError("logits must be a tensor on a GPU; there is no CPU fallback")
     if logits.dtype not in _TYPES:

@@ -113,6 +113,21 @@ def test_token_logprobs_arguments():
     assert B.lib.hsd_token_logprobs(None, 0, 1000, B.HSD_FP32, None, 1000, None, None, None, 0, None, None, None, 0) == B.HSD_OK
 
 
+def test_launches_that_would_not_fit_are_refused():
+    kv, big = _kv(), 1 << 60
+    assert B.lib.hsd_kv_quant_append(None, C.byref(kv), (1 << 29) + 1, FAKE, B.HSD_BF16, FAKE, FAKE, big, big, None) == B.HSD_ERANGE
+    assert B.lib.hsd_kv_quant_read(None, C.byref(kv), (1 << 29) + 1, FAKE, B.HSD_FP32, FAKE, FAKE, big, big) == B.HSD_ERANGE
+    b = _rows(total_q=(1 << 25) + 1)
+    assert B.lib.hsd_kv_quant_attention(None, C.byref(kv), C.byref(b), 16, B.HSD_BF16, 0.125, FAKE, 1024, FAKE, 1024, FAKE, 1 << 40) == B.HSD_ERANGE
+    # a scale that is finite, but not in powers of two
+    assert B.lib.hsd_kv_quant_attention(None, C.byref(kv), C.byref(_rows()), 16, B.HSD_BF16, 3e38, FAKE, 1024, FAKE, 1024, None, 0) == B.HSD_EINVAL
+    assert B.lib.hsd_token_logprobs(None, 1 << 24, 8, B.HSD_FP32, FAKE, 8, FAKE, FAKE, FAKE, 0, None, None, None, 0) == B.HSD_ERANGE
+    # decoder passes: no context, no pages
+    for fn in (B.lib.hsd_verify_quant, B.lib.hsd_prefill_quant):
+        assert fn(None, None, C.byref(_pool()), C.byref(kv), C.byref(_rows()), FAKE, 1 << 40) == B.HSD_EINVAL
+    assert B.hsd_workspace_quant_bytes(B.hsd_model_desc(), 16, 1, 8) == 0
+
+
 def test_without_a_gpu_there_is_no_fallback():
     import torch
     if torch.cuda.is_available():
