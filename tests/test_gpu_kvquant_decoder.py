@@ -236,3 +236,43 @@ def test_passes_that_an_8bit_cache_refuses():
     refused(B.HSD_EINVAL, layers=changed(k_scale=None))
     refused(B.HSD_EINVAL, pool=B.hsd_kv_pool(None, None, eng.n_blocks, None, _ptr(eng.free_count)))
     eng.close()
+
+
+@pytest.mark.parametrize("dtype,maxb", [("fp32", 8), ("bf16", 300)])
+def test_a_captured_8bit_pass_replays(dtype, maxb):
+    """A pass and its commit in a graph, replayed with the engine's own passes between: the bits of the eager pass each time."""
+    desc, seed = MODELS[dtype], 36
+    weights = W.make_weights(desc, seed)
+    eng = make_engine(desc, weights, 2, maxb, 64, n_blocks=16)
+    specs = [SequenceSpec(i, nv, 2, 0, 0.0) for i, nv in enumerate([20, 35])]
+    pend, _ = prefill(eng, desc, weights, seed, specs)
+    b = eng.prepare([0, 1], [np.asarray([pend[0], 5, 6], dtype=np.int32), np.asarray([pend[1]], dtype=np.int32)])
+    pages = (eng.k_pool, eng.v_pool, eng.k_scale, eng.v_scale)
+
+    def step():
+        eng.verify_prepared(b)
+        eng.commit()
+
+    def state():
+        torch.cuda.synchronize()
+        return [t.clone() for t in (eng.argmax[:4], eng.margin[:4], eng.accept_len[:2], eng.bonus[:2], eng.seq_len, eng.block_table) + pages]
+    eng.snapshot()
+    start = [t.clone() for t in pages]
+    step()
+    want = state()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step()
+    for _ in range(3):
+        eng.restore()
+        for t, s in zip(pages, start):
+            t.copy_(s)
+        graph.replay()
+        for got, ref in zip(state(), want):
+            assert torch.equal(got, ref)
+        step()      # and a pass of the engine's own, further on
+        torch.cuda.synchronize()
+    assert int(eng.status.item()) == 0
+    eng.close()
