@@ -57,7 +57,7 @@ QuantPlan plan_quant_attention(const hsd_kv_quant *kv, const hsd_batch *b, int32
   auto real_tiles = [&](int64_t c) { return (cols <= c * b->n_seq ? b->n_seq : cols / c + b->n_seq / 2) * kv->n_kv_heads; };
   // 64 columns a wave where that still gives every SIMD its two waves: they share what making operands of pages costs.  Below,
   // 32, of which a unit holds 16 waves.  us a call, 64 / 32 columns, by tiles of 64 (16 heads on 4): 576 (16 blocks of up to 257 rows
-  // on 1055 keys) 34.0 / 29.7, 1024 (4 of 2000 rows) 77.7 / 71.2, 2112 (64 of up to 256 rows on 1280) 95.4 / 96.6.
+  // on 1055 keys) 38.8 / 30.3, 1024 (4 of 2000 rows) 82.0 / 72.8, 2112 (64 of up to 256 rows on 1280) 96.2 / 104.7.
   const int64_t tiles64 = real_tiles(64);
   p.ct = f32 || tiles64 < 2048 ? 1 : 2;
   p.n_tiles = static_cast<int>(cols / (32 * p.ct) + b->n_seq);
@@ -98,7 +98,7 @@ struct ScorePlan {
 };
 ScorePlan plan_scores(int64_t n_rows, int64_t vocab, int piece) {
   ScorePlan p;
-  // (16 rows of 32768: 7 us in one part, 6 and 4 to join them in two)
+  // (16 rows of 32768 in fp32: 8.2 us in one part, 7.1 and 3.9 to join them in two)
   p.n_parts = static_cast<int>(std::max<int64_t>(std::min<int64_t>({kScoreParts, 512 / std::max<int64_t>(n_rows, 1), vocab / 32768}), 1));
   p.part_len = static_cast<int>(vocab);
   if (p.n_parts > 1) {
@@ -106,7 +106,8 @@ ScorePlan plan_scores(int64_t n_rows, int64_t vocab, int piece) {
     p.part_len = static_cast<int>((vocab + p.n_parts * unit - 1) / (p.n_parts * unit) * unit);
     p.n_parts = static_cast<int>((vocab + p.part_len - 1) / p.part_len);
   }
-  // us by waves a workgroup, 16 / 8 / 4: one row of 200000 21.3 / 22.5 / 28.5, 700 rows of 32768 24.0 / 20.2 / 22.7, 1856 56.6 / 47.2 / 43.4
+  // us a call by waves a workgroup, 16 / 8 / 4: one fp32 row of 200000 20.5 / 21.4 / 24.8, 700 bf16 rows of 32768 27.2 / 19.5 / 20.3, 1856
+  // 70.3 / 52.8 / 41.5 (all in turn among other sizes, caches cold)
   p.waves = n_rows * p.n_parts <= 256 ? 16 : (n_rows <= 1024 ? 8 : 4);
   return p;
 }
