@@ -37,9 +37,19 @@ struct QuantAttn {
   float scale;        // log2(e) times the softmax scale's magnitude
   uint32_t q_sign;    // its sign, to be put on the queries
   int n_tiles, n_splits;
+  int heads_log;          // kv heads 1, 2, 4, 8: their logarithm; -1 for others
+  uint32_t group_mul;     // x / group = x * group_mul >> kGroupShift for x < group + 64
+  uint32_t waves_mul;     // x / waves = the upper half of x * waves_mul, waves > 1, x < 2^28
   float *part_o;      // [n_splits][n_tiles][n_kv_heads][columns][64]
   float2 *part_ml;    // [n_splits][n_tiles][n_kv_heads][columns]: reference, sum
 };
+
+// Quotients by what the host knows are products: a division takes some twenty instructions one after the other, and a walk of
+// twelve steps had ten of them around it.  Exact: group <= 1024, so that x times what group_mul is rounded up by, group - 1 at most, stays
+// below 2^22; likewise 16 waves at most and 2^32.
+constexpr int kGroupShift = 22;
+inline uint32_t group_mul(int group) { return ((1u << kGroupShift) + group - 1) / group; }
+inline uint32_t waves_mul(int waves) { return static_cast<uint32_t>(((1ull << 32) + waves - 1) / waves); }
 
 // Queries below 2^30, keys whose page's scale is below 2^30 (448 * 2^30 at most) and a scale below 2^50 give exponents that are
 // finite.  Where one of them is not, every step looks for columns that are not: such a column's probabilities would spoil another one's row
@@ -102,8 +112,8 @@ __device__ __forceinline__ QuantTile find_tile(const QuantAttn &a, int t, int co
 __device__ __forceinline__ bool tile_of_block(const QuantAttn &a, int b, int &tile, int &h) {
   const int heads = a.kv.n_kv_heads, x = b & 7, u = b >> 3;
   int t;
-  if (heads <= 8 && 8 % heads == 0) {
-    h = x % heads, t = u * (8 / heads) + x / heads;
+  if (a.heads_log >= 0) {
+    h = x & (heads - 1), t = (u << (3 - a.heads_log)) + (x >> a.heads_log);
   } else if (heads % 8 == 0) {
     h = x + 8 * (u / a.n_tiles), t = u % a.n_tiles;
   } else {
@@ -112,16 +122,34 @@ __device__ __forceinline__ bool tile_of_block(const QuantAttn &a, int b, int &ti
   tile = a.n_tiles - 1 - t;
   return t < a.n_tiles && h < heads;
 }
-inline unsigned tile_blocks(int64_t n_tiles, int64_t heads) {
-  if (heads <= 8 && 8 % heads == 0) return static_cast<unsigned>((n_tiles + 8 / heads - 1) / (8 / heads) * 8);
+inline int heads_log(int heads) { return heads <= 8 && 8 % heads == 0 ? __builtin_ctz(heads) : -1; }
+inline unsigned tile_blocks(int64_t n_tiles, int heads) {
+  if (heads_log(heads) >= 0) return static_cast<unsigned>((n_tiles + 8 / heads - 1) / (8 / heads) * 8);
   return static_cast<unsigned>(n_tiles * heads);
 }
 
-// Pairs of pages that the columns of a tile see, and those of run z
-__device__ __forceinline__ int tile_keys(const QuantAttn &a, const QuantTile &q, int cols) {
-  return min(q.S + min(((q.j + 1) * cols - 1) / a.group + 1, q.n), a.max_blocks * kBlk);
+// Rows and heads of a tile's columns
+struct TileColumns {
+  int row0, head0;   // of the first one: row of the sequence, query head of the kv head
+  __device__ __forceinline__ TileColumns(const QuantAttn &a, const QuantTile &q, int cols) {
+    const uint32_t f = static_cast<uint32_t>(q.j) * cols, r = f / static_cast<uint32_t>(a.group);
+    row0 = scalar(static_cast<int>(r)), head0 = scalar(static_cast<int>(f - r * a.group));
+  }
+  __device__ __forceinline__ int row(const QuantAttn &a, int col, int &head) const {
+    const uint32_t x = head0 + col, r = x * a.group_mul >> kGroupShift;
+    head = static_cast<int>(x - r * a.group);
+    return row0 + static_cast<int>(r);
+  }
+};
+
+// Keys that the columns of a tile see, and pairs of pages of a run
+__device__ __forceinline__ int tile_keys(const QuantAttn &a, const QuantTile &q, const TileColumns &tc, int cols) {
+  int head;
+  return scalar(min(q.S + min(tc.row(a, cols - 1, head) + 1, q.n), a.max_blocks * kBlk));
 }
-__device__ __forceinline__ int run_pairs(int n_pairs, int n_splits) { return max((n_pairs + n_splits - 1) / n_splits, kSplitPairs); }
+__device__ __forceinline__ int run_pairs(int n_pairs, int n_splits) {
+  return n_splits == 1 ? max(n_pairs, kSplitPairs) : max((n_pairs + n_splits - 1) / n_splits, kSplitPairs);
+}
 
 // Eight values, four a half, as NS bf16 parts
 template <int NS>
@@ -171,17 +199,18 @@ __device__ __forceinline__ void store4(bf16 *p, const floatx4 &v) {
   *reinterpret_cast<u2 *>(p) = *reinterpret_cast<u2 *>(&b);
 }
 
-// grid: (tile_blocks, n_splits), block 64 * W, dynamic LDS quant_attn_lds(W, CT)
-// (16 waves leave 128 registers each, which 32 bf16 columns fit)
-constexpr int quant_attn_waves(bool f32, int ct) { return ct == 1 && !f32 ? 16 : 8; }
-inline int quant_attn_lds(int waves, int ct) { return waves > 1 ? waves * ct * (64 * 32 + 64) * static_cast<int>(sizeof(float)) : 0; }
+// grid: (tile_blocks, n_splits), block 64 * W, dynamic LDS quant_attn_lds(W)
+// (16 waves leave 128 registers each, which 32 bf16 columns fit; 64 columns are taken where tiles alone fill the chip: one wave.  Two of
+// those fit a SIMD.  With the queries in LDS three do: 1847 us where two take 1806, four blocks of 8193 rows.)
+constexpr int quant_attn_waves(bool f32, int ct) { return ct == 2 ? 1 : (f32 ? 8 : 16); }
+inline int quant_attn_lds(int waves) { return waves > 1 ? waves * (64 * 32 + 64) * static_cast<int>(sizeof(float)) : 0; }
 
 template <typename T, int CT>
-__global__ void __launch_bounds__(64 * quant_attn_waves(std::is_same<T, float>::value, CT)) k_attn_quant(QuantAttn a, const T *__restrict__ q, T *__restrict__ out) {
+__global__ void __launch_bounds__(64 * quant_attn_waves(std::is_same<T, float>::value, CT), CT == 2 ? 2 : 1) k_attn_quant(QuantAttn a, const T *__restrict__ q, T *__restrict__ out) {
   constexpr int NS = std::is_same<T, float>::value ? 3 : 1, C = 32 * CT;
   extern __shared__ __attribute__((aligned(16))) float lds[];
   const int lane = threadIdx.x & 63, hf = lane >> 5, c = lane & 31;
-  const int W = blockDim.x >> 6, z = blockIdx.y;
+  const int W = CT == 2 ? 1 : blockDim.x >> 6, z = blockIdx.y;
   int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   asm volatile("" : "+s"(w));   // (kept, and not made again at each use)
   int tile, h;
@@ -194,25 +223,27 @@ __global__ void __launch_bounds__(64 * quant_attn_waves(std::is_same<T, float>::
   int id0 = fetch(page_of(0, 0));   // (the first ones ahead of the length where the walk starts at the first page)
   const int n_cols = qt.n * a.group - qt.j * C;   // columns from this tile's first on
   if (n_cols <= 0) return;
-  // (quotients are formed in vector registers: back to scalar ones)
-  const int n_keys = scalar(tile_keys(a, qt, C)), n_pages = (n_keys + kBlk - 1) / kBlk, n_pairs = (n_pages + 1) / 2;
+  const TileColumns tc(a, qt, C);
+  const int n_keys = tile_keys(a, qt, tc, C), n_pages = (n_keys + kBlk - 1) / kBlk, n_pairs = (n_pages + 1) / 2;
   const int run = scalar(run_pairs(n_pairs, a.n_splits)), p0 = z * run, p1 = min(p0 + run, n_pairs);
   if (z > 0 && p0 >= p1) return;
   const bool whole = n_pairs <= run;
-  const int n_steps = p1 > p0 + w ? scalar((p1 - p0 - w + W - 1) / W) : 0;
+  const uint32_t ahead = p1 - p0 - w + W - 1;   // (a run has pairs, and w < W: not negative)
+  const int n_steps = W == 1 ? ahead : scalar(static_cast<int>(__umulhi(ahead, a.waves_mul)));
 
   // columns
   bf16x8 qf[CT][4][NS];
   int lim[CT];   // last position that the lane's column sees
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) {
-    const int f = qt.j * C + min(32 * ct + c, n_cols - 1), row = f / a.group, hd = f - row * a.group;
+    int hd;
+    const int row = tc.row(a, min(32 * ct + c, n_cols - 1), hd);
     lim[ct] = qt.S + row;
     const T *p = q + (qt.base + row) * a.q_stride + (h * a.group + hd) * kHd + 32 * hf;
 #pragma unroll
     for (int s = 0; s < 4; ++s) load_q8(p + 8 * s, a.q_sign, qf[ct][s]);
   }
-  const int lim_first = qt.S + scalar(qt.j * C / a.group);   // what every column sees
+  const int lim_first = qt.S + tc.row0;   // what every column sees
   float q_most = 0.f;   // (of what is no number too: the largest bits)
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct)
@@ -429,9 +460,9 @@ __global__ void __launch_bounds__(64 * quant_attn_waves(std::is_same<T, float>::
     const int col = 32 * ct + (ln & 31), dim = 16 * (i >> 1) + 8 * (ln >> 5) + 4 * (i & 1);
     if (col >= n_cols) return;
     if (whole) {
-      const int f = qt.j * C + col, row = f / a.group, hd = f - row * a.group;
-      if (sum == 0.f) x = floatx4{0.f, 0.f, 0.f, 0.f};
-      else x /= sum;
+      int hd;
+      const int row = tc.row(a, col, hd);
+      x *= sum == 0.f ? 0.f : 1.f / sum;   // (of a sum of 0 all terms are)
       store4(out + (qt.base + row) * a.o_stride + (h * a.group + hd) * kHd + dim, x);
     } else {
       const size_t at = ((static_cast<size_t>(z) * a.n_tiles + tile) * a.kv.n_kv_heads + h) * C + col;
@@ -446,32 +477,30 @@ __global__ void __launch_bounds__(64 * quant_attn_waves(std::is_same<T, float>::
       for (int i = 0; i < 8; ++i) put(ct, i, lane, piece(ct, i), seen[ct] ? ref[ct] : -INFINITY, l[ct][0]);
     return;
   }
-  float *const ml = lds + W * CT * 2048;   // [wave][part of 32 columns][reference | sum][32]
+  // (32 columns: 64 are one wave's)
+  float *const ml = lds + W * 2048;   // [wave][reference | sum][32]
+  if (c < n_cols)   // (a token of 4 heads: 4 of the 32)
 #pragma unroll
-  for (int ct = 0; ct < CT; ++ct) {
-    if (32 * ct + c < n_cols)   // (a token of 4 heads: 4 of the 32)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) *reinterpret_cast<floatx4 *>(lds + ((w * CT + ct) * 8 + i) * 256 + lane * 4) = piece(ct, i);
-    if (lane < 32) {
-      ml[(w * CT + ct) * 64 + lane] = seen[ct] ? ref[ct] : -INFINITY;
-      ml[(w * CT + ct) * 64 + 32 + lane] = l[ct][0];
-    }
+    for (int i = 0; i < 8; ++i) *reinterpret_cast<floatx4 *>(lds + (w * 8 + i) * 256 + lane * 4) = piece(0, i);
+  if (lane < 32) {
+    ml[w * 64 + lane] = seen[0] ? ref[0] : -INFINITY;
+    ml[w * 64 + 32 + lane] = l[0][0];
   }
   __syncthreads();
-  for (int item = threadIdx.x; item < 512 * CT; item += blockDim.x) {
-    const int ln = item & 63, i = (item >> 6) & 7, ct = item >> 9, col = ln & 31;
-    if (32 * ct + col >= n_cols) continue;
+  for (int item = threadIdx.x; item < 512; item += blockDim.x) {
+    const int ln = item & 63, i = item >> 6, col = ln & 31;
+    if (col >= n_cols) continue;
     float m = -INFINITY;
-    for (int u = 0; u < W; ++u) m = fmaxf(m, ml[(u * CT + ct) * 64 + col]);
+    for (int u = 0; u < W; ++u) m = fmaxf(m, ml[u * 64 + col]);
     const float base = m == -INFINITY ? 0.f : m;
     floatx4 x = {0.f, 0.f, 0.f, 0.f};
     float sum = 0.f;
     for (int u = 0; u < W; ++u) {
-      const float f = __builtin_amdgcn_exp2f(ml[(u * CT + ct) * 64 + col] - base);
-      x += f * *reinterpret_cast<const floatx4 *>(lds + ((u * CT + ct) * 8 + i) * 256 + ln * 4);
-      sum += f * ml[(u * CT + ct) * 64 + 32 + col];
+      const float f = __builtin_amdgcn_exp2f(ml[u * 64 + col] - base);
+      x += f * *reinterpret_cast<const floatx4 *>(lds + (u * 8 + i) * 256 + ln * 4);
+      sum += f * ml[u * 64 + 32 + col];
     }
-    put(ct, i, ln, x, m, sum);
+    put(0, i, ln, x, m, sum);
   }
 }
 
@@ -487,7 +516,8 @@ __global__ void __launch_bounds__(256) k_attn_quant_join(QuantAttn a, int cols, 
   const QuantTile qt = find_tile(a, tile, cols, lane);
   const int n_cols = qt.n * a.group - qt.j * cols, col = blockIdx.y * 4 + lc;
   if (static_cast<int>(blockIdx.y) * 4 >= n_cols) return;
-  const int n_pairs = ((tile_keys(a, qt, cols) + kBlk - 1) / kBlk + 1) / 2, run = run_pairs(n_pairs, a.n_splits);
+  const TileColumns tc(a, qt, cols);
+  const int n_pairs = ((tile_keys(a, qt, tc, cols) + kBlk - 1) / kBlk + 1) / 2, run = run_pairs(n_pairs, a.n_splits);
   if (n_pairs <= run) return;   // written already
   const int n = (n_pairs + run - 1) / run;
   const size_t step = static_cast<size_t>(a.n_tiles) * a.kv.n_kv_heads * cols;
@@ -514,9 +544,9 @@ __global__ void __launch_bounds__(256) k_attn_quant_join(QuantAttn a, int cols, 
   __syncthreads();
   if (w != 0 || col >= n_cols) return;
   x = (s_o[0][lane] + s_o[1][lane]) + (s_o[2][lane] + s_o[3][lane]);
-  if (sum == 0.f) x = floatx4{0.f, 0.f, 0.f, 0.f};
-  else x /= sum;
-  const int f = qt.j * cols + col, row = f / a.group, hd = f - row * a.group;
+  x *= sum == 0.f ? 0.f : 1.f / sum;
+  int hd;
+  const int row = tc.row(a, col, hd);
   store4(out + (qt.base + row) * a.o_stride + (h * a.group + hd) * kHd + 4 * i, x);
 }
 

@@ -69,8 +69,8 @@ QuantPlan plan_quant_attention(const hsd_kv_quant *kv, const hsd_batch *b, int32
   // keys over the waves: as many as fit the chip at once, and two at least (late tiles of a block see more keys than early ones:
   // 4 blocks of 2000 rows 89 us with one wave a tile, 71 with two)
   const int most = quant_attn_waves(f32, p.ct);
-  const int64_t fit = 256 * (f32 ? 8 : most) / (real * p.n_splits);
-  p.waves = static_cast<int>(std::max<int64_t>(std::min<int64_t>({most, std::max<int64_t>(fit, p.ct == 2 ? 1 : 2), max_pairs}), 1));
+  const int64_t fit = 256 * most / (real * p.n_splits);
+  p.waves = static_cast<int>(std::max<int64_t>(std::min<int64_t>({most, std::max<int64_t>(fit, 2), max_pairs}), 1));
   p.part_rows = p.n_splits > 1 ? static_cast<size_t>(groups) * p.n_splits * 32 * p.ct : 0;
   return p;
 }
@@ -78,9 +78,9 @@ QuantPlan plan_quant_attention(const hsd_kv_quant *kv, const hsd_batch *b, int32
 template <typename T, int CT>
 int launch_quant_attention(hipStream_t st, const QuantAttn &a, const QuantPlan &p, const T *q, T *out) {
   auto kern = k_attn_quant<T, CT>;
-  const int lds = quant_attn_lds(p.waves, CT);
+  const int lds = quant_attn_lds(p.waves);
   static const hipError_t attr_rc = hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                                        quant_attn_lds(quant_attn_waves(std::is_same<T, float>::value, CT), CT));
+                                                        quant_attn_lds(quant_attn_waves(std::is_same<T, float>::value, CT)));
   if (attr_rc != hipSuccess) return HSD_EHIP;
   const unsigned groups = static_cast<unsigned>(p.n_tiles) * a.kv.n_kv_heads;
   hipLaunchKernelGGL(kern, dim3(tile_blocks(p.n_tiles, a.kv.n_kv_heads), p.n_splits), dim3(64 * p.waves), lds, st, a, q, out);
@@ -140,7 +140,8 @@ int run_quant_attention(hipStream_t st, const hsd_kv_quant *kv, const hsd_batch 
   float *part = static_cast<float *>(ws);
   const QuantAttn a{quant_pages(kv), b->n_seq, b->total_q, b->n_slots, b->max_blocks_per_seq, n_q_heads, n_q_heads / kv->n_kv_heads, b->cu_q,
                     b->seq_slot, b->seq_len, b->block_table, q_stride, out_stride, std::max(std::fabs(scale2), 1.2e-38f),
-                    std::signbit(scale2) ? 0x80000000u : 0u, p.n_tiles, p.n_splits, part, reinterpret_cast<float2 *>(part + p.part_rows * HSD_HEAD_DIM)};
+                    std::signbit(scale2) ? 0x80000000u : 0u, p.n_tiles, p.n_splits, heads_log(kv->n_kv_heads), group_mul(n_q_heads / kv->n_kv_heads),
+                    waves_mul(p.waves), part, reinterpret_cast<float2 *>(part + p.part_rows * HSD_HEAD_DIM)};
   if (dtype == HSD_BF16) {
     const bf16 *x = static_cast<const bf16 *>(q);
     bf16 *y = static_cast<bf16 *>(out);
