@@ -66,11 +66,13 @@ QuantPlan plan_quant_attention(const hsd_kv_quant *kv, const hsd_batch *b, int32
   // keys over the workgroups where a wave of a full workgroup would take more than eight steps and the chip is not full
   p.n_splits = 1;
   if (b->max_blocks_per_seq > kSplitBlocks && real < 512) p.n_splits = static_cast<int>(std::min<int64_t>({(511 + real) / real, (max_pairs + 63) / 64, kMaxSplits}));
-  // keys over the waves: as many as fit the chip at once, and two at least (late tiles of a block see more keys than early ones:
-  // 4 blocks of 2000 rows 89 us with one wave a tile, 71 with two)
+  // keys over the waves: as many as let all workgroups run at once (but for a 64th of them, which start as the first ones end), and
+  // two at least (late tiles of a block see more keys than early ones).  us a call, 16 heads on 4: 810 tiles (4 blocks of 401 rows on 1055
+  // keys) 24.2 / 23.1 / 23.5 / 33.4 with 2 / 3 / 4 / 5 waves, of which 5 leave room for 768; 1026 (one of 2049 on 4127) 77.5 / 73.5 with 3 / 4; 1228 (16 of up to 257
+  // on 1055) 29.2 / 27.7 / 28.0 / 36.8 with 2 / 3 / 4 / 5; 4008 (4 of 2000) 89 / 70 / 72 with 1 / 2 / 3.
   const int most = quant_attn_waves(f32, p.ct);
-  const int64_t fit = 256 * most / (real * p.n_splits);
-  p.waves = static_cast<int>(std::max<int64_t>(std::min<int64_t>({most, std::max<int64_t>(fit, 2), max_pairs}), 1));
+  const int64_t all = real * p.n_splits, a_unit = (all - all / 64 + 255) / 256;
+  p.waves = static_cast<int>(std::max<int64_t>(std::min<int64_t>({most, std::max<int64_t>(most / a_unit, 2), max_pairs}), 1));
   p.part_rows = p.n_splits > 1 ? static_cast<size_t>(groups) * p.n_splits * 32 * p.ct : 0;
   return p;
 }
