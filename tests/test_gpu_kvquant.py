@@ -555,3 +555,37 @@ def test_python_refusals():
     from paper_2602_12957_amd.binding import HsdError
     with pytest.raises(HsdError):
         cache.attend(q, cu, scale=math.inf)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("ctx,lens,heads", [([40], [3], (96, 1)), ([100, 5], [2, 3], (400, 2)), ([33], [2], (1024, 1)), ([50, 20], [9, 4], (21, 3)),
+                                            ([70, 3], [5, 1], (48, 24)), ([20, 90], [3, 2], (32, 16))])
+def test_attend_with_many_heads(dtype, ctx, lens, heads):
+    """Query heads of a kv head over several tiles, and kv heads that are no power of two or more than eight."""
+    rng = np.random.default_rng(sum(ctx) + heads[0])
+    maxb = max((c + n) // PAGE + 1 for c, n in zip(ctx, lens))
+    cache = make_cache(len(ctx) * maxb, heads[1], len(ctx), maxb, shuffle=3)
+    fill(cache, rng, ctx, lens, dtype)
+    q = rand_rows(rng, sum(lens), heads[0], dtype, 0.3).cuda()
+    check_attend(cache, cache.attend(q, cu_of(lens)), q, ctx, lens, dtype)
+
+
+@pytest.mark.parametrize("ctx,lens,heads", [([300, 0], [500, 330], (160, 32)), ([100], [2100], (64, 64)), ([37, 500, 9], [1000, 1, 1100], (96, 32))])
+def test_attend_of_blocks_that_fill_the_chip(ctx, lens, heads):
+    """2048 tiles of 64 columns and more: those are taken by a wave each.  One sequence has a page without a block."""
+    rng = np.random.default_rng(sum(ctx))
+    maxb = max((c + n) // PAGE + 1 for c, n in zip(ctx, lens))
+    cache = make_cache(len(ctx) * maxb, heads[1], len(ctx), maxb, shuffle=4)
+    fill(cache, rng, ctx, lens, torch.bfloat16)
+    q = rand_rows(rng, sum(lens), heads[0], torch.bfloat16, 0.3).cuda()
+    rows = set(np.cumsum([0] + lens[:-1]).tolist()) | {sum(lens) - 1, lens[0] - 1, lens[0] // 2, 63, 64}
+    out = cache.attend(q, cu_of(lens))
+    check_attend(cache, out, q, ctx, lens, torch.bfloat16, rows=rows)
+    again = cache.attend(q, cu_of(lens))
+    assert torch.equal(out, again)
+    cache.block_table[0, 2] = -1
+    hidden = [np.arange(32, 48) if s == 0 else np.array([], int) for s in range(len(ctx))]
+    # (the values are read before: a hidden block has no place to read them from)
+    got = cache.attend(q, cu_of(lens))
+    cache.block_table[0, 2] = 0
+    check_attend(cache, got, q, ctx, lens, torch.bfloat16, rows=rows, hidden=hidden)
