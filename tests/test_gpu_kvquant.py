@@ -589,3 +589,35 @@ def test_attend_of_blocks_that_fill_the_chip(ctx, lens, heads):
     got = cache.attend(q, cu_of(lens))
     cache.block_table[0, 2] = 0
     check_attend(cache, got, q, ctx, lens, torch.bfloat16, rows=rows, hidden=hidden)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_pages_and_rows_beyond_32_bits(dtype):
+    """Codes of 4.5 GB each, in pages whose offsets differ by 2^32; rows of k, v, q and out that lie 2^30 elements apart."""
+    rng = np.random.default_rng(12)
+    ctx, lens = [70, 33], [1, 2]
+    cache = make_cache(1100000, 4, 2, 8)
+    far = (1 << 32) // (4 * 1024)       # blocks from one offset to the next that agrees in 32 bits
+    ids = [[i, i + far] for i in (0, 1, 7, 50000)]
+    ids = [b for pair in ids for b in pair] + [cache.n_blocks - 1, cache.n_blocks - 2]
+    cache.free_list[-len(ids):] = dev(np.array(ids[::-1], np.int32))
+    fill(cache, rng, ctx, lens, dtype)
+    assert set(cache.block_table[cache.block_table >= 0].tolist()) <= set(ids) and int((cache.block_table >= 0).sum()) >= 8
+    want = [sequence_values(cache, s, c + n) for s, (c, n) in enumerate(zip(ctx, lens))]
+    assert all(np.abs(w).sum() > 0 for w in want)
+    apart = (1 << 30) + 16
+    wide = torch.empty(2 * apart + 4096, dtype=dtype, device="cuda")
+    rows = rand_rows(rng, 3, 4, dtype).cuda()
+    k = wide.as_strided((3, 4, HD), (apart, HD, 1))
+    k.copy_(rows)
+    slots, _ = cache.reserve(cu_of(lens), 3)
+    cache.append(k, k, slots)           # (the rows of the block once more, with other values)
+    got = cache.read(slots, torch.float32)[0]     # half a step of the largest value that the pages hold, earlier tokens included
+    most = max(np.abs(w[0]).max() for w in want + [rows.float().cpu().numpy()[None]])
+    assert (got - rows.float()).abs().max() <= 2.0 ** -4 * most
+    q = rand_rows(rng, 3, 16, dtype, 0.3).cuda()
+    wide_q = wide.as_strided((3, 16, HD), (apart, HD, 1))
+    wide_q.copy_(q)
+    out = torch.empty_like(wide).as_strided((3, 16, HD), (apart, HD, 1))
+    cache.attend(wide_q, cu_of(lens), out=out)
+    check_attend(cache, out.contiguous(), q, ctx, lens, dtype)

@@ -276,3 +276,11 @@ def test_a_captured_8bit_pass_replays(dtype, maxb):
         torch.cuda.synchronize()
     assert int(eng.status.item()) == 0
     eng.close()
+
+
+def test_rounds_with_the_plain_projections(monkeypatch):
+    """HSD_DEBUG_FORCE_SIMPLE: other kernels in front of the same cache."""
+    import functools
+    import sys
+    monkeypatch.setattr(sys.modules[__name__], "make_engine", functools.partial(make_engine, debug={"force_simple": 1}))
+    test_rounds_on_an_8bit_cache("bf16", "region", 14)

@@ -188,3 +188,14 @@ def test_many_rows():
     rng = np.random.default_rng(7)
     logits, tokens = make(rng, 70000, 40, torch.float32)
     check(logits, tokens, 3)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_rows_beyond_32_bits(dtype):
+    """Rows that lie 2^30 elements apart."""
+    rng = np.random.default_rng(13)
+    logits, tokens = make(rng, 3, 1000, dtype)
+    apart = (1 << 30) + 3
+    wide = torch.empty(2 * apart + 1000, dtype=dtype, device="cuda").as_strided((3, 1000), (apart, 1))
+    wide.copy_(logits)
+    check(wide, tokens, 4)
