@@ -8,6 +8,9 @@
 //     dim 2 r + T, so that a lane ends with dims 16 b + 8 h .. + 7, b < 4, of its column
 // The row sums are 16x16x32 products with ones in half of the places, which sum both halves of each column at once: sums of the
 // rounded probabilities, whose rounding cancels in the quotient.
+// Probabilities in bf16 are off by half a step of 2^-8 each, which adds as much again to the rounding of the output: 2.1e-3 relative where
+// that alone is 1.6e-3, and 2.4e-3 on rows that few of very many keys carry. Single tokens on caches so long that their keys are split over
+// workgroups take two parts (NP), 16 bits, beside reads that they wait for anyway.
 // fp32 calls split queries and probabilities into three bf16 parts each (24 bits), three products in place of one.
 //
 // 32x32x16 and not 16x16x32, which takes as long per product and fits 16-column decoding better: beside the short instruction the
@@ -205,7 +208,7 @@ __device__ __forceinline__ void store4(bf16 *p, const floatx4 &v) {
 constexpr int quant_attn_waves(bool f32, int ct) { return ct == 2 ? 1 : (f32 ? 8 : 16); }
 inline int quant_attn_lds(int waves) { return waves > 1 ? waves * (64 * 32 + 64) * static_cast<int>(sizeof(float)) : 0; }
 
-template <typename T, int CT>
+template <typename T, int CT, int NP>
 __global__ void __launch_bounds__(64 * quant_attn_waves(std::is_same<T, float>::value, CT), CT == 2 ? 2 : 1) k_attn_quant(QuantAttn a, const T *__restrict__ q, T *__restrict__ out) {
   constexpr int NS = std::is_same<T, float>::value ? 3 : 1, C = 32 * CT;
   extern __shared__ __attribute__((aligned(16))) float lds[];
@@ -341,7 +344,7 @@ __global__ void __launch_bounds__(64 * quant_attn_waves(std::is_same<T, float>::
       for (int e = 0; e < 16; ++e) x[ct][e] = fmaf(y[ct][e], a.scale, -ref[ct]);
   };
   auto accumulate = [&](const float (&x)[CT][16]) {
-    bf16x8 pf[CT][2][NS];
+    bf16x8 pf[CT][2][NP];
 #pragma unroll
     for (int p = 0; p < 2; ++p)
 #pragma unroll
@@ -349,7 +352,7 @@ __global__ void __launch_bounds__(64 * quant_attn_waves(std::is_same<T, float>::
         float y[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) y[e] = __builtin_amdgcn_exp2f(x[ct][8 * p + e]);
-        split8<NS>(y, pf[ct][p]);
+        split8<NP>(y, pf[ct][p]);
       }
     bf16x8 v[2][2];
 #pragma unroll
@@ -362,7 +365,7 @@ __global__ void __launch_bounds__(64 * quant_attn_waves(std::is_same<T, float>::
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-        for (int n = NS - 1; n >= 0; --n) {
+        for (int n = NP - 1; n >= 0; --n) {
           l[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[ct][p][n], l[ct], 0, 0, 0);
           o[ct][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[p][0], pf[ct][p][n], o[ct][0], 0, 0, 0);
           o[ct][1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[p][1], pf[ct][p][n], o[ct][1], 0, 0, 0);

@@ -48,6 +48,7 @@ constexpr int kSplitBlocks = 256;   // keys are split over workgroups where tabl
 // How an attention call is split.  Lengths are on the device: the plan goes by rows, heads and what the tables can hold.
 struct QuantPlan {
   int ct, waves, n_tiles, n_splits;
+  int parts;          // of a bf16 call's probabilities
   size_t part_rows;   // rows of the workspace's parts
 };
 QuantPlan plan_quant_attention(const hsd_kv_quant *kv, const hsd_batch *b, int32_t n_q_heads, bool f32) {
@@ -73,13 +74,16 @@ QuantPlan plan_quant_attention(const hsd_kv_quant *kv, const hsd_batch *b, int32
   const int most = quant_attn_waves(f32, p.ct);
   const int64_t all = real * p.n_splits, a_unit = (all - all / 64 + 255) / 256;
   p.waves = static_cast<int>(std::max<int64_t>(std::min<int64_t>({most, std::max<int64_t>(most / a_unit, 2), max_pairs}), 1));
+  // two parts where the keys are split and a sequence's columns are one tile, so that pages are read once and wait for memory: 107.9 us
+  // where one part takes 105.3 (8 rows on 131072 keys); with two tiles and 16 a sequence 37.7 / 30.9 (8 of 16 rows on 8192) and 44.8 / 35.7
+  p.parts = p.n_splits > 1 && cols <= 32 * static_cast<int64_t>(b->n_seq) ? 2 : 1;
   p.part_rows = p.n_splits > 1 ? static_cast<size_t>(groups) * p.n_splits * 32 * p.ct : 0;
   return p;
 }
 
-template <typename T, int CT>
+template <typename T, int CT, int NP>
 int launch_quant_attention(hipStream_t st, const QuantAttn &a, const QuantPlan &p, const T *q, T *out) {
-  auto kern = k_attn_quant<T, CT>;
+  auto kern = k_attn_quant<T, CT, NP>;
   const int lds = quant_attn_lds(p.waves);
   static const hipError_t attr_rc = hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize,
                                                         quant_attn_lds(quant_attn_waves(std::is_same<T, float>::value, CT)));
@@ -147,9 +151,10 @@ int run_quant_attention(hipStream_t st, const hsd_kv_quant *kv, const hsd_batch 
   if (dtype == HSD_BF16) {
     const bf16 *x = static_cast<const bf16 *>(q);
     bf16 *y = static_cast<bf16 *>(out);
-    return p.ct == 1 ? launch_quant_attention<bf16, 1>(st, a, p, x, y) : launch_quant_attention<bf16, 2>(st, a, p, x, y);
+    if (p.parts == 2) return launch_quant_attention<bf16, 1, 2>(st, a, p, x, y);
+    return p.ct == 1 ? launch_quant_attention<bf16, 1, 1>(st, a, p, x, y) : launch_quant_attention<bf16, 2, 1>(st, a, p, x, y);
   }
-  return launch_quant_attention<float, 1>(st, a, p, static_cast<const float *>(q), static_cast<float *>(out));
+  return launch_quant_attention<float, 1, 3>(st, a, p, static_cast<const float *>(q), static_cast<float *>(out));
 }
 
 template <typename Src>
