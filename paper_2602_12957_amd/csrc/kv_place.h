@@ -41,7 +41,7 @@ __device__ __forceinline__ void place_rows(const KvPlace &p, int r, int r1, Cu c
 
 // One workgroup of 1024 threads: the reservation, and the rows where there are no more than kPlaceRows.  Entries that may want a
 // block are numbered through the sequences and a thread looks at every 1024th; their blocks stay in LDS for the rows.
-// A chain of dependent reads: bounds, lengths and the free count; the table's entries and the top of the free stack.  16 rows 4.7 us.
+// A chain of dependent reads: bounds, lengths and the free count; the table's entries and the top of the free stack.  16 rows 4.4 us.
 constexpr int kPlaceRows = 16384, kPlaceEntries = kPlaceRows / kBlk + 2 * HSD_MAX_SEQ, kPlaceFree = 1024;
 __global__ void __launch_bounds__(1024) k_kv_place(KvPlace p) {
   __shared__ int s_cu[HSD_MAX_SEQ + 1], s_len[HSD_MAX_SEQ], s_first[HSD_MAX_SEQ], s_id[kPlaceEntries], s_free[kPlaceFree], s_part[16], s_wave[16], s_flags;
