@@ -414,11 +414,15 @@ __global__ void __launch_bounds__(64 * quant_attn_waves(std::is_same<T, float>::
   bool careful = false;
   auto common = [&](int i) { return now.bad == 0 && 32 * (p0 + w + W * i) + 31 <= lim_first && all_seen && now.calm && !careful; };
   // Whether the sums so far stand: 0, or 1 if references have to move, 2 if the walk has to start again
+  // (Each half by itself: a maximum would drop a NaN, and a sum is one where the column 16 away, whose 0 it takes in, is infinite.)
   auto sums = [&]() {
-    float m = l[0][0];
+    auto above = [&](float bar) {
+      bool any = false;
 #pragma unroll
-    for (int ct = 1; ct < CT; ++ct) m = fmaxf(m, l[ct][0]);
-    return !__any(!(m <= kSumMost)) ? 0 : (__any(!(m <= kSumLost)) ? 2 : 1);
+      for (int ct = 0; ct < CT; ++ct) any = any || !(l[ct][0] <= bar);
+      return __any(any) != 0;
+    };
+    return !above(kSumMost) ? 0 : (above(kSumLost) ? 2 : 1);
   };
   // The walk: a general step, then common ones as long as they are.  (The general one stands outside the loop over the common
   // ones: joined in one loop, their registers cost 34 moves a step.)  Pages are requested without a condition, so that no wait is

@@ -1,0 +1,79 @@
+"""Attention over the 8-bit cache where its running reference moves: scores that rise by tens to hundreds of binary orders after a
+wave's first step, in every form of the kernel, against the definition in 64 bits.
+
+A wave walks every W-th pair of pages of its run.  FORMS are sized so that the keys in question lie in its second step or later: 64
+columns are one wave's, the others have 16 (bf16) or 8 (fp32) at most."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_kvquant import HD, PAGE, check_attend, cu_of, make_cache
+
+pytestmark = pytest.mark.gpu
+
+# type, cached tokens, rows, (query heads, kv heads), entries of the block table (None: as many as are needed; above 256 the keys are
+# split over workgroups)
+FORMS = {"64 columns, a row a half": (torch.bfloat16, 700, 2100, (64, 2), None),
+         "64 columns, eight rows a half": (torch.bfloat16, 700, 2100, (64, 16), None),
+         "32 columns, one row": (torch.bfloat16, 3000, 1, (16, 4), None),
+         "32 columns, a block": (torch.bfloat16, 1500, 70, (16, 4), None),
+         "32 columns, split keys": (torch.bfloat16, 9000, 20, (16, 4), 600),
+         "two parts, split keys": (torch.bfloat16, 9000, 1, (16, 4), 600),
+         "fp32, one row": (torch.float32, 3000, 1, (16, 4), None),
+         "fp32, a block": (torch.float32, 1500, 70, (16, 4), None),
+         "fp32, split keys": (torch.float32, 9000, 1, (16, 4), 600)}
+
+
+def place(cache, k, v, ctx, n):
+    """One sequence: ctx cached tokens and n rows behind them, whose blocks are taken and which are not committed."""
+    for a, b in ((0, ctx), (ctx, ctx + n)):
+        cu = cu_of([b - a])
+        slots, _ = cache.reserve(cu, b - a)
+        cache.append(k[a:b].cuda(), v[a:b].cuda(), slots)
+        if b == ctx:
+            cache.commit(cu, ctx)
+    assert int(cache.status.item()) == 0
+
+
+def setup(form, seed):
+    dtype, ctx, n, heads, maxb = FORMS[form]
+    rng = np.random.default_rng(seed)
+    cache = make_cache((ctx + n) // PAGE + 2, heads[1], 1, maxb or (ctx + n) // PAGE + 1, shuffle=seed)
+    k, v = (rng.standard_normal((ctx + n, heads[1], HD)) for _ in range(2))
+    q = 0.3 * rng.standard_normal((n, heads[0], HD))
+    k[:, :, 0] = q[:, :, 0] = 0.0
+    return dtype, ctx, n, heads, cache, rng, k, v, q
+
+
+def looked_at(rng, n):
+    """Rows to compare: the first ones, both sides of the middle, the last ones, and some."""
+    return set(range(n)) if n <= 2 else {0, 1, 4, n // 2, n - 1} | set(rng.integers(0, n, 3).tolist())
+
+
+# which columns (row * heads of the group + head) meet the keys that stand out
+COLUMNS = {"all": lambda f: f >= 0, "first half": lambda f: f // 32 % 2 == 0, "second half": lambda f: f // 32 % 2 == 1,
+           "two sixteen apart": lambda f: np.isin(f % 32, (5, 21)), "one": lambda f: f % 64 == 37}
+
+
+@pytest.mark.parametrize("order", ["rising", "falling"])
+@pytest.mark.parametrize("orders", [30, 60, 100, 200])
+@pytest.mark.parametrize("form", FORMS)
+def test_scores_that_jump_within_the_walk(form, orders, order):
+    """Keys in the middle, at the end and among the block's own exceed all others by `orders` binary orders and more."""
+    dtype, ctx, n, heads, cache, rng, k, v, q = setup(form, orders)
+    group = heads[0] // heads[1]
+    late, own = (20.0, 26.0) if order == "rising" else (10.0, 8.0)
+    for at, height in ((ctx // 2, 16.0), (ctx // 2 + 3, 16.0), (ctx - 5, late), (ctx - 45, late), (ctx + n // 2 if n > 1 else ctx - 70, own)):
+        k[at, :, 0] = height
+    k, v = (torch.from_numpy(x).to(dtype) for x in (k, v))
+    place(cache, k, v, ctx, n)
+    f = np.arange(n)[:, None] * group + np.arange(heads[0])[None] % group
+    for name in COLUMNS if group * n > 4 else ["all"]:
+        x = q.copy()
+        x[:, :, 0] = np.where(COLUMNS[name](f), orders / (0.125 * 16.0 * math.log2(math.e)), 0.0)
+        x = torch.from_numpy(x).to(dtype).cuda()
+        out = cache.attend(x, cu_of([n]))
+        assert bool(torch.isfinite(out).all()), name
+        check_attend(cache, out, x, [ctx], [n], dtype, rows=looked_at(rng, n))
