@@ -305,7 +305,8 @@ int hsd_tree_path(const int32_t *tokens, const int32_t *tree_end, int32_t n_rows
  * pointers may be NULL).  For every sequence in order, block-table entries that cover positions seq_len .. seq_len + q_len - 1
  * and hold no block (-1) take one from the free stack (a slot is not named by two sequences of a batch); row_slot[r] = 16 * block + position % 16 is then the place of packed row
  * r in every layer, -1 where there is none (see HSD_STATUS_*; with too few free blocks none is taken), and row_pos[r] its
- * position.  row_slot, row_pos: dev [total_q]; row_pos may be NULL.  seq_len is not modified: see hsd_kv_commit_rows. */
+ * position.  row_slot, row_pos: dev [total_q]; row_pos may be NULL.  seq_len is not modified: see hsd_kv_commit_rows.
+ * HSD_ERANGE, here and wherever a batch is read below: more than 2^29 rows, more than (2^31 - 1 - 2^29) / 16 blocks a table. */
 int hsd_kv_reserve(void *stream, const hsd_kv_pool *pool, const hsd_batch *batch, int32_t *row_slot, int32_t *row_pos);
 
 /* hsd_kv_commit_rollback for callers without a context: seq_len += 1 + accept_len[s] where accept_len[s] >= 0, nothing where it

@@ -3,10 +3,14 @@
 
 namespace {
 
+// A launch has fewer than 2^32 threads: rows that take 4 and 256 of them each.  Positions (cached tokens and rows) stay below 2^31.
+constexpr int kMostPlacedRows = 1 << 29, kMostScoredRows = (1 << 24) - 1;
+constexpr int kMostTableBlocks = (INT32_MAX - kMostPlacedRows) / HSD_KV_BLOCK_TOKENS;
+
 int check_rows(const hsd_batch *b) {
   if (b == nullptr || b->n_seq < 1 || b->total_q < 0 || b->max_blocks_per_seq < 1 || b->n_slots < 1) return HSD_EINVAL;
   if (b->seq_slot == nullptr && b->n_slots < b->n_seq) return HSD_EINVAL;
-  if (b->n_seq > HSD_MAX_SEQ || b->max_blocks_per_seq > INT32_MAX / HSD_KV_BLOCK_TOKENS) return HSD_ERANGE;
+  if (b->n_seq > HSD_MAX_SEQ || b->total_q > kMostPlacedRows || b->max_blocks_per_seq > kMostTableBlocks) return HSD_ERANGE;
   if (b->cu_q == nullptr || b->seq_len == nullptr || b->block_table == nullptr) return HSD_EINVAL;
   return b->tree_end != nullptr ? HSD_EINVAL : HSD_OK;   // chains only
 }
@@ -34,9 +38,6 @@ int check_workspace(const void *ws, size_t ws_bytes, size_t need) {
   if (ws == nullptr || (reinterpret_cast<uintptr_t>(ws) & 255) != 0) return HSD_EINVAL;
   return ws_bytes < need ? HSD_ENOSPC : HSD_OK;
 }
-
-// A launch has fewer than 2^32 threads: rows that take 4 and 256 of them each
-constexpr int kMostPlacedRows = 1 << 29, kMostScoredRows = (1 << 24) - 1;
 
 int check_heads(const hsd_kv_quant *kv, const hsd_batch *b, int32_t n_q_heads) {
   if (n_q_heads < 1 || n_q_heads % kv->n_kv_heads != 0) return HSD_EINVAL;

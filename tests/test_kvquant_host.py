@@ -140,3 +140,16 @@ def test_without_a_gpu_there_is_no_fallback():
         QuantKV(0, 1, 1, 4)
     with pytest.raises(ValueError):
         token_logprobs(torch.zeros(2, 8), torch.zeros(2, dtype=torch.int32))
+
+
+def test_rows_and_positions_whose_sums_pass_32_bits_are_refused():
+    """As many rows as append and read take, and tables whose positions leave room for them in 31 bits."""
+    kv, p = _kv(), _pool()
+    widest = ((1 << 31) - 1 - (1 << 29)) // 16
+    for kw in (dict(total_q=(1 << 29) + 1), dict(total_q=(1 << 31) - 1), dict(max_blocks_per_seq=widest + 1)):
+        b = _rows(**kw)
+        assert B.lib.hsd_kv_reserve(None, C.byref(p), C.byref(b), FAKE, FAKE) == B.HSD_ERANGE
+        assert B.lib.hsd_kv_commit_rows(None, C.byref(p), C.byref(b)) == B.HSD_ERANGE
+        assert B.lib.hsd_kv_quant_attention(None, C.byref(kv), C.byref(b), 16, B.HSD_BF16, 0.125, FAKE, 1024, FAKE, 1024, FAKE, 1 << 40) == B.HSD_ERANGE
+        assert B.hsd_kv_quant_attention_bytes(kv, b, 16) == 0
+    assert B.hsd_kv_quant_attention_bytes(kv, _rows(max_blocks_per_seq=widest), 16) > 0
