@@ -104,7 +104,8 @@ __device__ __forceinline__ QuantTile find_tile(const QuantAttn &a, int t, int co
   q.base = __builtin_amdgcn_readlane(cu, hit);
   q.n = m != 0 ? __builtin_amdgcn_readlane(end, hit) - q.base : 0;
   q.slot = __builtin_amdgcn_readlane(slot, hit);
-  q.S = max(__builtin_amdgcn_readlane(len, hit), 0);
+  // (a length that no table holds sees the whole table, as if it ended there: sums with it stay in range)
+  q.S = min(max(__builtin_amdgcn_readlane(len, hit), 0), a.max_blocks * kBlk);
   q.j = t - __builtin_amdgcn_readlane(start, hit);
   return q;
 }

@@ -32,7 +32,7 @@ __device__ __forceinline__ void place_rows(const KvPlace &p, int r, int r1, Cu c
   int s = seq_by(cu, p.n_seq, r), base = cu(s), end = cu(s + 1), S = len(s);
   for (; r < r1; ++r) {
     while (r >= end && s + 1 < p.n_seq) ++s, base = end, end = cu(s + 1), S = len(s);
-    const int pos = S + (r - base), bi = pos / kBlk;
+    const int pos = static_cast<int>(static_cast<uint32_t>(S) + static_cast<uint32_t>(r - base)), bi = pos / kBlk;   // (wrapped: negative)
     const int b = pos >= 0 && bi < p.max_blocks ? block(s, bi) : -1;
     p.row_slot[r] = b >= 0 && b < p.n_blocks ? b * kBlk + pos % kBlk : -1;
     if (p.row_pos != nullptr) p.row_pos[r] = pos;
@@ -56,9 +56,10 @@ __global__ void __launch_bounds__(1024) k_kv_place(KvPlace p) {
   for (int s = t; s < p.n_seq; s += 1024) {
     int bits = p.seq_slot != nullptr && p.seq_slot[s] != slot_of(p.seq_slot, s, p.n_slots) ? HSD_STATUS_BAD_SLOT : 0;
     const int S = s_len[s], n = s_cu[s + 1] - s_cu[s], lo = max(S, 0) / kBlk;
-    int hi = n > 0 ? (S + n + kBlk - 1) / kBlk : 0;
+    // (sums in 64 bits: a length that no table holds is reported like one that does not fit)
+    int64_t hi = n > 0 ? (static_cast<int64_t>(S) + n + kBlk - 1) / kBlk : 0;
     if (hi > p.max_blocks) bits |= HSD_STATUS_TABLE_OVERFLOW, hi = p.max_blocks;
-    s_first[s] = max(hi - lo, 0);
+    s_first[s] = max(static_cast<int>(hi) - lo, 0);
     if (bits) atomicOr(&s_flags, bits);
   }
   __syncthreads();

@@ -343,7 +343,7 @@ __global__ void __launch_bounds__(1024) k_kv_commit(int n_seq, const int32_t *__
       if (a > Lq - 1) a = Lq - 1;
       if (a >= 0) new_len = S + 1 + a;
     }
-    int keep = (new_len + kBlk - 1) / kBlk, hi = (S + Lq + kBlk - 1) / kBlk;
+    int keep = max((new_len + kBlk - 1) / kBlk, 0), hi = (S + Lq + kBlk - 1) / kBlk;   // (a length that wrapped stays within the table)
     if (hi > maxb) hi = maxb;
     int cnt = 0;
     for (int i = keep + lane; i < hi; i += kWave) {
@@ -365,7 +365,7 @@ __global__ void __launch_bounds__(1024) k_kv_commit(int n_seq, const int32_t *__
     int sl = slot_of(seq_slot, s, n_slots);
     int S = seq_len[sl], Lq = cu_q[s + 1] - cu_q[s];
     int new_len = s_new[s];
-    int keep = (new_len + kBlk - 1) / kBlk, hi = (S + Lq + kBlk - 1) / kBlk;
+    int keep = max((new_len + kBlk - 1) / kBlk, 0), hi = (S + Lq + kBlk - 1) / kBlk;
     if (hi > maxb) hi = maxb;
     int pushed = s_cnt[s];
     if (height >= 0) {

@@ -77,3 +77,25 @@ def test_scores_that_jump_within_the_walk(form, orders, order):
         out = cache.attend(x, cu_of([n]))
         assert bool(torch.isfinite(out).all()), name
         check_attend(cache, out, x, [ctx], [n], dtype, rows=looked_at(rng, n))
+
+
+@pytest.mark.parametrize("length", [20 * PAGE, 20 * PAGE + 5, (1 << 31) - 1, (1 << 31) - 40])
+def test_a_length_that_no_table_holds(length):
+    """Such a sequence has no place for rows, which is reported, and sees the whole table; the one beside it stays as it is."""
+    rng = np.random.default_rng(3)
+    cache = make_cache(41, 2, 2, 20)
+    x = torch.from_numpy(rng.standard_normal((2 * 20 * PAGE, 2, HD))).to(torch.bfloat16).cuda()
+    full = cu_of([20 * PAGE] * 2)
+    slots, _ = cache.reserve(full, 2 * 20 * PAGE)
+    cache.append(x, x.flip(0), slots)
+    q, cu = torch.from_numpy(0.3 * rng.standard_normal((53, 8, HD))).to(torch.bfloat16).cuda(), cu_of([50, 3])
+    cache.seq_len[0], cache.seq_len[1] = 20 * PAGE, 200
+    want = cache.attend(q, cu)
+    cache.seq_len[0] = length
+    table = cache.block_table.clone()
+    assert torch.equal(cache.attend(q, cu), want)
+    slots, pos = cache.reserve(cu, 53)
+    assert int(cache.status.item()) == 2 and int(cache.free_count.item()) == 1 and torch.equal(cache.block_table, table)
+    assert bool((slots[:50] == -1).all()) and bool((slots[50:] >= 0).all()) and pos[50:].tolist() == [200, 201, 202]
+    cache.commit(cu, 53, torch.tensor([45, 1], dtype=torch.int32, device="cuda"))
+    assert int(cache.seq_len[1].item()) == 202 and int(cache.free_count.item()) == 1 and torch.equal(cache.block_table, table)
