@@ -345,7 +345,8 @@ int hsd_kv_quant_read(void *stream, const hsd_kv_quant *kv, int32_t n_rows, cons
  * excepted). q, out: dev [total_q][n_q_heads][64] in dtype, rows q_stride / out_stride elements apart, aligned to their
  * elements; softmax_scale multiplies the products (0.125 for 64 dimensions; finite, also times log2(e)). HSD_ERANGE: more than
  * 2^29 rows times query heads, more than 1024 query heads. A position whose table entry holds no valid block is left out; a row
- * that sees none becomes 0. Softmax and sums in fp32; bf16 models round the probabilities to bf16 for the product with the
+ * that sees none becomes 0. Values of any magnitude that a page holds are averaged without overflow; a score of +inf or NaN makes its
+ * row and head NaN. Softmax and sums in fp32; bf16 models round the probabilities to bf16 for the product with the
  * values (to two bf16 parts where few rows see very many keys) and divide by the sum of the rounded ones. The same call gives the same bits; another batch around a row may change
  * how its keys are split and with it the last bits. workspace: hsd_kv_quant_attention_bytes(kv, batch, n_q_heads) bytes,
  * 256-byte aligned; NULL if that is 0 (which it also is where the call would refuse its arguments). */

@@ -62,6 +62,11 @@ constexpr float kCalmQuery = 0x1p30f, kCalmPage = 0x1p30f, kCalmScale = 0x1p50f;
 // may have left the range, the walk starts again with every step a general one.
 constexpr float kSumMost = 0x1p40f, kSumLost = 0x1p80f;
 constexpr float kRefSlack = 20.f;          // binary orders by which a score may exceed its column's reference before that moves
+// That holds for pages whose values' scale is at most kCalmValues: magnitudes below 2^47, sums of products below kSumLost times that.  A walk
+// that meets a larger one takes general steps alone, without the slack, and all values 2^32 smaller: no 2^32 keys make a sum that
+// overflows.  Smallest scale that an operand can be made with: 2^-126 (values below 2^-85 or so beside such a page lose bits).
+constexpr float kCalmValues = 0x1p38f, kWideFactor = 0x1p-32f, kWideLeast = 0x1p-126f;
+constexpr float kWideOrders = 32.f;
 constexpr int kSplitPairs = 16;            // a run of pairs for a workgroup of its own is no shorter
 
 // Tiles of `cols` columns.  Up to 64 sequences are numbered without gaps.  More: those of sequence s start at
@@ -281,6 +286,7 @@ __global__ void __launch_bounds__(64 * quant_attn_waves(std::is_same<T, float>::
   int id = 0;
   float ksc = 1.f, vsc = 1.f;
   unsigned long long bad = 0;   // bit l: the page of lane l has no valid block
+  bool wide = false;            // a page's values have a scale above kCalmValues
   auto batch = [&](int i0) {
     const int page = page_of(p0, i0);
     id = i0 == 0 && p0 == 0 ? id0 : fetch(page);
@@ -288,6 +294,8 @@ __global__ void __launch_bounds__(64 * quant_attn_waves(std::is_same<T, float>::
     bad = __ballot(!ok);
     id = (ok ? id : 0) * a.kv.n_kv_heads + h;
     ksc = a.kv.k_scale[id], vsc = a.kv.v_scale[id];
+    wide = wide || __any(ok && vsc > kCalmValues);
+    if (wide) vsc = fmaxf(vsc * kWideFactor, kWideLeast);
     // they are waited for here: behind the branch around this the wait would be for every load in flight, at each step
     asm volatile("" : "+v"(id), "+v"(ksc), "+v"(vsc));
   };
@@ -400,7 +408,7 @@ __global__ void __launch_bounds__(64 * quant_attn_waves(std::is_same<T, float>::
 #pragma unroll
       for (int e = 1; e < 16; ++e) m = fmaxf(m, x[ct][e]);
       m = half_max(m);
-      const bool move = m > (seen[ct] ? kRefSlack : -INFINITY);
+      const bool move = m > (seen[ct] ? (wide ? 0.f : kRefSlack) : -INFINITY);
       const float by = move ? m : 0.f, f = move && seen[ct] ? __builtin_amdgcn_exp2f(-m) : 1.f;   // (nothing seen: o and l are 0)
       o[ct][0] *= f, o[ct][1] *= f, l[ct] *= f;
       ref[ct] += by, seen[ct] = seen[ct] || move;
@@ -413,7 +421,7 @@ __global__ void __launch_bounds__(64 * quant_attn_waves(std::is_same<T, float>::
   };
   // Whether step i may be a common one: every column sees its keys and has seen some, and all is finite
   bool careful = false;
-  auto common = [&](int i) { return now.bad == 0 && 32 * (p0 + w + W * i) + 31 <= lim_first && all_seen && now.calm && !careful; };
+  auto common = [&](int i) { return now.bad == 0 && 32 * (p0 + w + W * i) + 31 <= lim_first && all_seen && now.calm && !careful && !wide; };
   // Whether the sums so far stand: 0, or 1 if references have to move, 2 if the walk has to start again
   // (Each half by itself: a maximum would drop a NaN, and a sum is one where the column 16 away, whose 0 it takes in, is infinite.)
   auto sums = [&]() {
@@ -434,6 +442,7 @@ __global__ void __launch_bounds__(64 * quant_attn_waves(std::is_same<T, float>::
       if (i == 0) {
         request_k(0, now);
         request_v(now);
+        careful = careful || wide;   // (known before the first step: nothing to start again)
       }
       general(i, min(i + 1, last));
       ++i;
@@ -445,7 +454,7 @@ __global__ void __launch_bounds__(64 * quant_attn_waves(std::is_same<T, float>::
         ++i;
         how = sums();
       }
-      if (how == 2 && !careful) {
+      if ((how == 2 || wide) && !careful) {
         careful = true, i = 0;
         clear();
       } else if (how == 1) {
@@ -457,8 +466,10 @@ __global__ void __launch_bounds__(64 * quant_attn_waves(std::is_same<T, float>::
   }
 
 #pragma unroll
-  for (int ct = 0; ct < CT; ++ct)
+  for (int ct = 0; ct < CT; ++ct) {
     if (spoilt[ct]) l[ct][0] = __uint_as_float(0x7fc00000u);
+    if (wide) l[ct][0] *= kWideFactor, ref[ct] += kWideOrders;   // (o is that much smaller already)
+  }
   // the waves' parts together, four dims of a column at a time: piece i of a lane is dims 16 (i / 2) + 8 hf + 4 (i % 2) ..
   auto piece = [&](int ct, int i) {
     const int e = 4 * (i >> 1) + 2 * (i & 1);

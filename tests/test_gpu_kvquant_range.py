@@ -99,3 +99,23 @@ def test_a_length_that_no_table_holds(length):
     assert bool((slots[:50] == -1).all()) and bool((slots[50:] >= 0).all()) and pos[50:].tolist() == [200, 201, 202]
     cache.commit(cu, 53, torch.tensor([45, 1], dtype=torch.int32, device="cuda"))
     assert int(cache.seq_len[1].item()) == 202 and int(cache.free_count.item()) == 1 and torch.equal(cache.block_table, table)
+
+
+@pytest.mark.parametrize("orders", [0, 100])
+@pytest.mark.parametrize("where", ["everywhere", "late page", "one key"])
+@pytest.mark.parametrize("form", FORMS)
+def test_values_up_to_the_largest_that_a_page_holds(form, where, orders):
+    """Averages are finite where sums over the keys are not; keys that stand out by 100 orders let those of 2^127 in at 2^-100."""
+    dtype, ctx, n, heads, cache, rng, k, v, q = setup(form, orders + 1)
+    k[[ctx // 2, ctx // 2 + 40], :, 0] = 16.0
+    q[:, :, 0] = orders / (0.125 * 16.0 * math.log2(math.e))
+    most = math.ldexp(448.0, 119)
+    at = {"everywhere": slice(None), "late page": slice((ctx - 20) // PAGE * PAGE, (ctx - 20) // PAGE * PAGE + PAGE), "one key": slice(ctx // 2 + 40, ctx // 2 + 41)}[where]
+    v[at] = np.sign(v[at]) * np.ldexp(1.0, rng.integers(90, 128, v[at].shape))
+    v[at, :, 5], v[at, :, 6] = most, -most
+    k, v = (torch.from_numpy(x).to(dtype) for x in (k, v))
+    place(cache, k, v, ctx, n)
+    x = torch.from_numpy(q).to(dtype).cuda()
+    out = cache.attend(x, cu_of([n]))
+    assert bool(torch.isfinite(out).all())
+    check_attend(cache, out, x, [ctx], [n], dtype, rows=looked_at(rng, n))
