@@ -300,8 +300,8 @@ int hsd_tree_path(const int32_t *tokens, const int32_t *tree_end, int32_t n_rows
  * own places rows, appends keys and values, attends and scores tokens with them.  The conventions at the top hold; nothing is
  * kept between calls; the kernels run on the current device, which has to be the tensors' and the stream's. */
 
-/* Places new rows in pages.  Of `batch` are read: n_seq, total_q, max_blocks_per_seq, n_slots, cu_q (cu_q[n_seq] = total_q;
- * a sequence may have no rows), seq_slot, seq_len, block_table, status; of `pool`: n_blocks, free_list, free_count (the page
+/* Places new rows in pages.  Of `batch` are read: n_seq, total_q, max_blocks_per_seq, n_slots, cu_q (cu_q[n_seq] <= total_q; a
+ * sequence may have no rows; rows behind the last one belong to none: slot -1, position 0), seq_slot, seq_len, block_table, status; of `pool`: n_blocks, free_list, free_count (the page
  * pointers may be NULL).  For every sequence in order, block-table entries that cover positions seq_len .. seq_len + q_len - 1
  * and hold no block (-1) take one from the free stack (a slot is not named by two sequences of a batch); row_slot[r] = 16 * block + position % 16 is then the place of packed row
  * r in every layer, -1 where there is none (see HSD_STATUS_*; with too few free blocks none is taken), and row_pos[r] its
@@ -346,7 +346,7 @@ int hsd_kv_quant_read(void *stream, const hsd_kv_quant *kv, int32_t n_rows, cons
  * elements; softmax_scale multiplies the products (0.125 for 64 dimensions; finite, also times log2(e)). HSD_ERANGE: more than
  * 2^29 rows times query heads, more than 1024 query heads. A position whose table entry holds no valid block is left out; a row
  * that sees none becomes 0. Values of any magnitude that a page holds are averaged without overflow; a score of +inf or NaN makes its
- * row and head NaN. Softmax and sums in fp32; bf16 models round the probabilities to bf16 for the product with the
+ * row and head NaN. Rows behind the last sequence are left as they are. Softmax and sums in fp32; bf16 models round the probabilities to bf16 for the product with the
  * values (to two bf16 parts where few rows see very many keys) and divide by the sum of the rounded ones. The same call gives the same bits; another batch around a row may change
  * how its keys are split and with it the last bits. workspace: hsd_kv_quant_attention_bytes(kv, batch, n_q_heads) bytes,
  * 256-byte aligned; NULL if that is 0 (which it also is where the call would refuse its arguments). */

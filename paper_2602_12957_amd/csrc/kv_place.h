@@ -32,8 +32,9 @@ __device__ __forceinline__ void place_rows(const KvPlace &p, int r, int r1, Cu c
   int s = seq_by(cu, p.n_seq, r), base = cu(s), end = cu(s + 1), S = len(s);
   for (; r < r1; ++r) {
     while (r >= end && s + 1 < p.n_seq) ++s, base = end, end = cu(s + 1), S = len(s);
-    const int pos = static_cast<int>(static_cast<uint32_t>(S) + static_cast<uint32_t>(r - base)), bi = pos / kBlk;   // (wrapped: negative)
-    const int b = pos >= 0 && bi < p.max_blocks ? block(s, bi) : -1;
+    const bool mine = r < end;   // (a row behind the last sequence has no place, and position 0)
+    const int pos = mine ? static_cast<int>(static_cast<uint32_t>(S) + static_cast<uint32_t>(r - base)) : 0, bi = pos / kBlk;   // (wrapped: negative)
+    const int b = mine && pos >= 0 && bi < p.max_blocks ? block(s, bi) : -1;
     p.row_slot[r] = b >= 0 && b < p.n_blocks ? b * kBlk + pos % kBlk : -1;
     if (p.row_pos != nullptr) p.row_pos[r] = pos;
   }

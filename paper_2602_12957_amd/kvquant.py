@@ -126,7 +126,8 @@ class QuantKV:
 
     def reserve(self, cu_q: torch.Tensor, total_q: int, seq_slot: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
         """Blocks for total_q new rows, sequence s owning rows cu_q[s] .. cu_q[s + 1] - 1 behind its seq_len tokens.
-        Returns (row_slot, row_pos), int32 [total_q]; row_slot is -1 where the pool or the table is too small (see status)."""
+        Returns (row_slot, row_pos), int32 [total_q]; row_slot is -1 where the pool or the table is too small (see status).
+        Rows from cu_q[n_seq] on, as in a padded batch, have slot -1 and position 0: append leaves them out, attend their output."""
         b = self._batch(cu_q, total_q, seq_slot)
         slot = torch.empty(total_q, dtype=torch.int32, device=self.dev)
         pos = torch.empty(total_q, dtype=torch.int32, device=self.dev)
