@@ -1,9 +1,10 @@
-"""Calls around the 8-bit cache that come in other shapes than a packed batch that fits: rows behind the last sequence."""
+"""Calls around the 8-bit cache that come in other shapes than a packed batch that fits: rows behind the last sequence, more rows than
+one workgroup places."""
 import numpy as np
 import pytest
 import torch
 
-from test_gpu_kvquant import HD, PAGE, check_attend, cu_of, dev, fill, make_cache, rand_rows
+from test_gpu_kvquant import HD, PAGE, check_attend, cu_of, dev, fill, make_cache, rand_rows, ref_reserve
 
 pytestmark = pytest.mark.gpu
 
@@ -55,3 +56,35 @@ def test_rows_behind_the_last_sequence(total):
             assert torch.equal(t, g)
         rows = {0, n - 1, n // 2} | set(rng.integers(0, n, 4).tolist())
         check_attend(cache, got[2][:n], q[:n], [33, 7, 50], want, torch.bfloat16, rows=rows)
+
+
+@pytest.mark.parametrize("seed,n_seq,ctx_hi,q_hi", [(0, 1, 300, 17000), (1, 5, 100, 9000), (2, 3, 3000, 20000), (3, 700, 60, 60), (4, 4096, 40, 12)])
+def test_more_rows_than_one_workgroup_places(seed, n_seq, ctx_hi, q_hi):
+    """Above 16384 rows a second kernel writes places and positions."""
+    rng = np.random.default_rng(seed)
+    n_slots = n_seq + 2
+    ctx, q = rng.integers(0, ctx_hi + 1, n_slots), rng.integers(q_hi * 2 // 3, q_hi + 1, n_seq)
+    q[rng.random(n_seq) < 0.1] = 0
+    q[0] = max(q[0], 17000 if n_seq < 100 else 0)
+    slots = rng.permutation(n_slots)[:n_seq]
+    maxb = int((ctx_hi + q.max()) // PAGE + 1) - (seed == 2)     # (one table that is too short)
+    n_blocks = int((ctx // PAGE + 1).sum() + (q // PAGE + 2).sum())
+    cache = make_cache(n_blocks, 1, n_slots, maxb, shuffle=seed)
+    ids = cache.free_list.cpu().numpy()
+    table, at = np.full((n_slots, maxb), -1, np.int32), 0
+    for i, c in enumerate(ctx):
+        b = -(-int(c) // PAGE)
+        table[i, :b] = ids[n_blocks - at - b:n_blocks - at][::-1]
+        at += b
+    cache.block_table.copy_(dev(table)), cache.seq_len.copy_(dev(ctx.astype(np.int32))), cache.free_count.fill_(n_blocks - at)
+    if seed == 2:
+        ctx[slots[0]] = maxb * PAGE - int(q[0]) + 20
+        cache.seq_len.copy_(dev(ctx.astype(np.int32)))
+    want = ref_reserve(ids, n_blocks - at, table, ctx, q, slots, n_blocks)
+    total = int(q.sum())
+    assert total > 16384
+    row_slot, row_pos = cache.reserve(cu_of(q), total, dev(slots.astype(np.int32)))
+    np.testing.assert_array_equal(row_slot.cpu().numpy(), want[0])
+    np.testing.assert_array_equal(row_pos.cpu().numpy(), want[1])
+    np.testing.assert_array_equal(cache.block_table.cpu().numpy(), want[2])
+    assert int(cache.free_count.item()) == want[3] and int(cache.status.item()) == want[4] == (2 if seed == 2 else 0)
