@@ -326,9 +326,9 @@ typedef struct hsd_kv_quant {
 
 /* Keys and values of n_rows rows into the pages at row_slot (as hsd_kv_reserve gives them; a row with a negative or too large
  * slot is left out).  k, v: dev [n_rows][n_kv_heads][64] in dtype, rows k_stride / v_stride elements apart, aligned to their
- * elements.  Rows that share a block have to follow one another in row_slot, in the order of their slots; a block
- * may not be named twice apart from that.  Slots of a touched block before its first new row keep their values, slots behind
- * its last one are cleared.  The scale is the smallest 2^e, -100 <= e <= 119, with 448 * 2^e >= every magnitude that the page
+ * elements.  Rows that share a block have to follow one another in row_slot (with no row that is left out between them), in the
+ * order of their slots, each once; a block may not be named twice apart from that.  Slots of a touched block before its last new
+ * row that are not among the rows keep their values, slots behind it are cleared.  The scale is the smallest 2^e, -100 <= e <= 119, with 448 * 2^e >= every magnitude that the page
  * then holds; values round to the nearest code, ties to even.  Infinities and magnitudes above 448 * 2^119 are held
  * as that, NaN as 0; NaN and infinities set HSD_STATUS_NOT_FINITE in *status (dev [1], or NULL).  HSD_ERANGE: more than 2^29
  * rows, here and in hsd_kv_quant_read. */

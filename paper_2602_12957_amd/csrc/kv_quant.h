@@ -104,8 +104,9 @@ __device__ __forceinline__ void quant_store8(bf16 *p, const float *v) {
 // Token of the j-th byte of half vh in a V page
 __device__ __forceinline__ int v_token(int j, int vh) { return 8 * (j >> 2) + 4 * vh + (j & 3); }
 
-// Runs: rows whose places are consecutive slots of one block.  A wave looks at rows r0 .. r0 + span - 1 (span <= 16) and takes
-// the runs that start there; one may reach 15 rows further.
+// Runs: rows that follow one another in one block, in the order of their slots: GAPS, slots may be left out; else they are consecutive.
+// A wave looks at rows r0 .. r0 + span - 1 (span <= 16) and takes the runs that start there; one may reach 15 rows further.
+template <bool GAPS>
 struct RowRuns {
   int slot;                 // lane l: place of row r0 - 1 + l, l <= 32; -1 without one
   unsigned long long start; // bit l: a run starts at row r0 - 1 + l
@@ -115,16 +116,22 @@ struct RowRuns {
     slot = lane <= 32 && r >= 0 && r < n_rows ? row_slot[r] : -1;
     if (slot >= n_slots) slot = -1;
     const int before = __shfl_up(slot, 1, kWave);
-    const bool go = lane > 0 && slot >= 0 && slot % kBlk != 0 && before == slot - 1;
+    const bool go = lane > 0 && slot >= 0 && (GAPS ? before >= 0 && before < slot && before / kBlk == slot / kBlk : slot % kBlk != 0 && before == slot - 1);
     more = __ballot(go);
     start = __ballot(lane >= 1 && lane <= span && slot >= 0 && !go);
   }
-  // the first run that is left: its row, place and number of rows; removes it
-  __device__ __forceinline__ void take(int r0, int &row, int &place, int &n) {
+  // the first run that is left: its row, place and number of rows, and which slots of the block they are; removes it
+  __device__ __forceinline__ uint32_t take(int r0, int &row, int &place, int &n) {
     const int l = __builtin_ctzll(start);
     start &= start - 1;
     row = r0 - 1 + l, place = __builtin_amdgcn_readlane(slot, l);
     n = 1 + __builtin_ctzll(~(more >> (l + 1)));
+    uint32_t tokens = ((1u << n) - 1) << place % kBlk;
+    if (GAPS && __builtin_amdgcn_readlane(slot, l + n - 1) != place + n - 1) {
+      tokens = 0;
+      for (int i = 0; i < n; ++i) tokens |= 1u << __builtin_amdgcn_readlane(slot, l + i) % kBlk;
+    }
+    return tokens;
   }
 };
 // Rows of a wave: one where that gives no more waves than the chip holds in a few rounds (a run's loads wait for one another),
@@ -159,8 +166,8 @@ struct QuantStaged {
   }
 };
 
-// New rows into the pages.  One wave a run and kv head: what the page keeps of earlier tokens (slots before the run's first) and
-// the new rows make up the page; slots behind them become 0.  A lane's 16 keys are its codes' operand order as they are, and its 8 tokens by 2
+// New rows into the pages.  One wave a run and kv head: what the page keeps of earlier tokens (slots before the run's last that are none
+// of its own) and the new rows make up the page; slots behind them become 0.  A lane's 16 keys are its codes' operand order as they are, and its 8 tokens by 2
 // dims of the values as well: no exchange between lanes but the page's largest magnitude.
 // 32772 bf16 rows of 4 heads: 50 MB in 14.2 us, 3.5 TB/s (a plain copy of that size moves 4.9); a few rows: 5 us, a chain of the places,
 // the rows and the page's old codes.  (Registers bounded for twice the waves a unit: slower, the loads of a run then wait for one another.)
@@ -171,30 +178,31 @@ __global__ void __launch_bounds__(256) k_quant_append(QuantKV kv, int n_rows, in
   const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, vh = lane >> 5, vr = lane & 31, h = blockIdx.y;
   const int r0 = (blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * span;
   if (r0 >= n_rows) return;
-  RowRuns runs(row_slot, n_rows, r0, span, kv.n_blocks * kBlk, lane);
+  RowRuns<true> runs(row_slot, n_rows, r0, span, kv.n_blocks * kBlk, lane);
   bool odd = false;
   while (runs.start != 0) {
     int r, place, n;
-    runs.take(r0, r, place, n);
-    const int off = place % kBlk, page = place / kBlk * kv.n_kv_heads + h;
+    const uint32_t tokens = runs.take(r0, r, place, n);
+    const int last = 31 - __builtin_clz(tokens), page = place / kBlk * kv.n_kv_heads + h;
+    // the run's row of a token is how many of its tokens are below
+    const uint32_t high = tokens >> 4 * vh;
+    const int low = __builtin_popcount(tokens & ((1u << 4 * vh) - 1));
+    auto v_has = [&](int j) { return (high >> v_token(j, 0) & 1) != 0; };
+    auto v_row = [&](int j) { return low + __builtin_popcount(high & ((1u << v_token(j, 0)) - 1)); };
+    const bool k_has = (tokens >> c & 1) != 0;
     u32x4 *kp = reinterpret_cast<u32x4 *>(kv.k_codes + static_cast<size_t>(page) * kPageCodes) + lane;
     u32x4 *vp = reinterpret_cast<u32x4 *>(kv.v_codes + static_cast<size_t>(page) * kPageCodes) + lane;
     float kx[16], vx[8][2];   // K: dims 16 g .. of token c; V: [token v_token(j)][dim 2 vr + e]
     // (loads without a condition, of the run's nearest row where a slot is not one of its: all are in flight at once)
-    const int ik = c - off;
-    src.keys16(r + min(max(ik, 0), n - 1), h, g, kx);
+    src.keys16(r + min(__builtin_popcount(tokens & ((1u << c) - 1)), n - 1), h, g, kx);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int iv = v_token(j, vh) - off;
-      src.values2(r + min(max(iv, 0), n - 1), h, vr, vx[j]);
-    }
+    for (int j = 0; j < 8; ++j) src.values2(r + min(v_row(j), n - 1), h, vr, vx[j]);
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const int iv = v_token(e >> 1, vh) - off;
-      kx[e] = ik >= 0 && ik < n ? quant_input(kx[e], odd) : 0.f;
-      vx[e >> 1][e & 1] = iv >= 0 && iv < n ? quant_input(vx[e >> 1][e & 1], odd) : 0.f;
+      kx[e] = k_has ? quant_input(kx[e], odd) : 0.f;
+      vx[e >> 1][e & 1] = v_has(e >> 1) ? quant_input(vx[e >> 1][e & 1], odd) : 0.f;
     }
-    if (off > 0) {
+    if (n <= last) {   // (there are slots before the last row that are not the run's)
       const u32x4 kc = *kp, vc = *vp;
       const float ks = kv.k_scale[page], vs = kv.v_scale[page];
 #pragma unroll
@@ -203,9 +211,9 @@ __global__ void __launch_bounds__(256) k_quant_append(QuantKV kv, int n_rows, in
         dequant4(kc[j], ks, x), dequant4(vc[j], vs, y);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          if (c < off) kx[4 * j + e] = x[e];
+          if (c < last && !k_has) kx[4 * j + e] = x[e];
           const int t = 4 * (j & 1) + e;
-          if (v_token(t, vh) < off) vx[t][j >> 1] = y[e];
+          if (v_token(t, vh) < last && !v_has(t)) vx[t][j >> 1] = y[e];
         }
       }
     }
@@ -240,7 +248,7 @@ __global__ void __launch_bounds__(256) k_quant_read(QuantKV kv, int n_rows, int 
   const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, vh = lane >> 5, vr = lane & 31, h = blockIdx.y;
   const int r0 = (blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * span;
   if (r0 >= n_rows) return;
-  RowRuns runs(row_slot, n_rows, r0, span, kv.n_blocks * kBlk, lane);
+  RowRuns<false> runs(row_slot, n_rows, r0, span, kv.n_blocks * kBlk, lane);
   unsigned long long none = __ballot(lane >= 1 && lane <= span && r0 - 1 + lane < n_rows && runs.slot < 0);
   while (none != 0) {
     const int r = r0 - 1 + __builtin_ctzll(none);

@@ -1,10 +1,10 @@
 """Calls around the 8-bit cache that come in other shapes than a packed batch that fits: rows behind the last sequence, more rows than
-one workgroup places."""
+one workgroup places, rows of a block with gaps."""
 import numpy as np
 import pytest
 import torch
 
-from test_gpu_kvquant import HD, PAGE, check_attend, cu_of, dev, fill, make_cache, rand_rows, ref_reserve
+from test_gpu_kvquant import HD, PAGE, RefCache, check_attend, cu_of, dev, fill, held, make_cache, rand_rows, ref_reserve
 
 pytestmark = pytest.mark.gpu
 
@@ -88,3 +88,39 @@ def test_more_rows_than_one_workgroup_places(seed, n_seq, ctx_hi, q_hi):
     np.testing.assert_array_equal(row_pos.cpu().numpy(), want[1])
     np.testing.assert_array_equal(cache.block_table.cpu().numpy(), want[2])
     assert int(cache.free_count.item()) == want[3] and int(cache.status.item()) == want[4] == (2 if seed == 2 else 0)
+
+
+class GappedCache(RefCache):
+    """The plain cache, for rows of a block that leave slots out: those before the last row keep their values."""
+
+    def append(self, k, v, slots):
+        runs = {}
+        for r, sl in enumerate(slots):
+            runs.setdefault(int(sl) // PAGE, []).append((int(sl) % PAGE, r))
+        for b, rows in runs.items():
+            for i, src in enumerate((k, v)):
+                page = self.x[i, b].copy()
+                page[:, rows[-1][0] + 1:] = 0.0
+                for off, r in rows:
+                    page[:, off] = src[r]
+                for h in range(page.shape[0]):
+                    self.x[i, b, h], self.e[i, b, h] = held(page[h])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("heads,n_blocks", [(1, 3), (2, 40), (3, 1500)])
+def test_rows_of_a_block_with_gaps(dtype, heads, n_blocks):
+    """Rows in the order of their slots that leave some out, block after block in any order; few rows (one a wave) and many (16)."""
+    rng = np.random.default_rng(heads)
+    cache, ref = make_cache(n_blocks, heads, 1, n_blocks), GappedCache(n_blocks, heads)
+    for keep in (1.0, 0.6, 0.2, 0.9):
+        slots = np.concatenate([b * PAGE + np.nonzero(rng.random(PAGE) < keep)[0] for b in rng.permutation(n_blocks)]).astype(np.int32)
+        k, v = rand_rows(rng, len(slots), heads, dtype), rand_rows(rng, len(slots), heads, dtype) * 11.0
+        k[::7] *= 50.0
+        cache.append(k.cuda(), v.cuda(), dev(slots))
+        ref.append(k.double().numpy(), v.double().numpy(), slots)
+        every = np.arange(n_blocks * PAGE, dtype=np.int32)
+        got = cache.read(dev(every), torch.float32)
+        for g, x in zip(got, ref.x):
+            np.testing.assert_array_equal(g.double().cpu().numpy(), x[every // PAGE, :, every % PAGE])
+    assert int(cache.status.item()) == 0
