@@ -9,7 +9,7 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_kvquant import HD, PAGE, check_attend, cu_of, make_cache
+from test_gpu_kvquant import EPS, HD, PAGE, check_attend, cu_of, make_cache
 
 pytestmark = pytest.mark.gpu
 
@@ -119,3 +119,34 @@ def test_values_up_to_the_largest_that_a_page_holds(form, where, orders):
     out = cache.attend(x, cu_of([n]))
     assert bool(torch.isfinite(out).all())
     check_attend(cache, out, x, [ctx], [n], dtype, rows=looked_at(rng, n))
+
+
+def two_key_case(seed):
+    """One row of 16 heads over 5000 keys of which two count, by nearly equal probabilities, with values that nearly cancel."""
+    rng = np.random.default_rng(seed)
+    cache = make_cache(320, 4, 1, 320)
+    k, v = np.zeros((5000, 4, HD)), rng.standard_normal((5000, 4, HD))
+    q = np.zeros((1, 16, HD))
+    k[:, :, 0], q[:, :, 0] = -16.0, 16.0      # 64 natural units below the two
+    k[[2000, 2010], :, 0] = 16.0
+    k[2010, :, 1], q[0, :, 1] = 1.0, -np.linspace(0.01, 0.9, 16)
+    v[2000], v[2010] = 1.0, -1.0
+    k, v, q = (torch.from_numpy(x).to(torch.bfloat16) for x in (k, v, q))
+    place(cache, k, v, 4999, 1)
+    return cache, q
+
+
+def test_probabilities_of_single_tokens_on_split_keys_carry_16_bits():
+    """o = (1 - p) / (1 + p): with p in one bf16 part it would be off by up to 2^-9 of the spread, which is 1; with two by 2^-17 at
+    most.  That the case tells the two apart is worked out from the rounding of p alone."""
+    cache, q = two_key_case(21)
+    out = cache.attend(q.cuda(), cu_of([1])).double().cpu().numpy()[0]
+    x = q.double().numpy()[0, :, 1] * 0.125
+    p = np.exp(x)
+    want = (1.0 - p) / (1.0 + p)
+    # two parts: 2^-16 of p; fp32: the score's two products and their sum (4 roundings of 256, times 0.125), exponent, exponential and
+    # sums (8 each), for both keys; the output's own half step
+    tol = 2.0 ** -16 + 2.0 ** -24 * 2 * (4 * 32 + 24) + EPS[torch.bfloat16] * np.abs(want)
+    one = torch.from_numpy(p).to(torch.bfloat16).double().numpy()
+    assert (np.abs((1.0 - one) / (1.0 + one) - want) > tol).sum() >= 8
+    assert (np.abs(out - want[:, None]) <= tol[:, None]).all(), float((np.abs(out - want[:, None]) / tol[:, None]).max())
