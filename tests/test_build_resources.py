@@ -45,3 +45,14 @@ def test_wide_attention_does_not_spill(tmp_path):
 def test_general_attention_and_fp32_gemm_do_not_spill(tmp_path, name, number):
     forms = {k[".name"]: k[".vgpr_spill_count"] + k[".private_segment_fixed_size"] for k in _kernels(tmp_path) if name in k[".name"]}
     assert len(forms) == number and {n: s for n, s in forms.items() if s} == {}
+
+
+def test_kernels_around_the_8bit_cache(tmp_path):
+    """The attention's forms of 16 waves have 128 registers and put one value that the walk does not touch aside; none other spills."""
+    kernels = {k[".name"]: (k[".vgpr_spill_count"], k[".private_segment_fixed_size"]) for k in _kernels(tmp_path)}
+    for name, number in (("12k_attn_quantI", 4), ("17k_attn_quant_joinI", 2), ("14k_quant_appendI", 4), ("12k_quant_readI", 2), ("10k_kv_placeE", 1),
+                         ("15k_kv_place_rowsE", 1), ("14k_token_scoresI", 6), ("19k_token_scores_joinI", 2)):
+        forms = {n: s for n, s in kernels.items() if name in n}
+        assert len(forms) == number, (name, sorted(forms))
+        sixteen = "attn_quantI" in name
+        assert {n: s for n, s in forms.items() if s > ((1, 8) if sixteen and "Li1ELi" in n and "4bf16" in n else (0, 0))} == {}
