@@ -115,6 +115,8 @@ class SpecDecoder:
 
     def __init__(self, engine: Engine, n_window: int = 3, max_packed: int = 128, log_tau: float = 0.0,
                  mode: str = "region"):
+        if engine.layers8 is not None:
+            raise ValueError('SpecDecoder verifies packed trees, which a cache in 8 bits does not take: use an engine with kv_cache="model"')
         self.eng, self.n_window, self.max_packed, self.log_tau, self.mode = engine, n_window, max_packed, log_tau, mode
 
     def run(self, slots: Sequence[int], pending: Sequence[int], draft_sets: Sequence[Sequence[Sequence[int]]],

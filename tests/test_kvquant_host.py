@@ -153,3 +153,12 @@ def test_rows_and_positions_whose_sums_pass_32_bits_are_refused():
         assert B.lib.hsd_kv_quant_attention(None, C.byref(kv), C.byref(b), 16, B.HSD_BF16, 0.125, FAKE, 1024, FAKE, 1024, FAKE, 1 << 40) == B.HSD_ERANGE
         assert B.hsd_kv_quant_attention_bytes(kv, b, 16) == 0
     assert B.hsd_kv_quant_attention_bytes(kv, _rows(max_blocks_per_seq=widest), 16) > 0
+
+
+def test_a_decoder_of_trees_is_refused_on_an_8bit_cache():
+    from types import SimpleNamespace
+
+    from paper_2602_12957_amd.specdecode import SpecDecoder
+    with pytest.raises(ValueError, match="packed trees"):
+        SpecDecoder(SimpleNamespace(layers8=(B.hsd_kv_quant * 1)()))
+    assert SpecDecoder(SimpleNamespace(layers8=None)).mode == "region"
