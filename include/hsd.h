@@ -360,7 +360,9 @@ int hsd_kv_quant_attention(void *stream, const hsd_kv_quant *kv, const hsd_batch
  * are used, its page pointers are not looked at. A row's keys and values are rounded to the model's type as always and then to
  * the page's codes, its own included: it attends to what the cache holds. Chains only: HSD_EINVAL with batch.tree_end;
  * attn_key_chunk is not looked at. The scale of a page follows from the rows in it, rejected ones included until they are
- * overwritten, so that a row's last bits depend on the block that it came in (by the values below 2^-6 of a scale). Commit with
+ * overwritten, so that a row's last bits depend on the block that it came in (by the values below 2^-6 of a scale); how its keys are
+ * split goes by the batch. Unlike on pages in the model's type, verifying a block may therefore choose another token than
+ * decoding one by one where two are nearly level. Commit with
  * hsd_kv_commit_rollback (the page pointers of its pool have to be set, to anything) or hsd_kv_commit_rows. workspace:
  * hsd_workspace_quant_bytes(desc, total_q, n_seq, max_blocks_per_seq) bytes at least, 256-byte aligned. */
 size_t hsd_workspace_quant_bytes(const hsd_model_desc *desc, int32_t max_total_q, int32_t max_n_seq, int32_t max_blocks_per_seq);

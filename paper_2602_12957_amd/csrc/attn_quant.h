@@ -18,8 +18,9 @@
 // them 271, for both, two waves a SIMD: 542 / 400.
 //
 // What bounds it: vector instructions, 74 a step of 32 keys by 32 columns and 16 exponentials, beside ten products: 20 of the 25 us that 16
-// blocks of up to 257 rows on 1055 keys take (16 heads on 4).  Four blocks of 8193 rows on 8192 keys: 1.71 ms, 0.96 PFLOP/s, where a large
-// product reaches 1.21.  One token of eight sequences on 131072 keys: 539 MB in 100 us and 5 to join, 5.1 TB/s.  One of 64 sequences on 512 to
+// blocks of up to 257 rows on 1055 keys take (16 heads on 4).  Four blocks of 8193 rows on 8192 keys: 1.67 to 1.76 ms by the box, 0.94 to 0.99
+// PFLOP/s, where a large product reaches 1.63.  One token of eight sequences on 131072 keys: 539 MB in 103 us and 5 to join, 5.2 TB/s, where a
+// bare read reaches 6.5.  One of 64 sequences on 512 to
 // 2048 keys: 13.5 us, of one 8.6: chains of four dependent reads (bounds, table, scales, codes), 3 us, and two joins' barriers.
 //
 // The waves of a workgroup share the columns and take every W-th pair of pages; the workgroups along grid.y take runs of

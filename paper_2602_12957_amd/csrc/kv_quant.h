@@ -169,7 +169,7 @@ struct QuantStaged {
 // New rows into the pages.  One wave a run and kv head: what the page keeps of earlier tokens (slots before the run's last that are none
 // of its own) and the new rows make up the page; slots behind them become 0.  A lane's 16 keys are its codes' operand order as they are, and its 8 tokens by 2
 // dims of the values as well: no exchange between lanes but the page's largest magnitude.
-// 32772 bf16 rows of 4 heads: 50 MB in 14.2 us, 3.5 TB/s (a plain copy of that size moves 4.9); a few rows: 5 us, a chain of the places,
+// 32772 bf16 rows of 4 heads: 50 MB in 14.5 us, 3.5 TB/s (a large copy moves 4.9), in fp32 84 MB in 18.4; a few rows: 5 us, a chain of the places,
 // the rows and the page's old codes.  (Registers bounded for twice the waves a unit: slower, the loads of a run then wait for one another.)
 // grid: (ceil(n_rows / (4 * span)), n_kv_heads), block 256
 template <typename Src>

@@ -11,7 +11,7 @@
 // (Groups of single pieces read a line for each: 1856 rows of 32749 bf16 logits with eight alternatives fetched 203 MB where the
 // logits are 122.)  What reaches the bound is listed in LDS (little more than k entries unless large logits lie 64 lines apart) and ranked.
 //
-// What bounds it: reading.  1856 bf16 rows of 32749, eight alternatives: 122 MB in 33 us, 3.7 TB/s, where a sum over as much reads 4.0; 16
+// What bounds it: reading.  1856 bf16 rows of 32749, eight alternatives: 122 MB in 33 us, 3.7 TB/s, where a bare read reaches 6.5; 16
 // fp32 rows of 32768, five: 8.2 us, what one workgroup can request at a time.
 #pragma once
 

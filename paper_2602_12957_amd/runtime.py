@@ -91,7 +91,8 @@ class Engine:
         """debug: {"sync_layers" | "force_simple": int, "gemm_cfg": (qkv, o, gate_up, down, lm_head)} ->
         hsd_debug_set (experiments and cross-checks only).
         kv_cache: "model" holds keys and values in the model's type, "fp8" in e4m3 codes with a power-of-two scale for each block
-        and kv head (half of a bf16 cache's bytes; chains only, no packed trees, no noalloc)."""
+        and kv head (half of a bf16 cache's bytes; chains only: no packed trees, hence no SpecDecoder; no noalloc; a row's last bits depend
+        on the batch, so that verification may differ from decoding where two tokens are nearly level)."""
         if not torch.cuda.is_available():
             raise RuntimeError("the HSD verification path needs a GPU (MI355X); there is no CPU fallback")
         if kv_cache not in ("model", "fp8"):
