@@ -343,7 +343,7 @@ int hsd_kv_quant_read(void *stream, const hsd_kv_quant *kv, int32_t n_rows, cons
 /* Attention over the pages: row i of sequence s sees positions 0 .. seq_len + i through block_table (its own rows appended
  * before); query head h reads kv head h / (n_q_heads / n_kv_heads). Of `batch` are read what hsd_kv_reserve reads (status
  * excepted). q, out: dev [total_q][n_q_heads][64] in dtype, rows q_stride / out_stride elements apart, aligned to their
- * elements; softmax_scale multiplies the products (0.125 for 64 dimensions; finite, also times log2(e)). HSD_ERANGE: more than
+ * elements (out may be q itself); softmax_scale multiplies the products (0.125 for 64 dimensions; finite, also times log2(e)). HSD_ERANGE: more than
  * 2^29 rows times query heads, more than 1024 query heads. A position whose table entry holds no valid block is left out; a row
  * that sees none becomes 0. Values of any magnitude that a page holds are averaged without overflow; a score of +inf or NaN makes its
  * row and head NaN. Rows behind the last sequence are left as they are. Softmax and sums in fp32; bf16 models round the probabilities to bf16 for the product with the

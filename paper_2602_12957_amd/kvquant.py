@@ -164,7 +164,7 @@ class QuantKV:
     def attend(self, q: torch.Tensor, cu_q: torch.Tensor, seq_slot: Optional[torch.Tensor] = None, layer: int = 0,
                scale: Optional[float] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Causal attention of the rows q [rows, n_q_heads, 64] over their sequences: row i of a sequence sees its seq_len
-        tokens and rows 0 .. i, whose keys and values have been appended.  scale: 1 / sqrt(64) by default."""
+        tokens and rows 0 .. i, whose keys and values have been appended.  scale: 1 / sqrt(64) by default; out: may be q."""
         if not isinstance(q, torch.Tensor) or q.dim() != 3 or q.shape[1] < 1 or q.shape[1] % self.n_kv_heads:
             raise ValueError(f"q must be [rows, n_q_heads, 64] with a multiple of {self.n_kv_heads} heads")
         n, heads, _ = q.shape

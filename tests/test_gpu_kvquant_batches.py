@@ -124,3 +124,15 @@ def test_rows_of_a_block_with_gaps(dtype, heads, n_blocks):
         for g, x in zip(got, ref.x):
             np.testing.assert_array_equal(g.double().cpu().numpy(), x[every // PAGE, :, every % PAGE])
     assert int(cache.status.item()) == 0
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("ctx,lens,heads,maxb", [([300, 20], [60, 1], (8, 2), None), ([5000, 9], [1, 3], (16, 4), 400), ([50], [2100], (64, 64), None)])
+def test_output_in_place_of_the_queries(dtype, ctx, lens, heads, maxb):
+    rng = np.random.default_rng(4)
+    need = max(-(-(c + n) // PAGE) for c, n in zip(ctx, lens))
+    cache = make_cache(len(ctx) * need, heads[1], len(ctx), maxb or need, shuffle=1)
+    fill(cache, rng, ctx, lens, dtype)
+    q, cu = rand_rows(rng, sum(lens), heads[0], dtype, 0.3).cuda(), cu_of(lens)
+    want = cache.attend(q, cu)
+    assert cache.attend(q, cu, out=q) is q and torch.equal(q, want)
