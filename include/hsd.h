@@ -316,8 +316,8 @@ int hsd_kv_commit_rows(void *stream, const hsd_kv_pool *pool, const hsd_batch *b
 
 /* Pages of one layer in 8 bits: e4m3 codes, and for each block and kv head one power-of-two scale of its keys and one of its
  * values, value = code * scale.  Block ids are those of a pool's free list.  A page's contents are written by
- * hsd_kv_quant_append and read by the calls below; the first slot of a page has to be written before a later one counts, as
- * sequences that grow from a block's start do.  k_codes and v_codes are 16-byte aligned. */
+ * hsd_kv_quant_append and read by the calls below; the first append to a page that comes from the free list names its
+ * first slot and leaves none out, as sequences that grow do (what is kept of a page is not looked at otherwise).  k_codes and v_codes are 16-byte aligned. */
 typedef struct hsd_kv_quant {
   void *k_codes, *v_codes;   /* dev [n_blocks][n_kv_heads][1024] bytes */
   float *k_scale, *v_scale;  /* dev [n_blocks][n_kv_heads]             */
