@@ -1,13 +1,13 @@
 """A decoder's projections in 8 bits, as calls that can be timed and compared.
 
 A layer on them adds the last projection to the residual stream, normalises and rounds the sum to 8 bits (`norm_rows`), and
-multiplies such rows with weights that are held in 8 bits as well (`linear`; `gated` for the gate and up projections with the
-SwiGLU between them, whose rows are rounded to 8 bits again for the down projection).  Codes are e4m3.  Rows have a power of two
+multiplies such rows with weights that are held in 8 bits as well (`linear`; in a feed-forward block `gated`, the gate and up
+projections with the SwiGLU between them, whose rows are rounded to 8 bits again, and `linear` for down).  Codes are e4m3.  Rows have a power of two
 for each 128 columns, the smallest 2^e with 448 * 2^e >= the largest magnitude of the block; weights have one scale for each
 block of 128 by 128, a power of two as well or any number of 32 bits.  Rows of codes are padded with zeros to whole blocks.
 
-With `own` false the operators run in plain torch, 32 bits, rounded once at the end.  Rows in 8 bits are returned as the values
-that they stand for, which bf16 holds exactly.
+With `own` false the operators run in plain torch, 32 bits, rounded once at the end.  Rows in 8 bits that a call returns are read
+back as the values that they stand for, which bf16 holds exactly.
 """
 import math
 from types import SimpleNamespace
@@ -40,12 +40,12 @@ def listed():
         dict(name="linear_odd_777", op="linear", rows=777, dim=1000, n_out=1537, scale="fp32", out="fp32"),
         # a large square product: the largest call
         dict(name="linear_square_8192", op="linear", rows=8192, dim=8192, n_out=8192, scale="pow2", out="bf16"),
-        # gate, up and SwiGLU while 16 sequences decode
-        dict(name="gated_step_16", op="gated", rows=16, dim=1024, n_out=4096, scale="pow2"),
+        # a feed-forward block while 16 sequences decode
+        dict(name="ffn_step_16", op="ffn", rows=16, dim=1024, d_ffn=4096, scale="pow2", out="bf16"),
         # the same for one round of 16 regions
-        dict(name="gated_region_1856", op="gated", rows=1856, dim=1024, n_out=4096, scale="pow2"),
-        # and for four pages of 8193 rows
-        dict(name="gated_page_32772", op="gated", rows=32772, dim=1024, n_out=4096, scale="fp32"),
+        dict(name="ffn_region_1856", op="ffn", rows=1856, dim=1024, d_ffn=4096, scale="pow2", out="bf16"),
+        # and for four pages of 8193 rows, weights that came with scales of their own
+        dict(name="ffn_page_32772", op="ffn", rows=32772, dim=1024, d_ffn=4096, scale="fp32", out="bf16"),
     ]
 
 
@@ -54,7 +54,7 @@ def _log(rng, lo, hi):
 
 
 def draw(rng):
-    op = rng.choice(["norm", "norm", "linear", "linear", "linear", "linear", "gated", "gated"])
+    op = rng.choice(["norm", "norm", "linear", "linear", "linear", "linear", "ffn", "ffn"])
     if op == "norm":
         dim = _log(rng, 16, 16384)
         return dict(op="norm", rows=_log(rng, 1, min(32768, (1 << 25) // dim)), dim=dim, x=rng.choice(["bf16", "bf16", "fp32"]),
@@ -64,9 +64,9 @@ def draw(rng):
         n_out = _log(rng, 8, 32768)
         most = min(32768, (1 << 27) // n_out, (1 << 37) // (n_out * dim))
         return dict(op="linear", rows=_log(rng, 1, max(2, most)), dim=dim, n_out=n_out, scale=scale, out=rng.choice(["bf16", "bf16", "fp32"]))
-    n_out = BLOCK * _log(rng, 1, 96)
-    most = min(32768, (1 << 26) // n_out, (1 << 36) // (n_out * dim))
-    return dict(op="gated", rows=_log(rng, 1, max(2, most)), dim=dim, n_out=n_out, scale=scale)
+    d_ffn = BLOCK * _log(rng, 1, 96)
+    most = min(32768, (1 << 27) // d_ffn, (1 << 36) // (d_ffn * dim))
+    return dict(op="ffn", rows=_log(rng, 1, max(2, most)), dim=dim, d_ffn=d_ffn, scale=scale, out="bf16")
 
 
 def _blocks(n):
@@ -79,10 +79,13 @@ def work(case):
     held = lambda n: rows * (n + _blocks(n))   # noqa: E731  codes and scales
     if case["op"] == "norm":   # x and the sum's old part in, the sum, the codes and scales and the values read back out
         return {"bytes": rows * dim * (size[case["x"]] + 2 * size[case["res"]] + 2) + held(dim) + 4 * dim, "flops": 8 * rows * dim}
-    n_w = case["n_out"] * (2 if case["op"] == "gated" else 1)
-    read = held(dim) + n_w * dim + _blocks(n_w) * _blocks(dim) * (1 if case["scale"] == "pow2" else 4)
-    wrote = rows * case["n_out"] * size[case["out"]] if case["op"] == "linear" else held(case["n_out"]) + 2 * rows * case["n_out"]
-    return {"bytes": read + wrote, "flops": 2 * rows * n_w * dim}
+    byte = 1 if case["scale"] == "pow2" else 4
+    if case["op"] == "linear":
+        held_w, products = [(case["n_out"], dim)], rows * dim * case["n_out"]
+    else:   # (the rows between the products need not leave the chip)
+        held_w, products = [(2 * case["d_ffn"], dim), (dim, case["d_ffn"])], 3 * rows * dim * case["d_ffn"]
+    read = held(dim) + sum(n * k + _blocks(n) * _blocks(k) * byte for n, k in held_w)
+    return {"bytes": read + rows * held_w[-1][0] * size[case["out"]], "flops": 2 * products}
 
 
 # ---------------------------------------------------------------------------------------------------- plain operators
@@ -127,8 +130,9 @@ def _plain(s):
     a, w = _row_values(*s.a, s.dim), _weight_values(*s.w, s.dim)
     if s.op == "linear":
         return torch.matmul(a, w.T).to(s.out)
-    g, u = torch.matmul(a, w[:s.n_out].T), torch.matmul(a, w[s.n_out:].T)
-    return _row_values(*_round_rows(g / (1.0 + torch.exp(-g)) * u), s.n_out).to(torch.bfloat16)
+    g, u = torch.matmul(a, w[:s.d_ffn].T), torch.matmul(a, w[s.d_ffn:].T)
+    y = _row_values(*_round_rows(g / (1.0 + torch.exp(-g)) * u), s.d_ffn)
+    return torch.matmul(y, _weight_values(*s.down, s.d_ffn).T).to(s.out)
 
 
 # ---------------------------------------------------------------------------------------------------- inputs
@@ -147,23 +151,30 @@ def _norm_inputs(case, seed):
     return x, res, 1.0 + 0.1 * torch.randn((dim,), generator=g, device=DEV)
 
 
-def _product_inputs(case, seed):
-    """Codes and scales of the rows and of the weights."""
-    g = torch.Generator(device=DEV).manual_seed(seed)
-    dim, n_w = case["dim"], case["n_out"] * (2 if case["op"] == "gated" else 1)
-    x = _activations(g, case["rows"], dim)
-    a = _round_rows(x * torch.rsqrt((x * x).mean(-1, keepdim=True) + EPS))
-    w = torch.randn((n_w, dim), generator=g, device=DEV) * (torch.exp(0.3 * torch.randn((n_w, 1), generator=g, device=DEV)) / math.sqrt(dim))
-    w = torch.nn.functional.pad(w, (0, -dim % BLOCK, 0, -n_w % BLOCK)).reshape(_blocks(n_w), BLOCK, _blocks(dim), BLOCK)
+def _weights(g, n_out, dim, kind):
+    """Codes and scales of a weight matrix whose rows differ in size."""
+    w = torch.randn((n_out, dim), generator=g, device=DEV) * (torch.exp(0.3 * torch.randn((n_out, 1), generator=g, device=DEV)) / math.sqrt(dim))
+    w = torch.nn.functional.pad(w, (0, -dim % BLOCK, 0, -n_out % BLOCK)).reshape(_blocks(n_out), BLOCK, _blocks(dim), BLOCK)
     top = w.abs().amax((1, 3))
-    if case["scale"] == "pow2":
-        m, x2 = torch.frexp(top)
-        e = torch.where(m <= 0.875, x2 - 9, x2 - 8).clamp(-126, 120)
+    if kind == "pow2":
+        m, x = torch.frexp(top)
+        e = torch.where(m <= 0.875, x - 9, x - 8).clamp(-126, 120)
         scale, s = (e + 127).to(torch.uint8), _two_to(e)
     else:
         scale = s = top / TOP
     codes = (w / s[:, None, :, None]).clamp(-TOP, TOP).to(torch.float8_e4m3fn)
-    return a, (codes.reshape(_blocks(n_w) * BLOCK, -1)[:n_w].view(torch.uint8), scale)
+    return codes.reshape(_blocks(n_out) * BLOCK, -1)[:n_out].view(torch.uint8), scale
+
+
+def _product_inputs(case, seed):
+    """Codes and scales of the rows and of the weights (a feed-forward block's: gate and up, then down)."""
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    dim = case["dim"]
+    x = _activations(g, case["rows"], dim)
+    a = _round_rows(x * torch.rsqrt((x * x).mean(-1, keepdim=True) + EPS))
+    if case["op"] == "linear":
+        return a, _weights(g, case["n_out"], dim, case["scale"]), None
+    return a, _weights(g, 2 * case["d_ffn"], dim, case["scale"]), _weights(g, dim, case["d_ffn"], case["scale"])
 
 
 def prepare(case, seed):
@@ -171,13 +182,15 @@ def prepare(case, seed):
     if s.op == "norm":
         s.x, s.res, s.gain = _norm_inputs(case, seed)
     else:
-        s.a, s.w = _product_inputs(case, seed)
-        s.n_out, s.out = case["n_out"], DTYPES[case.get("out", "bf16")]
+        s.a, s.w, s.down = _product_inputs(case, seed)
+        s.d_ffn, s.out = case.get("d_ffn"), DTYPES[case["out"]]
     if own:
         from paper_2602_12957_amd import linear8
         s.lib = linear8
         if s.op != "norm":
             s.rows8, s.weight8 = linear8.Rows8(*s.a, s.dim), linear8.Weight8(*s.w, s.dim)
+        if s.op == "ffn":
+            s.down8 = linear8.Weight8(*s.down, s.d_ffn)
     return s
 
 
@@ -189,7 +202,7 @@ def run(s):
         return {"values": rows8.read(), "sum": total}
     if s.op == "linear":
         return s.lib.linear(s.rows8, s.weight8, s.out)
-    return s.lib.gated(s.rows8, s.weight8).read()
+    return s.lib.linear(s.lib.gated(s.rows8, s.weight8), s.down8, s.out)
 
 
 # ---------------------------------------------------------------------------------------------------- in 64 bits
@@ -208,20 +221,24 @@ def _nearest(y):
     return out
 
 
+def _held_weights(codes, scale, dim):
+    s = torch.exp2(scale.double() - 127) if scale.dtype == torch.uint8 else scale.double()
+    of = torch.arange(codes.shape[0], device=DEV) // BLOCK
+    return codes.view(torch.float8_e4m3fn)[:, :dim].double() * s[of][:, torch.arange(dim, device=DEV) // BLOCK]
+
+
 def exact(case, seed):
     if case["op"] == "norm":
         x, res, gain = _norm_inputs(case, seed)
         h = x.double() + res.double()
         return {"values": _nearest(h / torch.sqrt(h.square().mean(-1, keepdim=True) + EPS) * gain.double()), "sum": h}
-    (codes, scale), (w_codes, w_scale) = _product_inputs(case, seed)
-    dim, n_out = case["dim"], case["n_out"]
-    col = torch.arange(dim, device=DEV) // BLOCK
-    of = torch.arange(w_codes.shape[0], device=DEV) // BLOCK
-    s_w = torch.exp2(w_scale.double() - 127) if case["scale"] == "pow2" else w_scale.double()
-    w = w_codes.view(torch.float8_e4m3fn)[:, :dim].double() * s_w[of][:, col]
+    a, w, down = _product_inputs(case, seed)
+    w, dim = _held_weights(*w, case["dim"]), case["dim"]
     parts = []
     for r in range(0, case["rows"], 4096):
-        a = codes[r:r + 4096].view(torch.float8_e4m3fn)[:, :dim].double() * torch.exp2(scale[r:r + 4096].double() - 127)[:, col]
-        y = a @ w.T
-        parts.append(y if case["op"] == "linear" else _nearest(y[:, :n_out] * torch.sigmoid(y[:, :n_out]) * y[:, n_out:]))
+        y = (a[0][r:r + 4096].view(torch.float8_e4m3fn).double() * torch.exp2(a[1][r:r + 4096].double() - 127).repeat_interleave(BLOCK, 1)[:, :a[0].shape[1]])[:, :dim] @ w.T
+        if case["op"] == "ffn":
+            gate, up = y.split(case["d_ffn"], 1)
+            y = _nearest(gate * torch.sigmoid(gate) * up) @ _held_weights(*down, case["d_ffn"]).T
+        parts.append(y)
     return torch.cat(parts)
