@@ -95,12 +95,12 @@ def _two_to(e):
 
 
 def _round_rows(y):
-    """e4m3 codes of rows (padded to whole blocks) and the exponents of their blocks, -127 .. 120 plus 127 as bytes."""
+    """e4m3 codes of rows (padded to whole blocks) and the exponents of their blocks, -100 .. 119 plus 127 as bytes."""
     n, dim = y.shape
     y = torch.nn.functional.pad(y, (0, -dim % BLOCK)).reshape(n, -1, BLOCK)
     top = y.abs().amax(-1)
     m, x = torch.frexp(top)                      # top = m * 2^x, m in [0.5, 1); 448 = 0.875 * 2^9
-    e = torch.where(m <= 0.875, x - 9, x - 8).clamp(-127, 120)
+    e = torch.where(m <= 0.875, x - 9, x - 8).clamp(-100, 119)
     e = torch.where(top > 0, e, torch.zeros_like(e))
     codes = (y * _two_to(-e)[..., None]).to(torch.float8_e4m3fn)
     scale = torch.nn.functional.pad(e + 127, (0, -e.shape[1] % 4)).to(torch.uint8)
@@ -111,7 +111,7 @@ def _row_values(codes, scale, dim):
     """What rows of codes stand for, in 32 bits."""
     n = codes.shape[0]
     y = codes.view(torch.float8_e4m3fn).float().reshape(n, -1, BLOCK)
-    s = _two_to((scale[:, :y.shape[1]].int() - 127).clamp(min=-126))   # (2^-127 does not occur on these inputs)
+    s = _two_to(scale[:, :y.shape[1]].int() - 127)
     return (y * s[..., None]).reshape(n, -1)[:, :dim]
 
 
@@ -158,7 +158,7 @@ def _weights(g, n_out, dim, kind):
     top = w.abs().amax((1, 3))
     if kind == "pow2":
         m, x = torch.frexp(top)
-        e = torch.where(m <= 0.875, x - 9, x - 8).clamp(-126, 120)
+        e = torch.where(m <= 0.875, x - 9, x - 8).clamp(-100, 119)
         scale, s = (e + 127).to(torch.uint8), _two_to(e)
     else:
         scale = s = top / TOP
@@ -214,7 +214,7 @@ def _nearest(y):
         top = part.abs().amax(1, keepdim=True)
         e = torch.ceil(torch.log2(top / TOP))
         e = torch.where(TOP * torch.exp2(e) < top, e + 1, torch.where(TOP * torch.exp2(e - 1) >= top, e - 1, e))
-        s = torch.exp2(torch.where(top > 0, e.clamp(-127, 120), torch.zeros_like(e)))
+        s = torch.exp2(torch.where(top > 0, e.clamp(-100, 119), torch.zeros_like(e)))
         v = part / s
         step = torch.exp2(torch.floor(torch.log2(v.abs().clamp(min=2.0 ** -6))) - 3)
         out[:, a:a + BLOCK] = torch.round(v / step) * step * s
