@@ -384,6 +384,64 @@ int hsd_token_logprobs(void *stream, int32_t n_rows, int32_t vocab, int32_t dtyp
                        const int32_t *tokens, float *logprob, float *entropy, int32_t n_top, int32_t *top_ids,
                        float *top_logprobs, void *workspace, size_t ws_bytes);
 
+/* ---------------------------------------------------------------------------------------------------------------
+ * Projections in 8 bits.  They need no context either: the conventions at the top hold, nothing is kept between calls, the kernels
+ * run on the current device, which has to be the tensors' and the stream's, and take no workspace.
+ *
+ * Rows in 8 bits: n_rows rows of dim values in blocks of HSD_QUANT_BLOCK columns, e4m3 codes (OCP) and one byte a block,
+ * value = code * 2^(byte - 127).  A row of codes is padded with zeros to whole blocks; the bytes behind a row's last block are never
+ * looked at.  NaN and infinities are held as NaN. */
+enum { HSD_QUANT_BLOCK = 128 };
+typedef struct hsd_rows_quant {
+  void *codes;          /* dev [n_rows][128 * ceil(dim / 128)], 16-byte aligned                                  */
+  uint8_t *scale;       /* dev [n_rows][ceil(dim / 128)], 4-byte aligned                                         */
+  int64_t code_stride;  /* bytes from row to row: a multiple of 16, whole blocks at least                        */
+  int64_t scale_stride; /* the same of scale: a multiple of 4, and at least the blocks rounded up to one         */
+} hsd_rows_quant;
+
+/* Weights in 8 bits, [n_out, dim] row-major in blocks of 128 rows by 128 columns: codes as above, one scale a block, a byte as above
+ * (HSD_SCALE_POW2: the matrix unit applies it) or any finite float (HSD_SCALE_FP32: value = code * scale). */
+enum { HSD_SCALE_FP32 = 0, HSD_SCALE_POW2 = 1 };
+typedef struct hsd_weight_quant {
+  const void *codes;    /* dev [n_out][128 * ceil(dim / 128)], 16-byte aligned                                   */
+  const void *scale;    /* dev [ceil(n_out / 128)][ceil(dim / 128)] bytes or floats, aligned to them             */
+  int64_t code_stride;  /* bytes: a multiple of 16, whole blocks at least                                        */
+  int64_t scale_stride; /* elements from row to row of blocks, whole blocks at least                             */
+  int32_t scale_type;   /* HSD_SCALE_FP32 or HSD_SCALE_POW2                                                      */
+} hsd_weight_quant;
+
+/* Sizes, here and below: dim (and d_ffn) up to 2^20, fewer than 2^24 rows and weight rows, else HSD_ERANGE; n_rows may be 0.  Rows of x, residual, sum and
+ * out lie *_stride elements apart (dim of them at least) and are aligned to their elements; dtype (of x or out): HSD_BF16 or HSD_FP32.
+ *
+ * x [n_rows, dim] to 8 bits.  A block's byte is e + 127, e the least in -100 .. 119 with 448 * 2^e >= every finite magnitude
+ * in it (0 where all are 0); values round to the nearest code, ties to even, those beyond 448 * 2^119 to that. */
+int hsd_quant_rows(void *stream, int32_t n_rows, int32_t dim, int32_t dtype, const void *x, int64_t x_stride, const hsd_rows_quant *out);
+
+/* Root-mean-square norm with the residual's addition: h = x + residual in fp32, written to sum (in the residual's type; may be residual itself, or NULL), and
+ * h * gain / sqrt(mean(h^2) + eps) of the unrounded h to 8 bits, as hsd_quant_rows.  residual NULL: h = x (then sum is NULL, and
+ * res_dtype still one of the two); gain: dev [dim] fp32 or NULL (1).  eps >= 0.  A row whose squares' sum is not finite in fp32 is held as NaN. */
+int hsd_quant_norm_rows(void *stream, int32_t n_rows, int32_t dim, int32_t dtype, const void *x, int64_t x_stride, int32_t res_dtype,
+                        const void *residual, int64_t res_stride, void *sum, int64_t sum_stride, const float *gain, float eps,
+                        const hsd_rows_quant *out);
+
+/* The values that rows in 8 bits stand for, to out: exact in both types (of rows that
+ * the calls here wrote; with bytes below 27 from elsewhere the smallest may round). */
+int hsd_quant_read_rows(void *stream, int32_t n_rows, int32_t dim, const hsd_rows_quant *rows, int32_t dtype, void *out, int64_t out_stride);
+
+/* w [n_out, dim] to 8 bits in blocks of 128 by 128, once for a model: bytes as in hsd_quant_rows, or floats: the largest finite magnitude / 448, 1
+ * where that is 0.  Writes out->codes and out->scale. */
+int hsd_quant_weights(void *stream, int32_t n_out, int32_t dim, int32_t dtype, const void *w, int64_t w_stride, const hsd_weight_quant *out);
+
+/* out[m][n] = sum_k rows[m][k] * w[n][k], [n_rows, n_out] in dtype, of the values that both stand for.  Sums in fp32; products of codes are exact.  The
+ * same call gives the same bits. */
+int hsd_quant_linear(void *stream, int32_t n_rows, int32_t n_out, int32_t dim, const hsd_rows_quant *rows, const hsd_weight_quant *w, int32_t dtype,
+                     void *out, int64_t out_stride);
+
+/* silu(gate) * up, gate = rows * w[0 .. d_ffn - 1]^T and up = rows * w[d_ffn .. 2 d_ffn - 1]^T in fp32, to 8 bits as hsd_quant_rows:
+ * out is [n_rows, d_ffn], d_ffn a multiple of 128. */
+int hsd_quant_gated(void *stream, int32_t n_rows, int32_t d_ffn, int32_t dim, const hsd_rows_quant *rows, const hsd_weight_quant *w,
+                    const hsd_rows_quant *out);
+
 #ifdef __cplusplus
 }
 #endif

@@ -21,6 +21,7 @@ HSD_OK, HSD_EINVAL, HSD_ENOSPC, HSD_ERANGE, HSD_EARCH, HSD_ENODEV, HSD_EHIP = 0,
 HSD_FP32, HSD_BF16 = 0, 1
 HSD_STATUS_POOL_EXHAUSTED, HSD_STATUS_TABLE_OVERFLOW, HSD_STATUS_BAD_SLOT, HSD_STATUS_BAD_TREE, HSD_STATUS_NOT_FINITE = 1, 2, 4, 8, 16
 HSD_KV_BLOCK_TOKENS, HSD_HEAD_DIM, HSD_MAX_SEQ, HSD_MAX_TOP = 16, 64, 4096, 32
+HSD_QUANT_BLOCK, HSD_SCALE_FP32, HSD_SCALE_POW2 = 128, 0, 1
 
 i32, f32, vp = C.c_int32, C.c_float, C.c_void_p
 
@@ -71,6 +72,14 @@ class hsd_kv_quant(C.Structure):
     _fields_ = [("k_codes", vp), ("v_codes", vp), ("k_scale", vp), ("v_scale", vp), ("n_blocks", i32), ("n_kv_heads", i32)]
 
 
+class hsd_rows_quant(C.Structure):
+    _fields_ = [("codes", vp), ("scale", vp), ("code_stride", C.c_int64), ("scale_stride", C.c_int64)]
+
+
+class hsd_weight_quant(C.Structure):
+    _fields_ = [("codes", vp), ("scale", vp), ("code_stride", C.c_int64), ("scale_stride", C.c_int64), ("scale_type", i32)]
+
+
 _P = C.POINTER
 lib.hsd_status_string.restype = C.c_char_p
 lib.hsd_status_string.argtypes = [C.c_int]
@@ -106,7 +115,8 @@ EXPORTS = ["hsd_probe_launch", "hsd_verify_region_batch_noalloc", "hsd_noalloc_s
            "hsd_workspace_bytes", "hsd_kv_pool_init", "hsd_verify_region_batch", "hsd_verify_page",
            "hsd_kv_commit_rollback", "hsd_prefill", "hsd_drafts_create", "hsd_drafts_destroy", "hsd_drafts_tree", "hsd_tree_path",
            "hsd_kv_reserve", "hsd_kv_commit_rows", "hsd_kv_quant_append", "hsd_kv_quant_read", "hsd_kv_quant_attention_bytes",
-           "hsd_kv_quant_attention", "hsd_workspace_quant_bytes", "hsd_verify_quant", "hsd_prefill_quant", "hsd_token_logprobs_bytes", "hsd_token_logprobs"]
+           "hsd_kv_quant_attention", "hsd_workspace_quant_bytes", "hsd_verify_quant", "hsd_prefill_quant", "hsd_token_logprobs_bytes", "hsd_token_logprobs",
+           "hsd_quant_rows", "hsd_quant_norm_rows", "hsd_quant_read_rows", "hsd_quant_weights", "hsd_quant_linear", "hsd_quant_gated"]
 lib.hsd_drafts_create.argtypes = [vp, vp, i32, C.POINTER(vp)]
 lib.hsd_drafts_destroy.argtypes, lib.hsd_drafts_destroy.restype = [vp], None
 lib.hsd_drafts_tree.argtypes = [vp, vp, i32, C.c_int64, C.c_int64, i32, vp, vp, vp, C.POINTER(i32)]
@@ -123,6 +133,13 @@ for _n in ("hsd_verify_quant", "hsd_prefill_quant"):
     getattr(lib, _n).argtypes = [vp, vp, _P(hsd_kv_pool), _P(hsd_kv_quant), _P(hsd_batch), vp, szt]
 lib.hsd_token_logprobs_bytes.argtypes, lib.hsd_token_logprobs_bytes.restype = [i32, i32, i32], szt
 lib.hsd_token_logprobs.argtypes = [vp, i32, i32, i32, vp, i64, vp, vp, vp, i32, vp, vp, vp, szt]
+
+lib.hsd_quant_rows.argtypes = [vp, i32, i32, i32, vp, i64, _P(hsd_rows_quant)]
+lib.hsd_quant_norm_rows.argtypes = [vp, i32, i32, i32, vp, i64, i32, vp, i64, vp, i64, vp, f32, _P(hsd_rows_quant)]
+lib.hsd_quant_read_rows.argtypes = [vp, i32, i32, _P(hsd_rows_quant), i32, vp, i64]
+lib.hsd_quant_weights.argtypes = [vp, i32, i32, i32, vp, i64, _P(hsd_weight_quant)]
+lib.hsd_quant_linear.argtypes = [vp, i32, i32, i32, _P(hsd_rows_quant), _P(hsd_weight_quant), i32, vp, i64]
+lib.hsd_quant_gated.argtypes = [vp, i32, i32, i32, _P(hsd_rows_quant), _P(hsd_weight_quant), _P(hsd_rows_quant)]
 
 
 class HsdError(RuntimeError):
@@ -214,3 +231,21 @@ def hsd_verify_quant(ctx, stream, pool, layers, batch, ws, ws_bytes):
     check("hsd_verify_quant", lib.hsd_verify_quant(ctx, stream, C.byref(pool), layers, C.byref(batch), ws, ws_bytes))
 def hsd_prefill_quant(ctx, stream, pool, layers, batch, ws, ws_bytes):
     check("hsd_prefill_quant", lib.hsd_prefill_quant(ctx, stream, C.byref(pool), layers, C.byref(batch), ws, ws_bytes))
+
+def hsd_quant_rows(stream, n_rows, dim, dtype, x, x_stride, out):
+    rc = lib.hsd_quant_rows(stream, n_rows, dim, dtype, x, x_stride, out)
+    if rc: check("hsd_quant_rows", rc)
+def hsd_quant_norm_rows(stream, n_rows, dim, dtype, x, x_stride, res_dtype, residual, res_stride, total, sum_stride, gain, eps, out):
+    rc = lib.hsd_quant_norm_rows(stream, n_rows, dim, dtype, x, x_stride, res_dtype, residual, res_stride, total, sum_stride, gain, eps, out)
+    if rc: check("hsd_quant_norm_rows", rc)
+def hsd_quant_read_rows(stream, n_rows, dim, rows, dtype, out, out_stride):
+    rc = lib.hsd_quant_read_rows(stream, n_rows, dim, rows, dtype, out, out_stride)
+    if rc: check("hsd_quant_read_rows", rc)
+def hsd_quant_weights(stream, n_out, dim, dtype, w, w_stride, out):
+    check("hsd_quant_weights", lib.hsd_quant_weights(stream, n_out, dim, dtype, w, w_stride, out))
+def hsd_quant_linear(stream, n_rows, n_out, dim, rows, w, dtype, out, out_stride):
+    rc = lib.hsd_quant_linear(stream, n_rows, n_out, dim, rows, w, dtype, out, out_stride)
+    if rc: check("hsd_quant_linear", rc)
+def hsd_quant_gated(stream, n_rows, d_ffn, dim, rows, w, out):
+    rc = lib.hsd_quant_gated(stream, n_rows, d_ffn, dim, rows, w, out)
+    if rc: check("hsd_quant_gated", rc)

@@ -26,11 +26,13 @@
 #include "gemm_mfma_r.h"
 #include "probes.h"
 #include "gemm_f32.h"
+#include "gemm_quant.h"
 #include "gemm_simple.h"
 #include "kv_place.h"
 #include "kv_quant.h"
 #include "misc_kernels.h"
 #include "pass_setup.h"
+#include "rows_quant.h"
 #include "token_scores.h"
 
 using namespace hsd;
@@ -1219,3 +1221,4 @@ int hsd_tree_path(const int32_t *tokens, const int32_t *tree_end, int32_t n_rows
 }  // extern "C"
 
 #include "ops_api.h"
+#include "linear_api.h"

@@ -1,0 +1,187 @@
+// Rows and weights held in 8 bits: made, normalised, read.
+//
+// A row of `dim` values is held in blocks of 128: e4m3 codes, the last block padded with zeros, and one byte a block for a power of
+// two: value = code * 2^(byte - 127), byte - 127 the least e in -100 .. 119 with 448 * 2^e >= the largest finite magnitude of the
+// block (0 for a block of zeros), as the 8-bit cache's pages have it (scale_exp).  A power of two costs no accuracy (codes are floating point: a value's step is 2^-4 of it down to
+// 2^-6 * 2^e), the matrix unit applies it by itself (its byte operands are these bytes), and a value is exact in bf16.  NaN and infinities are
+// held as NaN, so that what is computed from them shows it.
+#pragma once
+
+#include "common.h"
+#include "kv_quant.h"
+
+namespace hsd {
+
+constexpr int kQuantBlock = 128;
+
+struct RowsQuant {
+  uint8_t *codes, *scale;             // rows code_stride and scale_stride bytes apart
+  int64_t code_stride, scale_stride;
+};
+
+// magnitude of y that counts for its block's scale: infinities and NaN do not
+__device__ __forceinline__ float finite_mag(float y) { return fabsf(y) < INFINITY ? fabsf(y) : 0.f; }
+// y * 2^-e as a code's argument: at most 448 in magnitude (larger ones, with the largest e, as that), or NaN
+__device__ __forceinline__ float code_arg(float y, float inv) { return fabsf(y) < INFINITY ? __builtin_amdgcn_fmed3f(y * inv, -448.f, 448.f) : NAN; }
+__device__ __forceinline__ float two_to_byte(uint32_t b) { return b ? __uint_as_float(b << 23) : 0x1p-127f; }          // 2^(b - 127)
+
+// largest value over a row of 16 lanes, in all of them
+__device__ __forceinline__ float max16(float x) {
+  x = fmaxf(x, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x128, 0xf, 0xf, true)));   // row_ror:8
+  x = fmaxf(x, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x124, 0xf, 0xf, true)));
+  x = fmaxf(x, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x122, 0xf, 0xf, true)));
+  return fmaxf(x, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x121, 0xf, 0xf, true)));
+}
+
+// Eight values from column c of a row of dim (those behind its end as 0)
+template <typename T>
+__device__ __forceinline__ void load8(const T *row, int c, int dim, float *v) {
+  if (c + 8 <= dim) {
+    quant_load4(row + c, v), quant_load4(row + c + 4, v + 4);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = c + i < dim ? to_f32(row[c + i]) : 0.f;
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store8(T *row, int c, int dim, const float *v) {
+  if (c + 8 <= dim) {
+    if constexpr (sizeof(T) == 4) {
+      quant_store4(row + c, v), quant_store4(row + c + 4, v + 4);
+    } else {
+      typedef uint32_t u4 __attribute__((ext_vector_type(4), aligned(2)));
+      u4 x;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = f32_to_bf16(v[2 * i]) | static_cast<uint32_t>(f32_to_bf16(v[2 * i + 1])) << 16;
+      *reinterpret_cast<u4 *>(row + c) = x;
+    }
+  } else {
+    for (int i = 0; i < 8; ++i)
+      if (c + i < dim) row[c + i] = from_f32<T>(v[i]);
+  }
+}
+
+// Eight values of a block that 16 neighbouring lanes hold, to codes; the first of the lanes writes the block's byte
+__device__ __forceinline__ void store_codes8(const RowsQuant &out, int64_t r, int c, const float *y) {
+  float top = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = fmaxf(top, finite_mag(y[i]));
+  top = max16(top);
+  const int e = scale_exp(top);
+  const float inv = exp2_int(-e);
+  uint2 q;
+  q.x = quant4(code_arg(y[0], inv), code_arg(y[1], inv), code_arg(y[2], inv), code_arg(y[3], inv));
+  q.y = quant4(code_arg(y[4], inv), code_arg(y[5], inv), code_arg(y[6], inv), code_arg(y[7], inv));
+  *reinterpret_cast<uint2 *>(out.codes + r * out.code_stride + c) = q;
+  if ((c & (kQuantBlock - 1)) == 0) out.scale[r * out.scale_stride + c / kQuantBlock] = static_cast<uint8_t>(e + 127);
+}
+
+struct NormRows {
+  int64_t n_rows;
+  int32_t dim;
+  int32_t norm;                        // 0: the values as they are
+  const float *gain;                   // or nullptr: 1
+  float eps, inv_dim;
+  int64_t x_stride, res_stride, sum_stride;
+  RowsQuant out;
+};
+
+// y = h * gain / sqrt(mean(h^2) + eps), h = x + residual, to 8 bits; h to `sum`.  One workgroup a row.
+template <typename TX, typename TR>
+__global__ void __launch_bounds__(256) k_quant_rows(const NormRows a, const TX *x, const TR *res, TR *sum) {
+  __shared__ float part[4];
+  const int t = threadIdx.x;
+  const int64_t r = blockIdx.x;
+  const TX *xr = x + r * a.x_stride;
+  const TR *rr = res ? res + r * a.res_stride : nullptr;
+  TR *sr = sum ? sum + r * a.sum_stride : nullptr;
+  const int width = (a.dim + kQuantBlock - 1) / kQuantBlock * kQuantBlock;
+  float rstd = 1.f;
+  if (a.norm) {
+    float ss = 0.f;
+    for (int c = 8 * t; c < width; c += 2048) {
+      float h[8], g[8];
+      load8(xr, c, a.dim, h);
+      if (rr) load8(rr, c, a.dim, g);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float v = rr ? h[i] + g[i] : h[i];
+        ss = __builtin_fmaf(v, v, ss);
+      }
+    }
+    ss = wave_sum(ss);
+    if ((t & 63) == 0) part[t >> 6] = ss;
+    __syncthreads();
+    ss = part[0] + part[1] + part[2] + part[3];
+    rstd = ss < INFINITY ? 1.f / sqrtf(__builtin_fmaf(ss, a.inv_dim, a.eps)) : NAN;
+  }
+  for (int c = 8 * t; c < width; c += 2048) {
+    float h[8], g[8];
+    load8(xr, c, a.dim, h);
+    if (rr) {
+      load8(rr, c, a.dim, g);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) h[i] += g[i];
+    }
+    if (sr) store8(sr, c, a.dim, h);
+    if (a.norm) {
+      if (a.gain) load8(a.gain, c, a.dim, g);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) h[i] = c + i < a.dim ? h[i] * rstd * (a.gain ? g[i] : 1.f) : 0.f;
+    }
+    store_codes8(a.out, r, c, h);
+  }
+}
+
+// The values of rows in 8 bits (exact in both types)
+template <typename T>
+__global__ void __launch_bounds__(256) k_quant_read_rows(const RowsQuant q, int64_t n_rows, int dim, T *out, int64_t out_stride) {
+  const int64_t r = blockIdx.x;
+  for (int c = 8 * threadIdx.x; c < dim; c += 2048) {
+    const uint2 w = *reinterpret_cast<const uint2 *>(q.codes + r * q.code_stride + c);
+    const float s = two_to_byte(q.scale[r * q.scale_stride + c / kQuantBlock]);
+    float v[8];
+    dequant4(w.x, s, v), dequant4(w.y, s, v + 4);
+    store8(out + r * out_stride, c, dim, v);
+  }
+}
+
+// Weights in blocks of 128 by 128: one workgroup a block.  The scale is a power of two as for rows, or (a float) the largest magnitude / 448.
+template <typename T>
+__global__ void __launch_bounds__(256) k_quant_weights(int n_out, int dim, const T *w, int64_t w_stride, uint8_t *codes, int64_t code_stride,
+                                                       uint8_t *byte, float *scale, int64_t scale_stride) {
+  __shared__ float part[4];
+  const int t = threadIdx.x, c = blockIdx.x * kQuantBlock + 8 * (t & 15);
+  const int64_t r0 = static_cast<int64_t>(blockIdx.y) * kQuantBlock + (t >> 4);
+  float v[8][8], top = 0.f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    if (r0 + 16 * j < n_out) load8(w + (r0 + 16 * j) * w_stride, c, dim, v[j]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (r0 + 16 * j >= n_out) v[j][i] = 0.f;
+      top = fmaxf(top, finite_mag(v[j][i]));
+    }
+  }
+  top = wave_max(top);
+  if ((t & 63) == 0) part[t >> 6] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+  const float s = top > 0.f ? fmaxf(top / 448.f, 0x1p-126f) : 1.f;   // (smaller ones would lose bits of their own)
+  const int e = scale_exp(top);
+  const float inv = exp2_int(-e);
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    if (r0 + 16 * j < n_out) {
+      float q[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) q[i] = scale ? (fabsf(v[j][i]) < INFINITY ? __builtin_amdgcn_fmed3f(v[j][i] / s, -448.f, 448.f) : NAN) : code_arg(v[j][i], inv);
+      *reinterpret_cast<uint2 *>(codes + (r0 + 16 * j) * code_stride + c) = uint2{quant4(q[0], q[1], q[2], q[3]), quant4(q[4], q[5], q[6], q[7])};
+    }
+  if (t == 0) {
+    if (scale) scale[blockIdx.y * scale_stride + blockIdx.x] = s;
+    else byte[blockIdx.y * scale_stride + blockIdx.x] = static_cast<uint8_t>(e + 127);
+  }
+}
+
+}  // namespace hsd

@@ -1,0 +1,125 @@
+"""Rows and weights in 8 bits from their definition, in 64 bits, for the tests of the operators on them."""
+import torch
+
+BLOCK = 128
+U = 2.0 ** -24          # half a step of fp32, relative
+HALF = {torch.bfloat16: 2.0 ** -8, torch.float32: U}
+
+
+def e4m3_values():
+    """What each code stands for (NaN for 127 and 255)."""
+    c = torch.arange(256)
+    e, m = (c >> 3) & 15, c & 7
+    v = torch.where(e > 0, (8 + m).double() * 2.0 ** (e.double() - 10), m.double() * 2.0 ** -9)
+    v = torch.where(c >= 128, -v, v)
+    v[127] = v[255] = float("nan")
+    return v
+
+
+def row_values(codes, scale, dim):
+    v = e4m3_values().to(codes.device)[codes.long()]
+    s = torch.exp2(scale[:, :codes.shape[1] // BLOCK].double() - 127).repeat_interleave(BLOCK, 1)
+    return (v * s)[:, :dim]
+
+
+def weight_values(codes, scale, dim):
+    v = e4m3_values().to(codes.device)[codes.long()]
+    s = torch.exp2(scale.double() - 127) if scale.dtype == torch.uint8 else scale.double()
+    return (v * s.repeat_interleave(BLOCK, 0)[:len(codes)].repeat_interleave(BLOCK, 1)[:, :codes.shape[1]])[:, :dim]
+
+
+def exponent(top):
+    """Least e in -100 .. 119 with 448 * 2^e >= top (119 where none is); 0 where top is 0."""
+    e = torch.full_like(top, -100.0)
+    for k in range(-99, 120):
+        e = torch.where(448.0 * 2.0 ** (k - 1) < top, torch.full_like(e, float(k)), e)
+    return torch.where(top > 0, e, torch.zeros_like(e))
+
+
+def block_tops(y):
+    """Largest finite magnitude of each 128 columns."""
+    y = torch.where(torch.isfinite(y), y.abs(), torch.zeros_like(y))
+    return torch.nn.functional.pad(y, (0, -y.shape[1] % BLOCK)).reshape(len(y), -(-y.shape[1] // BLOCK), BLOCK).amax(-1)
+
+
+def check_rows(rows8, y, err):
+    """Codes and scales of rows that stand for y (64 bits), each value known to the computation within err (a tensor or number, absolute): the
+    exponent is that of the block's largest magnitude, the code a nearest one; places behind dim hold zero, NaN and infinities NaN."""
+    codes, scale, dim = rows8.codes, rows8.scale, rows8.dim
+    blocks = -(-dim // BLOCK)
+    assert y.shape == (rows8.rows, dim)
+    err = torch.zeros_like(y) + err
+    fine = torch.isfinite(y)
+    err = torch.where(fine, err, torch.zeros_like(err))
+    mag = torch.where(fine, y.abs(), torch.zeros_like(y))
+    e = scale[:, :blocks].double() - 127
+    lo, hi = exponent(block_tops((mag - err).clamp(min=0))), exponent(block_tops(mag + err))
+    top0 = block_tops(mag + err) == 0
+    assert bool(torch.where(top0, e == 0, (e >= lo) & (e <= hi) | (block_tops((mag - err).clamp(min=0)) == 0)).all()), "exponents"
+    v = row_values(codes, scale, dim)
+    assert bool((torch.isnan(v) == ~fine).all()), "NaN"
+    assert not bool((codes[:, dim:blocks * BLOCK] & 127).any()), "padding"
+    s = torch.exp2(e).repeat_interleave(BLOCK, 1)[:, :dim]
+    step = torch.exp2(torch.floor(torch.log2(((mag + err) / s).clamp(min=2.0 ** -6))) - 3) * s
+    off = torch.where(fine, (v - y.clamp(-448 * 2.0 ** 119, 448 * 2.0 ** 119)).abs(), torch.zeros_like(y))
+    bad = off > step / 2 + err
+    assert not bool(bad.any()), (int(bad.sum()), float((off / step)[bad].max()))
+
+
+def random_rows(n, dim, seed, dtype=torch.bfloat16, device="cuda:0", spread=1.0):
+    g = torch.Generator(device=device).manual_seed(seed)
+    x = torch.randn((n, dim), generator=g, device=device) * torch.exp(spread * torch.randn((dim,), generator=g, device=device))
+    return x.to(dtype)
+
+
+def random_rows8(n, dim, seed, device="cuda:0"):
+    """Any codes but NaN, and bytes of powers of two that differ by up to 2^12."""
+    from paper_2602_12957_amd.linear8 import Rows8
+    g = torch.Generator(device=device).manual_seed(seed)
+    r = Rows8.empty(n, dim, device)
+    c = torch.randint(256, r.codes.shape, generator=g, device=device)
+    c = torch.where((c & 127) == 127, c - 1, c)
+    c[:, dim:] = 0
+    r.codes.copy_(c.to(torch.uint8))
+    r.scale.copy_(torch.randint(112, 125, r.scale.shape, generator=g, device=device).to(torch.uint8))
+    return r
+
+
+def random_weight8(n_out, dim, seed, scale=torch.uint8, device="cuda:0"):
+    from paper_2602_12957_amd.linear8 import Weight8
+    g = torch.Generator(device=device).manual_seed(seed)
+    blocks = -(-dim // BLOCK)
+    c = torch.randint(256, (n_out, blocks * BLOCK), generator=g, device=device)
+    c = torch.where((c & 127) == 127, c - 1, c)
+    c[:, dim:] = 0
+    if scale == torch.uint8:
+        s = torch.randint(112, 125, (-(-n_out // BLOCK), blocks), generator=g, device=device).to(torch.uint8)
+    else:
+        s = torch.randn((-(-n_out // BLOCK), blocks), generator=g, device=device) * 0.01   # (any number: negative ones too)
+    return Weight8(c.to(torch.uint8), s, dim)
+
+
+def product(rows8, w8):
+    """rows * w^T in 64 bits, the sums of the products' magnitudes, and how far the sums may be off that one call makes.
+
+    Products of codes are exact.  bf16 results: the matrix unit adds eight products at once, aligned to the largest of them and cut 13 bits
+    below its power of two: at most 7 products lose up to 2^-13 of the largest each (7 * 2^-13 of the magnitudes' sum, worst).  Its
+    accumulators, the scales and the sums of blocks round in fp32: fewer than dim / 8 + 3 * blocks + 8 roundings of at most the magnitudes' sum.  fp32 results: every addition
+    rounds in fp32, dim of them and the same ones of the scales."""
+    a, w = row_values(rows8.codes, rows8.scale, rows8.dim), weight_values(w8.codes, w8.scale, rows8.dim)
+    y, mag = a @ w.T, a.abs() @ w.abs().T
+    k, blocks = rows8.dim, -(-rows8.dim // BLOCK)
+    return y, mag, {torch.bfloat16: (7 * 2.0 ** -13 + (k / 8 + 3 * blocks + 8) * U) * mag, torch.float32: (k + 3 * blocks + 8) * U * mag}
+
+
+def check_product(got, rows8, w8):
+    y, mag, err = product(rows8, w8)
+    assert got.shape == y.shape
+    h = HALF[got.dtype]
+    off = (got.double() - y).abs()
+    most = err[got.dtype] * (1 + h) + h * y.abs() + 2.0 ** -126
+    bad = ~(off <= most)
+    assert not bool(bad.any()), (int(bad.sum()), float((off / most).max()))
+    # taken together they are far nearer than that: cuts go either way, and a result's error is that of its rounding, at most half a step
+    rms = lambda t: float(t.square().mean().sqrt())   # noqa: E731
+    assert rms(off) <= h * rms(y) + (2.0 ** -13 if got.dtype == torch.bfloat16 else rows8.dim * U) * rms(mag) / max(1.0, rows8.dim) ** 0.5 + 2.0 ** -126
