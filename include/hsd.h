@@ -389,13 +389,13 @@ int hsd_token_logprobs(void *stream, int32_t n_rows, int32_t vocab, int32_t dtyp
  * run on the current device, which has to be the tensors' and the stream's, and take no workspace.
  *
  * Rows in 8 bits: n_rows rows of dim values in blocks of HSD_QUANT_BLOCK columns, e4m3 codes (OCP) and one byte a block,
- * value = code * 2^(byte - 127).  A row of codes is padded with zeros to whole blocks; the bytes behind a row's last block are never
- * looked at.  NaN and infinities are held as NaN. */
+ * value = code * 2^(byte - 127), 27 <= byte <= 246 (others have no meaning here).  A row of codes is padded with zeros to whole blocks; what
+ * lies behind a row's last block is never looked at.  NaN and infinities are held as NaN. */
 enum { HSD_QUANT_BLOCK = 128 };
 typedef struct hsd_rows_quant {
   void *codes;          /* dev [n_rows][128 * ceil(dim / 128)], 16-byte aligned                                  */
   uint8_t *scale;       /* dev [n_rows][ceil(dim / 128)], 4-byte aligned                                         */
-  int64_t code_stride;  /* bytes from row to row: a multiple of 16, whole blocks at least                        */
+  int64_t code_stride;  /* bytes from row to row: a multiple of 16, whole blocks at least, 2^23 at most         */
   int64_t scale_stride; /* the same of scale: a multiple of 4, and at least the blocks rounded up to one         */
 } hsd_rows_quant;
 
@@ -424,8 +424,7 @@ int hsd_quant_norm_rows(void *stream, int32_t n_rows, int32_t dim, int32_t dtype
                         const void *residual, int64_t res_stride, void *sum, int64_t sum_stride, const float *gain, float eps,
                         const hsd_rows_quant *out);
 
-/* The values that rows in 8 bits stand for, to out: exact in both types (of rows that
- * the calls here wrote; with bytes below 27 from elsewhere the smallest may round). */
+/* The values that rows in 8 bits stand for, to out: exact in both types. */
 int hsd_quant_read_rows(void *stream, int32_t n_rows, int32_t dim, const hsd_rows_quant *rows, int32_t dtype, void *out, int64_t out_stride);
 
 /* w [n_out, dim] to 8 bits in blocks of 128 by 128, once for a model: bytes as in hsd_quant_rows, or floats: the largest finite magnitude / 448, 1

@@ -1,66 +1,348 @@
-// Products of rows and weights that are held in 8 bits.
+// Products of rows and weights that are held in 8 bits, tiles of many rows.
 //
-// out[m][n] = sum over blocks b of 128 columns of 2^(sa[m][b] - 127) * sw[n / 128][b] * sum_k a[m][k] w[n][k]
+//   out[m][n] = sum over blocks b of 128 columns of 2^(sa[m][b] - 127) * sw[n / 128][b] * sum_k a[m][k] w[n][k]
 #pragma once
 
 #include "rows_quant.h"
 
 namespace hsd {
 
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
 struct WeightQuant {
   const uint8_t *codes;
   const void *scale;        // bytes (powers of two) or floats
   int64_t code_stride, scale_stride;
-  int32_t bytes;            // whether they are bytes
 };
-// A block's sum times its row's and its weights' scales (exponents together: each alone may leave fp32's range)
-__device__ __forceinline__ float scaled(float sum, uint32_t row_byte, const WeightQuant &w, int64_t i) {
-  if (w.bytes) return ldexpf(sum, static_cast<int>(row_byte) + static_cast<const uint8_t *>(w.scale)[i] - 254);
-  return ldexpf(sum * static_cast<const float *>(w.scale)[i], static_cast<int>(row_byte) - 127);
+
+// Two LDS-direct loads of 1 KB: lane l's 16 bytes at base + off0 (off1) go to dst + 16 l (dst + STEP + 16 l).  In asm: the
+// compiler would otherwise wait for every load in flight before each LDS read.  No register is written; the reads wait by
+// quant_wait and a barrier.  m0 is put back as it was found.
+template <int STEP>
+__device__ __forceinline__ void lds_load_pair(uint32_t dst, const uint8_t *base, uint32_t off0, uint32_t off1) {
+  uint32_t m0;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %1\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %2, %4\n\t"
+      "s_add_u32 m0, m0, %5\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %3, %4\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(m0)
+      : "s"(dst), "v"(off0), "v"(off1), "s"(base), "i"(STEP)
+      : "memory", "scc");
+}
+__device__ __forceinline__ void lds_load_one(uint32_t dst, const uint8_t *base, uint32_t off) {
+  uint32_t m0;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %1\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %2, %3\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(m0)
+      : "s"(dst), "v"(off), "s"(base)
+      : "memory");
+}
+// All of this wave's loads have landed, and its LDS reads are done
+__device__ __forceinline__ void quant_wait() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0);
+  asm volatile("" ::: "memory");
 }
 
-__device__ __forceinline__ float dot4(uint32_t a, uint32_t b, float s) {
-  float x[4], y[4];
-  dequant4(a, 1.f, x), dequant4(b, 1.f, y);
+template <int BM_, int BN_, int WM_, int WN_>
+struct ProductTile {
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NW = WM_ * WN_;
+  static constexpr int TA = BM / WM / 32, TW = BN / WN / 32;      // 32x32 sub-tiles of a wave: rows, weight rows
+  static constexpr int kStage = (BM + BN) * kQuantBlock;          // a block of 128 columns of the tile's rows and weight rows
+  static constexpr int kLoadsA = BM / 8 / NW, kLoadsW = BN / 8 / NW;   // 1 KB loads of a wave and stage
+  static constexpr int kLds = 2 * kStage;
+  static constexpr int kWaves = BM * BN / NW > 128 * 64 ? 1 : 2;  // of a SIMD
+  static_assert(kLoadsA % 2 == 0 && kLoadsW % 2 == 0 && BM / 8 % NW == 0 && BN / 8 % NW == 0, "loads go in pairs of one operand");
+};
+
+// Tile of a workgroup: XCD x (workgroup id mod 8) takes a contiguous run of an order that goes through bands of eight tiles of rows,
+// so that the tiles an XCD works on at a time share few rows and few weights (32 of 8192^3: 8 by 4 tiles, 24 MB through its L2 a round; row after row they would take 66).
+__device__ __forceinline__ void quant_tile_of(int id, int tiles_m, int tiles_n, int &tm, int &tn) {
+  const int all = tiles_m * tiles_n, full = all / 8 * 8;
+  const int p = id < full ? id % 8 * (full / 8) + id / 8 : id;
+  const int band = p / (8 * tiles_n), rest = p - band * 8 * tiles_n, high = min(8, tiles_m - 8 * band);
+  tn = rest / high;
+  tm = 8 * band + rest - tn * high;
+}
+
+// silu(g) * u
+__device__ __forceinline__ float swiglu(float g, float u) {
+  return g * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * g)) * u;
+}
+
+// The 32 codes of a fragment as bf16, times a power of two (exact): operands of four bf16 products
+struct Fragment16 {
+  bf16x8 v[4];
+};
+__device__ __forceinline__ Fragment16 widen(const i32x8 &f, float scale) {
+  Fragment16 r;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) s = __builtin_fmaf(x[i], y[i], s);
-  return s;
-}
-
-// One output of a row and a weight row
-__device__ __forceinline__ float plain_product(const RowsQuant &a, const WeightQuant &w, int64_t m, int64_t n, int blocks) {
-  float sum = 0.f;
-  for (int b = 0; b < blocks; ++b) {
-    const uint32_t *x = reinterpret_cast<const uint32_t *>(a.codes + m * a.code_stride + b * kQuantBlock);
-    const uint32_t *y = reinterpret_cast<const uint32_t *>(w.codes + n * w.code_stride + b * kQuantBlock);
-    float s = 0.f;
-    for (int i = 0; i < kQuantBlock / 4; ++i) s = dot4(x[i], y[i], s);
-    sum += scaled(s, a.scale[m * a.scale_stride + b], w, n / kQuantBlock * w.scale_stride + b);
+  for (int i = 0; i < 4; ++i) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f[2 * i], scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f[2 * i], scale, true);
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f[2 * i + 1], scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f[2 * i + 1], scale, true);
+    r.v[i] = bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
   }
-  return sum;
+  return r;
 }
 
-// A thread an output: grid (columns / 256, rows)
-template <typename T>
-__global__ void __launch_bounds__(256) k_quant_linear(const RowsQuant a, const WeightQuant w, int64_t m0, int n_out, int blocks, T *out, int64_t out_stride) {
-  const int64_t m = m0 + blockIdx.y;
-  const int n = blockIdx.x * 256 + threadIdx.x;
-  if (n < n_out) out[m * out_stride + n] = from_f32<T>(plain_product(a, w, m, n, blocks));
-}
+// GATED: gate and up rows of 128 output columns (BN = 256), silu(gate) * up to 8 bits; else out.  FLOATS: weight scales are floats.
+// EXACT: bf16 products of the codes instead of the 8-bit ones.
+template <typename Cfg, bool GATED, bool FLOATS, bool EXACT, typename T>
+__global__ void __launch_bounds__(64 * Cfg::NW, Cfg::kWaves) k_gemm_quant(const RowsQuant a, const WeightQuant w, int M, int N, int nk, T *__restrict__ out, int64_t out_stride,
+                                                              const RowsQuant q) {
+  constexpr int BM = Cfg::BM, BN = Cfg::BN, TA = Cfg::TA, TW = Cfg::TW, NW = Cfg::NW;
+  constexpr int COLS = GATED ? BN / 2 : BN;
+  static_assert(!GATED || (COLS == kQuantBlock && TW % 2 == 0), "a workgroup has whole blocks of the rows that it rounds");
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int wi = wave / Cfg::WN, wj = wave % Cfg::WN;
+  int tm, tn;
+  quant_tile_of(blockIdx.x, (M + BM - 1) / BM, (N + COLS - 1) / COLS, tm, tn);
+  const int m0 = tm * BM, n0 = tn * COLS;
 
-// silu(gate) * up of 128 columns of one row, to 8 bits: grid (columns / 128, rows)
-__global__ void __launch_bounds__(128) k_quant_gated(const RowsQuant a, const WeightQuant w, int64_t m0, int d_ffn, int blocks, const RowsQuant out) {
-  __shared__ float y[kQuantBlock];
-  const int64_t m = m0 + blockIdx.y;
-  const int t = threadIdx.x, n = blockIdx.x * kQuantBlock + t;
-  const float g = plain_product(a, w, m, n, blocks), u = plain_product(a, w, m, d_ffn + n, blocks);
-  y[t] = g / (1.f + expf(-g)) * u;
-  __syncthreads();
-  if (t < 16) {
-    float v[8];
+  // ---- loads.  Load i of a stage covers tile rows 8 i .. 8 i + 7 (rows, then weight rows); lane l fetches, for row 8 i + l / 8, the 16-byte
+  // piece that belongs at position l % 8: piece p of row r lies at p ^ ((r >> 1) & 7), so that reads of 16 rows cover all banks.
+  // Rows behind the last one are that one again (their products are never stored).
+  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char *)smem_raw));
+  const uint8_t *base_a = a.codes + m0 * a.code_stride, *base_w = w.codes + n0 * w.code_stride;
+  if (GATED && NW == 8 && (wave & 4)) base_w += N * w.code_stride;   // (of eight waves, 4 to 7 fetch up rows)
+  uint32_t off_a[Cfg::kLoadsA], off_w[Cfg::kLoadsW];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = y[8 * t + i];
-    store_codes8(out, m, blockIdx.x * kQuantBlock + 8 * t, v);
+  for (int j = 0; j < Cfg::kLoadsA; ++j) {
+    const int r = (j * NW + wave) * 8 + (lane >> 3);
+    off_a[j] = min(r, M - 1 - m0) * static_cast<uint32_t>(a.code_stride) + ((lane & 7) ^ ((r >> 1) & 7)) * 16;
+  }
+#pragma unroll
+  for (int j = 0; j < Cfg::kLoadsW; ++j) {
+    const int r = (j * NW + wave) * 8 + (lane >> 3);
+    // gate and up alternate by 32 rows: weight row 64 g + 32 u + x of the tile is row n0 + 32 g + x of the gate or of the up projection
+    const int row = GATED ? (r >> 6) * 32 + (r & 31) : min(r, N - 1 - n0);
+    off_w[j] = row * static_cast<uint32_t>(w.code_stride) + ((lane & 7) ^ ((r >> 1) & 7)) * 16;
+  }
+  auto request = [&](int stage, int kt, int j) {   // loads 2 j and 2 j + 1 of block kt into a stage
+    const uint32_t dst = lds0 + stage * Cfg::kStage + wave * 1024;
+    if (j < Cfg::kLoadsA / 2) {
+      lds_load_pair<NW * 1024>(dst + 2 * j * NW * 1024, base_a + kt * kQuantBlock, off_a[2 * j], off_a[2 * j + 1]);
+    } else {
+      const int k = j - Cfg::kLoadsA / 2;
+      const uint8_t *b = base_w + kt * kQuantBlock;
+      if constexpr (GATED && NW == 4) {   // (of four waves, every second load is of up rows)
+        lds_load_one(dst + (Cfg::kLoadsA + 2 * k) * NW * 1024, b, off_w[2 * k]);
+        lds_load_one(dst + (Cfg::kLoadsA + 2 * k + 1) * NW * 1024, b + N * w.code_stride, off_w[2 * k + 1]);
+      } else {
+        lds_load_pair<NW * 1024>(dst + (Cfg::kLoadsA + 2 * k) * NW * 1024, b, off_w[2 * k], off_w[2 * k + 1]);
+      }
+    }
+  };
+  constexpr int PAIRS = (Cfg::kLoadsA + Cfg::kLoadsW) / 2;
+#pragma unroll
+  for (int j = 0; j < PAIRS; ++j) request(0, 0, j);
+#pragma unroll
+  for (int j = 0; j < PAIRS; ++j) request(1, min(1, nk - 1), j);
+
+  // ---- scales.  Rows: four blocks' bytes at a time, those of the lane's row in each sub-tile.  Weights: lane l holds block 64 i + l's.
+  const uint8_t *scale_a[TA];
+  uint32_t sa[TA], sa_next[TA];
+#pragma unroll
+  for (int i = 0; i < TA; ++i) {
+    scale_a[i] = a.scale + min(m0 + wi * (BM / Cfg::WM) + i * 32 + (lane & 31), M - 1) * a.scale_stride;
+    sa[i] = *reinterpret_cast<const uint32_t *>(scale_a[i]);
+    sa_next[i] = 0;
+  }
+  auto weight_scales = [&](int64_t row, int kt) -> uint32_t {   // of blocks kt + lane
+    const int64_t i = row / kQuantBlock * w.scale_stride + min(kt + lane, nk - 1);
+    return FLOATS ? static_cast<const uint32_t *>(w.scale)[i] : static_cast<const uint8_t *>(w.scale)[i];
+  };
+  // (a wave's weight rows lie in one block, or in one of the gate and one of the up projection)
+  const int64_t wrow = GATED ? n0 : min(n0 + wj * (BN / Cfg::WN), N - 1);
+  uint32_t ws[GATED ? 2 : 1];
+  ws[0] = weight_scales(wrow, 0);
+  if constexpr (GATED) ws[1] = weight_scales(wrow + N, 0);
+
+  // (block: the sums of the block at hand, where its scale is a float)
+  floatx16 acc[TW][TA], block[FLOATS ? TW : 1][FLOATS ? TA : 1];
+  const floatx16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < TW; ++i)
+#pragma unroll
+    for (int j = 0; j < TA; ++j) {
+      acc[i][j] = zero;
+      if constexpr (FLOATS) block[i][j] = zero;
+    }
+  float factor[2] = {0.f, 0.f};   // of the block before (FLOATS)
+  auto add_block = [&](int i, int j) {
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[i][j][v] = __builtin_fmaf(block[i][j][v], factor[GATED ? i & 1 : 0], acc[i][j][v]);
+  };
+
+  // ---- fragments: row lane % 32 of a sub-tile, of its 64 bytes of a half block the 32 of lane / 32
+  const int fr = lane & 31, sw = (fr >> 1) & 7, kg = lane >> 5;
+  int off_f[4];
+#pragma unroll
+  for (int p = 0; p < 4; ++p) off_f[p] = fr * kQuantBlock + (((p >> 1) * 4 + kg * 2 + (p & 1)) ^ sw) * 16;
+  const int row_a = wi * (BM / Cfg::WM) * kQuantBlock, row_w = (BM + wj * (BN / Cfg::WN)) * kQuantBlock;
+  i32x8 fa[2][TA], fw[2][TW];
+  auto fragment = [&](const unsigned char *p, int half) {
+    const i32x4 lo = *reinterpret_cast<const i32x4 *>(p + off_f[2 * half]), hi = *reinterpret_cast<const i32x4 *>(p + off_f[2 * half + 1]);
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  auto read = [&](int buf, int stage, int half, int n) {   // fragment n of a half block: weights, then rows
+    const unsigned char *p = smem_raw + stage * Cfg::kStage;
+    if (n < TW) fw[buf][n] = fragment(p + row_w + n * 32 * kQuantBlock, half);
+    else fa[buf][n - TW] = fragment(p + row_a + (n - TW) * 32 * kQuantBlock, half);
+  };
+  uint32_t ws_now[2] = {0, 0};
+  // The products of a half block, with what else the step has to do dealt out between them: FRAGS reads of the next half block, LOADS requests
+  constexpr int PRODUCTS = TA * TW, FRAGS = TA + TW;
+  auto step = [&](int buf, auto &&other, int others) {
+    Fragment16 cw[EXACT ? TW : 1], ca;
+    if constexpr (EXACT) {
+#pragma unroll
+      for (int i = 0; i < TW; ++i) cw[i] = widen(fw[buf][i], FLOATS ? 1.f : two_to_byte(ws_now[GATED ? i & 1 : 0]));
+    }
+#pragma unroll
+    for (int n = 0; n < PRODUCTS; ++n) {
+      const int j = n / TW, i = n % TW;
+      if constexpr (FLOATS) {
+        if (buf == 0) add_block(i, j), block[i][j] = zero;
+      }
+      floatx16 &sum = FLOATS ? block[FLOATS ? i : 0][FLOATS ? j : 0] : acc[i][j];
+      if constexpr (EXACT) {
+        if (i == 0) ca = widen(fa[buf][j], two_to_byte(sa[j] & 255));
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cw[i].v[k], ca.v[k], sum, 0, 0, 0);
+      } else {
+        sum = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fw[buf][i], fa[buf][j], sum, 0, 0, 0, FLOATS ? 127 : ws_now[GATED ? i & 1 : 0], 0, sa[j]);
+      }
+      for (int k = n * others / PRODUCTS; k < (n + 1) * others / PRODUCTS; ++k) other(k);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  quant_wait();   // (both stages; the first is all that is needed)
+  __builtin_amdgcn_s_barrier();
+#pragma unroll
+  for (int n = 0; n < FRAGS; ++n) read(0, 0, 0, n);
+  for (int kt = 0; kt < nk; ++kt) {
+    const int stage = kt & 1;
+    if constexpr (FLOATS) factor[0] = __uint_as_float(ws_now[0]), factor[1] = __uint_as_float(ws_now[1]);
+    ws_now[0] = __builtin_amdgcn_readlane(ws[0], kt & 63);
+    if constexpr (GATED) ws_now[1] = __builtin_amdgcn_readlane(ws[1], kt & 63);
+    __builtin_amdgcn_sched_barrier(0);
+    step(0, [&](int k) { read(1, stage, 1, k); }, FRAGS);
+    quant_wait();
+    __builtin_amdgcn_s_barrier();   // the stage has been read by all, the next one is complete
+    __builtin_amdgcn_sched_barrier(0);
+    // (behind the last blocks the loads and reads are of the last block again: nothing looks at them)
+    const int ahead = min(kt + 2, nk - 1);
+    step(1, [&](int k) { if (k < FRAGS) read(0, stage ^ 1, 0, k); else request(stage, ahead, k - FRAGS); }, FRAGS + PAIRS);
+#pragma unroll
+    for (int i = 0; i < TA; ++i) sa[i] = (kt & 3) == 3 ? sa_next[i] : sa[i] >> 8;
+    if ((kt & 3) == 1 && kt + 3 < nk) {
+#pragma unroll
+      for (int i = 0; i < TA; ++i) sa_next[i] = *reinterpret_cast<const uint32_t *>(scale_a[i] + kt + 3);
+    }
+    if ((kt & 63) == 63 && kt + 1 < nk) {
+      ws[0] = weight_scales(wrow, kt + 1);
+      if constexpr (GATED) ws[1] = weight_scales(wrow + N, kt + 1);
+    }
+  }
+  if constexpr (FLOATS) {
+    factor[0] = __uint_as_float(ws_now[0]), factor[1] = __uint_as_float(ws_now[1]);
+#pragma unroll
+    for (int i = 0; i < TW; ++i)
+#pragma unroll
+      for (int j = 0; j < TA; ++j) add_block(i, j);
+  }
+  quant_wait();   // (of the loads that nothing looks at too: results go through the same memory)
+
+  // ---- results: lane l has row l % 32 of a sub-tile and, of its 32 weight rows, 8 (v / 4) + 4 (l / 32) + v % 4
+  __syncthreads();
+  if constexpr (!GATED) {
+    // through LDS, so that adjacent lanes store adjacent pieces of a row
+    constexpr int W = TW * 32, ROW = W * sizeof(T) + 16, LPR = W * sizeof(T) / 16, PER = 16 / sizeof(T);
+    unsigned char *mine = smem_raw + wave * 32 * ROW;
+    static_assert(NW * 32 * ROW <= Cfg::kLds, "results are staged in the operands' place");
+    const int c0 = n0 + wj * W;
+#pragma unroll
+    for (int j = 0; j < TA; ++j) {
+#pragma unroll
+      for (int i = 0; i < TW; ++i)
+#pragma unroll
+        for (int v = 0; v < 16; v += 4) {
+          T *p = reinterpret_cast<T *>(mine + fr * ROW) + i * 32 + 2 * v + 4 * kg;
+          if constexpr (sizeof(T) == 4) {
+            *reinterpret_cast<floatx4 *>(p) = floatx4{acc[i][j][v], acc[i][j][v + 1], acc[i][j][v + 2], acc[i][j][v + 3]};
+          } else {
+            const floatx4 f = {acc[i][j][v], acc[i][j][v + 1], acc[i][j][v + 2], acc[i][j][v + 3]};
+            *reinterpret_cast<bf16x4 *>(p) = __builtin_convertvector(f, bf16x4);
+          }
+        }
+      const int r0 = m0 + wi * (BM / Cfg::WM) + j * 32;
+#pragma unroll
+      for (int s = 0; s < 32 * LPR / 64; ++s) {
+        const int r = s * (64 / LPR) + lane / LPR, c = lane % LPR * PER;
+        const u32x4 x = *reinterpret_cast<const u32x4 *>(mine + r * ROW + lane % LPR * 16);
+        if (r0 + r < M && c0 + c < N) {
+          T *p = out + (r0 + r) * out_stride + c0 + c;
+          if (c0 + c + PER <= N) {
+            typedef uint32_t u4 __attribute__((ext_vector_type(4), aligned(2)));
+            *reinterpret_cast<u4 *>(p) = x;
+          } else {
+            const T *y = reinterpret_cast<const T *>(mine + r * ROW + lane % LPR * 16);
+            for (int k = 0; c0 + c + k < N; ++k) p[k] = y[k];
+          }
+        }
+      }
+    }
+  } else {
+    constexpr int P = TW / 2, ROW = kQuantBlock + 16;
+    float *top = reinterpret_cast<float *>(smem_raw + BM * ROW);   // [BM][WN]
+    static_assert(BM * ROW + BM * Cfg::WN * 4 <= Cfg::kLds, "results are staged in the operands' place");
+#pragma unroll
+    for (int j = 0; j < TA; ++j) {
+      float m = 0.f;
+#pragma unroll
+      for (int i = 0; i < P; ++i)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          acc[2 * i][j][v] = swiglu(acc[2 * i][j][v], acc[2 * i + 1][j][v]);
+          m = fmaxf(m, finite_mag(acc[2 * i][j][v]));
+        }
+      m = half_max(m);
+      if (lane < 32) top[(wi * (BM / Cfg::WM) + j * 32 + fr) * Cfg::WN + wj] = m;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < TA; ++j) {
+      const int r = wi * (BM / Cfg::WM) + j * 32 + fr;
+      float m = 0.f;
+#pragma unroll
+      for (int i = 0; i < Cfg::WN; ++i) m = fmaxf(m, top[r * Cfg::WN + i]);
+      const int e = scale_exp(m);
+      const float inv = exp2_int(-e);
+#pragma unroll
+      for (int i = 0; i < P; ++i)
+#pragma unroll
+        for (int v = 0; v < 16; v += 4)
+          *reinterpret_cast<uint32_t *>(smem_raw + r * ROW + (wj * P + i) * 32 + 2 * v + 4 * kg) =
+              quant4(code_arg(acc[2 * i][j][v], inv), code_arg(acc[2 * i][j][v + 1], inv), code_arg(acc[2 * i][j][v + 2], inv), code_arg(acc[2 * i][j][v + 3], inv));
+      if (wj == 0 && kg == 0 && m0 + r < M) q.scale[(m0 + r) * q.scale_stride + tn] = static_cast<uint8_t>(e + 127);
+    }
+    __syncthreads();
+    for (int r = t >> 3; r < BM && m0 + r < M; r += 8 * NW)
+      *reinterpret_cast<u32x4 *>(q.codes + (m0 + r) * q.code_stride + n0 + (t & 7) * 16) = *reinterpret_cast<const u32x4 *>(smem_raw + r * ROW + (t & 7) * 16);
   }
 }
 

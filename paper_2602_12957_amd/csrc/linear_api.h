@@ -73,15 +73,16 @@ int hsd_quant_linear(void *stream, int32_t n_rows, int32_t n_out, int32_t dim, c
   if (n_rows == 0) return HSD_OK;
   if (out == nullptr || out_stride < n_out) return HSD_EINVAL;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  for (int32_t m = 0; m < n_rows; m += 65535) {
-    const dim3 grid((n_out + 255) / 256, std::min(n_rows - m, 65535));
-    if (dtype == HSD_BF16)
-      hipLaunchKernelGGL((k_quant_linear<bf16>), grid, dim3(256), 0, st, rows_quant(rows), weight_quant(w), m, n_out, quant_blocks(dim), static_cast<bf16 *>(out), out_stride);
-    else
-      hipLaunchKernelGGL((k_quant_linear<float>), grid, dim3(256), 0, st, rows_quant(rows), weight_quant(w), m, n_out, quant_blocks(dim), static_cast<float *>(out), out_stride);
-    HSD_LAUNCH_CHECK();
+  const RowsQuant a = rows_quant(rows);
+  const WeightQuant b = weight_quant(w);
+  const int nk = quant_blocks(dim);
+  const bool floats = w->scale_type == HSD_SCALE_FP32;
+  if (dtype == HSD_BF16) {
+    bf16 *y = static_cast<bf16 *>(out);
+    return floats ? run_linear<true, false>(st, a, b, n_rows, n_out, nk, y, out_stride) : run_linear<false, false>(st, a, b, n_rows, n_out, nk, y, out_stride);
   }
-  return HSD_OK;
+  float *y = static_cast<float *>(out);
+  return floats ? run_linear<true, true>(st, a, b, n_rows, n_out, nk, y, out_stride) : run_linear<false, true>(st, a, b, n_rows, n_out, nk, y, out_stride);
 }
 
 int hsd_quant_gated(void *stream, int32_t n_rows, int32_t d_ffn, int32_t dim, const hsd_rows_quant *rows, const hsd_weight_quant *w,
@@ -95,12 +96,9 @@ int hsd_quant_gated(void *stream, int32_t n_rows, int32_t d_ffn, int32_t dim, co
   if (rc != HSD_OK) return rc;
   if (n_rows == 0) return HSD_OK;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  for (int32_t m = 0; m < n_rows; m += 65535) {
-    hipLaunchKernelGGL(k_quant_gated, dim3(d_ffn / kQuantBlock, std::min(n_rows - m, 65535)), dim3(128), 0, st, rows_quant(rows), weight_quant(w), m, d_ffn,
-                       quant_blocks(dim), rows_quant(out));
-    HSD_LAUNCH_CHECK();
-  }
-  return HSD_OK;
+  const int nk = quant_blocks(dim);
+  if (w->scale_type == HSD_SCALE_FP32) return run_gated<true>(st, rows_quant(rows), weight_quant(w), n_rows, d_ffn, nk, rows_quant(out));
+  return run_gated<false>(st, rows_quant(rows), weight_quant(w), n_rows, d_ffn, nk, rows_quant(out));
 }
 
 }  // extern "C"

@@ -4,6 +4,7 @@
 namespace {
 
 constexpr int kMostQuantRows = (1 << 24) - 1, kMostQuantDim = 1 << 20;   // a launch has fewer than 2^32 threads, 256 of them a row
+constexpr int64_t kMostCodeStride = 1 << 23;                             // offsets within a tile of 256 rows take 31 bits
 
 int quant_blocks(int32_t dim) { return (dim + kQuantBlock - 1) / kQuantBlock; }
 
@@ -14,6 +15,7 @@ int check_rows_quant(const hsd_rows_quant *q, int32_t n_rows, int32_t dim) {
   if (q == nullptr || q->codes == nullptr || q->scale == nullptr) return HSD_EINVAL;
   if ((reinterpret_cast<uintptr_t>(q->codes) & 15) != 0 || (reinterpret_cast<uintptr_t>(q->scale) & 3) != 0) return HSD_EINVAL;
   if ((q->code_stride & 15) != 0 || (q->scale_stride & 3) != 0) return HSD_EINVAL;
+  if (q->code_stride > kMostCodeStride) return HSD_ERANGE;
   const int64_t blocks = quant_blocks(dim);
   return q->code_stride < blocks * kQuantBlock || q->scale_stride < (blocks + 3) / 4 * 4 ? HSD_EINVAL : HSD_OK;
 }
@@ -23,6 +25,7 @@ int check_weight_quant(const hsd_weight_quant *w, int32_t n_out, int32_t dim) {
   if (n_out > kMostQuantRows || dim > kMostQuantDim) return HSD_ERANGE;
   if (w->codes == nullptr || w->scale == nullptr || (w->scale_type != HSD_SCALE_FP32 && w->scale_type != HSD_SCALE_POW2)) return HSD_EINVAL;
   if ((reinterpret_cast<uintptr_t>(w->codes) & 15) != 0 || (w->code_stride & 15) != 0) return HSD_EINVAL;
+  if (w->code_stride > kMostCodeStride) return HSD_ERANGE;
   if (w->scale_type == HSD_SCALE_FP32 && (reinterpret_cast<uintptr_t>(w->scale) & 3) != 0) return HSD_EINVAL;
   const int64_t blocks = quant_blocks(dim);
   return w->code_stride < blocks * kQuantBlock || w->scale_stride < blocks ? HSD_EINVAL : HSD_OK;
@@ -30,7 +33,7 @@ int check_weight_quant(const hsd_weight_quant *w, int32_t n_out, int32_t dim) {
 
 RowsQuant rows_quant(const hsd_rows_quant *q) { return RowsQuant{static_cast<uint8_t *>(q->codes), q->scale, q->code_stride, q->scale_stride}; }
 WeightQuant weight_quant(const hsd_weight_quant *w) {
-  return WeightQuant{static_cast<const uint8_t *>(w->codes), w->scale, w->code_stride, w->scale_stride, w->scale_type == HSD_SCALE_POW2};
+  return WeightQuant{static_cast<const uint8_t *>(w->codes), w->scale, w->code_stride, w->scale_stride};
 }
 
 template <typename TX, typename TR>
@@ -44,6 +47,62 @@ int launch_norm(hipStream_t st, const NormRows &a, const void *x, const void *re
 int run_norm(hipStream_t st, const NormRows &a, int32_t x_dtype, const void *x, int32_t res_dtype, const void *res, void *sum) {
   if (x_dtype == HSD_BF16) return res_dtype == HSD_BF16 ? launch_norm<bf16, bf16>(st, a, x, res, sum) : launch_norm<bf16, float>(st, a, x, res, sum);
   return res_dtype == HSD_BF16 ? launch_norm<float, bf16>(st, a, x, res, sum) : launch_norm<float, float>(st, a, x, res, sum);
+}
+
+// Products of many rows
+template <typename Cfg, bool GATED, bool FLOATS, bool EXACT, typename T>
+int launch_product(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, int N, int nk, T *out, int64_t out_stride, const RowsQuant &q) {
+  auto kern = k_gemm_quant<Cfg, GATED, FLOATS, EXACT, T>;
+  static const hipError_t attr_rc = hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, Cfg::kLds);
+  if (attr_rc != hipSuccess) return HSD_EHIP;
+  constexpr int COLS = GATED ? Cfg::BN / 2 : Cfg::BN;
+  const int64_t tiles = static_cast<int64_t>((M + Cfg::BM - 1) / Cfg::BM) * ((N + COLS - 1) / COLS);
+  if (tiles > INT32_MAX / (64 * Cfg::NW)) return HSD_ERANGE;
+  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(tiles)), dim3(64 * Cfg::NW), Cfg::kLds, st, a, w, M, N, nk, out, out_stride, q);
+  HSD_LAUNCH_CHECK();
+  return HSD_OK;
+}
+
+int64_t quant_tiles(int M, int N, int bm, int bn) { return static_cast<int64_t>((M + bm - 1) / bm) * ((N + bn - 1) / bn); }
+
+template <bool FLOATS, bool EXACT, typename T>
+int run_linear(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, int N, int nk, T *out, int64_t out_stride) {
+  const RowsQuant none{};
+#ifdef HSD_QUANT_TRY
+  const char *e = getenv("HSD_QCFG");
+  const int cfg = e ? atoi(e) : -1;
+  if constexpr (!FLOATS && !EXACT) { if (cfg == 0) return launch_product<ProductTile<256, 256, 2, 2>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none); }
+  if constexpr (!EXACT) { if (cfg == 1) return launch_product<ProductTile<256, 128, 4, 2>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none); }
+  if constexpr (!EXACT) { if (cfg == 4) return launch_product<ProductTile<128, 256, 2, 4>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none); }
+  if constexpr (!(FLOATS && EXACT)) { if (cfg == 2) return launch_product<ProductTile<128, 128, 2, 2>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none); }
+  if (cfg == 3) return launch_product<ProductTile<64, 128, 2, 2>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
+  if (cfg == 5) return launch_product<ProductTile<64, 64, 2, 2>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
+#endif
+  if constexpr (!FLOATS && !EXACT) {
+    if (quant_tiles(M, N, 256, 256) >= 192) return launch_product<ProductTile<256, 256, 2, 2>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
+  }
+  if constexpr (!(FLOATS && EXACT)) {
+    if (quant_tiles(M, N, 128, 128) >= 256) return launch_product<ProductTile<128, 128, 2, 2>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
+  }
+  if (quant_tiles(M, N, 64, 128) >= 192) return launch_product<ProductTile<64, 128, 2, 2>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
+  return launch_product<ProductTile<64, 64, 2, 2>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
+}
+
+template <bool FLOATS>
+int run_gated(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, int N, int nk, const RowsQuant &q) {
+  bf16 *none = nullptr;
+#ifdef HSD_QUANT_TRY
+  const char *e = getenv("HSD_QCFG");
+  const int cfg = e ? atoi(e) : -1;
+  if constexpr (!FLOATS) { if (cfg == 0) return launch_product<ProductTile<256, 256, 2, 2>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q); }
+  if (cfg == 1 || cfg == 4) return launch_product<ProductTile<128, 256, 2, 4>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
+  if (cfg == 3) return launch_product<ProductTile<64, 256, 1, 4>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
+#endif
+  if constexpr (!FLOATS) {
+    if (quant_tiles(M, N, 256, 128) >= 192) return launch_product<ProductTile<256, 256, 2, 2>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
+  }
+  if (quant_tiles(M, N, 128, 128) >= 192) return launch_product<ProductTile<128, 256, 2, 4>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
+  return launch_product<ProductTile<64, 256, 1, 4>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
 }
 
 }  // namespace
