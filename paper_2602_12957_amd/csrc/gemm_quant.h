@@ -16,26 +16,10 @@ struct WeightQuant {
   int64_t code_stride, scale_stride;
 };
 
-// Two LDS-direct loads of 1 KB: lane l's 16 bytes at base + off0 (off1) go to dst + 16 l (dst + STEP + 16 l).  In asm: the
-// compiler would otherwise wait for every load in flight before each LDS read.  No register is written; the reads wait by
-// quant_wait and a barrier.  m0 is put back as it was found.
-template <int STEP>
-__device__ __forceinline__ void lds_load_pair(uint32_t dst, const uint8_t *base, uint32_t off0, uint32_t off1) {
-  uint32_t m0;
-  asm volatile(
-      "s_mov_b32 %0, m0\n\t"
-      "s_mov_b32 m0, %1\n\t"
-      "s_nop 0\n\t"
-      "global_load_lds_dwordx4 %2, %4\n\t"
-      "s_add_u32 m0, m0, %5\n\t"
-      "s_nop 0\n\t"
-      "global_load_lds_dwordx4 %3, %4\n\t"
-      "s_mov_b32 m0, %0"
-      : "=&s"(m0)
-      : "s"(dst), "v"(off0), "v"(off1), "s"(base), "i"(STEP)
-      : "memory", "scc");
-}
-__device__ __forceinline__ void lds_load_one(uint32_t dst, const uint8_t *base, uint32_t off) {
+// An LDS-direct load of 1 KB: lane l's 16 bytes at base + off go to dst + 16 l; and one of 256 bytes, 4 a lane.  In asm: the compiler would
+// otherwise wait for every load in flight before each LDS read.  No register is written; the reads wait by quant_wait and a
+// barrier.  m0 is put back as it was found.
+__device__ __forceinline__ void lds_load_1k(uint32_t dst, const uint8_t *base, uint32_t off) {
   uint32_t m0;
   asm volatile(
       "s_mov_b32 %0, m0\n\t"
@@ -47,22 +31,43 @@ __device__ __forceinline__ void lds_load_one(uint32_t dst, const uint8_t *base, 
       : "s"(dst), "v"(off), "s"(base)
       : "memory");
 }
-// All of this wave's loads have landed, and its LDS reads are done
+__device__ __forceinline__ void lds_load_256(uint32_t dst, const uint8_t *base, uint64_t off) {
+  uint32_t m0;
+  const uint64_t p = reinterpret_cast<uint64_t>(base) + off;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %1\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dword %2, off\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(m0)
+      : "s"(dst), "v"(p)
+      : "memory");
+}
+// All but the N newest of this wave's loads have landed, and its LDS reads are done
+template <int N>
 __device__ __forceinline__ void quant_wait() {
+  static_assert(N < 64, "what the counter holds");
   asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0);
+  __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (0 << 8) | ((N >> 4) << 14));
   asm volatile("" ::: "memory");
 }
 
-template <int BM_, int BN_, int WM_, int WN_>
+// A tile of BM rows by BN weight rows, WM by WN waves; operands in a ring of S slices of 64 Q columns.
+template <int BM_, int BN_, int WM_, int WN_, int Q_, int S_>
 struct ProductTile {
-  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NW = WM_ * WN_;
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NW = WM_ * WN_, Q = Q_, S = S_;
   static constexpr int TA = BM / WM / 32, TW = BN / WN / 32;      // 32x32 sub-tiles of a wave: rows, weight rows
-  static constexpr int kStage = (BM + BN) * kQuantBlock;          // a block of 128 columns of the tile's rows and weight rows
-  static constexpr int kLoadsA = BM / 8 / NW, kLoadsW = BN / 8 / NW;   // 1 KB loads of a wave and stage
-  static constexpr int kLds = 2 * kStage;
+  static constexpr int kRow = 64 * Q;                             // bytes of a row in a slice
+  static constexpr int kScales = NW * 256;                        // the rows' bytes of four blocks, behind the codes
+  static constexpr int kSlice = (BM + BN) * kRow + kScales;
+  static constexpr int kPerLoad = 1024 / kRow;                    // rows of a 1 KB load
+  static constexpr int kLoadsA = BM / kPerLoad / NW, kLoadsW = BN / kPerLoad / NW, kLoads = kLoadsA + kLoadsW;   // of a wave and slice
+  static constexpr int kLds = S * kSlice;
   static constexpr int kWaves = BM * BN / NW > 128 * 64 ? 1 : 2;  // of a SIMD
-  static_assert(kLoadsA % 2 == 0 && kLoadsW % 2 == 0 && BM / 8 % NW == 0 && BN / 8 % NW == 0, "loads go in pairs of one operand");
+  static_assert(Q == 1 || Q == 2, "a slice is a block of 128 columns or half of one");
+  static_assert(BM / kPerLoad % NW == 0 && BN / kPerLoad % NW == 0 && BM <= 64 * NW, "loads divide evenly");
+  static_assert(S >= 2 && (S - 1) * (kLoads + 1) < 64 && kLds <= 160 * 1024, "slices in flight");
 };
 
 // Tile of a workgroup: XCD x (workgroup id mod 8) takes a contiguous run of an order that goes through bands of eight tiles of rows,
@@ -111,64 +116,61 @@ __global__ void __launch_bounds__(64 * Cfg::NW, Cfg::kWaves) k_gemm_quant(const 
   quant_tile_of(blockIdx.x, (M + BM - 1) / BM, (N + COLS - 1) / COLS, tm, tn);
   const int m0 = tm * BM, n0 = tn * COLS;
 
-  // ---- loads.  Load i of a stage covers tile rows 8 i .. 8 i + 7 (rows, then weight rows); lane l fetches, for row 8 i + l / 8, the 16-byte
-  // piece that belongs at position l % 8: piece p of row r lies at p ^ ((r >> 1) & 7), so that reads of 16 rows cover all banks.
+  // ---- loads.  Load i of a slice covers RPL tile rows from RPL i on (rows, then weight rows); lane l fetches, for row RPL i + l / LPW, the
+  // 16-byte piece that belongs at position l % LPW: a row's pieces lie XORed by the row, so that reads of 16 rows cover all banks.
   // Rows behind the last one are that one again (their products are never stored).
+  constexpr int Q = Cfg::Q, S = Cfg::S, RPL = Cfg::kPerLoad, LPW = Cfg::kRow / 16, SHIFT = Q == 2 ? 1 : 2;
   const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char *)smem_raw));
-  const uint8_t *base_a = a.codes + m0 * a.code_stride, *base_w = w.codes + n0 * w.code_stride;
-  if (GATED && NW == 8 && (wave & 4)) base_w += N * w.code_stride;   // (of eight waves, 4 to 7 fetch up rows)
+  const uint8_t *base_a = a.codes + m0 * a.code_stride, *base_w = w.codes + n0 * w.code_stride, *base_u = GATED ? base_w + N * w.code_stride : base_w;
   uint32_t off_a[Cfg::kLoadsA], off_w[Cfg::kLoadsW];
 #pragma unroll
   for (int j = 0; j < Cfg::kLoadsA; ++j) {
-    const int r = (j * NW + wave) * 8 + (lane >> 3);
-    off_a[j] = min(r, M - 1 - m0) * static_cast<uint32_t>(a.code_stride) + ((lane & 7) ^ ((r >> 1) & 7)) * 16;
+    const int r = (j * NW + wave) * RPL + lane / LPW;
+    off_a[j] = min(r, M - 1 - m0) * static_cast<uint32_t>(a.code_stride) + ((lane ^ (r >> SHIFT)) % LPW) * 16;
   }
 #pragma unroll
   for (int j = 0; j < Cfg::kLoadsW; ++j) {
-    const int r = (j * NW + wave) * 8 + (lane >> 3);
+    const int r = (j * NW + wave) * RPL + lane / LPW;
     // gate and up alternate by 32 rows: weight row 64 g + 32 u + x of the tile is row n0 + 32 g + x of the gate or of the up projection
     const int row = GATED ? (r >> 6) * 32 + (r & 31) : min(r, N - 1 - n0);
-    off_w[j] = row * static_cast<uint32_t>(w.code_stride) + ((lane & 7) ^ ((r >> 1) & 7)) * 16;
+    off_w[j] = row * static_cast<uint32_t>(w.code_stride) + ((lane ^ (r >> SHIFT)) % LPW) * 16;
   }
-  auto request = [&](int stage, int kt, int j) {   // loads 2 j and 2 j + 1 of block kt into a stage
-    const uint32_t dst = lds0 + stage * Cfg::kStage + wave * 1024;
-    if (j < Cfg::kLoadsA / 2) {
-      lds_load_pair<NW * 1024>(dst + 2 * j * NW * 1024, base_a + kt * kQuantBlock, off_a[2 * j], off_a[2 * j + 1]);
+  const uint64_t off_s = min(m0 + t, M - 1) * a.scale_stride;   // (t: the row; of those behind the tile's nothing is read)
+  const int slices = nk * (2 / Q);
+  constexpr int LOADS = Cfg::kLoads + 1;
+  auto request = [&](int slice, uint32_t place, int j) {   // load j of a slice into its place
+    const uint32_t dst = place + wave * 1024;
+    const int col = slice * Cfg::kRow;
+    if (j < Cfg::kLoadsA) {
+      lds_load_1k(dst + j * NW * 1024, base_a + col, off_a[j]);
+    } else if (j < Cfg::kLoads) {
+      const int k = j - Cfg::kLoadsA;
+      const bool up = GATED && (((k * NW + wave) * RPL) >> 5 & 1);
+      lds_load_1k(dst + j * NW * 1024, (up ? base_u : base_w) + col, off_w[k]);
     } else {
-      const int k = j - Cfg::kLoadsA / 2;
-      const uint8_t *b = base_w + kt * kQuantBlock;
-      if constexpr (GATED && NW == 4) {   // (of four waves, every second load is of up rows)
-        lds_load_one(dst + (Cfg::kLoadsA + 2 * k) * NW * 1024, b, off_w[2 * k]);
-        lds_load_one(dst + (Cfg::kLoadsA + 2 * k + 1) * NW * 1024, b + N * w.code_stride, off_w[2 * k + 1]);
-      } else {
-        lds_load_pair<NW * 1024>(dst + (Cfg::kLoadsA + 2 * k) * NW * 1024, b, off_w[2 * k], off_w[2 * k + 1]);
-      }
+      lds_load_256(place + (BM + BN) * Cfg::kRow + wave * 256, a.scale, off_s + (slice / (2 / Q) & ~3));
     }
   };
-  constexpr int PAIRS = (Cfg::kLoadsA + Cfg::kLoadsW) / 2;
 #pragma unroll
-  for (int j = 0; j < PAIRS; ++j) request(0, 0, j);
+  for (int s = 0; s < S; ++s)
 #pragma unroll
-  for (int j = 0; j < PAIRS; ++j) request(1, min(1, nk - 1), j);
+    for (int j = 0; j < LOADS; ++j) request(min(s, slices - 1), lds0 + s * Cfg::kSlice, j);
 
-  // ---- scales.  Rows: four blocks' bytes at a time, those of the lane's row in each sub-tile.  Weights: lane l holds block 64 i + l's.
-  const uint8_t *scale_a[TA];
+  // ---- scales.  A wave's weight rows lie in one block of 128, or in one of the gate and one of the up projection: their scales come
+  // through the scalar unit, a block ahead (vector loads would be waited for with all the slices behind them).
   uint32_t sa[TA], sa_next[TA];
-#pragma unroll
-  for (int i = 0; i < TA; ++i) {
-    scale_a[i] = a.scale + min(m0 + wi * (BM / Cfg::WM) + i * 32 + (lane & 31), M - 1) * a.scale_stride;
-    sa[i] = *reinterpret_cast<const uint32_t *>(scale_a[i]);
-    sa_next[i] = 0;
-  }
-  auto weight_scales = [&](int64_t row, int kt) -> uint32_t {   // of blocks kt + lane
-    const int64_t i = row / kQuantBlock * w.scale_stride + min(kt + lane, nk - 1);
-    return FLOATS ? static_cast<const uint32_t *>(w.scale)[i] : static_cast<const uint8_t *>(w.scale)[i];
-  };
-  // (a wave's weight rows lie in one block, or in one of the gate and one of the up projection)
   const int64_t wrow = GATED ? n0 : min(n0 + wj * (BN / Cfg::WN), N - 1);
-  uint32_t ws[GATED ? 2 : 1];
-  ws[0] = weight_scales(wrow, 0);
-  if constexpr (GATED) ws[1] = weight_scales(wrow + N, 0);
+  const int64_t ws_at[2] = {wrow / kQuantBlock * w.scale_stride, (wrow + N) / kQuantBlock * w.scale_stride};
+  uint32_t ws_now[2] = {0, 0}, ws_next[2] = {0, 0};
+  auto weight_scales = [&](int kt) {
+#pragma unroll
+    for (int i = 0; i < (GATED ? 2 : 1); ++i) {
+      typedef const __attribute__((address_space(4))) uint32_t *Const;
+      const uint64_t p = reinterpret_cast<uint64_t>(w.scale) + (FLOATS ? 4 : 1) * (ws_at[i] + kt);
+      const uint32_t x = *reinterpret_cast<Const>(p & ~uint64_t{3});   // (a byte's word)
+      ws_next[i] = FLOATS ? x : x >> (8 * (p & 3)) & 255;
+    }
+  };
 
   // (block: the sums of the block at hand, where its scale is a float)
   floatx16 acc[TW][TA], block[FLOATS ? TW : 1][FLOATS ? TA : 1];
@@ -187,22 +189,25 @@ __global__ void __launch_bounds__(64 * Cfg::NW, Cfg::kWaves) k_gemm_quant(const 
   };
 
   // ---- fragments: row lane % 32 of a sub-tile, of its 64 bytes of a half block the 32 of lane / 32
-  const int fr = lane & 31, sw = (fr >> 1) & 7, kg = lane >> 5;
-  int off_f[4];
+  const int fr = lane & 31, kg = lane >> 5;
+  int off_f[2 * Q];
 #pragma unroll
-  for (int p = 0; p < 4; ++p) off_f[p] = fr * kQuantBlock + (((p >> 1) * 4 + kg * 2 + (p & 1)) ^ sw) * 16;
-  const int row_a = wi * (BM / Cfg::WM) * kQuantBlock, row_w = (BM + wj * (BN / Cfg::WN)) * kQuantBlock;
+  for (int p = 0; p < 2 * Q; ++p) off_f[p] = fr * Cfg::kRow + (((p >> 1) * 4 + kg * 2 + (p & 1)) ^ ((fr >> SHIFT) % LPW)) * 16;
+  const int row_a = wi * (BM / Cfg::WM) * Cfg::kRow, row_w = (BM + wj * (BN / Cfg::WN)) * Cfg::kRow;
   i32x8 fa[2][TA], fw[2][TW];
   auto fragment = [&](const unsigned char *p, int half) {
     const i32x4 lo = *reinterpret_cast<const i32x4 *>(p + off_f[2 * half]), hi = *reinterpret_cast<const i32x4 *>(p + off_f[2 * half + 1]);
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   };
-  auto read = [&](int buf, int stage, int half, int n) {   // fragment n of a half block: weights, then rows
-    const unsigned char *p = smem_raw + stage * Cfg::kStage;
-    if (n < TW) fw[buf][n] = fragment(p + row_w + n * 32 * kQuantBlock, half);
-    else fa[buf][n - TW] = fragment(p + row_a + (n - TW) * 32 * kQuantBlock, half);
+  auto read = [&](int buf, const unsigned char *p, int half, int n) {   // fragment n of a half block: weights, then rows
+    if (n < TW) fw[buf][n] = fragment(p + row_w + n * 32 * Cfg::kRow, half);
+    else fa[buf][n - TW] = fragment(p + row_a + (n - TW) * 32 * Cfg::kRow, half);
   };
-  uint32_t ws_now[2] = {0, 0};
+  auto row_scales = [&](const unsigned char *p, int kt) {
+#pragma unroll
+    for (int i = 0; i < TA; ++i)
+      sa_next[i] = *reinterpret_cast<const uint32_t *>(p + (BM + BN) * Cfg::kRow + (wi * (BM / Cfg::WM) + i * 32 + fr) * 4) >> (8 * (kt & 3));
+  };
   // The products of a half block, with what else the step has to do dealt out between them: FRAGS reads of the next half block, LOADS requests
   constexpr int PRODUCTS = TA * TW, FRAGS = TA + TW;
   auto step = [&](int buf, auto &&other, int others) {
@@ -230,32 +235,49 @@ __global__ void __launch_bounds__(64 * Cfg::NW, Cfg::kWaves) k_gemm_quant(const 
     }
   };
 
-  quant_wait();   // (both stages; the first is all that is needed)
+  constexpr int LATER = (S - 2) * LOADS;   // loads of the slices that may still be in flight when the next one is needed
+  weight_scales(0);
+  quant_wait<LATER + LOADS>();
   __builtin_amdgcn_s_barrier();
 #pragma unroll
-  for (int n = 0; n < FRAGS; ++n) read(0, 0, 0, n);
+  for (int n = 0; n < FRAGS; ++n) read(0, smem_raw, 0, n);
+  row_scales(smem_raw, 0);
+  int at = 0;   // place of the slice at hand
+  // What precedes the last step of a slice: all waves have read it, and the next one is complete
+  auto turn = [&]() {
+    quant_wait<LATER>();
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+  };
   for (int kt = 0; kt < nk; ++kt) {
-    const int stage = kt & 1;
     if constexpr (FLOATS) factor[0] = __uint_as_float(ws_now[0]), factor[1] = __uint_as_float(ws_now[1]);
-    ws_now[0] = __builtin_amdgcn_readlane(ws[0], kt & 63);
-    if constexpr (GATED) ws_now[1] = __builtin_amdgcn_readlane(ws[1], kt & 63);
-    __builtin_amdgcn_sched_barrier(0);
-    step(0, [&](int k) { read(1, stage, 1, k); }, FRAGS);
-    quant_wait();
-    __builtin_amdgcn_s_barrier();   // the stage has been read by all, the next one is complete
-    __builtin_amdgcn_sched_barrier(0);
-    // (behind the last blocks the loads and reads are of the last block again: nothing looks at them)
-    const int ahead = min(kt + 2, nk - 1);
-    step(1, [&](int k) { if (k < FRAGS) read(0, stage ^ 1, 0, k); else request(stage, ahead, k - FRAGS); }, FRAGS + PAIRS);
+    ws_now[0] = ws_next[0], ws_now[1] = ws_next[1];
+    weight_scales(min(kt + 1, nk - 1));
 #pragma unroll
-    for (int i = 0; i < TA; ++i) sa[i] = (kt & 3) == 3 ? sa_next[i] : sa[i] >> 8;
-    if ((kt & 3) == 1 && kt + 3 < nk) {
+    for (int i = 0; i < TA; ++i) sa[i] = sa_next[i];
+    __builtin_amdgcn_sched_barrier(0);
+    // (behind the last slices the requests and reads are of the last one, or of an older one's place: nothing looks at them)
+    if constexpr (Q == 2) {
+      const unsigned char *here = smem_raw + at * Cfg::kSlice;
+      const uint32_t place = lds0 + at * Cfg::kSlice;
+      at = at + 1 == S ? 0 : at + 1;
+      const unsigned char *next = smem_raw + at * Cfg::kSlice;
+      step(0, [&](int k) { read(1, here, 1, k); }, FRAGS);
+      turn();
+      const int ahead = min(kt + S, slices - 1);
+      row_scales(next, kt + 1);
+      step(1, [&](int k) { if (k < FRAGS) read(0, next, 0, k); else request(ahead, place, k - FRAGS); }, FRAGS + LOADS);
+    } else {
 #pragma unroll
-      for (int i = 0; i < TA; ++i) sa_next[i] = *reinterpret_cast<const uint32_t *>(scale_a[i] + kt + 3);
-    }
-    if ((kt & 63) == 63 && kt + 1 < nk) {
-      ws[0] = weight_scales(wrow, kt + 1);
-      if constexpr (GATED) ws[1] = weight_scales(wrow + N, kt + 1);
+      for (int half = 0; half < 2; ++half) {
+        const uint32_t place = lds0 + at * Cfg::kSlice;
+        at = at + 1 == S ? 0 : at + 1;
+        const unsigned char *next = smem_raw + at * Cfg::kSlice;
+        turn();
+        const int ahead = min(2 * kt + half + S, slices - 1);
+        if (half == 1) row_scales(next, kt + 1);
+        step(half, [&](int k) { if (k < FRAGS) read(half ^ 1, next, 0, k); else request(ahead, place, k - FRAGS); }, FRAGS + LOADS);
+      }
     }
   }
   if constexpr (FLOATS) {
@@ -265,7 +287,7 @@ __global__ void __launch_bounds__(64 * Cfg::NW, Cfg::kWaves) k_gemm_quant(const 
 #pragma unroll
       for (int j = 0; j < TA; ++j) add_block(i, j);
   }
-  quant_wait();   // (of the loads that nothing looks at too: results go through the same memory)
+  quant_wait<0>();   // (of the loads that nothing looks at too: results go through the same memory)
 
   // ---- results: lane l has row l % 32 of a sub-tile and, of its 32 weight rows, 8 (v / 4) + 4 (l / 32) + v % 4
   __syncthreads();

@@ -71,21 +71,26 @@ int run_linear(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, 
 #ifdef HSD_QUANT_TRY
   const char *e = getenv("HSD_QCFG");
   const int cfg = e ? atoi(e) : -1;
-  if constexpr (!FLOATS && !EXACT) { if (cfg == 0) return launch_product<ProductTile<256, 256, 2, 2>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none); }
-  if constexpr (!EXACT) { if (cfg == 1) return launch_product<ProductTile<256, 128, 4, 2>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none); }
-  if constexpr (!EXACT) { if (cfg == 4) return launch_product<ProductTile<128, 256, 2, 4>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none); }
-  if constexpr (!(FLOATS && EXACT)) { if (cfg == 2) return launch_product<ProductTile<128, 128, 2, 2>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none); }
-  if (cfg == 3) return launch_product<ProductTile<64, 128, 2, 2>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
-  if (cfg == 5) return launch_product<ProductTile<64, 64, 2, 2>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
+#define TRY(ok, id, ...) if constexpr (ok) { if (cfg == id) return launch_product<ProductTile<__VA_ARGS__>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none); }
+  TRY(!FLOATS && !EXACT, 0, 256, 256, 2, 2, 1, 4)
+  TRY(!FLOATS && !EXACT, 6, 256, 256, 2, 2, 2, 2)
+  TRY(!FLOATS && !EXACT, 7, 256, 256, 2, 4, 1, 4)
+  TRY(!EXACT, 1, 256, 128, 4, 2, 2, 3)
+  TRY(!EXACT, 4, 128, 256, 2, 4, 2, 3)
+  TRY(!EXACT, 11, 256, 128, 4, 2, 1, 6)
+  TRY(true, 2, 128, 128, 2, 2, 2, 4)
+  TRY(true, 8, 128, 128, 2, 2, 2, 2)
+  TRY(true, 3, 64, 128, 2, 2, 2, 6)
+  TRY(true, 9, 64, 128, 2, 2, 2, 3)
+  TRY(true, 5, 64, 64, 2, 2, 2, 4)
+  TRY(true, 10, 64, 64, 2, 2, 2, 8)
 #endif
   if constexpr (!FLOATS && !EXACT) {
-    if (quant_tiles(M, N, 256, 256) >= 192) return launch_product<ProductTile<256, 256, 2, 2>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
+    if (quant_tiles(M, N, 256, 256) >= 192) return launch_product<ProductTile<256, 256, 2, 2, 1, 4>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
   }
-  if constexpr (!(FLOATS && EXACT)) {
-    if (quant_tiles(M, N, 128, 128) >= 256) return launch_product<ProductTile<128, 128, 2, 2>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
-  }
-  if (quant_tiles(M, N, 64, 128) >= 192) return launch_product<ProductTile<64, 128, 2, 2>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
-  return launch_product<ProductTile<64, 64, 2, 2>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
+  if (quant_tiles(M, N, 128, 128) >= 256) return launch_product<ProductTile<128, 128, 2, 2, 2, 2>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
+  if (quant_tiles(M, N, 64, 128) >= 192) return launch_product<ProductTile<64, 128, 2, 2, 2, 6>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
+  return launch_product<ProductTile<64, 64, 2, 2, 2, 4>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
 }
 
 template <bool FLOATS>
@@ -94,15 +99,19 @@ int run_gated(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, i
 #ifdef HSD_QUANT_TRY
   const char *e = getenv("HSD_QCFG");
   const int cfg = e ? atoi(e) : -1;
-  if constexpr (!FLOATS) { if (cfg == 0) return launch_product<ProductTile<256, 256, 2, 2>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q); }
-  if (cfg == 1 || cfg == 4) return launch_product<ProductTile<128, 256, 2, 4>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
-  if (cfg == 3) return launch_product<ProductTile<64, 256, 1, 4>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
+#define TRYG(ok, id, ...) if constexpr (ok) { if (cfg == id) return launch_product<ProductTile<__VA_ARGS__>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q); }
+  TRYG(!FLOATS, 0, 256, 256, 2, 2, 1, 4)
+  TRYG(!FLOATS, 6, 256, 256, 2, 2, 2, 2)
+  TRYG(!FLOATS, 7, 256, 256, 2, 4, 1, 4)
+  TRYG(true, 4, 128, 256, 2, 4, 2, 3)
+  TRYG(true, 1, 128, 256, 2, 4, 1, 6)
+  TRYG(true, 3, 64, 256, 1, 4, 2, 3)
 #endif
   if constexpr (!FLOATS) {
-    if (quant_tiles(M, N, 256, 128) >= 192) return launch_product<ProductTile<256, 256, 2, 2>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
+    if (quant_tiles(M, N, 256, 128) >= 192) return launch_product<ProductTile<256, 256, 2, 2, 1, 4>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
   }
-  if (quant_tiles(M, N, 128, 128) >= 192) return launch_product<ProductTile<128, 256, 2, 4>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
-  return launch_product<ProductTile<64, 256, 1, 4>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
+  if (quant_tiles(M, N, 128, 128) >= 192) return launch_product<ProductTile<128, 256, 2, 4, 2, 3>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
+  return launch_product<ProductTile<64, 256, 1, 4, 2, 3>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
 }
 
 }  // namespace
