@@ -27,6 +27,7 @@
 #include "probes.h"
 #include "gemm_f32.h"
 #include "gemm_quant.h"
+#include "gemm_quant_few.h"
 #include "gemm_simple.h"
 #include "kv_place.h"
 #include "kv_quant.h"

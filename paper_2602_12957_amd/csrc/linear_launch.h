@@ -63,6 +63,28 @@ int launch_product(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int
   return HSD_OK;
 }
 
+// Products of up to 64 rows
+template <bool GATED, bool FLOATS, bool EXACT, int MT, typename T>
+int launch_few(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, int N, int nk, T *out, int64_t out_stride, const RowsQuant &q) {
+  using Few = FewRows<MT>;
+  auto kern = k_gemm_quant_few<GATED, FLOATS, EXACT, MT, T>;
+  constexpr int per_wave = Few::kSlots * Few::kBlock;
+  static_assert(!GATED || Few::kMostWaves == 16, "a wave for each 16 of the gate's and the up projection's 128 rows");
+  static const hipError_t attr_rc = hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, Few::kMostWaves * per_wave);
+  if (attr_rc != hipSuccess) return HSD_EHIP;
+  const int waves = GATED ? 16 : std::min(nk, Few::kMostWaves), cols = GATED ? kQuantBlock : 16;
+  hipLaunchKernelGGL(kern, dim3((N + cols - 1) / cols), dim3(64 * waves), waves * per_wave, st, a, w, M, N, nk, out, out_stride, q);
+  HSD_LAUNCH_CHECK();
+  return HSD_OK;
+}
+template <bool FLOATS, bool EXACT, typename T>
+int launch_few_rows(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, int N, int nk, T *out, int64_t out_stride) {
+  const RowsQuant none{};
+  if (M <= 16) return launch_few<false, FLOATS, EXACT, 1, T>(st, a, w, M, N, nk, out, out_stride, none);
+  if (M <= 32) return launch_few<false, FLOATS, EXACT, 2, T>(st, a, w, M, N, nk, out, out_stride, none);
+  return launch_few<false, FLOATS, EXACT, 4, T>(st, a, w, M, N, nk, out, out_stride, none);
+}
+
 int64_t quant_tiles(int M, int N, int bm, int bn) { return static_cast<int64_t>((M + bm - 1) / bm) * ((N + bn - 1) / bn); }
 
 template <bool FLOATS, bool EXACT, typename T>
@@ -78,6 +100,7 @@ int run_linear(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, 
   TRY(!EXACT, 1, 256, 128, 4, 2, 2, 3)
   TRY(!EXACT, 4, 128, 256, 2, 4, 2, 3)
   TRY(!EXACT, 11, 256, 128, 4, 2, 1, 6)
+  if (cfg == 20) return launch_few_rows<FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride);
   TRY(true, 2, 128, 128, 2, 2, 2, 4)
   TRY(true, 8, 128, 128, 2, 2, 2, 2)
   TRY(true, 3, 64, 128, 2, 2, 2, 6)
@@ -85,11 +108,12 @@ int run_linear(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, 
   TRY(true, 5, 64, 64, 2, 2, 2, 4)
   TRY(true, 10, 64, 64, 2, 2, 2, 8)
 #endif
+  if (M <= 16 || (M <= 64 && quant_tiles(M, N, 64, 64) < 128)) return launch_few_rows<FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride);
   if constexpr (!FLOATS && !EXACT) {
-    if (quant_tiles(M, N, 256, 256) >= 192) return launch_product<ProductTile<256, 256, 2, 2, 1, 4>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
+    if (quant_tiles(M, N, 256, 256) >= 192) return launch_product<ProductTile<256, 256, 2, 2, 2, 2>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
   }
   if (quant_tiles(M, N, 128, 128) >= 256) return launch_product<ProductTile<128, 128, 2, 2, 2, 2>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
-  if (quant_tiles(M, N, 64, 128) >= 192) return launch_product<ProductTile<64, 128, 2, 2, 2, 6>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
+  if (quant_tiles(M, N, 64, 128) >= 192) return launch_product<ProductTile<64, 128, 2, 2, 2, 3>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
   return launch_product<ProductTile<64, 64, 2, 2, 2, 4>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
 }
 
@@ -100,6 +124,8 @@ int run_gated(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, i
   const char *e = getenv("HSD_QCFG");
   const int cfg = e ? atoi(e) : -1;
 #define TRYG(ok, id, ...) if constexpr (ok) { if (cfg == id) return launch_product<ProductTile<__VA_ARGS__>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q); }
+  TRYG(true, 9, 64, 256, 1, 4, 2, 2)
+  if (cfg == 20) return launch_few<true, FLOATS, false, 1, bf16>(st, a, w, M, N, nk, none, 0, q);
   TRYG(!FLOATS, 0, 256, 256, 2, 2, 1, 4)
   TRYG(!FLOATS, 6, 256, 256, 2, 2, 2, 2)
   TRYG(!FLOATS, 7, 256, 256, 2, 4, 1, 4)
@@ -107,8 +133,9 @@ int run_gated(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, i
   TRYG(true, 1, 128, 256, 2, 4, 1, 6)
   TRYG(true, 3, 64, 256, 1, 4, 2, 3)
 #endif
+  if (M <= 16) return launch_few<true, FLOATS, false, 1, bf16>(st, a, w, M, N, nk, none, 0, q);
   if constexpr (!FLOATS) {
-    if (quant_tiles(M, N, 256, 128) >= 192) return launch_product<ProductTile<256, 256, 2, 2, 1, 4>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
+    if (quant_tiles(M, N, 256, 128) >= 192) return launch_product<ProductTile<256, 256, 2, 2, 2, 2>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
   }
   if (quant_tiles(M, N, 128, 128) >= 192) return launch_product<ProductTile<128, 256, 2, 4, 2, 3>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
   return launch_product<ProductTile<64, 256, 1, 4, 2, 3>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
