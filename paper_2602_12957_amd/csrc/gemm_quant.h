@@ -16,33 +16,36 @@ struct WeightQuant {
   int64_t code_stride, scale_stride;
 };
 
-// An LDS-direct load of 1 KB: lane l's 16 bytes at base + off go to dst + 16 l; and one of 256 bytes, 4 a lane.  In asm: the compiler would
-// otherwise wait for every load in flight before each LDS read.  No register is written; the reads wait by quant_wait and a
-// barrier.  m0 is put back as it was found.
-__device__ __forceinline__ void lds_load_1k(uint32_t dst, const uint8_t *base, uint32_t off) {
-  uint32_t m0;
-  asm volatile(
-      "s_mov_b32 %0, m0\n\t"
-      "s_mov_b32 m0, %1\n\t"
-      "s_nop 0\n\t"
-      "global_load_lds_dwordx4 %2, %3\n\t"
-      "s_mov_b32 m0, %0"
-      : "=&s"(m0)
-      : "s"(dst), "v"(off), "s"(base)
-      : "memory");
+// N LDS-direct loads of 1 KB, N = 1, 2 or 4: lane l's 16 bytes of load j go to dst + 1024 j + 16 l; they come from base - 3072 + off[j] + 1024 j (an
+// instruction's offset moves both addresses).  In asm: the compiler would otherwise wait for every load in flight before each LDS
+// read.  No register is written; the reads wait by quant_wait and a barrier.  m0 is put back as it was found.
+constexpr int kLoadBias = 3072;
+template <int N>
+__device__ __forceinline__ void lds_load(uint32_t dst, uint64_t b, const uint32_t *off) {
+  static_assert(N == 1 || N == 2 || N == 4, "loads of a group");
+  uint32_t m0;   // (the base is the same in all lanes, which the compiler does not always see)
+  const uint64_t p = (static_cast<uint64_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(b >> 32))) << 32) |
+                     static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(b)));
+  if constexpr (N == 1)
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"
+                 "global_load_lds_dwordx4 %2, %3\n\t"
+                 "s_mov_b32 m0, %0" : "=&s"(m0) : "s"(dst), "v"(off[0]), "s"(p) : "memory");
+  else if constexpr (N == 2)
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"
+                 "global_load_lds_dwordx4 %2, %4\n\tglobal_load_lds_dwordx4 %3, %4 offset:1024\n\t"
+                 "s_mov_b32 m0, %0" : "=&s"(m0) : "s"(dst), "v"(off[0]), "v"(off[1]), "s"(p) : "memory");
+  else
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"
+                 "global_load_lds_dwordx4 %2, %6\n\tglobal_load_lds_dwordx4 %3, %6 offset:1024\n\t"
+                 "global_load_lds_dwordx4 %4, %6 offset:2048\n\tglobal_load_lds_dwordx4 %5, %6 offset:3072\n\t"
+                 "s_mov_b32 m0, %0" : "=&s"(m0) : "s"(dst), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(p) : "memory");
 }
-__device__ __forceinline__ void lds_load_256(uint32_t dst, const uint8_t *base, uint64_t off) {
+// One of 256 bytes, 4 a lane
+__device__ __forceinline__ void lds_load_256(uint32_t dst, uint64_t p) {
   uint32_t m0;
-  const uint64_t p = reinterpret_cast<uint64_t>(base) + off;
-  asm volatile(
-      "s_mov_b32 %0, m0\n\t"
-      "s_mov_b32 m0, %1\n\t"
-      "s_nop 0\n\t"
-      "global_load_lds_dword %2, off\n\t"
-      "s_mov_b32 m0, %0"
-      : "=&s"(m0)
-      : "s"(dst), "v"(p)
-      : "memory");
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"
+               "global_load_lds_dword %2, off\n\t"
+               "s_mov_b32 m0, %0" : "=&s"(m0) : "s"(dst), "v"(p) : "memory");
 }
 // All but the N newest of this wave's loads have landed, and its LDS reads are done
 template <int N>
@@ -53,21 +56,33 @@ __device__ __forceinline__ void quant_wait() {
   asm volatile("" ::: "memory");
 }
 
-// A tile of BM rows by BN weight rows, WM by WN waves; operands in a ring of S slices of 64 Q columns.
-template <int BM_, int BN_, int WM_, int WN_, int Q_, int S_>
+// A tile of BM rows by BN weight rows, WM by WN waves; operands in a ring of S slices of 64 Q columns.  G groups of such waves share out the
+// blocks of columns, with a ring each; their sums are joined at the end.
+template <int BM_, int BN_, int WM_, int WN_, int Q_, int S_, int G_ = 1>
 struct ProductTile {
-  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NW = WM_ * WN_, Q = Q_, S = S_;
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NW = WM_ * WN_, Q = Q_, S = S_, G = G_;
   static constexpr int TA = BM / WM / 32, TW = BN / WN / 32;      // 32x32 sub-tiles of a wave: rows, weight rows
   static constexpr int kRow = 64 * Q;                             // bytes of a row in a slice
   static constexpr int kScales = NW * 256;                        // the rows' bytes of four blocks, behind the codes
   static constexpr int kSlice = (BM + BN) * kRow + kScales;
   static constexpr int kPerLoad = 1024 / kRow;                    // rows of a 1 KB load
   static constexpr int kLoadsA = BM / kPerLoad / NW, kLoadsW = BN / kPerLoad / NW, kLoads = kLoadsA + kLoadsW;   // of a wave and slice
-  static constexpr int kLds = S * kSlice;
-  static constexpr int kWaves = BM * BN / NW > 128 * 64 ? 1 : 2;  // of a SIMD
+  static constexpr int kPass = 2 < BN / WN / 32 ? 2 : BN / WN / 32;   // sub-tiles of columns that a wave stores at a time
+  static constexpr int kRing = S * kSlice;
+  static constexpr int out_bytes(bool gated, int size) {          // of results on their way
+    return gated ? WM * 32 * (kQuantBlock + 16) + BM * WN * 4 : NW * 32 * (kPass * 32 * size + 16);
+  }
+  static constexpr int kLds = G * kRing;
+  static constexpr int group_a = kLoadsA % 4 == 0 ? 4 : kLoadsA % 2 == 0 ? 2 : 1;                       // loads that go together
+  static constexpr int group_w(bool gated) {                                                          // (of one projection)
+    const int most = gated ? 32 / kPerLoad : 4;
+    return kLoadsW % 4 == 0 && most >= 4 ? 4 : kLoadsW % 2 == 0 && most >= 2 ? 2 : 1;
+  }
+  static constexpr int kWaves = BM * BN / NW > 128 * 64 ? 1 : G > 2 ? G : 2;  // of a SIMD
+  static_assert(G == 1 || (Q == 2 && NW == 4 && (G - 1) * BM * BN * 4 + 32 * 1024 <= G * kRing), "sums are joined in the rings' place");
   static_assert(Q == 1 || Q == 2, "a slice is a block of 128 columns or half of one");
   static_assert(BM / kPerLoad % NW == 0 && BN / kPerLoad % NW == 0 && BM <= 64 * NW, "loads divide evenly");
-  static_assert(S >= 2 && (S - 1) * (kLoads + 1) < 64 && kLds <= 160 * 1024, "slices in flight");
+  static_assert(S >= 2 && (S - 1) * (kLoads + 1) < 64 && kRing <= 160 * 1024, "slices in flight");
 };
 
 // Tile of a workgroup: XCD x (workgroup id mod 8) takes a contiguous run of an order that goes through bands of eight tiles of rows,
@@ -101,87 +116,88 @@ __device__ __forceinline__ Fragment16 widen(const i32x8 &f, float scale) {
   return r;
 }
 
+// All of this wave's LDS operations are done, then those of all
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
 // GATED: gate and up rows of 128 output columns (BN = 256), silu(gate) * up to 8 bits; else out.  FLOATS: weight scales are floats.
-// EXACT: bf16 products of the codes instead of the 8-bit ones.
+// EXACT: bf16 products of the codes instead of the 8-bit ones.  Grid: tiles.
 template <typename Cfg, bool GATED, bool FLOATS, bool EXACT, typename T>
-__global__ void __launch_bounds__(64 * Cfg::NW, Cfg::kWaves) k_gemm_quant(const RowsQuant a, const WeightQuant w, int M, int N, int nk, T *__restrict__ out, int64_t out_stride,
-                                                              const RowsQuant q) {
-  constexpr int BM = Cfg::BM, BN = Cfg::BN, TA = Cfg::TA, TW = Cfg::TW, NW = Cfg::NW;
+__global__ void __launch_bounds__(64 * Cfg::NW * Cfg::G, Cfg::kWaves) k_gemm_quant(const RowsQuant a, const WeightQuant w, int M, int N, int nk, T *__restrict__ out,
+                                                                          int64_t out_stride, const RowsQuant q) {
+  constexpr int BM = Cfg::BM, BN = Cfg::BN, TA = Cfg::TA, TW = Cfg::TW, NW = Cfg::NW, G = Cfg::G;
   constexpr int COLS = GATED ? BN / 2 : BN;
   static_assert(!GATED || (COLS == kQuantBlock && TW % 2 == 0), "a workgroup has whole blocks of the rows that it rounds");
+  static_assert(Cfg::out_bytes(GATED, sizeof(T)) <= Cfg::kRing, "results are staged in the operands' place");
   extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
-  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int group = G > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / (64 * NW)) : 0;
+  const int t = threadIdx.x - group * 64 * NW, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);   // of the group
   const int wi = wave / Cfg::WN, wj = wave % Cfg::WN;
+  unsigned char *const ring = smem_raw + group * Cfg::kRing;
   int tm, tn;
   quant_tile_of(blockIdx.x, (M + BM - 1) / BM, (N + COLS - 1) / COLS, tm, tn);
   const int m0 = tm * BM, n0 = tn * COLS;
 
-  // ---- loads.  Load i of a slice covers RPL tile rows from RPL i on (rows, then weight rows); lane l fetches, for row RPL i + l / LPW, the
-  // 16-byte piece that belongs at position l % LPW: a row's pieces lie XORed by the row, so that reads of 16 rows cover all banks.
-  // Rows behind the last one are that one again (their products are never stored).
+  // ---- loads.  A wave's load j of a slice covers the RPL tile rows from RPL (wave kLoads + j) on (rows, and weight rows); lane l fetches, for row l / LPW
+  // of them, the 16-byte piece that belongs at position l % LPW: a row's pieces lie XORed by the row, so that reads of 16 rows cover all banks.
+  // Rows behind the last one are that one again (their products are never stored).  Gate and up alternate by 32 rows: weight row
+  // 64 g + 32 u + x of the tile is row n0 + 32 g + x of the gate or of the up projection.
   constexpr int Q = Cfg::Q, S = Cfg::S, RPL = Cfg::kPerLoad, LPW = Cfg::kRow / 16, SHIFT = Q == 2 ? 1 : 2;
-  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char *)smem_raw));
-  const uint8_t *base_a = a.codes + m0 * a.code_stride, *base_w = w.codes + n0 * w.code_stride, *base_u = GATED ? base_w + N * w.code_stride : base_w;
+  constexpr int GA = Cfg::group_a, GW = Cfg::group_w(GATED);
+  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char *)ring));
+  const uint64_t base_a = reinterpret_cast<uint64_t>(a.codes) + m0 * a.code_stride - kLoadBias;
+  const uint64_t base_w = reinterpret_cast<uint64_t>(w.codes) + n0 * w.code_stride - kLoadBias, up_rows = GATED ? N * w.code_stride : 0;
   uint32_t off_a[Cfg::kLoadsA], off_w[Cfg::kLoadsW];
 #pragma unroll
   for (int j = 0; j < Cfg::kLoadsA; ++j) {
-    const int r = (j * NW + wave) * RPL + lane / LPW;
-    off_a[j] = min(r, M - 1 - m0) * static_cast<uint32_t>(a.code_stride) + ((lane ^ (r >> SHIFT)) % LPW) * 16;
+    const int r = (wave * Cfg::kLoadsA + j) * RPL + lane / LPW;
+    off_a[j] = min(r, M - 1 - m0) * static_cast<uint32_t>(a.code_stride) + ((lane ^ (r >> SHIFT)) % LPW) * 16 + kLoadBias - j % GA * 1024;
   }
 #pragma unroll
   for (int j = 0; j < Cfg::kLoadsW; ++j) {
-    const int r = (j * NW + wave) * RPL + lane / LPW;
-    // gate and up alternate by 32 rows: weight row 64 g + 32 u + x of the tile is row n0 + 32 g + x of the gate or of the up projection
-    const int row = GATED ? (r >> 6) * 32 + (r & 31) : min(r, N - 1 - n0);
-    off_w[j] = row * static_cast<uint32_t>(w.code_stride) + ((lane ^ (r >> SHIFT)) % LPW) * 16;
+    const int r = (wave * Cfg::kLoadsW + j) * RPL + lane / LPW, row = GATED ? (r >> 6) * 32 + (r & 31) : min(r, N - 1 - n0);
+    off_w[j] = row * static_cast<uint32_t>(w.code_stride) + ((lane ^ (r >> SHIFT)) % LPW) * 16 + kLoadBias - j % GW * 1024;
   }
-  const uint64_t off_s = min(m0 + t, M - 1) * a.scale_stride;   // (t: the row; of those behind the tile's nothing is read)
-  const int slices = nk * (2 / Q);
-  constexpr int LOADS = Cfg::kLoads + 1;
-  auto request = [&](int slice, uint32_t place, int j) {   // load j of a slice into its place
-    const uint32_t dst = place + wave * 1024;
-    const int col = slice * Cfg::kRow;
-    if (j < Cfg::kLoadsA) {
-      lds_load_1k(dst + j * NW * 1024, base_a + col, off_a[j]);
-    } else if (j < Cfg::kLoads) {
-      const int k = j - Cfg::kLoadsA;
-      const bool up = GATED && (((k * NW + wave) * RPL) >> 5 & 1);
-      lds_load_1k(dst + j * NW * 1024, (up ? base_u : base_w) + col, off_w[k]);
+  const uint64_t scales_a = reinterpret_cast<uint64_t>(a.scale) + min(m0 + t, M - 1) * a.scale_stride;   // (of row t; behind the tile's rows nobody reads)
+  const int mine = nk / G, slices = mine * (2 / Q);   // blocks of the group: group, group + G, ...
+  constexpr int LOADS = Cfg::kLoads + 1, REQUESTS = Cfg::kLoadsA / GA + Cfg::kLoadsW / GW + 1;
+  auto request = [&](int slice, uint32_t place, int j) {   // request j of a slice into its place
+    const int col = (slice * G + group) * Cfg::kRow;
+    if (j < Cfg::kLoadsA / GA) {
+      lds_load<GA>(place + (wave * Cfg::kLoadsA + j * GA) * 1024, base_a + col, off_a + j * GA);
+    } else if (j < REQUESTS - 1) {
+      const int k = (j - Cfg::kLoadsA / GA) * GW;
+      const bool up = GATED && (((wave * Cfg::kLoadsW + k) * RPL) >> 5 & 1);
+      lds_load<GW>(place + BM * Cfg::kRow + (wave * Cfg::kLoadsW + k) * 1024, base_w + (up ? up_rows : 0) + col, off_w + k);
     } else {
-      lds_load_256(place + (BM + BN) * Cfg::kRow + wave * 256, a.scale, off_s + (slice / (2 / Q) & ~3));
+      lds_load_256(place + (BM + BN) * Cfg::kRow + wave * 256, scales_a + ((slice / (2 / Q) * G + group) & ~3));
     }
   };
 #pragma unroll
   for (int s = 0; s < S; ++s)
 #pragma unroll
-    for (int j = 0; j < LOADS; ++j) request(min(s, slices - 1), lds0 + s * Cfg::kSlice, j);
+    for (int j = 0; j < REQUESTS; ++j) request(min(s, slices - 1), lds0 + s * Cfg::kSlice, j);
 
-  // ---- scales.  A wave's weight rows lie in one block of 128, or in one of the gate and one of the up projection: their scales come
-  // through the scalar unit, a block ahead (vector loads would be waited for with all the slices behind them).
-  uint32_t sa[TA], sa_next[TA];
-  const int64_t wrow = GATED ? n0 : min(n0 + wj * (BN / Cfg::WN), N - 1);
+  // ---- scales.  The weights' come through the scalar unit, a block ahead (vector loads would be waited for with all the slices behind them).
+  uint32_t sa[TA], sa_next[TA], ws_now[2] = {0, 0}, ws_next[2] = {0, 0};
+  const int64_t wrow = GATED ? n0 : min(n0 + wj * (BN / Cfg::WN), N - 1);   // a wave's weight rows lie in one block of 128, or in one of the gate and one of up
   const int64_t ws_at[2] = {wrow / kQuantBlock * w.scale_stride, (wrow + N) / kQuantBlock * w.scale_stride};
-  uint32_t ws_now[2] = {0, 0}, ws_next[2] = {0, 0};
-  auto weight_scales = [&](int kt) {
+  auto weight_scales = [&](int kb) {
 #pragma unroll
     for (int i = 0; i < (GATED ? 2 : 1); ++i) {
       typedef const __attribute__((address_space(4))) uint32_t *Const;
-      const uint64_t p = reinterpret_cast<uint64_t>(w.scale) + (FLOATS ? 4 : 1) * (ws_at[i] + kt);
-      const uint32_t x = *reinterpret_cast<Const>(p & ~uint64_t{3});   // (a byte's word)
-      ws_next[i] = FLOATS ? x : x >> (8 * (p & 3)) & 255;
+      const uint64_t p = reinterpret_cast<uint64_t>(w.scale) + (FLOATS ? 4 : 1) * (ws_at[i] + kb);
+      const uint32_t v = *reinterpret_cast<Const>(p & ~uint64_t{3});   // (a byte's word)
+      ws_next[i] = FLOATS ? v : v >> (8 * (p & 3)) & 255;
     }
   };
 
   // (block: the sums of the block at hand, where its scale is a float)
   floatx16 acc[TW][TA], block[FLOATS ? TW : 1][FLOATS ? TA : 1];
   const floatx16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int i = 0; i < TW; ++i)
-#pragma unroll
-    for (int j = 0; j < TA; ++j) {
-      acc[i][j] = zero;
-      if constexpr (FLOATS) block[i][j] = zero;
-    }
   float factor[2] = {0.f, 0.f};   // of the block before (FLOATS)
   auto add_block = [&](int i, int j) {
 #pragma unroll
@@ -203,12 +219,12 @@ __global__ void __launch_bounds__(64 * Cfg::NW, Cfg::kWaves) k_gemm_quant(const 
     if (n < TW) fw[buf][n] = fragment(p + row_w + n * 32 * Cfg::kRow, half);
     else fa[buf][n - TW] = fragment(p + row_a + (n - TW) * 32 * Cfg::kRow, half);
   };
-  auto row_scales = [&](const unsigned char *p, int kt) {
+  auto row_scales = [&](const unsigned char *p, int kb) {
 #pragma unroll
     for (int i = 0; i < TA; ++i)
-      sa_next[i] = *reinterpret_cast<const uint32_t *>(p + (BM + BN) * Cfg::kRow + (wi * (BM / Cfg::WM) + i * 32 + fr) * 4) >> (8 * (kt & 3));
+      sa_next[i] = *reinterpret_cast<const uint32_t *>(p + (BM + BN) * Cfg::kRow + (wi * (BM / Cfg::WM) + i * 32 + fr) * 4) >> (8 * (kb & 3));
   };
-  // The products of a half block, with what else the step has to do dealt out between them: FRAGS reads of the next half block, LOADS requests
+  // The products of a half block, with what else the step has to do dealt out between them
   constexpr int PRODUCTS = TA * TW, FRAGS = TA + TW;
   auto step = [&](int buf, auto &&other, int others) {
     Fragment16 cw[EXACT ? TW : 1], ca;
@@ -236,47 +252,55 @@ __global__ void __launch_bounds__(64 * Cfg::NW, Cfg::kWaves) k_gemm_quant(const 
   };
 
   constexpr int LATER = (S - 2) * LOADS;   // loads of the slices that may still be in flight when the next one is needed
-  weight_scales(0);
-  quant_wait<LATER + LOADS>();
-  __builtin_amdgcn_s_barrier();
-#pragma unroll
-  for (int n = 0; n < FRAGS; ++n) read(0, smem_raw, 0, n);
-  row_scales(smem_raw, 0);
-  int at = 0;   // place of the slice at hand
   // What precedes the last step of a slice: all waves have read it, and the next one is complete
   auto turn = [&]() {
     quant_wait<LATER>();
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
   };
-  for (int kt = 0; kt < nk; ++kt) {
+  weight_scales(group);
+  quant_wait<LATER + LOADS>();
+  __builtin_amdgcn_s_barrier();
+#pragma unroll
+  for (int n = 0; n < FRAGS; ++n) read(0, ring, 0, n);
+  row_scales(ring, group);
+  int at = 0;   // place of the slice at hand
+#pragma unroll
+  for (int i = 0; i < TW; ++i)
+#pragma unroll
+    for (int j = 0; j < TA; ++j) {
+      acc[i][j] = zero;
+      if constexpr (FLOATS) block[i][j] = zero;
+    }
+  for (int kt = 0; kt < mine; ++kt) {
     if constexpr (FLOATS) factor[0] = __uint_as_float(ws_now[0]), factor[1] = __uint_as_float(ws_now[1]);
     ws_now[0] = ws_next[0], ws_now[1] = ws_next[1];
-    weight_scales(min(kt + 1, nk - 1));
+    const int kb_next = min(kt + 1, mine - 1) * G + group;
+    weight_scales(kb_next);
 #pragma unroll
     for (int i = 0; i < TA; ++i) sa[i] = sa_next[i];
     __builtin_amdgcn_sched_barrier(0);
     // (behind the last slices the requests and reads are of the last one, or of an older one's place: nothing looks at them)
     if constexpr (Q == 2) {
-      const unsigned char *here = smem_raw + at * Cfg::kSlice;
+      const unsigned char *here = ring + at * Cfg::kSlice;
       const uint32_t place = lds0 + at * Cfg::kSlice;
       at = at + 1 == S ? 0 : at + 1;
-      const unsigned char *next = smem_raw + at * Cfg::kSlice;
+      const unsigned char *next = ring + at * Cfg::kSlice;
       step(0, [&](int k) { read(1, here, 1, k); }, FRAGS);
       turn();
       const int ahead = min(kt + S, slices - 1);
-      row_scales(next, kt + 1);
-      step(1, [&](int k) { if (k < FRAGS) read(0, next, 0, k); else request(ahead, place, k - FRAGS); }, FRAGS + LOADS);
+      row_scales(next, kb_next);
+      step(1, [&](int k) { if (k < REQUESTS) request(ahead, place, k); else read(0, next, 0, k - REQUESTS); }, REQUESTS + FRAGS);
     } else {
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         const uint32_t place = lds0 + at * Cfg::kSlice;
         at = at + 1 == S ? 0 : at + 1;
-        const unsigned char *next = smem_raw + at * Cfg::kSlice;
+        const unsigned char *next = ring + at * Cfg::kSlice;
         turn();
         const int ahead = min(2 * kt + half + S, slices - 1);
-        if (half == 1) row_scales(next, kt + 1);
-        step(half, [&](int k) { if (k < FRAGS) read(half ^ 1, next, 0, k); else request(ahead, place, k - FRAGS); }, FRAGS + LOADS);
+        if (half == 1) row_scales(next, kb_next);
+        step(half, [&](int k) { if (k < REQUESTS) request(ahead, place, k); else read(half ^ 1, next, 0, k - REQUESTS); }, REQUESTS + FRAGS);
       }
     }
   }
@@ -287,51 +311,70 @@ __global__ void __launch_bounds__(64 * Cfg::NW, Cfg::kWaves) k_gemm_quant(const 
 #pragma unroll
       for (int j = 0; j < TA; ++j) add_block(i, j);
   }
-  quant_wait<0>();   // (of the loads that nothing looks at too: results go through the same memory)
-
   // ---- results: lane l has row l % 32 of a sub-tile and, of its 32 weight rows, 8 (v / 4) + 4 (l / 32) + v % 4
-  __syncthreads();
+  unsigned char *stage = smem_raw;
+  quant_wait<0>();   // (of the loads that nothing looks at too: results go through the same memory)
+  __builtin_amdgcn_s_barrier();
+  if constexpr (G > 1) {   // the groups' sums, in their order, to the first one's
+    floatx4 *part = reinterpret_cast<floatx4 *>(smem_raw + 32 * 1024);
+    constexpr int PARTS = TW * TA * 4;   // of a lane
+    if (group > 0) {
+#pragma unroll
+      for (int i = 0; i < PARTS; ++i) {
+        const floatx16 &x = acc[i / 4 / TA][i / 4 % TA];
+        part[((group - 1) * PARTS + i) * 64 * NW + t] = floatx4{x[4 * (i & 3)], x[4 * (i & 3) + 1], x[4 * (i & 3) + 2], x[4 * (i & 3) + 3]};
+      }
+    }
+    lds_barrier();
+    if (group > 0) return;
+#pragma unroll
+    for (int k = 0; k < G - 1; ++k)
+#pragma unroll
+      for (int i = 0; i < PARTS; ++i) {
+        const floatx4 x = part[(k * PARTS + i) * 64 * NW + t];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) acc[i / 4 / TA][i / 4 % TA][4 * (i & 3) + v] += x[v];
+      }
+  }
   if constexpr (!GATED) {
-    // through LDS, so that adjacent lanes store adjacent pieces of a row
-    constexpr int W = TW * 32, ROW = W * sizeof(T) + 16, LPR = W * sizeof(T) / 16, PER = 16 / sizeof(T);
-    unsigned char *mine = smem_raw + wave * 32 * ROW;
-    static_assert(NW * 32 * ROW <= Cfg::kLds, "results are staged in the operands' place");
-    const int c0 = n0 + wj * W;
+    // through LDS (a wave's own), so that adjacent lanes store adjacent pieces of a row
+    constexpr int PASS = Cfg::kPass, W = PASS * 32, ROW = W * sizeof(T) + 16, LPR = W * sizeof(T) / 16, PER = 16 / sizeof(T);
+    unsigned char *mine = stage + wave * 32 * ROW;
 #pragma unroll
-    for (int j = 0; j < TA; ++j) {
+    for (int j = 0; j < TA; ++j)
 #pragma unroll
-      for (int i = 0; i < TW; ++i)
+      for (int i0 = 0; i0 < TW; i0 += PASS) {
 #pragma unroll
-        for (int v = 0; v < 16; v += 4) {
-          T *p = reinterpret_cast<T *>(mine + fr * ROW) + i * 32 + 2 * v + 4 * kg;
-          if constexpr (sizeof(T) == 4) {
-            *reinterpret_cast<floatx4 *>(p) = floatx4{acc[i][j][v], acc[i][j][v + 1], acc[i][j][v + 2], acc[i][j][v + 3]};
-          } else {
-            const floatx4 f = {acc[i][j][v], acc[i][j][v + 1], acc[i][j][v + 2], acc[i][j][v + 3]};
-            *reinterpret_cast<bf16x4 *>(p) = __builtin_convertvector(f, bf16x4);
+        for (int i = 0; i < PASS; ++i)
+#pragma unroll
+          for (int v = 0; v < 16; v += 4) {
+            T *p = reinterpret_cast<T *>(mine + fr * ROW) + i * 32 + 2 * v + 4 * kg;
+            const floatx16 &x = acc[i0 + i][j];
+            const floatx4 f = {x[v], x[v + 1], x[v + 2], x[v + 3]};
+            if constexpr (sizeof(T) == 4) *reinterpret_cast<floatx4 *>(p) = f;
+            else *reinterpret_cast<bf16x4 *>(p) = __builtin_convertvector(f, bf16x4);
           }
-        }
-      const int r0 = m0 + wi * (BM / Cfg::WM) + j * 32;
+        const int row0 = m0 + wi * (BM / Cfg::WM) + j * 32, c0 = n0 + wj * (BN / Cfg::WN) + i0 * 32;
 #pragma unroll
-      for (int s = 0; s < 32 * LPR / 64; ++s) {
-        const int r = s * (64 / LPR) + lane / LPR, c = lane % LPR * PER;
-        const u32x4 x = *reinterpret_cast<const u32x4 *>(mine + r * ROW + lane % LPR * 16);
-        if (r0 + r < M && c0 + c < N) {
-          T *p = out + (r0 + r) * out_stride + c0 + c;
-          if (c0 + c + PER <= N) {
-            typedef uint32_t u4 __attribute__((ext_vector_type(4), aligned(2)));
-            *reinterpret_cast<u4 *>(p) = x;
-          } else {
-            const T *y = reinterpret_cast<const T *>(mine + r * ROW + lane % LPR * 16);
-            for (int k = 0; c0 + c + k < N; ++k) p[k] = y[k];
+        for (int s = 0; s < 32 * LPR / 64; ++s) {
+          const int r = s * (64 / LPR) + lane / LPR, c = lane % LPR * PER;
+          const u32x4 x = *reinterpret_cast<const u32x4 *>(mine + r * ROW + lane % LPR * 16);
+          if (row0 + r < M && c0 + c < N) {
+            T *p = out + (row0 + r) * out_stride + c0 + c;
+            if (c0 + c + PER <= N) {
+              typedef uint32_t u4 __attribute__((ext_vector_type(4), aligned(2)));
+              *reinterpret_cast<u4 *>(p) = x;
+            } else {
+              const T *y = reinterpret_cast<const T *>(mine + r * ROW + lane % LPR * 16);
+              for (int k = 0; c0 + c + k < N; ++k) p[k] = y[k];
+            }
           }
         }
       }
-    }
   } else {
+    // 32 rows of each row of waves at a time: a row's 128 columns meet in LDS
     constexpr int P = TW / 2, ROW = kQuantBlock + 16;
-    float *top = reinterpret_cast<float *>(smem_raw + BM * ROW);   // [BM][WN]
-    static_assert(BM * ROW + BM * Cfg::WN * 4 <= Cfg::kLds, "results are staged in the operands' place");
+    float *top = reinterpret_cast<float *>(stage + Cfg::WM * 32 * ROW);   // [BM][WN]
 #pragma unroll
     for (int j = 0; j < TA; ++j) {
       float m = 0.f;
@@ -340,12 +383,23 @@ __global__ void __launch_bounds__(64 * Cfg::NW, Cfg::kWaves) k_gemm_quant(const 
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
           acc[2 * i][j][v] = swiglu(acc[2 * i][j][v], acc[2 * i + 1][j][v]);
-          m = fmaxf(m, finite_mag(acc[2 * i][j][v]));
+          m = fmaxf(m, fabsf(acc[2 * i][j][v]));
         }
+      if (__builtin_expect(__any(!(m <= 448.f * 0x1p119f)), 0)) {   // infinities do not count, and what is beyond the largest scale is cut
+        m = 0.f;
+#pragma unroll
+        for (int i = 0; i < P; ++i)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            const float y = acc[2 * i][j][v];
+            m = fmaxf(m, finite_mag(y));
+            acc[2 * i][j][v] = fabsf(y) < INFINITY ? __builtin_amdgcn_fmed3f(y, -448.f * 0x1p119f, 448.f * 0x1p119f) : NAN;
+          }
+      }
       m = half_max(m);
       if (lane < 32) top[(wi * (BM / Cfg::WM) + j * 32 + fr) * Cfg::WN + wj] = m;
     }
-    __syncthreads();
+    lds_barrier();
 #pragma unroll
     for (int j = 0; j < TA; ++j) {
       const int r = wi * (BM / Cfg::WM) + j * 32 + fr;
@@ -354,17 +408,22 @@ __global__ void __launch_bounds__(64 * Cfg::NW, Cfg::kWaves) k_gemm_quant(const 
       for (int i = 0; i < Cfg::WN; ++i) m = fmaxf(m, top[r * Cfg::WN + i]);
       const int e = scale_exp(m);
       const float inv = exp2_int(-e);
+      if (j > 0) lds_barrier();   // (the rows before have been stored)
 #pragma unroll
       for (int i = 0; i < P; ++i)
 #pragma unroll
-        for (int v = 0; v < 16; v += 4)
-          *reinterpret_cast<uint32_t *>(smem_raw + r * ROW + (wj * P + i) * 32 + 2 * v + 4 * kg) =
-              quant4(code_arg(acc[2 * i][j][v], inv), code_arg(acc[2 * i][j][v + 1], inv), code_arg(acc[2 * i][j][v + 2], inv), code_arg(acc[2 * i][j][v + 3], inv));
+        for (int v = 0; v < 16; v += 4) {
+          const floatx16 &y = acc[2 * i][j];
+          *reinterpret_cast<uint32_t *>(stage + (wi * 32 + fr) * ROW + (wj * P + i) * 32 + 2 * v + 4 * kg) =
+              quant4(y[v] * inv, y[v + 1] * inv, y[v + 2] * inv, y[v + 3] * inv);
+        }
       if (wj == 0 && kg == 0 && m0 + r < M) q.scale[(m0 + r) * q.scale_stride + tn] = static_cast<uint8_t>(e + 127);
+      lds_barrier();
+      for (int x = t >> 3; x < 32 * Cfg::WM; x += 8 * NW) {
+        const int row = m0 + (x >> 5) * (BM / Cfg::WM) + j * 32 + (x & 31);
+        if (row < M) *reinterpret_cast<u32x4 *>(q.codes + row * q.code_stride + n0 + (t & 7) * 16) = *reinterpret_cast<const u32x4 *>(stage + x * ROW + (t & 7) * 16);
+      }
     }
-    __syncthreads();
-    for (int r = t >> 3; r < BM && m0 + r < M; r += 8 * NW)
-      *reinterpret_cast<u32x4 *>(q.codes + (m0 + r) * q.code_stride + n0 + (t & 7) * 16) = *reinterpret_cast<const u32x4 *>(smem_raw + r * ROW + (t & 7) * 16);
   }
 }
 

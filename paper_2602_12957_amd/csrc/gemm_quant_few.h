@@ -34,24 +34,23 @@ __global__ void __launch_bounds__(64 * FewRows<MT>::kMostWaves) k_gemm_quant_few
   // reads of 16 rows cover all banks).  Rows behind the last one are that one again, and not stored.
   unsigned char *mine = smem_raw + wave * S * Few::kBlock;
   const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char *)mine));
-  const uint8_t *base_w = w.codes + n0 * w.code_stride;
+  const uint64_t base_w = reinterpret_cast<uint64_t>(w.codes) + n0 * w.code_stride - kLoadBias, base_a = reinterpret_cast<uint64_t>(a.codes) - kLoadBias;
   uint32_t off_w[2], off_a[2 * MT];
 #pragma unroll
   for (int j = 0; j < 2 + 2 * MT; ++j) {
     const int r = (j < 2 ? 8 * j : 8 * j - 16) + (lane >> 3);
     const uint32_t piece = ((lane ^ (r >> 1)) & 7) * 16;
-    if (j < 2) off_w[j] = (GATED ? r : min(static_cast<int64_t>(r), N - 1 - n0)) * static_cast<uint32_t>(w.code_stride) + piece;
-    else off_a[j - 2] = min(r, M - 1) * static_cast<uint32_t>(a.code_stride) + piece;
+    if (j < 2) off_w[j] = (GATED ? r : min(static_cast<int64_t>(r), N - 1 - n0)) * static_cast<uint32_t>(w.code_stride) + piece + kLoadBias - j * 1024;
+    else off_a[j - 2] = min(r, M - 1) * static_cast<uint32_t>(a.code_stride) + piece + kLoadBias - j % 2 * 1024;
   }
-  const uint64_t off_s = min(lane, M - 1) * a.scale_stride;
+  const uint64_t scales_a = reinterpret_cast<uint64_t>(a.scale) + min(lane, M - 1) * a.scale_stride;
   auto request = [&](int kb, int slot) {
     const int b = min(kb, nk - 1), col = b * kQuantBlock;
     const uint32_t dst = lds0 + slot * Few::kBlock;
+    lds_load<2>(dst, base_w + col, off_w);
 #pragma unroll
-    for (int j = 0; j < 2; ++j) lds_load_1k(dst + j * 1024, base_w + col, off_w[j]);
-#pragma unroll
-    for (int j = 0; j < 2 * MT; ++j) lds_load_1k(dst + (2 + j) * 1024, a.codes + col, off_a[j]);
-    lds_load_256(dst + (2 + 2 * MT) * 1024, a.scale, off_s + (b & ~3));
+    for (int j = 0; j < MT; ++j) lds_load<2>(dst + (2 + 2 * j) * 1024, base_a + col, off_a + 2 * j);
+    lds_load_256(dst + (2 + 2 * MT) * 1024, scales_a + (b & ~3));
   };
   const int64_t ws_at = n0 / kQuantBlock * w.scale_stride;   // (16 weight rows lie in one block of 128)
   auto weight_scale = [&](int kb) -> uint32_t {

@@ -35,10 +35,13 @@ int hsd_quant_read_rows(void *stream, int32_t n_rows, int32_t dim, const hsd_row
   if (n_rows == 0) return HSD_OK;
   if (out == nullptr || out_stride < dim) return HSD_EINVAL;
   hipStream_t st = static_cast<hipStream_t>(stream);
+  int lanes = 16;   // of a row
+  while (lanes < 256 && 8 * lanes < dim) lanes *= 2;
+  const dim3 grid((static_cast<unsigned>(n_rows) + 256 / lanes - 1) / (256 / lanes));
   if (dtype == HSD_BF16)
-    hipLaunchKernelGGL((k_quant_read_rows<bf16>), dim3(n_rows), dim3(256), 0, st, rows_quant(rows), n_rows, dim, static_cast<bf16 *>(out), out_stride);
+    hipLaunchKernelGGL((k_quant_read_rows<bf16>), grid, dim3(256), 0, st, rows_quant(rows), n_rows, dim, lanes, static_cast<bf16 *>(out), out_stride);
   else
-    hipLaunchKernelGGL((k_quant_read_rows<float>), dim3(n_rows), dim3(256), 0, st, rows_quant(rows), n_rows, dim, static_cast<float *>(out), out_stride);
+    hipLaunchKernelGGL((k_quant_read_rows<float>), grid, dim3(256), 0, st, rows_quant(rows), n_rows, dim, lanes, static_cast<float *>(out), out_stride);
   HSD_LAUNCH_CHECK();
   return HSD_OK;
 }

@@ -38,8 +38,20 @@ WeightQuant weight_quant(const hsd_weight_quant *w) {
 
 template <typename TX, typename TR>
 int launch_norm(hipStream_t st, const NormRows &a, const void *x, const void *res, void *sum) {
-  hipLaunchKernelGGL((k_quant_rows<TX, TR>), dim3(static_cast<unsigned>(a.n_rows)), dim3(256), 0, st, a, static_cast<const TX *>(x),
-                     static_cast<const TR *>(res), static_cast<TR *>(sum));
+  const TX *px = static_cast<const TX *>(x);
+  const TR *pr = static_cast<const TR *>(res);
+  TR *ps = static_cast<TR *>(sum);
+  auto launch = [&](auto kern, int wpr) {
+    const int rows = std::max(4 / wpr, 1);   // of a workgroup; one where it takes several waves
+    const int per = wpr == 1 ? rows : 1;
+    hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>((a.n_rows + per - 1) / per)), dim3(64 * wpr * per), 0, st, a, wpr, px, pr, ps);
+  };
+  // few rows: a lane's eight columns at a time, so that a row is short; many: up to 32, so that a row is a wave's own
+  const int waves1 = (a.dim + 511) / 512, waves2 = (a.dim + 1023) / 1024, waves4 = (a.dim + 2047) / 2048;
+  if (waves1 == 1 || (waves1 <= 16 && a.n_rows * waves1 <= 1024)) launch(k_quant_rows<TX, TR, 1>, waves1);
+  else if (waves2 == 1) launch(k_quant_rows<TX, TR, 2>, 1);
+  else if (waves4 <= 16) launch(k_quant_rows<TX, TR, 4>, waves4);
+  else launch(k_quant_rows<TX, TR, 0>, 16);
   HSD_LAUNCH_CHECK();
   return HSD_OK;
 }
@@ -57,8 +69,8 @@ int launch_product(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int
   if (attr_rc != hipSuccess) return HSD_EHIP;
   constexpr int COLS = GATED ? Cfg::BN / 2 : Cfg::BN;
   const int64_t tiles = static_cast<int64_t>((M + Cfg::BM - 1) / Cfg::BM) * ((N + COLS - 1) / COLS);
-  if (tiles > INT32_MAX / (64 * Cfg::NW)) return HSD_ERANGE;
-  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(tiles)), dim3(64 * Cfg::NW), Cfg::kLds, st, a, w, M, N, nk, out, out_stride, q);
+  if (tiles > INT32_MAX / (64 * Cfg::NW * Cfg::G)) return HSD_ERANGE;
+  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(tiles)), dim3(64 * Cfg::NW * Cfg::G), Cfg::kLds, st, a, w, M, N, nk, out, out_stride, q);
   HSD_LAUNCH_CHECK();
   return HSD_OK;
 }
@@ -94,10 +106,11 @@ int run_linear(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, 
   const char *e = getenv("HSD_QCFG");
   const int cfg = e ? atoi(e) : -1;
 #define TRY(ok, id, ...) if constexpr (ok) { if (cfg == id) return launch_product<ProductTile<__VA_ARGS__>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none); }
-  TRY(!FLOATS && !EXACT, 0, 256, 256, 2, 2, 1, 4)
   TRY(!FLOATS && !EXACT, 6, 256, 256, 2, 2, 2, 2)
-  TRY(!FLOATS && !EXACT, 7, 256, 256, 2, 4, 1, 4)
   TRY(!EXACT, 1, 256, 128, 4, 2, 2, 3)
+  TRY(!FLOATS && !EXACT, 12, 128, 256, 2, 2, 1, 3)
+  TRY(!FLOATS && !EXACT, 13, 256, 128, 2, 2, 1, 3)
+  TRY(!FLOATS && !EXACT, 14, 128, 256, 2, 2, 2, 2)
   TRY(!EXACT, 4, 128, 256, 2, 4, 2, 3)
   TRY(!EXACT, 11, 256, 128, 4, 2, 1, 6)
   if (cfg == 20) return launch_few_rows<FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride);
@@ -106,6 +119,16 @@ int run_linear(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, 
   TRY(true, 3, 64, 128, 2, 2, 2, 6)
   TRY(true, 9, 64, 128, 2, 2, 2, 3)
   TRY(true, 5, 64, 64, 2, 2, 2, 4)
+  if (nk % 2 == 0) {
+  TRY(true, 30, 64, 128, 2, 2, 2, 3, 2)
+  TRY(true, 31, 64, 128, 2, 2, 2, 2, 2)
+  TRY(true, 32, 64, 64, 2, 2, 2, 4, 2)
+  TRY(true, 33, 64, 64, 2, 2, 2, 2, 2)
+  TRY(true, 35, 128, 128, 2, 2, 2, 2, 2)
+  }
+  if (nk % 4 == 0) {
+  TRY(true, 34, 64, 64, 2, 2, 2, 2, 4)
+  }
   TRY(true, 10, 64, 64, 2, 2, 2, 8)
 #endif
   if (M <= 16 || (M <= 64 && quant_tiles(M, N, 64, 64) < 128)) return launch_few_rows<FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride);
@@ -126,9 +149,9 @@ int run_gated(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, i
 #define TRYG(ok, id, ...) if constexpr (ok) { if (cfg == id) return launch_product<ProductTile<__VA_ARGS__>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q); }
   TRYG(true, 9, 64, 256, 1, 4, 2, 2)
   if (cfg == 20) return launch_few<true, FLOATS, false, 1, bf16>(st, a, w, M, N, nk, none, 0, q);
-  TRYG(!FLOATS, 0, 256, 256, 2, 2, 1, 4)
   TRYG(!FLOATS, 6, 256, 256, 2, 2, 2, 2)
-  TRYG(!FLOATS, 7, 256, 256, 2, 4, 1, 4)
+  TRYG(!FLOATS, 12, 128, 256, 2, 2, 1, 3)
+  TRYG(!FLOATS, 14, 128, 256, 2, 2, 2, 2)
   TRYG(true, 4, 128, 256, 2, 4, 2, 3)
   TRYG(true, 1, 128, 256, 2, 4, 1, 6)
   TRYG(true, 3, 64, 256, 1, 4, 2, 3)

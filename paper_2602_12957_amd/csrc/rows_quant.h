@@ -86,58 +86,88 @@ struct NormRows {
   RowsQuant out;
 };
 
-// y = h * gain / sqrt(mean(h^2) + eps), h = x + residual, to 8 bits; h to `sum`.  One workgroup a row.
-template <typename TX, typename TR>
-__global__ void __launch_bounds__(256) k_quant_rows(const NormRows a, const TX *x, const TR *res, TR *sum) {
-  __shared__ float part[4];
-  const int t = threadIdx.x;
-  const int64_t r = blockIdx.x;
+// y = h * gain / sqrt(mean(h^2) + eps), h = x + residual, to 8 bits; h to `sum`.  `wpr` waves a row, its values in registers between the
+// two looks at them: 8 R a lane (a lane has 8 neighbouring columns of each 512 wpr; 16 lanes a block).  R = 0: any width, read
+// twice.  Grid: rows / (blockDim / (64 wpr)).
+template <typename TX, typename TR, int R>
+__global__ void __launch_bounds__(1024) k_quant_rows(const NormRows a, int wpr, const TX *x, const TR *res, TR *sum) {
+  __shared__ float part[16];
+  const int t = threadIdx.x, in_row = t % (64 * wpr), step = 512 * wpr;
+  const int64_t r = static_cast<int64_t>(blockIdx.x) * (blockDim.x / (64 * wpr)) + t / (64 * wpr);
+  if (r >= a.n_rows) return;   // (whole waves; with more than one a row a workgroup has one row)
   const TX *xr = x + r * a.x_stride;
   const TR *rr = res ? res + r * a.res_stride : nullptr;
   TR *sr = sum ? sum + r * a.sum_stride : nullptr;
   const int width = (a.dim + kQuantBlock - 1) / kQuantBlock * kQuantBlock;
-  float rstd = 1.f;
-  if (a.norm) {
-    float ss = 0.f;
-    for (int c = 8 * t; c < width; c += 2048) {
-      float h[8], g[8];
-      load8(xr, c, a.dim, h);
-      if (rr) load8(rr, c, a.dim, g);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float v = rr ? h[i] + g[i] : h[i];
-        ss = __builtin_fmaf(v, v, ss);
-      }
-    }
-    ss = wave_sum(ss);
-    if ((t & 63) == 0) part[t >> 6] = ss;
-    __syncthreads();
-    ss = part[0] + part[1] + part[2] + part[3];
-    rstd = ss < INFINITY ? 1.f / sqrtf(__builtin_fmaf(ss, a.inv_dim, a.eps)) : NAN;
-  }
-  for (int c = 8 * t; c < width; c += 2048) {
-    float h[8], g[8];
+  auto take = [&](int c, float *h) {
     load8(xr, c, a.dim, h);
     if (rr) {
+      float g[8];
       load8(rr, c, a.dim, g);
 #pragma unroll
       for (int i = 0; i < 8; ++i) h[i] += g[i];
     }
-    if (sr) store8(sr, c, a.dim, h);
-    if (a.norm) {
-      if (a.gain) load8(a.gain, c, a.dim, g);
+  };
+  float h[R ? R : 1][8], gain[R ? R : 1][8], ss = 0.f, rstd = 1.f;
+  auto square = [&](const float *v) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) h[i] = c + i < a.dim ? h[i] * rstd * (a.gain ? g[i] : 1.f) : 0.f;
+    for (int i = 0; i < 8; ++i) ss = __builtin_fmaf(v[i], v[i], ss);
+  };
+  if constexpr (R > 0) {
+#pragma unroll
+    for (int k = 0; k < R; ++k)
+      if (8 * in_row + k * step < width) take(8 * in_row + k * step, h[k]);
+    if (a.gain) {
+#pragma unroll
+      for (int k = 0; k < R; ++k)
+        if (8 * in_row + k * step < width) load8(a.gain, 8 * in_row + k * step, a.dim, gain[k]);
     }
-    store_codes8(a.out, r, c, h);
+  }
+  if (a.norm) {
+    if constexpr (R > 0) {
+#pragma unroll
+      for (int k = 0; k < R; ++k)
+        if (8 * in_row + k * step < width) square(h[k]);
+    } else {
+      for (int c = 8 * in_row; c < width; c += step) take(c, h[0]), square(h[0]);
+    }
+    ss = wave_sum(ss);
+    if (wpr > 1) {
+      if ((t & 63) == 0) part[t >> 6] = ss;
+      __syncthreads();
+      ss = 0.f;
+      for (int k = 0; k < wpr; ++k) ss += part[k];
+    }
+    rstd = ss < INFINITY ? 1.f / sqrtf(__builtin_fmaf(ss, a.inv_dim, a.eps)) : NAN;
+  }
+  auto give = [&](int c, float *v, const float *g) {
+    if (sr) store8(sr, c, a.dim, v);
+    if (a.norm) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = c + i < a.dim ? v[i] * rstd * (a.gain ? g[i] : 1.f) : 0.f;
+    }
+    store_codes8(a.out, r, c, v);
+  };
+  if constexpr (R > 0) {
+#pragma unroll
+    for (int k = 0; k < R; ++k)
+      if (8 * in_row + k * step < width) give(8 * in_row + k * step, h[k], gain[k]);
+  } else {
+    for (int c = 8 * in_row; c < width; c += step) {
+      take(c, h[0]);
+      if (a.gain) load8(a.gain, c, a.dim, gain[0]);
+      give(c, h[0], gain[0]);
+    }
   }
 }
 
 // The values of rows in 8 bits (exact in both types)
+// (`lanes` of a workgroup's 256 threads a row, a power of two)
 template <typename T>
-__global__ void __launch_bounds__(256) k_quant_read_rows(const RowsQuant q, int64_t n_rows, int dim, T *out, int64_t out_stride) {
-  const int64_t r = blockIdx.x;
-  for (int c = 8 * threadIdx.x; c < dim; c += 2048) {
+__global__ void __launch_bounds__(256) k_quant_read_rows(const RowsQuant q, int64_t n_rows, int dim, int lanes, T *out, int64_t out_stride) {
+  const int64_t r = static_cast<int64_t>(blockIdx.x) * (256 / lanes) + threadIdx.x / lanes;
+  if (r >= n_rows) return;
+  for (int c = 8 * (threadIdx.x & (lanes - 1)); c < dim; c += 8 * lanes) {
     const uint2 w = *reinterpret_cast<const uint2 *>(q.codes + r * q.code_stride + c);
     const float s = two_to_byte(q.scale[r * q.scale_stride + c / kQuantBlock]);
     float v[8];
