@@ -56,33 +56,27 @@ __device__ __forceinline__ void quant_wait() {
   asm volatile("" ::: "memory");
 }
 
-// A tile of BM rows by BN weight rows, WM by WN waves; operands in a ring of S slices of 64 Q columns.  G groups of such waves share out the
-// blocks of columns, with a ring each; their sums are joined at the end.
-template <int BM_, int BN_, int WM_, int WN_, int Q_, int S_, int G_ = 1>
+// A tile of BM rows by BN weight rows, WM by WN waves; operands in a ring of S slices, each a block of 128 columns.  A step between two
+// looks at LDS is half a block (H = 1) or a whole one (H = 2).  ASK: as many waves again that only request.
+template <int BM_, int BN_, int WM_, int WN_, int S_, int H_ = 1, bool ASK_ = false>
 struct ProductTile {
-  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NW = WM_ * WN_, Q = Q_, S = S_, G = G_;
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NW = WM_ * WN_, S = S_, H = H_;
+  static constexpr bool ASK = ASK_;
   static constexpr int TA = BM / WM / 32, TW = BN / WN / 32;      // 32x32 sub-tiles of a wave: rows, weight rows
-  static constexpr int kRow = 64 * Q;                             // bytes of a row in a slice
-  static constexpr int kScales = NW * 256;                        // the rows' bytes of four blocks, behind the codes
-  static constexpr int kSlice = (BM + BN) * kRow + kScales;
-  static constexpr int kPerLoad = 1024 / kRow;                    // rows of a 1 KB load
-  static constexpr int kLoadsA = BM / kPerLoad / NW, kLoadsW = BN / kPerLoad / NW, kLoads = kLoadsA + kLoadsW;   // of a wave and slice
-  static constexpr int kPass = 2 < BN / WN / 32 ? 2 : BN / WN / 32;   // sub-tiles of columns that a wave stores at a time
-  static constexpr int kRing = S * kSlice;
+  static constexpr int kSlice = (BM + BN) * kQuantBlock;
+  static constexpr int kScales = NW * 256;                        // the rows' bytes of four blocks, in a ring of their own behind the slices
+  static constexpr int kWords = (S + 3) / 4 + 1;                  // ... of so many: those of the blocks under way
+  static constexpr int kLoadsA = BM / 8 / NW, kLoadsW = BN / 8 / NW, kLoads = kLoadsA + kLoadsW;   // 1 KB loads of a wave and slice
+  static constexpr int kPass = TW < 2 ? TW : 2;                   // sub-tiles of columns that a wave stores at a time
+  static constexpr int kRing = S * kSlice, kLds = kRing + (kWords + 1) * kScales, kThreads = 64 * NW * (ASK ? 2 : 1);
   static constexpr int out_bytes(bool gated, int size) {          // of results on their way
     return gated ? WM * 32 * (kQuantBlock + 16) + BM * WN * 4 : NW * 32 * (kPass * 32 * size + 16);
   }
-  static constexpr int kLds = G * kRing;
-  static constexpr int group_a = kLoadsA % 4 == 0 ? 4 : kLoadsA % 2 == 0 ? 2 : 1;                       // loads that go together
-  static constexpr int group_w(bool gated) {                                                          // (of one projection)
-    const int most = gated ? 32 / kPerLoad : 4;
-    return kLoadsW % 4 == 0 && most >= 4 ? 4 : kLoadsW % 2 == 0 && most >= 2 ? 2 : 1;
-  }
-  static constexpr int kWaves = BM * BN / NW > 128 * 64 ? 1 : G > 2 ? G : 2;  // of a SIMD
-  static_assert(G == 1 || (Q == 2 && NW == 4 && (G - 1) * BM * BN * 4 + 32 * 1024 <= G * kRing), "sums are joined in the rings' place");
-  static_assert(Q == 1 || Q == 2, "a slice is a block of 128 columns or half of one");
-  static_assert(BM / kPerLoad % NW == 0 && BN / kPerLoad % NW == 0 && BM <= 64 * NW, "loads divide evenly");
-  static_assert(S >= 2 && (S - 1) * (kLoads + 1) < 64 && kRing <= 160 * 1024, "slices in flight");
+  static constexpr int kGroupA = kLoadsA % 4 == 0 ? 4 : kLoadsA % 2 == 0 ? 2 : 1, kGroupW = kLoadsW % 4 == 0 ? 4 : kLoadsW % 2 == 0 ? 2 : 1;   // loads that go together
+  static constexpr int kWaves = BM * BN / NW > 128 * 64 ? 1 : 2;  // of a SIMD
+  static_assert(H == 1 || H == 2, "half a block or a whole one");
+  static_assert(BM / 8 % NW == 0 && BN / 8 % NW == 0 && BM <= 64 * NW, "loads divide evenly");
+  static_assert(S >= 2 && (S - 1) * (kLoads + 1) < 64 && kLds <= 160 * 1024, "slices in flight");
 };
 
 // Tile of a workgroup: XCD x (workgroup id mod 8) takes a contiguous run of an order that goes through bands of eight tiles of rows,
@@ -126,63 +120,85 @@ __device__ __forceinline__ void lds_barrier() {
 // GATED: gate and up rows of 128 output columns (BN = 256), silu(gate) * up to 8 bits; else out.  FLOATS: weight scales are floats.
 // EXACT: bf16 products of the codes instead of the 8-bit ones.  Grid: tiles.
 template <typename Cfg, bool GATED, bool FLOATS, bool EXACT, typename T>
-__global__ void __launch_bounds__(64 * Cfg::NW * Cfg::G, Cfg::kWaves) k_gemm_quant(const RowsQuant a, const WeightQuant w, int M, int N, int nk, T *__restrict__ out,
+__global__ void __launch_bounds__(Cfg::kThreads, Cfg::kWaves) k_gemm_quant(const RowsQuant a, const WeightQuant w, int M, int N, int nk, T *__restrict__ out,
                                                                           int64_t out_stride, const RowsQuant q) {
-  constexpr int BM = Cfg::BM, BN = Cfg::BN, TA = Cfg::TA, TW = Cfg::TW, NW = Cfg::NW, G = Cfg::G;
+  constexpr int BM = Cfg::BM, BN = Cfg::BN, TA = Cfg::TA, TW = Cfg::TW, NW = Cfg::NW, S = Cfg::S, H = Cfg::H;
   constexpr int COLS = GATED ? BN / 2 : BN;
   static_assert(!GATED || (COLS == kQuantBlock && TW % 2 == 0), "a workgroup has whole blocks of the rows that it rounds");
-  static_assert(Cfg::out_bytes(GATED, sizeof(T)) <= Cfg::kRing, "results are staged in the operands' place");
+  static_assert(Cfg::out_bytes(GATED, sizeof(T)) <= Cfg::kLds, "results are staged in the operands' place");
   extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
-  const int group = G > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / (64 * NW)) : 0;
-  const int t = threadIdx.x - group * 64 * NW, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);   // of the group
+  const bool asks = Cfg::ASK && threadIdx.x >= 64 * NW;
+  const int t = threadIdx.x - (asks ? 64 * NW : 0), lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int wi = wave / Cfg::WN, wj = wave % Cfg::WN;
-  unsigned char *const ring = smem_raw + group * Cfg::kRing;
   int tm, tn;
   quant_tile_of(blockIdx.x, (M + BM - 1) / BM, (N + COLS - 1) / COLS, tm, tn);
   const int m0 = tm * BM, n0 = tn * COLS;
 
-  // ---- loads.  A wave's load j of a slice covers the RPL tile rows from RPL (wave kLoads + j) on (rows, and weight rows); lane l fetches, for row l / LPW
-  // of them, the 16-byte piece that belongs at position l % LPW: a row's pieces lie XORed by the row, so that reads of 16 rows cover all banks.
+  // ---- loads.  A wave's load j of a slice covers the eight tile rows from 8 (wave kLoads + j) on (rows, and weight rows); lane l fetches, for row l / 8 of
+  // them, the 16-byte piece that belongs at position l % 8: a row's pieces lie XORed by the row, so that reads of 16 rows cover all banks.
   // Rows behind the last one are that one again (their products are never stored).  Gate and up alternate by 32 rows: weight row
   // 64 g + 32 u + x of the tile is row n0 + 32 g + x of the gate or of the up projection.
-  constexpr int Q = Cfg::Q, S = Cfg::S, RPL = Cfg::kPerLoad, LPW = Cfg::kRow / 16, SHIFT = Q == 2 ? 1 : 2;
-  constexpr int GA = Cfg::group_a, GW = Cfg::group_w(GATED);
-  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char *)ring));
+  constexpr int GA = Cfg::kGroupA, GW = Cfg::kGroupW;
+  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char *)smem_raw));
   const uint64_t base_a = reinterpret_cast<uint64_t>(a.codes) + m0 * a.code_stride - kLoadBias;
   const uint64_t base_w = reinterpret_cast<uint64_t>(w.codes) + n0 * w.code_stride - kLoadBias, up_rows = GATED ? N * w.code_stride : 0;
   uint32_t off_a[Cfg::kLoadsA], off_w[Cfg::kLoadsW];
 #pragma unroll
   for (int j = 0; j < Cfg::kLoadsA; ++j) {
-    const int r = (wave * Cfg::kLoadsA + j) * RPL + lane / LPW;
-    off_a[j] = min(r, M - 1 - m0) * static_cast<uint32_t>(a.code_stride) + ((lane ^ (r >> SHIFT)) % LPW) * 16 + kLoadBias - j % GA * 1024;
+    const int r = (wave * Cfg::kLoadsA + j) * 8 + (lane >> 3);
+    off_a[j] = min(r, M - 1 - m0) * static_cast<uint32_t>(a.code_stride) + ((lane ^ (r >> 1)) & 7) * 16 + kLoadBias - j % GA * 1024;
   }
 #pragma unroll
   for (int j = 0; j < Cfg::kLoadsW; ++j) {
-    const int r = (wave * Cfg::kLoadsW + j) * RPL + lane / LPW, row = GATED ? (r >> 6) * 32 + (r & 31) : min(r, N - 1 - n0);
-    off_w[j] = row * static_cast<uint32_t>(w.code_stride) + ((lane ^ (r >> SHIFT)) % LPW) * 16 + kLoadBias - j % GW * 1024;
+    const int r = (wave * Cfg::kLoadsW + j) * 8 + (lane >> 3), row = GATED ? (r >> 6) * 32 + (r & 31) : min(r, N - 1 - n0);
+    off_w[j] = row * static_cast<uint32_t>(w.code_stride) + ((lane ^ (r >> 1)) & 7) * 16 + kLoadBias - j % GW * 1024;
   }
-  const uint64_t scales_a = reinterpret_cast<uint64_t>(a.scale) + min(m0 + t, M - 1) * a.scale_stride;   // (of row t; behind the tile's rows nobody reads)
-  const int mine = nk / G, slices = mine * (2 / Q);   // blocks of the group: group, group + G, ...
+  // row t's bytes (lanes behind the tile's rows all take one word: a load's 64 lanes cost what the lines that they touch do)
+  const uint64_t scales_a = reinterpret_cast<uint64_t>(a.scale) + m0 * a.scale_stride, off_s = t < BM ? min(t, M - 1 - m0) * a.scale_stride : 0;
   constexpr int LOADS = Cfg::kLoads + 1, REQUESTS = Cfg::kLoadsA / GA + Cfg::kLoadsW / GW + 1;
-  auto request = [&](int slice, uint32_t place, int j) {   // request j of a slice into its place
-    const int col = (slice * G + group) * Cfg::kRow;
+  auto request = [&](int kb, uint32_t place, int j) {   // request j of block kb into a slice's place
+    const int col = kb * kQuantBlock;
     if (j < Cfg::kLoadsA / GA) {
       lds_load<GA>(place + (wave * Cfg::kLoadsA + j * GA) * 1024, base_a + col, off_a + j * GA);
     } else if (j < REQUESTS - 1) {
       const int k = (j - Cfg::kLoadsA / GA) * GW;
-      const bool up = GATED && (((wave * Cfg::kLoadsW + k) * RPL) >> 5 & 1);
-      lds_load<GW>(place + BM * Cfg::kRow + (wave * Cfg::kLoadsW + k) * 1024, base_w + (up ? up_rows : 0) + col, off_w + k);
+      const bool up = GATED && ((wave * Cfg::kLoadsW + k) >> 2 & 1);
+      lds_load<GW>(place + BM * kQuantBlock + (wave * Cfg::kLoadsW + k) * 1024, base_w + (up ? up_rows : 0) + col, off_w + k);
     } else {
-      lds_load_256(place + (BM + BN) * Cfg::kRow + wave * 256, scales_a + ((slice / (2 / Q) * G + group) & ~3));
+      // the rows' bytes come by words, with the first of a word's blocks; otherwise one word for all, to the place behind, so that
+      // every slice has as many loads
+      const bool fresh = (kb & 3) == 0;
+      lds_load_256(lds0 + Cfg::kRing + (fresh ? (kb >> 2) % Cfg::kWords : Cfg::kWords) * Cfg::kScales + wave * 256,
+                   scales_a + (kb & ~3) + (off_s & (fresh ? ~uint64_t{0} : 0)));
     }
   };
+  constexpr int LATER = (S - 2) * LOADS;   // loads of the slices that may still be in flight when the next one is needed
+  if (!Cfg::ASK || asks) {
 #pragma unroll
-  for (int s = 0; s < S; ++s)
+    for (int s = 0; s < S; ++s)
 #pragma unroll
-    for (int j = 0; j < REQUESTS; ++j) request(min(s, slices - 1), lds0 + s * Cfg::kSlice, j);
+      for (int j = 0; j < REQUESTS; ++j) request(min(s, nk - 1), lds0 + s * Cfg::kSlice, j);
+  }
+  if constexpr (Cfg::ASK) {
+    if (asks) {   // passes the barriers that the others pass
+      quant_wait<LATER + LOADS>();
+      __builtin_amdgcn_s_barrier();
+      for (int kt = 0, at = 0; kt < nk; ++kt) {
+        quant_wait<LATER>();
+        __builtin_amdgcn_s_barrier();
+        const uint32_t place = lds0 + at * Cfg::kSlice;
+        at = at + 1 == S ? 0 : at + 1;
+#pragma unroll
+        for (int j = 0; j < REQUESTS; ++j) request(min(kt + S, nk - 1), place, j);
+      }
+      quant_wait<0>();
+      __builtin_amdgcn_s_barrier();
+      return;
+    }
+  }
 
   // ---- scales.  The weights' come through the scalar unit, a block ahead (vector loads would be waited for with all the slices behind them).
-  uint32_t sa[TA], sa_next[TA], ws_now[2] = {0, 0}, ws_next[2] = {0, 0};
+  uint32_t sa[TA], sa_next[TA], ws_now[2] = {0, 0}, ws_next[2] = {0, 0}, ws_byte[2];
   const int64_t wrow = GATED ? n0 : min(n0 + wj * (BN / Cfg::WN), N - 1);   // a wave's weight rows lie in one block of 128, or in one of the gate and one of up
   const int64_t ws_at[2] = {wrow / kQuantBlock * w.scale_stride, (wrow + N) / kQuantBlock * w.scale_stride};
   auto weight_scales = [&](int kb) {
@@ -190,8 +206,8 @@ __global__ void __launch_bounds__(64 * Cfg::NW * Cfg::G, Cfg::kWaves) k_gemm_qua
     for (int i = 0; i < (GATED ? 2 : 1); ++i) {
       typedef const __attribute__((address_space(4))) uint32_t *Const;
       const uint64_t p = reinterpret_cast<uint64_t>(w.scale) + (FLOATS ? 4 : 1) * (ws_at[i] + kb);
-      const uint32_t v = *reinterpret_cast<Const>(p & ~uint64_t{3});   // (a byte's word)
-      ws_next[i] = FLOATS ? v : v >> (8 * (p & 3)) & 255;
+      ws_next[i] = *reinterpret_cast<Const>(p & ~uint64_t{3});   // (a byte's word; it is looked at a block later, and so are the rows' words)
+      ws_byte[i] = 8 * (p & 3);
     }
   };
 
@@ -206,64 +222,66 @@ __global__ void __launch_bounds__(64 * Cfg::NW * Cfg::G, Cfg::kWaves) k_gemm_qua
 
   // ---- fragments: row lane % 32 of a sub-tile, of its 64 bytes of a half block the 32 of lane / 32
   const int fr = lane & 31, kg = lane >> 5;
-  int off_f[2 * Q];
+  int off_f[4];
 #pragma unroll
-  for (int p = 0; p < 2 * Q; ++p) off_f[p] = fr * Cfg::kRow + (((p >> 1) * 4 + kg * 2 + (p & 1)) ^ ((fr >> SHIFT) % LPW)) * 16;
-  const int row_a = wi * (BM / Cfg::WM) * Cfg::kRow, row_w = (BM + wj * (BN / Cfg::WN)) * Cfg::kRow;
-  i32x8 fa[2][TA], fw[2][TW];
+  for (int p = 0; p < 4; ++p) off_f[p] = fr * kQuantBlock + (((p >> 1) * 4 + kg * 2 + (p & 1)) ^ ((fr >> 1) & 7)) * 16;
+  const int row_a = wi * (BM / Cfg::WM) * kQuantBlock, row_w = (BM + wj * (BN / Cfg::WN)) * kQuantBlock;
+  i32x8 fa[2][H][TA], fw[2][H][TW];
   auto fragment = [&](const unsigned char *p, int half) {
     const i32x4 lo = *reinterpret_cast<const i32x4 *>(p + off_f[2 * half]), hi = *reinterpret_cast<const i32x4 *>(p + off_f[2 * half + 1]);
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   };
-  auto read = [&](int buf, const unsigned char *p, int half, int n) {   // fragment n of a half block: weights, then rows
-    if (n < TW) fw[buf][n] = fragment(p + row_w + n * 32 * Cfg::kRow, half);
-    else fa[buf][n - TW] = fragment(p + row_a + (n - TW) * 32 * Cfg::kRow, half);
+  auto read = [&](int buf, const unsigned char *p, int half, int n) {   // fragment n of a step's (weights, then rows), from half block `half` on
+    const int h = n / (TA + TW), k = n % (TA + TW);
+    if (k < TW) fw[buf][h][k] = fragment(p + row_w + k * 32 * kQuantBlock, half + h);
+    else fa[buf][h][k - TW] = fragment(p + row_a + (k - TW) * 32 * kQuantBlock, half + h);
   };
-  auto row_scales = [&](const unsigned char *p, int kb) {
+  auto row_scales = [&](int kb) {   // words of block kb (looked at when it begins)
+    const unsigned char *p = smem_raw + Cfg::kRing + (kb >> 2) % Cfg::kWords * Cfg::kScales;
 #pragma unroll
-    for (int i = 0; i < TA; ++i)
-      sa_next[i] = *reinterpret_cast<const uint32_t *>(p + (BM + BN) * Cfg::kRow + (wi * (BM / Cfg::WM) + i * 32 + fr) * 4) >> (8 * (kb & 3));
+    for (int i = 0; i < TA; ++i) sa_next[i] = *reinterpret_cast<const uint32_t *>(p + (wi * (BM / Cfg::WM) + i * 32 + fr) * 4);
   };
-  // The products of a half block, with what else the step has to do dealt out between them
-  constexpr int PRODUCTS = TA * TW, FRAGS = TA + TW;
-  auto step = [&](int buf, auto &&other, int others) {
+  // The products of a step, with what else it has to do dealt out between them; `begin`: it begins a block
+  constexpr int PRODUCTS = TA * TW, FRAGS = H * (TA + TW), OWN = Cfg::ASK ? 0 : REQUESTS;   // (requests among the products)
+  auto step = [&](int buf, bool begin, auto &&other, int others) {
     Fragment16 cw[EXACT ? TW : 1], ca;
-    if constexpr (EXACT) {
 #pragma unroll
-      for (int i = 0; i < TW; ++i) cw[i] = widen(fw[buf][i], FLOATS ? 1.f : two_to_byte(ws_now[GATED ? i & 1 : 0]));
-    }
+    for (int n = 0; n < H * PRODUCTS; ++n) {
+      const int h = n / PRODUCTS, j = n % PRODUCTS / TW, i = n % TW;
+      if constexpr (EXACT) {
+        if (n % PRODUCTS == 0) {
 #pragma unroll
-    for (int n = 0; n < PRODUCTS; ++n) {
-      const int j = n / TW, i = n % TW;
+          for (int k = 0; k < TW; ++k) cw[k] = widen(fw[buf][h][k], FLOATS ? 1.f : two_to_byte(ws_now[GATED ? k & 1 : 0]));
+        }
+      }
       if constexpr (FLOATS) {
-        if (buf == 0) add_block(i, j), block[i][j] = zero;
+        if (begin && h == 0) add_block(i, j), block[i][j] = zero;
       }
       floatx16 &sum = FLOATS ? block[FLOATS ? i : 0][FLOATS ? j : 0] : acc[i][j];
       if constexpr (EXACT) {
-        if (i == 0) ca = widen(fa[buf][j], two_to_byte(sa[j] & 255));
+        if (i == 0) ca = widen(fa[buf][h][j], two_to_byte(sa[j] & 255));
 #pragma unroll
         for (int k = 0; k < 4; ++k) sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cw[i].v[k], ca.v[k], sum, 0, 0, 0);
       } else {
-        sum = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fw[buf][i], fa[buf][j], sum, 0, 0, 0, FLOATS ? 127 : ws_now[GATED ? i & 1 : 0], 0, sa[j]);
+        sum = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fw[buf][h][i], fa[buf][h][j], sum, 0, 0, 0, FLOATS ? 127 : ws_now[GATED ? i & 1 : 0], 0, sa[j]);
       }
-      for (int k = n * others / PRODUCTS; k < (n + 1) * others / PRODUCTS; ++k) other(k);
+      for (int k = n * others / (H * PRODUCTS); k < (n + 1) * others / (H * PRODUCTS); ++k) other(k);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
 
-  constexpr int LATER = (S - 2) * LOADS;   // loads of the slices that may still be in flight when the next one is needed
   // What precedes the last step of a slice: all waves have read it, and the next one is complete
   auto turn = [&]() {
-    quant_wait<LATER>();
+    quant_wait<Cfg::ASK ? 63 : LATER>();
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
   };
-  weight_scales(group);
-  quant_wait<LATER + LOADS>();
+  weight_scales(0);
+  quant_wait<Cfg::ASK ? 63 : LATER + LOADS>();
   __builtin_amdgcn_s_barrier();
 #pragma unroll
-  for (int n = 0; n < FRAGS; ++n) read(0, ring, 0, n);
-  row_scales(ring, group);
+  for (int n = 0; n < FRAGS; ++n) read(0, smem_raw, 0, n);
+  row_scales(0);
   int at = 0;   // place of the slice at hand
 #pragma unroll
   for (int i = 0; i < TW; ++i)
@@ -272,37 +290,34 @@ __global__ void __launch_bounds__(64 * Cfg::NW * Cfg::G, Cfg::kWaves) k_gemm_qua
       acc[i][j] = zero;
       if constexpr (FLOATS) block[i][j] = zero;
     }
-  for (int kt = 0; kt < mine; ++kt) {
+  auto begin_block = [&](int kt) {   // scales of the block at hand, and the next one's requested
     if constexpr (FLOATS) factor[0] = __uint_as_float(ws_now[0]), factor[1] = __uint_as_float(ws_now[1]);
-    ws_now[0] = ws_next[0], ws_now[1] = ws_next[1];
-    const int kb_next = min(kt + 1, mine - 1) * G + group;
-    weight_scales(kb_next);
 #pragma unroll
-    for (int i = 0; i < TA; ++i) sa[i] = sa_next[i];
+    for (int i = 0; i < (GATED ? 2 : 1); ++i) ws_now[i] = FLOATS ? ws_next[i] : ws_next[i] >> ws_byte[i] & 255;
+#pragma unroll
+    for (int i = 0; i < TA; ++i) sa[i] = sa_next[i] >> (8 * (kt & 3));
+    weight_scales(min(kt + 1, nk - 1));
     __builtin_amdgcn_sched_barrier(0);
-    // (behind the last slices the requests and reads are of the last one, or of an older one's place: nothing looks at them)
-    if constexpr (Q == 2) {
-      const unsigned char *here = ring + at * Cfg::kSlice;
-      const uint32_t place = lds0 + at * Cfg::kSlice;
-      at = at + 1 == S ? 0 : at + 1;
-      const unsigned char *next = ring + at * Cfg::kSlice;
-      step(0, [&](int k) { read(1, here, 1, k); }, FRAGS);
-      turn();
-      const int ahead = min(kt + S, slices - 1);
-      row_scales(next, kb_next);
-      step(1, [&](int k) { if (k < REQUESTS) request(ahead, place, k); else read(0, next, 0, k - REQUESTS); }, REQUESTS + FRAGS);
-    } else {
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const uint32_t place = lds0 + at * Cfg::kSlice;
-        at = at + 1 == S ? 0 : at + 1;
-        const unsigned char *next = ring + at * Cfg::kSlice;
-        turn();
-        const int ahead = min(2 * kt + half + S, slices - 1);
-        if (half == 1) row_scales(next, kb_next);
-        step(half, [&](int k) { if (k < REQUESTS) request(ahead, place, k); else read(half ^ 1, next, 0, k - REQUESTS); }, REQUESTS + FRAGS);
-      }
-    }
+  };
+  // Block kt; its fragments, or those of its first half, are in registers.  `u`: the set that a whole block is in.
+  // (behind the last blocks the requests and reads are of the last one, or of an older one's place: nothing looks at them)
+  auto do_block = [&](int kt, int u) {
+    begin_block(kt);
+    const unsigned char *here = smem_raw + at * Cfg::kSlice;
+    const uint32_t place = lds0 + at * Cfg::kSlice;
+    at = at + 1 == S ? 0 : at + 1;
+    const unsigned char *next = smem_raw + at * Cfg::kSlice;
+    if constexpr (H == 1) step(0, true, [&](int k) { read(1, here, 1, k); }, FRAGS);
+    turn();
+    const int ahead = min(kt + S, nk - 1), into = H == 1 ? 0 : u ^ 1;
+    row_scales(min(kt + 1, nk - 1));
+    step(H == 1 ? 1 : u, H == 2, [&](int k) { if (k < OWN) request(ahead, place, k); else read(into, next, 0, k - OWN); }, OWN + FRAGS);
+  };
+  if constexpr (H == 1) {
+    for (int kt = 0; kt < nk; ++kt) do_block(kt, 0);
+  } else {
+    for (int kt = 0; kt + 1 < nk; kt += 2) do_block(kt, 0), do_block(kt + 1, 1);
+    if (nk & 1) do_block(nk - 1, 0);
   }
   if constexpr (FLOATS) {
     factor[0] = __uint_as_float(ws_now[0]), factor[1] = __uint_as_float(ws_now[1]);
@@ -315,27 +330,6 @@ __global__ void __launch_bounds__(64 * Cfg::NW * Cfg::G, Cfg::kWaves) k_gemm_qua
   unsigned char *stage = smem_raw;
   quant_wait<0>();   // (of the loads that nothing looks at too: results go through the same memory)
   __builtin_amdgcn_s_barrier();
-  if constexpr (G > 1) {   // the groups' sums, in their order, to the first one's
-    floatx4 *part = reinterpret_cast<floatx4 *>(smem_raw + 32 * 1024);
-    constexpr int PARTS = TW * TA * 4;   // of a lane
-    if (group > 0) {
-#pragma unroll
-      for (int i = 0; i < PARTS; ++i) {
-        const floatx16 &x = acc[i / 4 / TA][i / 4 % TA];
-        part[((group - 1) * PARTS + i) * 64 * NW + t] = floatx4{x[4 * (i & 3)], x[4 * (i & 3) + 1], x[4 * (i & 3) + 2], x[4 * (i & 3) + 3]};
-      }
-    }
-    lds_barrier();
-    if (group > 0) return;
-#pragma unroll
-    for (int k = 0; k < G - 1; ++k)
-#pragma unroll
-      for (int i = 0; i < PARTS; ++i) {
-        const floatx4 x = part[(k * PARTS + i) * 64 * NW + t];
-#pragma unroll
-        for (int v = 0; v < 4; ++v) acc[i / 4 / TA][i / 4 % TA][4 * (i & 3) + v] += x[v];
-      }
-  }
   if constexpr (!GATED) {
     // through LDS (a wave's own), so that adjacent lanes store adjacent pieces of a row
     constexpr int PASS = Cfg::kPass, W = PASS * 32, ROW = W * sizeof(T) + 16, LPR = W * sizeof(T) / 16, PER = 16 / sizeof(T);

@@ -69,8 +69,8 @@ int launch_product(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int
   if (attr_rc != hipSuccess) return HSD_EHIP;
   constexpr int COLS = GATED ? Cfg::BN / 2 : Cfg::BN;
   const int64_t tiles = static_cast<int64_t>((M + Cfg::BM - 1) / Cfg::BM) * ((N + COLS - 1) / COLS);
-  if (tiles > INT32_MAX / (64 * Cfg::NW * Cfg::G)) return HSD_ERANGE;
-  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(tiles)), dim3(64 * Cfg::NW * Cfg::G), Cfg::kLds, st, a, w, M, N, nk, out, out_stride, q);
+  if (tiles > INT32_MAX / Cfg::kThreads) return HSD_ERANGE;
+  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(tiles)), dim3(Cfg::kThreads), Cfg::kLds, st, a, w, M, N, nk, out, out_stride, q);
   HSD_LAUNCH_CHECK();
   return HSD_OK;
 }
@@ -106,38 +106,24 @@ int run_linear(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, 
   const char *e = getenv("HSD_QCFG");
   const int cfg = e ? atoi(e) : -1;
 #define TRY(ok, id, ...) if constexpr (ok) { if (cfg == id) return launch_product<ProductTile<__VA_ARGS__>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none); }
-  TRY(!FLOATS && !EXACT, 6, 256, 256, 2, 2, 2, 2)
-  TRY(!EXACT, 1, 256, 128, 4, 2, 2, 3)
-  TRY(!FLOATS && !EXACT, 12, 128, 256, 2, 2, 1, 3)
-  TRY(!FLOATS && !EXACT, 13, 256, 128, 2, 2, 1, 3)
-  TRY(!FLOATS && !EXACT, 14, 128, 256, 2, 2, 2, 2)
-  TRY(!EXACT, 4, 128, 256, 2, 4, 2, 3)
-  TRY(!EXACT, 11, 256, 128, 4, 2, 1, 6)
+  TRY(!FLOATS && !EXACT, 6, 256, 256, 2, 2, 2)
+  TRY(!EXACT, 1, 256, 128, 4, 2, 3)
+  TRY(true, 8, 128, 128, 2, 2, 2)
   if (cfg == 20) return launch_few_rows<FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride);
-  TRY(true, 2, 128, 128, 2, 2, 2, 4)
-  TRY(true, 8, 128, 128, 2, 2, 2, 2)
-  TRY(true, 3, 64, 128, 2, 2, 2, 6)
-  TRY(true, 9, 64, 128, 2, 2, 2, 3)
-  TRY(true, 5, 64, 64, 2, 2, 2, 4)
-  if (nk % 2 == 0) {
-  TRY(true, 30, 64, 128, 2, 2, 2, 3, 2)
-  TRY(true, 31, 64, 128, 2, 2, 2, 2, 2)
-  TRY(true, 32, 64, 64, 2, 2, 2, 4, 2)
-  TRY(true, 33, 64, 64, 2, 2, 2, 2, 2)
-  TRY(true, 35, 128, 128, 2, 2, 2, 2, 2)
-  }
-  if (nk % 4 == 0) {
-  TRY(true, 34, 64, 64, 2, 2, 2, 2, 4)
-  }
-  TRY(true, 10, 64, 64, 2, 2, 2, 8)
+  TRY(true, 50, 64, 128, 2, 2, 5, 2, true)
+  TRY(true, 51, 64, 128, 2, 2, 3, 2, true)
+  TRY(true, 58, 64, 128, 2, 2, 3, 1, true)
+  TRY(true, 52, 64, 64, 2, 2, 4, 2, true)
+  TRY(!(FLOATS && EXACT), 56, 128, 128, 2, 2, 4, 1, true)
+  TRY(!FLOATS && !EXACT, 54, 128, 128, 2, 2, 4, 2, true)
 #endif
   if (M <= 16 || (M <= 64 && quant_tiles(M, N, 64, 64) < 128)) return launch_few_rows<FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride);
   if constexpr (!FLOATS && !EXACT) {
-    if (quant_tiles(M, N, 256, 256) >= 192) return launch_product<ProductTile<256, 256, 2, 2, 2, 2>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
+    if (quant_tiles(M, N, 256, 256) >= 192) return launch_product<ProductTile<256, 256, 2, 2, 2>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
   }
-  if (quant_tiles(M, N, 128, 128) >= 256) return launch_product<ProductTile<128, 128, 2, 2, 2, 2>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
-  if (quant_tiles(M, N, 64, 128) >= 192) return launch_product<ProductTile<64, 128, 2, 2, 2, 3>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
-  return launch_product<ProductTile<64, 64, 2, 2, 2, 4>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
+  if (quant_tiles(M, N, 128, 128) >= 256) return launch_product<ProductTile<128, 128, 2, 2, 2>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
+  if (quant_tiles(M, N, 64, 128) >= 192) return launch_product<ProductTile<64, 128, 2, 2, 3, 2, true>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
+  return launch_product<ProductTile<64, 64, 2, 2, 4, 2, true>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
 }
 
 template <bool FLOATS>
@@ -147,21 +133,20 @@ int run_gated(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, i
   const char *e = getenv("HSD_QCFG");
   const int cfg = e ? atoi(e) : -1;
 #define TRYG(ok, id, ...) if constexpr (ok) { if (cfg == id) return launch_product<ProductTile<__VA_ARGS__>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q); }
-  TRYG(true, 9, 64, 256, 1, 4, 2, 2)
   if (cfg == 20) return launch_few<true, FLOATS, false, 1, bf16>(st, a, w, M, N, nk, none, 0, q);
-  TRYG(!FLOATS, 6, 256, 256, 2, 2, 2, 2)
-  TRYG(!FLOATS, 12, 128, 256, 2, 2, 1, 3)
-  TRYG(!FLOATS, 14, 128, 256, 2, 2, 2, 2)
-  TRYG(true, 4, 128, 256, 2, 4, 2, 3)
-  TRYG(true, 1, 128, 256, 2, 4, 1, 6)
-  TRYG(true, 3, 64, 256, 1, 4, 2, 3)
+  TRYG(!FLOATS, 6, 256, 256, 2, 2, 2)
+  TRYG(true, 4, 128, 256, 2, 4, 3)
+  TRYG(!FLOATS, 60, 128, 256, 2, 2, 3, 1, true)
+  TRYG(true, 61, 64, 256, 1, 4, 3, 1, true)
+  TRYG(!FLOATS, 62, 64, 256, 1, 4, 3, 2, true)
+  TRYG(true, 3, 64, 256, 1, 4, 3)
 #endif
   if (M <= 16) return launch_few<true, FLOATS, false, 1, bf16>(st, a, w, M, N, nk, none, 0, q);
   if constexpr (!FLOATS) {
-    if (quant_tiles(M, N, 256, 128) >= 192) return launch_product<ProductTile<256, 256, 2, 2, 2, 2>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
+    if (quant_tiles(M, N, 256, 128) >= 192) return launch_product<ProductTile<256, 256, 2, 2, 2>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
   }
-  if (quant_tiles(M, N, 128, 128) >= 192) return launch_product<ProductTile<128, 256, 2, 4, 2, 3>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
-  return launch_product<ProductTile<64, 256, 1, 4, 2, 3>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
+  if (quant_tiles(M, N, 128, 128) >= 192) return launch_product<ProductTile<128, 256, 2, 4, 3>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
+  return launch_product<ProductTile<64, 256, 1, 4, 3, 1, true>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
 }
 
 }  // namespace
