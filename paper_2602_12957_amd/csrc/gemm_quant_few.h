@@ -17,18 +17,16 @@ struct FewRows {
   static constexpr int kMostWaves = MT == 1 ? 16 : 160 * 1024 / (kSlots * kBlock) > 8 ? 8 : 160 * 1024 / (kSlots * kBlock);
 };
 
-// MT: pieces of 16 rows.  Linear: waves blockDim / 64, workgroup x has columns 16 x ...  GATED: 16 waves, 8 pieces of the gate's and 8 of
-// the up projection's 128 columns, each with all blocks.  EXACT: codes become bf16 (with their powers of two, exactly) for four
-// 16x16x32 products instead of one 16x16x128.
-template <bool GATED, bool FLOATS, bool EXACT, int MT, typename T>
+// MT: pieces of 16 rows.  Workgroup x has columns 16 x ... 16 x + 15.  EXACT: codes become bf16 (with their powers of two, exactly) for
+// four 16x16x32 products instead of one 16x16x128.
+template <bool FLOATS, bool EXACT, int MT, typename T>
 __global__ void __launch_bounds__(64 * FewRows<MT>::kMostWaves) k_gemm_quant_few(const RowsQuant a, const WeightQuant w, int M, int N, int nk, T *__restrict__ out,
-                                                                                 int64_t out_stride, const RowsQuant q) {
+                                                                                 int64_t out_stride) {
   using Few = FewRows<MT>;
   constexpr int S = Few::kSlots, LOADS = 2 + 2 * MT + 1;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), waves = blockDim.x >> 6, l16 = lane & 15, g = lane >> 4;
-  const int64_t n0 = GATED ? (wave >= 8 ? N : 0) + blockIdx.x * kQuantBlock + (wave & 7) * 16 : blockIdx.x * 16;   // first weight row
-  const int first = GATED ? 0 : wave, every = GATED ? 1 : waves;
+  const int64_t n0 = blockIdx.x * 16;   // first weight row
 
   // ---- loads: 8 rows of a block each, lane l the piece of row l / 8 that belongs at l % 8 (pieces lie XORed by the row, so that
   // reads of 16 rows cover all banks).  Rows behind the last one are that one again, and not stored.
@@ -40,7 +38,7 @@ __global__ void __launch_bounds__(64 * FewRows<MT>::kMostWaves) k_gemm_quant_few
   for (int j = 0; j < 2 + 2 * MT; ++j) {
     const int r = (j < 2 ? 8 * j : 8 * j - 16) + (lane >> 3);
     const uint32_t piece = ((lane ^ (r >> 1)) & 7) * 16;
-    if (j < 2) off_w[j] = (GATED ? r : min(static_cast<int64_t>(r), N - 1 - n0)) * static_cast<uint32_t>(w.code_stride) + piece + kLoadBias - j * 1024;
+    if (j < 2) off_w[j] = min(static_cast<int64_t>(r), N - 1 - n0) * static_cast<uint32_t>(w.code_stride) + piece + kLoadBias - j * 1024;
     else off_a[j - 2] = min(r, M - 1) * static_cast<uint32_t>(a.code_stride) + piece + kLoadBias - j % 2 * 1024;
   }
   const uint64_t scales_a = reinterpret_cast<uint64_t>(a.scale) + min(lane, M - 1) * a.scale_stride;
@@ -71,8 +69,8 @@ __global__ void __launch_bounds__(64 * FewRows<MT>::kMostWaves) k_gemm_quant_few
   };
   int slot = 0;
 #pragma unroll
-  for (int s = 0; s < S; ++s) request(first + s * every, s);
-  for (int kb = first; kb < nk; kb += every) {
+  for (int s = 0; s < S; ++s) request(wave + s * waves, s);
+  for (int kb = wave; kb < nk; kb += waves) {
     const uint32_t sw = weight_scale(kb);
     quant_wait<(S - 1) * LOADS>();
     const unsigned char *b = mine + slot * Few::kBlock;
@@ -84,9 +82,9 @@ __global__ void __launch_bounds__(64 * FewRows<MT>::kMostWaves) k_gemm_quant_few
       ca[j] = codes(b + (1 + j) * 2048);
       sa[j] = *reinterpret_cast<const uint32_t *>(b + (1 + MT) * 2048 + (16 * j + l16) * 4) >> (8 * (kb & 3)) & 255;
     }
-    if (kb + S * every < nk + every) {   // (no more than one request beyond the end: the count of those in flight stays)
+    if (kb + S * waves < nk + waves) {   // (no more than one request beyond the end: the count of those in flight stays)
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      request(kb + S * every, slot);
+      request(kb + S * waves, slot);
     }
     slot = slot + 1 == S ? 0 : slot + 1;
     Fragment16 fw;
@@ -114,46 +112,29 @@ __global__ void __launch_bounds__(64 * FewRows<MT>::kMostWaves) k_gemm_quant_few
 
   // results: lane l has row l % 16 of a piece of rows and weight rows 4 (l / 16) + v of a piece of weights
   floatx4 *part = reinterpret_cast<floatx4 *>(smem_raw);
-  if constexpr (!GATED) {
 #pragma unroll
-    for (int j = 0; j < MT; ++j) part[((wave * MT + j) * 16 + l16) * 4 + g] = acc[j];   // [wave][row][column / 4]
-    __syncthreads();
-    for (int x = t; x < MT * 64; x += 64 * waves) {
-      floatx4 s = part[x];
-      for (int k = 1; k < waves; ++k) s += part[k * MT * 64 + x];
-      const int m = x / 4;
-      const int64_t n = n0 + x % 4 * 4;
-      if (m < M && n < N) {
-        T *p = out + m * out_stride + n;
-        if (n + 4 <= N) {
-          const float v[4] = {s[0], s[1], s[2], s[3]};
-          if constexpr (sizeof(T) == 4) {
-            quant_store4(p, v);
-          } else {
-            typedef uint32_t u2 __attribute__((ext_vector_type(2), aligned(2)));
-            *reinterpret_cast<u2 *>(p) = u2{f32_to_bf16(v[0]) | static_cast<uint32_t>(f32_to_bf16(v[1])) << 16, f32_to_bf16(v[2]) | static_cast<uint32_t>(f32_to_bf16(v[3])) << 16};
-          }
+  for (int j = 0; j < MT; ++j) part[((wave * MT + j) * 16 + l16) * 4 + g] = acc[j];   // [wave][row][column / 4]
+  __syncthreads();
+  for (int x = t; x < MT * 64; x += 64 * waves) {
+    floatx4 s = part[x];
+    for (int k = 1; k < waves; ++k) s += part[k * MT * 64 + x];
+    const int m = x / 4;
+    const int64_t n = n0 + x % 4 * 4;
+    if (m < M && n < N) {
+      T *p = out + m * out_stride + n;
+      if (n + 4 <= N) {
+        const float v[4] = {s[0], s[1], s[2], s[3]};
+        if constexpr (sizeof(T) == 4) {
+          quant_store4(p, v);
         } else {
-#pragma unroll
-          for (int k = 0; k < 3; ++k)
-            if (n + k < N) p[k] = from_f32<T>(s[k]);
+          typedef __bf16 b4 __attribute__((ext_vector_type(4), aligned(2)));
+          *reinterpret_cast<b4 *>(p) = __builtin_convertvector(s, bf16x4);
         }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+          if (n + k < N) p[k] = rounded<T>(s[k]);
       }
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < MT; ++j) part[((wave >> 3) * MT * 16 + 16 * j + l16) * 32 + (wave & 7) * 4 + g] = acc[j];   // [gate, up][row][column / 4]
-    __syncthreads();
-    for (int x = t; x < MT * 16 * 16; x += 64 * waves) {   // eight columns each; 16 lanes have a row's block
-      const int m = x >> 4, c = x & 15;
-      float y[8];
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const floatx4 gate = part[m * 32 + 2 * c + k], up = part[(MT * 16 + m) * 32 + 2 * c + k];
-#pragma unroll
-        for (int v = 0; v < 4; ++v) y[4 * k + v] = swiglu(gate[v], up[v]);
-      }
-      if (m < M) store_codes8(q, m, blockIdx.x * kQuantBlock + 8 * c, y);   // (whole rows of 16 lanes leave together)
     }
   }
 }

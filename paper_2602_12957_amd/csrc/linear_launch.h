@@ -61,7 +61,8 @@ int run_norm(hipStream_t st, const NormRows &a, int32_t x_dtype, const void *x, 
   return res_dtype == HSD_BF16 ? launch_norm<float, bf16>(st, a, x, res, sum) : launch_norm<float, float>(st, a, x, res, sum);
 }
 
-// Products of many rows
+constexpr int kUnits = 256;   // compute units
+
 template <typename Cfg, bool GATED, bool FLOATS, bool EXACT, typename T>
 int launch_product(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, int N, int nk, T *out, int64_t out_stride, const RowsQuant &q) {
   auto kern = k_gemm_quant<Cfg, GATED, FLOATS, EXACT, T>;
@@ -75,78 +76,78 @@ int launch_product(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int
   return HSD_OK;
 }
 
-// Products of up to 64 rows
-template <bool GATED, bool FLOATS, bool EXACT, int MT, typename T>
-int launch_few(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, int N, int nk, T *out, int64_t out_stride, const RowsQuant &q) {
+template <bool FLOATS, bool EXACT, int MT, typename T>
+int launch_few(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, int N, int nk, T *out, int64_t out_stride) {
   using Few = FewRows<MT>;
-  auto kern = k_gemm_quant_few<GATED, FLOATS, EXACT, MT, T>;
+  auto kern = k_gemm_quant_few<FLOATS, EXACT, MT, T>;
   constexpr int per_wave = Few::kSlots * Few::kBlock;
-  static_assert(!GATED || Few::kMostWaves == 16, "a wave for each 16 of the gate's and the up projection's 128 rows");
   static const hipError_t attr_rc = hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, Few::kMostWaves * per_wave);
   if (attr_rc != hipSuccess) return HSD_EHIP;
-  const int waves = GATED ? 16 : std::min(nk, Few::kMostWaves), cols = GATED ? kQuantBlock : 16;
-  hipLaunchKernelGGL(kern, dim3((N + cols - 1) / cols), dim3(64 * waves), waves * per_wave, st, a, w, M, N, nk, out, out_stride, q);
+  const int waves = std::min(nk, Few::kMostWaves);
+  hipLaunchKernelGGL(kern, dim3((N + 15) / 16), dim3(64 * waves), waves * per_wave, st, a, w, M, N, nk, out, out_stride);
   HSD_LAUNCH_CHECK();
   return HSD_OK;
 }
-template <bool FLOATS, bool EXACT, typename T>
-int launch_few_rows(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, int N, int nk, T *out, int64_t out_stride) {
-  const RowsQuant none{};
-  if (M <= 16) return launch_few<false, FLOATS, EXACT, 1, T>(st, a, w, M, N, nk, out, out_stride, none);
-  if (M <= 32) return launch_few<false, FLOATS, EXACT, 2, T>(st, a, w, M, N, nk, out, out_stride, none);
-  return launch_few<false, FLOATS, EXACT, 4, T>(st, a, w, M, N, nk, out, out_stride, none);
-}
 
 int64_t quant_tiles(int M, int N, int bm, int bn) { return static_cast<int64_t>((M + bm - 1) / bm) * ((N + bn - 1) / bn); }
+int64_t rounds(int64_t tiles) { return (tiles + kUnits - 1) / kUnits; }
+// Rows at the end of a call that would cost tiles of 256 rows a round of their own over the chip, and that go by themselves instead (32772 rows
+// of 4096 to 1024, four of them in 516 - 512 tiles: 164 us in one launch, 134 in two); 0: none
+int last_rows(int M, int N, int bn) {
+  const int rest = M % 256;
+  return rest > 0 && rest <= 64 && M > 256 && rounds(quant_tiles(M, N, 256, bn)) > rounds(quant_tiles(M - rest, N, 256, bn)) ? rest : 0;
+}
+RowsQuant rows_from(const RowsQuant &r, int64_t m) { return RowsQuant{r.codes + m * r.code_stride, r.scale + m * r.scale_stride, r.code_stride, r.scale_stride}; }
 
+// The form of a product goes by how many tiles it has: the smallest tiles that leave no second round over the chip (a compute unit works as fast on
+// one large tile as on a small one, until it has all that the matrix unit can do); us a call, by tiles of 64x64 / 64x128 / 128x128 / 128x128 two a
+// unit / 256x256, 1024 columns to 1024, 4096 and 16384 rows of weights:
+//   200 rows to 4096  4.7 /  5.5 /  6.8                   512 to 4096   7.1 /  5.9 /  7.3 /  8.8 / 18.1     1024 to 4096   12.1 /  9.0 /  8.3 /  9.5 / 18.6
+//   2048 to 4096     20.9 / 15.4 / 14.4 / 13.4 / 20.0     4096 to 4096 38.4 / 28.1 / 26.4 / 23.3 / 22.0     4096 to 16384 184.5 / 138.7 / 138.5 / 110.7 / 81.4
+// Few rows: a split of K over waves (k_gemm_quant_few), where that makes enough workgroups but not too many, each of which reads all rows: 64 rows of 4096 to
+// 1024 6.9 where tiles take 8.6, to 4096 8.3 / 8.7; 16 of 8192 to 8192 17.1 / 20.1, of 4096 to 16384 21.0 / 16.8.
 template <bool FLOATS, bool EXACT, typename T>
 int run_linear(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, int N, int nk, T *out, int64_t out_stride) {
   const RowsQuant none{};
-#ifdef HSD_QUANT_TRY
-  const char *e = getenv("HSD_QCFG");
-  const int cfg = e ? atoi(e) : -1;
-#define TRY(ok, id, ...) if constexpr (ok) { if (cfg == id) return launch_product<ProductTile<__VA_ARGS__>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none); }
-  TRY(!FLOATS && !EXACT, 6, 256, 256, 2, 2, 2)
-  TRY(!EXACT, 1, 256, 128, 4, 2, 3)
-  TRY(true, 8, 128, 128, 2, 2, 2)
-  if (cfg == 20) return launch_few_rows<FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride);
-  TRY(true, 50, 64, 128, 2, 2, 5, 2, true)
-  TRY(true, 51, 64, 128, 2, 2, 3, 2, true)
-  TRY(true, 58, 64, 128, 2, 2, 3, 1, true)
-  TRY(true, 52, 64, 64, 2, 2, 4, 2, true)
-  TRY(!(FLOATS && EXACT), 56, 128, 128, 2, 2, 4, 1, true)
-  TRY(!FLOATS && !EXACT, 54, 128, 128, 2, 2, 4, 2, true)
-#endif
-  if (M <= 16 || (M <= 64 && quant_tiles(M, N, 64, 64) < 128)) return launch_few_rows<FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride);
-  if constexpr (!FLOATS && !EXACT) {
-    if (quant_tiles(M, N, 256, 256) >= 192) return launch_product<ProductTile<256, 256, 2, 2, 2>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
+  if ((M <= 64 && N <= 4096) || (M <= 16 && N <= 8192)) {
+    if (M <= 16) return launch_few<FLOATS, EXACT, 1, T>(st, a, w, M, N, nk, out, out_stride);
+    if (M <= 32) return launch_few<FLOATS, EXACT, 2, T>(st, a, w, M, N, nk, out, out_stride);
+    return launch_few<FLOATS, EXACT, 4, T>(st, a, w, M, N, nk, out, out_stride);
   }
-  if (quant_tiles(M, N, 128, 128) >= 256) return launch_product<ProductTile<128, 128, 2, 2, 2>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
-  if (quant_tiles(M, N, 64, 128) >= 192) return launch_product<ProductTile<64, 128, 2, 2, 3, 2, true>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
-  return launch_product<ProductTile<64, 64, 2, 2, 4, 2, true>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
+  if (quant_tiles(M, N, 64, 64) <= kUnits) return launch_product<ProductTile<64, 64, 2, 2, 4, 2, true>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
+  if (quant_tiles(M, N, 64, 128) <= kUnits) return launch_product<ProductTile<64, 128, 2, 2, 3, 2, true>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
+  if constexpr (EXACT) {
+    // (the codes' bf16 forms take the registers of larger tiles with float scales: 4096 rows of 4096 to 4096 145 us in tiles of 64x128, 178 of 128x128)
+    if constexpr (FLOATS) return launch_product<ProductTile<64, 128, 2, 2, 3, 1, true>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
+    else return launch_product<ProductTile<128, 128, 2, 2, 2>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
+  } else {
+    const int64_t tiles = quant_tiles(M, N, 128, 128);
+    if (tiles <= kUnits) return launch_product<ProductTile<128, 128, 2, 2, 4, FLOATS ? 1 : 2, true>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
+    if (tiles <= 2 * kUnits) return launch_product<ProductTile<128, 128, 2, 2, 2>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
+    // with float scales a block's sums stand beside the sums: half a tile has the registers for both
+    using Cfg = ProductTile<256, FLOATS ? 128 : 256, FLOATS ? 4 : 2, 2, FLOATS ? 3 : 2>;
+    const int rest = last_rows(M, N, Cfg::BN);
+    const int rc = launch_product<Cfg, false, FLOATS, EXACT, T>(st, a, w, M - rest, N, nk, out, out_stride, none);
+    if (rc != HSD_OK || rest == 0) return rc;
+    return run_linear<FLOATS, EXACT, T>(st, rows_from(a, M - rest), w, rest, N, nk, out + (M - rest) * out_stride, out_stride);
+  }
 }
 
+// Gate and up: tiles of 64, 128 and 256 rows by 128 columns of both.  us a call, 1024 columns to 4096: 512 rows 8.5 / 10.4 / 19.0, 1024 15.5 / 12.2 / 19.5,
+// 1856 28.0 / 21.7 / 21.3, 32768 430 / 339 / 316
 template <bool FLOATS>
 int run_gated(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, int N, int nk, const RowsQuant &q) {
   bf16 *none = nullptr;
-#ifdef HSD_QUANT_TRY
-  const char *e = getenv("HSD_QCFG");
-  const int cfg = e ? atoi(e) : -1;
-#define TRYG(ok, id, ...) if constexpr (ok) { if (cfg == id) return launch_product<ProductTile<__VA_ARGS__>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q); }
-  if (cfg == 20) return launch_few<true, FLOATS, false, 1, bf16>(st, a, w, M, N, nk, none, 0, q);
-  TRYG(!FLOATS, 6, 256, 256, 2, 2, 2)
-  TRYG(true, 4, 128, 256, 2, 4, 3)
-  TRYG(!FLOATS, 60, 128, 256, 2, 2, 3, 1, true)
-  TRYG(true, 61, 64, 256, 1, 4, 3, 1, true)
-  TRYG(!FLOATS, 62, 64, 256, 1, 4, 3, 2, true)
-  TRYG(true, 3, 64, 256, 1, 4, 3)
-#endif
-  if (M <= 16) return launch_few<true, FLOATS, false, 1, bf16>(st, a, w, M, N, nk, none, 0, q);
-  if constexpr (!FLOATS) {
-    if (quant_tiles(M, N, 256, 128) >= 192) return launch_product<ProductTile<256, 256, 2, 2, 2>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
+  if (quant_tiles(M, N, 64, 128) <= kUnits) return launch_product<ProductTile<64, 256, 1, 4, 3, 1, true>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
+  if constexpr (FLOATS) {
+    return launch_product<ProductTile<128, 256, 2, 4, 3>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
+  } else {
+    if (quant_tiles(M, N, 128, 128) <= kUnits) return launch_product<ProductTile<128, 256, 2, 2, 3, 1, true>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
+    const int rest = last_rows(M, N, 128);
+    const int rc = launch_product<ProductTile<256, 256, 2, 2, 2>, true, FLOATS, false, bf16>(st, a, w, M - rest, N, nk, none, 0, q);
+    if (rc != HSD_OK || rest == 0) return rc;
+    return run_gated<FLOATS>(st, rows_from(a, M - rest), w, rest, N, nk, rows_from(q, M - rest));
   }
-  if (quant_tiles(M, N, 128, 128) >= 192) return launch_product<ProductTile<128, 256, 2, 4, 3>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
-  return launch_product<ProductTile<64, 256, 1, 4, 3, 1, true>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
 }
 
 }  // namespace

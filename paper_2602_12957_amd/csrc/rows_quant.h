@@ -33,6 +33,13 @@ __device__ __forceinline__ float max16(float x) {
   return fmaxf(x, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x121, 0xf, 0xf, true)));
 }
 
+// x in T, nearest, ties to even; NaN stays NaN
+template <typename T>
+__device__ __forceinline__ T rounded(float x) {
+  if constexpr (sizeof(T) == 4) return x;
+  else return __builtin_bit_cast(T, static_cast<__bf16>(x));
+}
+
 // Eight values from column c of a row of dim (those behind its end as 0)
 template <typename T>
 __device__ __forceinline__ void load8(const T *row, int c, int dim, float *v) {
@@ -49,15 +56,13 @@ __device__ __forceinline__ void store8(T *row, int c, int dim, const float *v) {
     if constexpr (sizeof(T) == 4) {
       quant_store4(row + c, v), quant_store4(row + c + 4, v + 4);
     } else {
-      typedef uint32_t u4 __attribute__((ext_vector_type(4), aligned(2)));
-      u4 x;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = f32_to_bf16(v[2 * i]) | static_cast<uint32_t>(f32_to_bf16(v[2 * i + 1])) << 16;
-      *reinterpret_cast<u4 *>(row + c) = x;
+      typedef __bf16 b8 __attribute__((ext_vector_type(8), aligned(2)));
+      const floatx8 f = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
+      *reinterpret_cast<b8 *>(row + c) = __builtin_convertvector(f, bf16x8);
     }
   } else {
     for (int i = 0; i < 8; ++i)
-      if (c + i < dim) row[c + i] = from_f32<T>(v[i]);
+      if (c + i < dim) row[c + i] = rounded<T>(v[i]);
   }
 }
 

@@ -52,7 +52,7 @@ def _held(name: str, t: torch.Tensor, rows: int, least: int, step: int, index: i
 class Rows8:
     """Rows of `dim` values in 8 bits.  codes: uint8 [rows, 128 * ceil(dim / 128)], e4m3, zeros behind dim; scale: uint8 [rows, ceil(dim / 128)
     rounded up to a multiple of 4], value = code * 2^(scale - 127)."""
-    __slots__ = ("codes", "scale", "dim", "rows", "index", "c")
+    __slots__ = ("_codes", "_scale", "_room", "dim", "rows", "index", "device", "c")
 
     def __init__(self, codes: torch.Tensor, scale: torch.Tensor, dim: int):
         if dim < 1 or not isinstance(codes, torch.Tensor) or codes.dim() != 2:
@@ -63,27 +63,39 @@ class Rows8:
         ss = _held("scale", scale, n, -(-blocks // 4) * 4, 4, self.index)
         if codes.data_ptr() % 16 or scale.data_ptr() % 4:
             raise ValueError("codes must be aligned to 16 bytes and scale to 4")
-        self.codes, self.scale, self.dim, self.rows = codes, scale, dim, n
+        self._codes, self._scale, self._room, self.dim, self.rows, self.device = codes, scale, None, dim, n, codes.device
         self.c = B.hsd_rows_quant(codes.data_ptr(), scale.data_ptr(), cs, ss)
 
     @classmethod
     def empty(cls, rows: int, dim: int, device) -> "Rows8":
-        """Room for rows that a call writes."""
+        """Room for rows that a call writes: one tensor, the codes and the bytes behind them."""
         blocks = (dim + _BLOCK - 1) // _BLOCK
         width, bytes_ = blocks * _BLOCK, (blocks + 3) // 4 * 4
-        room = torch.empty(rows * (width + bytes_), dtype=torch.uint8, device=device)
         r = cls.__new__(cls)
-        r.codes, r.scale = room[:rows * width].view(rows, width), room[rows * width:].view(rows, bytes_)
-        r.dim, r.rows, r.index = dim, rows, room.get_device()
+        r._codes = r._scale = None
+        r._room = room = torch.empty(rows * (width + bytes_), dtype=torch.uint8, device=device)
+        r.dim, r.rows, r.index, r.device = dim, rows, room.get_device(), room.device
         p = room.data_ptr()
         r.c = B.hsd_rows_quant(p, p + rows * width, width, bytes_)
         return r
+
+    @property
+    def codes(self) -> torch.Tensor:
+        if self._codes is None:
+            self._codes = self._room[:self.rows * self.c.code_stride].view(self.rows, self.c.code_stride)
+        return self._codes
+
+    @property
+    def scale(self) -> torch.Tensor:
+        if self._scale is None:
+            self._scale = self._room[self.rows * self.c.code_stride:].view(self.rows, self.c.scale_stride)
+        return self._scale
 
     def read(self, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
         """The values, [rows, dim], exact in both types."""
         if dtype not in _TYPES:
             raise ValueError(f"bfloat16 or float32, got {dtype}")
-        out = torch.empty((self.rows, self.dim), dtype=dtype, device=self.codes.device)
+        out = torch.empty((self.rows, self.dim), dtype=dtype, device=self.device)
         with B.on_device(self.index):
             B.hsd_quant_read_rows(B.current_stream(self.index), self.rows, self.dim, self.c, _TYPES[dtype], out.data_ptr(), self.dim)
         return out
@@ -173,7 +185,7 @@ def linear(rows: Rows8, w: Weight8, dtype: torch.dtype = torch.bfloat16, out: Op
     if out is None:
         if dtype not in _TYPES:
             raise ValueError(f"bfloat16 or float32, got {dtype}")
-        out, stride = torch.empty((rows.rows, w.n_out), dtype=dtype, device=rows.codes.device), w.n_out
+        out, stride = torch.empty((rows.rows, w.n_out), dtype=dtype, device=rows.device), w.n_out
     else:
         stride = _matrix("out", out, rows.index, (rows.rows, w.n_out))
     with B.on_device(rows.index):
@@ -187,7 +199,7 @@ def gated(rows: Rows8, w: Weight8) -> Rows8:
     d_ffn = w.n_out // 2
     if w.n_out != 2 * d_ffn or d_ffn % _BLOCK:
         raise ValueError(f"gate and up must have a multiple of {_BLOCK} rows each, got {w.n_out} together")
-    out = Rows8.empty(rows.rows, d_ffn, rows.codes.device)
+    out = Rows8.empty(rows.rows, d_ffn, rows.device)
     with B.on_device(rows.index):
         B.hsd_quant_gated(B.current_stream(rows.index), rows.rows, d_ffn, rows.dim, rows.c, w.c, out.c)
     return out

@@ -139,7 +139,8 @@ def test_weights_that_are_no_numbers():
 SIZES = [(1, 1, 1), (1, 16, 128), (1, 1536, 1024), (2, 17, 129), (3, 128, 384), (15, 130, 512), (16, 64, 640), (17, 257, 1000), (31, 100, 100), (32, 32, 2048), (33, 1000, 896),
          (48, 129, 4096), (63, 96, 256), (64, 1024, 4096), (65, 255, 1024), (96, 513, 300), (127, 127, 127), (128, 128, 128), (129, 129, 129), (130, 1, 513),
          (200, 384, 1152), (255, 640, 2176), (256, 256, 256), (257, 257, 257), (300, 1537, 777), (511, 100, 128), (512, 1024, 1024), (777, 1537, 1000), (1000, 900, 4096),
-         (1025, 1030, 640), (1856, 1024, 512), (2050, 520, 1920), (4100, 300, 256), (70000, 5, 130)]
+         (1025, 1030, 640), (1856, 1024, 512), (2050, 520, 1920), (4100, 300, 256), (70000, 5, 130),
+         (1500, 1600, 512), (2050, 2050, 300), (2500, 4200, 130), (4097, 2600, 257), (8196, 2048, 128), (16390, 1030, 384), (64, 4097, 300), (16, 8192, 257), (17, 8200, 129), (5, 9000, 640)]
 
 
 @pytest.mark.parametrize("rows,n_out,dim", SIZES)
@@ -213,7 +214,8 @@ def test_scales_from_end_to_end():
 
 # ------------------------------------------------------------------------------------------------------------ gate and up
 @pytest.mark.parametrize("rows,d_ffn,dim", [(1, 128, 1), (1, 256, 1024), (5, 128, 128), (16, 384, 1000), (17, 128, 300), (33, 256, 640), (64, 512, 512), (65, 128, 1024), (100, 256, 129),
-                                            (128, 128, 256), (129, 384, 384), (200, 128, 4096), (256, 256, 256), (257, 640, 896), (600, 1024, 512), (1856, 256, 1024), (70000, 128, 100)])
+                                            (128, 128, 256), (129, 384, 384), (200, 128, 4096), (256, 256, 256), (257, 640, 896), (600, 1024, 512), (1856, 256, 1024), (70000, 128, 100), (1100, 2048, 129),
+                                            (2100, 2048, 300), (8196, 1024, 128), (4097, 1152, 257)])
 @pytest.mark.parametrize("scale", [torch.uint8, F32])
 def test_gated(rows, d_ffn, dim, scale):
     L = lib()
