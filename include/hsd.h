@@ -417,9 +417,9 @@ typedef struct hsd_weight_quant {
  * in it (0 where all are 0); values round to the nearest code, ties to even, those beyond 448 * 2^119 to that. */
 int hsd_quant_rows(void *stream, int32_t n_rows, int32_t dim, int32_t dtype, const void *x, int64_t x_stride, const hsd_rows_quant *out);
 
-/* Root-mean-square norm with the residual's addition: h = x + residual in fp32, written to sum (in the residual's type; may be residual itself, or NULL), and
- * h * gain / sqrt(mean(h^2) + eps) of the unrounded h to 8 bits, as hsd_quant_rows.  residual NULL: h = x (then sum is NULL, and
- * res_dtype still one of the two); gain: dev [dim] fp32 or NULL (1).  eps >= 0.  A row whose squares' sum is not finite in fp32 is held as NaN. */
+/* Root-mean-square norm with the residual's addition: h = x + residual, written to sum (rounded once from fp32 to the residual's type; may be residual
+ * itself, or NULL), and h * gain / sqrt(mean(h^2) + eps), in 64 bits from the unrounded h, to 8 bits, as hsd_quant_rows.  residual NULL: h = x (then sum
+ * is NULL, and res_dtype still one of the two); gain: dev [dim] fp32 or NULL (1).  eps >= 0. */
 int hsd_quant_norm_rows(void *stream, int32_t n_rows, int32_t dim, int32_t dtype, const void *x, int64_t x_stride, int32_t res_dtype,
                         const void *residual, int64_t res_stride, void *sum, int64_t sum_stride, const float *gain, float eps,
                         const hsd_rows_quant *out);
@@ -428,7 +428,7 @@ int hsd_quant_norm_rows(void *stream, int32_t n_rows, int32_t dim, int32_t dtype
 int hsd_quant_read_rows(void *stream, int32_t n_rows, int32_t dim, const hsd_rows_quant *rows, int32_t dtype, void *out, int64_t out_stride);
 
 /* w [n_out, dim] to 8 bits in blocks of 128 by 128, once for a model: bytes as in hsd_quant_rows, or floats: the largest finite magnitude / 448, 1
- * where that is 0.  Writes out->codes and out->scale. */
+ * where that is 0.  Writes out->codes and out->scale.  n_out beyond 65535 * 128: HSD_ERANGE. */
 int hsd_quant_weights(void *stream, int32_t n_out, int32_t dim, int32_t dtype, const void *w, int64_t w_stride, const hsd_weight_quant *out);
 
 /* out[m][n] = sum_k rows[m][k] * w[n][k], [n_rows, n_out] in dtype, of the values that both stand for.  Sums in fp32; products of codes are exact.  The

@@ -11,7 +11,7 @@ int hsd_quant_rows(void *stream, int32_t n_rows, int32_t dim, int32_t dtype, con
   if (!is_type(dtype)) return HSD_EINVAL;
   if (n_rows == 0) return HSD_OK;
   if (x == nullptr || x_stride < dim) return HSD_EINVAL;
-  const NormRows a{n_rows, dim, 0, nullptr, 0.f, 0.f, x_stride, 0, 0, rows_quant(out)};
+  const NormRows a{n_rows, dim, 0, nullptr, 0., x_stride, 0, 0, rows_quant(out)};
   return run_norm(static_cast<hipStream_t>(stream), a, dtype, x, dtype, nullptr, nullptr);
 }
 
@@ -24,7 +24,7 @@ int hsd_quant_norm_rows(void *stream, int32_t n_rows, int32_t dim, int32_t dtype
   if (n_rows == 0) return HSD_OK;
   if (x == nullptr || x_stride < dim || (residual != nullptr && res_stride < dim) || (sum != nullptr && sum_stride < dim)) return HSD_EINVAL;
   if (residual == nullptr && sum != nullptr) return HSD_EINVAL;
-  const NormRows a{n_rows, dim, 1, gain, eps, 1.f / static_cast<float>(dim), x_stride, res_stride, sum_stride, rows_quant(out)};
+  const NormRows a{n_rows, dim, 1, gain, eps, x_stride, res_stride, sum_stride, rows_quant(out)};
   return run_norm(static_cast<hipStream_t>(stream), a, dtype, x, res_dtype, residual, sum);
 }
 

@@ -1,9 +1,11 @@
 // What the operators on rows and weights in 8 bits check, and their launches.
 #pragma once
 
+#include <atomic>
+
 namespace {
 
-constexpr int kMostQuantRows = (1 << 24) - 1, kMostQuantDim = 1 << 20;   // a launch has fewer than 2^32 threads, 256 of them a row
+constexpr int kMostQuantRows = (1 << 24) - 1, kMostQuantDim = 1 << 20;   // a launch has fewer than 2^32 threads, up to 256 of them a row (the norm's: below)
 constexpr int64_t kMostCodeStride = 1 << 23;                             // offsets within a tile of 256 rows take 31 bits
 
 int quant_blocks(int32_t dim) { return (dim + kQuantBlock - 1) / kQuantBlock; }
@@ -38,19 +40,24 @@ WeightQuant weight_quant(const hsd_weight_quant *w) {
 
 template <typename TX, typename TR>
 int launch_norm(hipStream_t st, const NormRows &a, const void *x, const void *res, void *sum) {
-  const TX *px = static_cast<const TX *>(x);
-  const TR *pr = static_cast<const TR *>(res);
-  TR *ps = static_cast<TR *>(sum);
+  // (up to 1024 threads a row: launches of 2^31 threads at most)
   auto launch = [&](auto kern, int wpr) {
-    const int rows = std::max(4 / wpr, 1);   // of a workgroup; one where it takes several waves
-    const int per = wpr == 1 ? rows : 1;
-    hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>((a.n_rows + per - 1) / per)), dim3(64 * wpr * per), 0, st, a, wpr, px, pr, ps);
+    const int held = wpr == 1 ? 4 : 1, most = (1 << 25) / wpr;   // rows of a workgroup and of a launch
+    NormRows b = a;
+    for (int64_t first = 0; first < a.n_rows; first += most) {
+      const TX *px = static_cast<const TX *>(x) + first * a.x_stride;
+      const TR *pr = res ? static_cast<const TR *>(res) + first * a.res_stride : nullptr;
+      TR *ps = sum ? static_cast<TR *>(sum) + first * a.sum_stride : nullptr;
+      b.n_rows = std::min<int64_t>(most, a.n_rows - first);
+      b.out.codes = a.out.codes + first * a.out.code_stride, b.out.scale = a.out.scale + first * a.out.scale_stride;
+      hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>((b.n_rows + held - 1) / held)), dim3(64 * wpr * held), 0, st, b, wpr, px, pr, ps);
+    }
   };
   // few rows: a lane's eight columns at a time, so that a row is short; many: up to 32, so that a row is a wave's own
   const int waves1 = (a.dim + 511) / 512, waves2 = (a.dim + 1023) / 1024, waves4 = (a.dim + 2047) / 2048;
   if (waves1 == 1 || (waves1 <= 16 && a.n_rows * waves1 <= 1024)) launch(k_quant_rows<TX, TR, 1>, waves1);
   else if (waves2 == 1) launch(k_quant_rows<TX, TR, 2>, 1);
-  else if (waves4 <= 16) launch(k_quant_rows<TX, TR, 4>, waves4);
+  else if (waves4 <= 8) launch(k_quant_rows<TX, TR, 4>, waves4);
   else launch(k_quant_rows<TX, TR, 0>, 16);
   HSD_LAUNCH_CHECK();
   return HSD_OK;
@@ -63,11 +70,22 @@ int run_norm(hipStream_t st, const NormRows &a, int32_t x_dtype, const void *x, 
 
 constexpr int kUnits = 256;   // compute units
 
+// Lets a kernel have `bytes` of LDS on the current device (asked for once a device; `done`: a bit a device, of the kernel's own)
+hipError_t allow_lds(const void *kern, int bytes, std::atomic<uint64_t> &done) {
+  int dev = 0;
+  if (const hipError_t rc = hipGetDevice(&dev); rc != hipSuccess) return rc;
+  const uint64_t bit = uint64_t{1} << (dev & 63);
+  if (dev < 64 && (done.load(std::memory_order_relaxed) & bit) != 0) return hipSuccess;
+  const hipError_t rc = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (rc == hipSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return rc;
+}
+
 template <typename Cfg, bool GATED, bool FLOATS, bool EXACT, typename T>
 int launch_product(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, int N, int nk, T *out, int64_t out_stride, const RowsQuant &q) {
   auto kern = k_gemm_quant<Cfg, GATED, FLOATS, EXACT, T>;
-  static const hipError_t attr_rc = hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, Cfg::kLds);
-  if (attr_rc != hipSuccess) return HSD_EHIP;
+  static std::atomic<uint64_t> done{0};
+  if (allow_lds(reinterpret_cast<const void *>(kern), Cfg::kLds, done) != hipSuccess) return HSD_EHIP;
   constexpr int COLS = GATED ? Cfg::BN / 2 : Cfg::BN;
   const int64_t tiles = static_cast<int64_t>((M + Cfg::BM - 1) / Cfg::BM) * ((N + COLS - 1) / COLS);
   if (tiles > INT32_MAX / Cfg::kThreads) return HSD_ERANGE;
@@ -81,8 +99,8 @@ int launch_few(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, 
   using Few = FewRows<MT>;
   auto kern = k_gemm_quant_few<FLOATS, EXACT, MT, T>;
   constexpr int per_wave = Few::kSlots * Few::kBlock;
-  static const hipError_t attr_rc = hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, Few::kMostWaves * per_wave);
-  if (attr_rc != hipSuccess) return HSD_EHIP;
+  static std::atomic<uint64_t> done{0};
+  if (allow_lds(reinterpret_cast<const void *>(kern), Few::kMostWaves * per_wave, done) != hipSuccess) return HSD_EHIP;
   const int waves = std::min(nk, Few::kMostWaves);
   hipLaunchKernelGGL(kern, dim3((N + 15) / 16), dim3(64 * waves), waves * per_wave, st, a, w, M, N, nk, out, out_stride);
   HSD_LAUNCH_CHECK();
@@ -133,11 +151,13 @@ int run_linear(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, 
   }
 }
 
-// Gate and up: tiles of 64, 128 and 256 rows by 128 columns of both.  us a call, 1024 columns to 4096: 512 rows 8.5 / 10.4 / 19.0, 1024 15.5 / 12.2 / 19.5,
+// Gate and up: up to 64 rows with bf16 products of the codes (the weights' reading is what counts there, 16 rows of 1024 to 4096 9.0 us and 7.3 with 8-bit ones,
+// and rows in 8 bits then differ from the definition's no more than by fp32's roundings); more in tiles of 64, 128 and 256 rows by 128 columns of both.  us a call, 1024 columns to 4096: 512 rows 8.5 / 10.4 / 19.0, 1024 15.5 / 12.2 / 19.5,
 // 1856 28.0 / 21.7 / 21.3, 32768 430 / 339 / 316
 template <bool FLOATS>
 int run_gated(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, int N, int nk, const RowsQuant &q) {
   bf16 *none = nullptr;
+  if (M <= 64) return launch_product<ProductTile<64, 256, 1, 4, 3, 1, true>, true, FLOATS, true, bf16>(st, a, w, M, N, nk, none, 0, q);
   if (quant_tiles(M, N, 64, 128) <= kUnits) return launch_product<ProductTile<64, 256, 1, 4, 3, 1, true>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
   if constexpr (FLOATS) {
     return launch_product<ProductTile<128, 256, 2, 4, 3>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);

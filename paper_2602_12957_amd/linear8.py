@@ -18,6 +18,7 @@ from . import binding as B
 
 _TYPES = {torch.bfloat16: B.HSD_BF16, torch.float32: B.HSD_FP32}
 _BLOCK = B.HSD_QUANT_BLOCK
+_CODES, _BYTES = (torch.uint8, torch.float8_e4m3fn), (torch.uint8, torch.float8_e8m0fnu)
 
 
 def _matrix(name: str, t: torch.Tensor, index: int = -1, shape=None) -> int:
@@ -37,7 +38,7 @@ def _matrix(name: str, t: torch.Tensor, index: int = -1, shape=None) -> int:
     return s[0] if n > 1 else m
 
 
-def _held(name: str, t: torch.Tensor, rows: int, least: int, step: int, index: int, types=(torch.uint8,)) -> int:
+def _held(name: str, t: torch.Tensor, rows: int, least: int, step: int, index: int, types) -> int:
     """A tensor of codes or scales, [rows, at least `least`]; returns the distance of its rows."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in types or (index >= 0 and t.get_device() != index):
         raise ValueError(f"{name} must be a {' or '.join(str(x) for x in types)} tensor on {'a GPU' if index < 0 else f'cuda:{index}'}")
@@ -50,17 +51,17 @@ def _held(name: str, t: torch.Tensor, rows: int, least: int, step: int, index: i
 
 
 class Rows8:
-    """Rows of `dim` values in 8 bits.  codes: uint8 [rows, 128 * ceil(dim / 128)], e4m3, zeros behind dim; scale: uint8 [rows, ceil(dim / 128)
-    rounded up to a multiple of 4], value = code * 2^(scale - 127)."""
+    """Rows of `dim` values in 8 bits.  codes: uint8 (or float8_e4m3fn) [rows, 128 * ceil(dim / 128)], zeros behind dim; scale: uint8 (or
+    float8_e8m0fnu) [rows, ceil(dim / 128) rounded up to a multiple of 4]; value = code * 2^(scale - 127)."""
     __slots__ = ("_codes", "_scale", "_room", "dim", "rows", "index", "device", "c")
 
     def __init__(self, codes: torch.Tensor, scale: torch.Tensor, dim: int):
         if dim < 1 or not isinstance(codes, torch.Tensor) or codes.dim() != 2:
             raise ValueError("rows in 8 bits: dim must be positive and codes [rows, 128 * ceil(dim / 128)]")
         n, blocks = codes.shape[0], -(-dim // _BLOCK)
-        cs = _held("codes", codes, n, blocks * _BLOCK, 16, -1)
+        cs = _held("codes", codes, n, blocks * _BLOCK, 16, -1, _CODES)
         self.index = codes.get_device()
-        ss = _held("scale", scale, n, -(-blocks // 4) * 4, 4, self.index)
+        ss = _held("scale", scale, n, -(-blocks // 4) * 4, 4, self.index, _BYTES)
         if codes.data_ptr() % 16 or scale.data_ptr() % 4:
             raise ValueError("codes must be aligned to 16 bytes and scale to 4")
         self._codes, self._scale, self._room, self.dim, self.rows, self.device = codes, scale, None, dim, n, codes.device
@@ -69,12 +70,16 @@ class Rows8:
     @classmethod
     def empty(cls, rows: int, dim: int, device) -> "Rows8":
         """Room for rows that a call writes: one tensor, the codes and the bytes behind them."""
+        if rows < 0 or dim < 1:
+            raise ValueError(f"rows must not be negative and dim must be positive, got {rows} and {dim}")
         blocks = (dim + _BLOCK - 1) // _BLOCK
         width, bytes_ = blocks * _BLOCK, (blocks + 3) // 4 * 4
         r = cls.__new__(cls)
         r._codes = r._scale = None
         r._room = room = torch.empty(rows * (width + bytes_), dtype=torch.uint8, device=device)
         r.dim, r.rows, r.index, r.device = dim, rows, room.get_device(), room.device
+        if r.index < 0:
+            raise ValueError("rows in 8 bits are held on a GPU; there is no CPU fallback")
         p = room.data_ptr()
         r.c = B.hsd_rows_quant(p, p + rows * width, width, bytes_)
         return r
@@ -102,21 +107,22 @@ class Rows8:
 
 
 class Weight8:
-    """A weight matrix [n_out, dim] in 8 bits, blocks of 128 rows by 128 columns.  codes: uint8 [n_out, 128 * ceil(dim / 128)], e4m3, zeros
-    behind dim; scale: [ceil(n_out / 128), ceil(dim / 128)], uint8 (value = code * 2^(scale - 127)) or float32 (value = code * scale)."""
+    """A weight matrix [n_out, dim] in 8 bits, blocks of 128 rows by 128 columns.  codes: uint8 (or float8_e4m3fn) [n_out, 128 * ceil(dim / 128)],
+    zeros behind dim; scale: [ceil(n_out / 128), ceil(dim / 128)], uint8 or float8_e8m0fnu (value = code * 2^(scale - 127)) or float32
+    (value = code * scale)."""
     __slots__ = ("codes", "scale", "dim", "n_out", "index", "c")
 
     def __init__(self, codes: torch.Tensor, scale: torch.Tensor, dim: int):
         if dim < 1 or not isinstance(codes, torch.Tensor) or codes.dim() != 2 or codes.shape[0] < 1:
             raise ValueError("weights in 8 bits: dim must be positive and codes [n_out, 128 * ceil(dim / 128)]")
         n, blocks = codes.shape[0], -(-dim // _BLOCK)
-        cs = _held("codes", codes, n, blocks * _BLOCK, 16, -1)
+        cs = _held("codes", codes, n, blocks * _BLOCK, 16, -1, _CODES)
         self.index = codes.get_device()
-        ss = _held("scale", scale, -(-n // _BLOCK), blocks, 1, self.index, (torch.uint8, torch.float32))
+        ss = _held("scale", scale, -(-n // _BLOCK), blocks, 1, self.index, _BYTES + (torch.float32,))
         if codes.data_ptr() % 16:
             raise ValueError("codes must be aligned to 16 bytes")
         self.codes, self.scale, self.dim, self.n_out = codes, scale, dim, n
-        self.c = B.hsd_weight_quant(codes.data_ptr(), scale.data_ptr(), cs, ss, B.HSD_SCALE_POW2 if scale.dtype == torch.uint8 else B.HSD_SCALE_FP32)
+        self.c = B.hsd_weight_quant(codes.data_ptr(), scale.data_ptr(), cs, ss, B.HSD_SCALE_FP32 if scale.dtype == torch.float32 else B.HSD_SCALE_POW2)
 
     @classmethod
     def quantize(cls, w: torch.Tensor, scale: torch.dtype = torch.uint8) -> "Weight8":
@@ -147,7 +153,7 @@ def norm_rows(x: torch.Tensor, gain: Optional[torch.Tensor] = None, eps: float =
               out: Optional[torch.Tensor] = None) -> Tuple[Rows8, torch.Tensor]:
     """h = x + residual, and h * gain / sqrt(mean(h^2) + eps) in 8 bits.  Returns (rows, h): h in the residual's type, in `out` if given (which may be
     residual itself) or a new tensor; x itself without a residual.  x and residual: [rows, dim], bfloat16 or float32 each; gain:
-    float32 [dim].  h is added and normalised in 32 bits."""
+    float32 [dim].  The norm is of the unrounded h, in 64 bits."""
     xs = _matrix("x", x)
     n, dim = x.shape
     index = x.get_device()
