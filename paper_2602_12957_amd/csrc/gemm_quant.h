@@ -110,6 +110,19 @@ __device__ __forceinline__ Fragment16 widen(const i32x8 &f, float scale) {
   return r;
 }
 
+// A finite float scale as the matrix unit takes it: scale = part * 2^(byte - 127) * 2^-less, part in +-[1, 2).  (`less`: to be taken from the rows' exponents, which
+// are at least -100: 0 but for scales below 2^-126; a scale of 0 takes everything from them, so that all products vanish and NaN stays.)
+struct ScaleParts {
+  float part;
+  uint32_t byte, less;
+};
+__device__ __forceinline__ ScaleParts scale_parts(uint32_t u) {
+  const uint32_t sign = u & 0x80000000u, man = u & 0x7fffffu, e = u >> 23 & 255;
+  const uint32_t up = man ? __builtin_clz(man) - 8 : 0;   // to bring a subnormal one's first bit to where it is not written
+  if (e != 0) return {__uint_as_float(sign | 0x3f800000u | man), e, 0u};
+  return {__uint_as_float(sign | 0x3f800000u | (man << up & 0x7fffffu)), 0u, man ? up - 1 : 255u};
+}
+
 // All of this wave's LDS operations are done, then those of all
 __device__ __forceinline__ void lds_barrier() {
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -117,6 +130,10 @@ __device__ __forceinline__ void lds_barrier() {
   asm volatile("" ::: "memory");
 }
 
+// Float scales: in exact products a block's sums stand beside the sums, and are added times its scale.  With 8-bit ones that would take the registers of half a tile
+// (32768 rows of 1024 to 4096 gated 387 us, 333 with the sums alone; 32768 of 4096 to 1024 165 us and 138): the unit applies a scale's power of two, and the rest, in +-[1, 2), stays in the sums:
+// they are kept divided by that of the block at hand, times the one before and over the next from block to block.
+//
 // GATED: gate and up rows of 128 output columns (BN = 256), silu(gate) * up to 8 bits; else out.  FLOATS: weight scales are floats.
 // EXACT: bf16 products of the codes instead of the 8-bit ones.  Grid: tiles.
 template <typename Cfg, bool GATED, bool FLOATS, bool EXACT, typename T>
@@ -198,7 +215,7 @@ __global__ void __launch_bounds__(Cfg::kThreads, Cfg::kWaves) k_gemm_quant(const
   }
 
   // ---- scales.  The weights' come through the scalar unit, a block ahead (vector loads would be waited for with all the slices behind them).
-  uint32_t sa[TA], sa_next[TA], ws_now[2] = {0, 0}, ws_next[2] = {0, 0}, ws_byte[2];
+  uint32_t sa[FLOATS && !EXACT && GATED ? 2 : 1][TA], sa_next[TA], ws_now[2] = {0, 0}, ws_next[2] = {0, 0}, ws_byte[2];
   const int64_t wrow = GATED ? n0 : min(n0 + wj * (BN / Cfg::WN), N - 1);   // a wave's weight rows lie in one block of 128, or in one of the gate and one of up
   const int64_t ws_at[2] = {wrow / kQuantBlock * w.scale_stride, (wrow + N) / kQuantBlock * w.scale_stride};
   auto weight_scales = [&](int kb) {
@@ -211,13 +228,17 @@ __global__ void __launch_bounds__(Cfg::kThreads, Cfg::kWaves) k_gemm_quant(const
     }
   };
 
-  // (block: the sums of the block at hand, where its scale is a float)
-  floatx16 acc[TW][TA], block[FLOATS ? TW : 1][FLOATS ? TA : 1];
+  // (block: the sums of the block at hand)
+  constexpr bool BLOCKS = FLOATS && EXACT, PARTS = FLOATS && !EXACT;
+  floatx16 acc[TW][TA], block[BLOCKS ? TW : 1][BLOCKS ? TA : 1];
   const floatx16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  float factor[2] = {0.f, 0.f};   // of the block before (FLOATS)
+  float factor[2] = {0.f, 0.f}, part[2] = {1.f, 1.f};   // scales of the block before (BLOCKS) or what the sums are to be multiplied by (PARTS); parts of the block at hand
   auto add_block = [&](int i, int j) {
 #pragma unroll
-    for (int v = 0; v < 16; ++v) acc[i][j][v] = __builtin_fmaf(block[i][j][v], factor[GATED ? i & 1 : 0], acc[i][j][v]);
+    for (int v = 0; v < 16; ++v) {
+      if constexpr (BLOCKS) acc[i][j][v] = __builtin_fmaf(block[i][j][v], factor[GATED ? i & 1 : 0], acc[i][j][v]);
+      else acc[i][j][v] *= factor[GATED ? i & 1 : 0];
+    }
   };
 
   // ---- fragments: row lane % 32 of a sub-tile, of its 64 bytes of a half block the 32 of lane / 32
@@ -255,15 +276,18 @@ __global__ void __launch_bounds__(Cfg::kThreads, Cfg::kWaves) k_gemm_quant(const
         }
       }
       if constexpr (FLOATS) {
-        if (begin && h == 0) add_block(i, j), block[i][j] = zero;
+        if (begin && h == 0) {
+          add_block(i, j);
+          if constexpr (BLOCKS) block[i][j] = zero;
+        }
       }
-      floatx16 &sum = FLOATS ? block[FLOATS ? i : 0][FLOATS ? j : 0] : acc[i][j];
+      floatx16 &sum = BLOCKS ? block[BLOCKS ? i : 0][BLOCKS ? j : 0] : acc[i][j];
       if constexpr (EXACT) {
-        if (i == 0) ca = widen(fa[buf][h][j], two_to_byte(sa[j] & 255));
+        if (i == 0) ca = widen(fa[buf][h][j], two_to_byte(sa[0][j] & 255));
 #pragma unroll
         for (int k = 0; k < 4; ++k) sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cw[i].v[k], ca.v[k], sum, 0, 0, 0);
       } else {
-        sum = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fw[buf][h][i], fa[buf][h][j], sum, 0, 0, 0, FLOATS ? 127 : ws_now[GATED ? i & 1 : 0], 0, sa[j]);
+        sum = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fw[buf][h][i], fa[buf][h][j], sum, 0, 0, 0, ws_now[GATED ? i & 1 : 0], 0, sa[PARTS && GATED ? i & 1 : 0][j]);
       }
       for (int k = n * others / (H * PRODUCTS); k < (n + 1) * others / (H * PRODUCTS); ++k) other(k);
       __builtin_amdgcn_sched_barrier(0);
@@ -288,14 +312,26 @@ __global__ void __launch_bounds__(Cfg::kThreads, Cfg::kWaves) k_gemm_quant(const
 #pragma unroll
     for (int j = 0; j < TA; ++j) {
       acc[i][j] = zero;
-      if constexpr (FLOATS) block[i][j] = zero;
+      if constexpr (BLOCKS) block[i][j] = zero;
     }
   auto begin_block = [&](int kt) {   // scales of the block at hand, and the next one's requested
-    if constexpr (FLOATS) factor[0] = __uint_as_float(ws_now[0]), factor[1] = __uint_as_float(ws_now[1]);
+    if constexpr (BLOCKS) factor[0] = __uint_as_float(ws_now[0]), factor[1] = __uint_as_float(ws_now[1]);
+    uint32_t less[2] = {0, 0};
 #pragma unroll
-    for (int i = 0; i < (GATED ? 2 : 1); ++i) ws_now[i] = FLOATS ? ws_next[i] : ws_next[i] >> ws_byte[i] & 255;
+    for (int i = 0; i < (GATED ? 2 : 1); ++i) {
+      if constexpr (PARTS) {
+        const ScaleParts p = scale_parts(ws_next[i]);
+        factor[i] = part[i] / p.part, part[i] = p.part, ws_now[i] = p.byte, less[i] = p.less;
+      } else {
+        ws_now[i] = FLOATS ? ws_next[i] : ws_next[i] >> ws_byte[i] & 255;
+      }
+    }
 #pragma unroll
-    for (int i = 0; i < TA; ++i) sa[i] = sa_next[i] >> (8 * (kt & 3));
+    for (int i = 0; i < TA; ++i) {
+      const uint32_t x = sa_next[i] >> (8 * (kt & 3));
+      sa[0][i] = PARTS ? __builtin_elementwise_sub_sat(x & 255, less[0]) : x;
+      if constexpr (PARTS && GATED) sa[1][i] = __builtin_elementwise_sub_sat(x & 255, less[1]);
+    }
     weight_scales(min(kt + 1, nk - 1));
     __builtin_amdgcn_sched_barrier(0);
   };
@@ -320,7 +356,7 @@ __global__ void __launch_bounds__(Cfg::kThreads, Cfg::kWaves) k_gemm_quant(const
     if (nk & 1) do_block(nk - 1, 0);
   }
   if constexpr (FLOATS) {
-    factor[0] = __uint_as_float(ws_now[0]), factor[1] = __uint_as_float(ws_now[1]);
+    factor[0] = BLOCKS ? __uint_as_float(ws_now[0]) : part[0], factor[1] = BLOCKS ? __uint_as_float(ws_now[1]) : part[1];
 #pragma unroll
     for (int i = 0; i < TW; ++i)
 #pragma unroll

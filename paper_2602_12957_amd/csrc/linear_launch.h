@@ -140,10 +140,9 @@ int run_linear(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, 
     else return launch_product<ProductTile<128, 128, 2, 2, 2>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
   } else {
     const int64_t tiles = quant_tiles(M, N, 128, 128);
-    if (tiles <= kUnits) return launch_product<ProductTile<128, 128, 2, 2, 4, FLOATS ? 1 : 2, true>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
+    if (tiles <= kUnits) return launch_product<ProductTile<128, 128, 2, 2, 4, 2, true>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
     if (tiles <= 2 * kUnits) return launch_product<ProductTile<128, 128, 2, 2, 2>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
-    // with float scales a block's sums stand beside the sums: half a tile has the registers for both
-    using Cfg = ProductTile<256, FLOATS ? 128 : 256, FLOATS ? 4 : 2, 2, FLOATS ? 3 : 2>;
+    using Cfg = ProductTile<256, 256, FLOATS ? 4 : 2, 2, 2>;   // (float scales: eight waves, whose sums the vector unit can multiply where they are)
     const int rest = last_rows(M, N, Cfg::BN);
     const int rc = launch_product<Cfg, false, FLOATS, EXACT, T>(st, a, w, M - rest, N, nk, out, out_stride, none);
     if (rc != HSD_OK || rest == 0) return rc;
@@ -159,15 +158,11 @@ int run_gated(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, i
   bf16 *none = nullptr;
   if (M <= 64) return launch_product<ProductTile<64, 256, 1, 4, 3, 1, true>, true, FLOATS, true, bf16>(st, a, w, M, N, nk, none, 0, q);
   if (quant_tiles(M, N, 64, 128) <= kUnits) return launch_product<ProductTile<64, 256, 1, 4, 3, 1, true>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
-  if constexpr (FLOATS) {
-    return launch_product<ProductTile<128, 256, 2, 4, 3>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
-  } else {
-    if (quant_tiles(M, N, 128, 128) <= kUnits) return launch_product<ProductTile<128, 256, 2, 2, 3, 1, true>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
-    const int rest = last_rows(M, N, 128);
-    const int rc = launch_product<ProductTile<256, 256, 2, 2, 2>, true, FLOATS, false, bf16>(st, a, w, M - rest, N, nk, none, 0, q);
-    if (rc != HSD_OK || rest == 0) return rc;
-    return run_gated<FLOATS>(st, rows_from(a, M - rest), w, rest, N, nk, rows_from(q, M - rest));
-  }
+  if (quant_tiles(M, N, 128, 128) <= kUnits) return launch_product<ProductTile<128, 256, 2, 2, 3, 1, true>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
+  const int rest = last_rows(M, N, 128);
+  const int rc = launch_product<ProductTile<256, 256, FLOATS ? 4 : 2, 2, 2>, true, FLOATS, false, bf16>(st, a, w, M - rest, N, nk, none, 0, q);
+  if (rc != HSD_OK || rest == 0) return rc;
+  return run_gated<FLOATS>(st, rows_from(a, M - rest), w, rest, N, nk, rows_from(q, M - rest));
 }
 
 }  // namespace

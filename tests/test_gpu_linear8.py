@@ -219,6 +219,25 @@ def test_nan_stays_in_its_row_and_column(rows, n_out, dim):
         assert torch.equal(got, want)
 
 
+@pytest.mark.parametrize("rows", [8, 100, 300, 2100, 5000])
+def test_float_scales_that_are_small_or_zero(rows):
+    """Scales of 0, subnormal and just normal ones, and large ones, beside each other, with rows' scales that bring their blocks' products together."""
+    L = lib()
+    a, w = random_rows8(rows, 1024, rows), random_weight8(512, 1024, 3, F32)
+    s = torch.tensor([1.0, 0.0, 2.0 ** -149, -3e-42, 1.7e-38, 0.0, 1e25, -1.9], device=DEV)
+    w.scale.copy_(torch.stack([s.roll(k) for k in range(4)]))
+    a.scale.copy_(torch.randint(112, 125, (1, 8), generator=torch.Generator(device=DEV).manual_seed(5), device=DEV).expand(rows, 8))
+    for dtype in (BF, F32):
+        check_product(L.linear(a, w, dtype), a, w)
+    small = torch.where(s.abs() < 1e-37, s, torch.zeros_like(s))   # only those, against large scales of the rows
+    w.scale.copy_(torch.stack([small.roll(k) for k in range(4)]))
+    a.scale.fill_(215)
+    for dtype in (BF, F32):
+        check_product(L.linear(a, w, dtype), a, w)
+    w.scale[:2] = 0                                                # gates of 0
+    assert not bool((L.gated(a, w).codes & 127).any())
+
+
 def test_scales_from_end_to_end():
     """Blocks whose powers of two are the smallest and the largest that rows and weights hold: results beyond fp32 are infinite, those
     below vanish, those between are right."""
