@@ -142,7 +142,9 @@ int run_linear(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, 
     const int64_t tiles = quant_tiles(M, N, 128, 128);
     if (tiles <= kUnits) return launch_product<ProductTile<128, 128, 2, 2, 4, 2, true>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
     if (tiles <= 2 * kUnits) return launch_product<ProductTile<128, 128, 2, 2, 2>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
-    using Cfg = ProductTile<256, 256, FLOATS ? 4 : 2, 2, 2>;   // (float scales: eight waves, whose sums the vector unit can multiply where they are)
+    // (eight waves: two a SIMD, one's first reads and results beside the other's products, and sums that the vector unit can multiply where they are, for
+    // float scales.  Four, whose operands come from LDS two thirds as often: 32768 rows of 4096 to 1024 128.8 us, here 124.5; 8192^3 437, here 443)
+    using Cfg = ProductTile<256, 256, 4, 2, 2>;
     const int rest = last_rows(M, N, Cfg::BN);
     const int rc = launch_product<Cfg, false, FLOATS, EXACT, T>(st, a, w, M - rest, N, nk, out, out_stride, none);
     if (rc != HSD_OK || rest == 0) return rc;
@@ -151,8 +153,9 @@ int run_linear(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, 
 }
 
 // Gate and up: up to 64 rows with bf16 products of the codes (the weights' reading is what counts there, 16 rows of 1024 to 4096 9.0 us and 7.3 with 8-bit ones,
-// and rows in 8 bits then differ from the definition's no more than by fp32's roundings); more in tiles of 64, 128 and 256 rows by 128 columns of both.  us a call, 1024 columns to 4096: 512 rows 8.5 / 10.4 / 19.0, 1024 15.5 / 12.2 / 19.5,
-// 1856 28.0 / 21.7 / 21.3, 32768 430 / 339 / 316
+// and rows in 8 bits then differ from the definition's no more than by fp32's roundings); more in tiles of 64, 128 and 256 rows by 128 columns of both.  us a call,
+// 1024 columns to 4096: 512 rows 8.5 / 10.4 / 19.0, 1024 15.5 / 12.2 / 19.5, 1856 28.0 / 21.7 / 20.5, 32768 430 / 339 / 293 (with float scales 333; tiles of
+// 256 rows in four waves 22.2 and 309)
 template <bool FLOATS>
 int run_gated(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, int N, int nk, const RowsQuant &q) {
   bf16 *none = nullptr;
@@ -160,7 +163,7 @@ int run_gated(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, i
   if (quant_tiles(M, N, 64, 128) <= kUnits) return launch_product<ProductTile<64, 256, 1, 4, 3, 1, true>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
   if (quant_tiles(M, N, 128, 128) <= kUnits) return launch_product<ProductTile<128, 256, 2, 2, 3, 1, true>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
   const int rest = last_rows(M, N, 128);
-  const int rc = launch_product<ProductTile<256, 256, FLOATS ? 4 : 2, 2, 2>, true, FLOATS, false, bf16>(st, a, w, M - rest, N, nk, none, 0, q);
+  const int rc = launch_product<ProductTile<256, 256, 4, 2, 2>, true, FLOATS, false, bf16>(st, a, w, M - rest, N, nk, none, 0, q);
   if (rc != HSD_OK || rest == 0) return rc;
   return run_gated<FLOATS>(st, rows_from(a, M - rest), w, rest, N, nk, rows_from(q, M - rest));
 }

@@ -27,4 +27,4 @@ def test_kernels_of_the_projections_in_8_bits(tmp_path):
         forms = {k[".name"]: (k[".vgpr_spill_count"], k[".private_segment_fixed_size"], k[".vgpr_count"]) for k in kernels if name in k[".name"]}
         assert forms, name
         assert {n: f for n, f in forms.items() if f[0] or f[1]} == {}
-        assert {n: f for n, f in forms.items() if f[2] > (512 if "Li256ELi256E" in n else 256)} == {}
+        assert {n: f for n, f in forms.items() if f[2] > 256} == {}
