@@ -152,13 +152,15 @@ int run_linear(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, 
   }
 }
 
-// Gate and up: up to 64 rows with bf16 products of the codes (the weights' reading is what counts there, 16 rows of 1024 to 4096 9.0 us and 7.3 with 8-bit ones,
-// and rows in 8 bits then differ from the definition's no more than by fp32's roundings); more in tiles of 64, 128 and 256 rows by 128 columns of both.  us a call,
+// Gate and up: up to 64 rows with bf16 products of the codes (rows in 8 bits then differ from the definition's by fp32's roundings alone), in tiles of 32 rows
+// where those leave no second round: 16 rows of 1024 to 4096 8.1 us, in tiles of 64 rows 10.2, and 7.3 with 8-bit products; 64 rows 8.2 and 10.4.
+// More rows in tiles of 64, 128 and 256 by 128 columns of both.  us a call,
 // 1024 columns to 4096: 512 rows 8.5 / 10.4 / 19.0, 1024 15.5 / 12.2 / 19.5, 1856 28.0 / 21.7 / 20.5, 32768 430 / 339 / 293 (with float scales 333; tiles of
 // 256 rows in four waves 22.2 and 309)
 template <bool FLOATS>
 int run_gated(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, int N, int nk, const RowsQuant &q) {
   bf16 *none = nullptr;
+  if (M <= 64 && quant_tiles(M, N, 32, 128) <= kUnits) return launch_product<ProductTile<32, 256, 1, 4, 4, 2, true>, true, FLOATS, true, bf16>(st, a, w, M, N, nk, none, 0, q);
   if (M <= 64) return launch_product<ProductTile<64, 256, 1, 4, 3, 1, true>, true, FLOATS, true, bf16>(st, a, w, M, N, nk, none, 0, q);
   if (quant_tiles(M, N, 64, 128) <= kUnits) return launch_product<ProductTile<64, 256, 1, 4, 3, 1, true>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
   if (quant_tiles(M, N, 128, 128) <= kUnits) return launch_product<ProductTile<128, 256, 2, 2, 3, 1, true>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
