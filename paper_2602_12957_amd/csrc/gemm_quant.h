@@ -94,33 +94,34 @@ __device__ __forceinline__ float swiglu(float g, float u) {
   return g * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * g)) * u;
 }
 
-// The 32 codes of a fragment as bf16, times a power of two (exact): operands of four bf16 products
-struct Fragment16 {
-  bf16x8 v[4];
-};
-__device__ __forceinline__ Fragment16 widen(const i32x8 &f, float scale) {
-  Fragment16 r;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f[2 * i], scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f[2 * i], scale, true);
-    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f[2 * i + 1], scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f[2 * i + 1], scale, true);
-    r.v[i] = bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-  }
-  return r;
+// Eight of a fragment's 32 codes as bf16, times a power of two (exact): an operand of a bf16 product
+__device__ __forceinline__ bf16x8 widen(const i32x8 &f, int k, float scale) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f[2 * k], scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f[2 * k], scale, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f[2 * k + 1], scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f[2 * k + 1], scale, true);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// A finite float scale as the matrix unit takes it: scale = part * 2^(byte - 127) * 2^-less, part in +-[1, 2).  (`less`: to be taken from the rows' exponents, which
-// are at least -100: 0 but for scales below 2^-126; a scale of 0 takes everything from them, so that all products vanish and NaN stays.)
+// A finite float scale as products take it: scale = part * 2^(byte - 127) * 2^-less, part in +-[1, 2).  `less` is to be taken from the rows' exponents, which
+// are at least -100: 0 but for scales below 2^-126; a scale of 0 takes everything from them, so that all products vanish and NaN stays.  EXACT: bytes within
+// 9 .. 245, so that a code times the power of two is a bf16 number; the rest is taken from the rows' too (what then leaves bf16's range there leaves fp32's in the product).
 struct ScaleParts {
   float part;
-  uint32_t byte, less;
+  uint32_t byte;
+  int less;
 };
+template <bool EXACT>
 __device__ __forceinline__ ScaleParts scale_parts(uint32_t u) {
   const uint32_t sign = u & 0x80000000u, man = u & 0x7fffffu, e = u >> 23 & 255;
   const uint32_t up = man ? __builtin_clz(man) - 8 : 0;   // to bring a subnormal one's first bit to where it is not written
-  if (e != 0) return {__uint_as_float(sign | 0x3f800000u | man), e, 0u};
-  return {__uint_as_float(sign | 0x3f800000u | (man << up & 0x7fffffu)), 0u, man ? up - 1 : 255u};
+  ScaleParts p;
+  if (e != 0) p = {__uint_as_float(sign | 0x3f800000u | man), e, 0};
+  else p = {__uint_as_float(sign | 0x3f800000u | (man << up & 0x7fffffu)), 0u, man ? static_cast<int>(up) - 1 : 255};
+  if constexpr (EXACT) {
+    const int b = p.byte, c = min(max(b, 9), 245);
+    p.byte = c, p.less += c - b;
+  }
+  return p;
 }
 
 // All of this wave's LDS operations are done, then those of all
@@ -130,12 +131,12 @@ __device__ __forceinline__ void lds_barrier() {
   asm volatile("" ::: "memory");
 }
 
-// Float scales: in exact products a block's sums stand beside the sums, and are added times its scale.  With 8-bit ones that would take the registers of half a tile
-// (32768 rows of 1024 to 4096 gated 387 us, 333 with the sums alone; 32768 of 4096 to 1024 165 us and 138): the unit applies a scale's power of two, and the rest, in +-[1, 2), stays in the sums:
-// they are kept divided by that of the block at hand, times the one before and over the next from block to block.
+// Float scales: exact products for fp32 results have a block's own sums beside the sums, added times its scale. Elsewhere that would take the registers of half a tile
+// (32768 rows of 4096 to 1024 165 us, here 138; where tiles are small it is the faster and the more exact, 777 rows of 1000 to 1537 8.2 and 9.1): operands carry a scale's power of two, and the sums its rest, in +-[1, 2): they are kept divided by that of the block at hand, so multiplied by the one before
+// over the next from block to block.
 //
 // GATED: gate and up rows of 128 output columns (BN = 256), silu(gate) * up to 8 bits; else out.  FLOATS: weight scales are floats.
-// EXACT: bf16 products of the codes instead of the 8-bit ones.  Grid: tiles.
+// EXACT: bf16 products of the codes instead of the 8-bit ones, by quarters of half a block (a quarter's operands are all that is in registers in 16 bits).  Grid: tiles.
 template <typename Cfg, bool GATED, bool FLOATS, bool EXACT, typename T>
 __global__ void __launch_bounds__(Cfg::kThreads, Cfg::kWaves) k_gemm_quant(const RowsQuant a, const WeightQuant w, int M, int N, int nk, T *__restrict__ out,
                                                                           int64_t out_stride, const RowsQuant q) {
@@ -215,7 +216,8 @@ __global__ void __launch_bounds__(Cfg::kThreads, Cfg::kWaves) k_gemm_quant(const
   }
 
   // ---- scales.  The weights' come through the scalar unit, a block ahead (vector loads would be waited for with all the slices behind them).
-  uint32_t sa[FLOATS && !EXACT && GATED ? 2 : 1][TA], sa_next[TA], ws_now[2] = {0, 0}, ws_next[2] = {0, 0}, ws_byte[2];
+  constexpr int kApart = FLOATS && GATED ? 2 : 1;
+  uint32_t sa[kApart][TA], sa_next[TA], ws_now[2] = {0, 0}, ws_next[2] = {0, 0}, ws_byte[2];
   const int64_t wrow = GATED ? n0 : min(n0 + wj * (BN / Cfg::WN), N - 1);   // a wave's weight rows lie in one block of 128, or in one of the gate and one of up
   const int64_t ws_at[2] = {wrow / kQuantBlock * w.scale_stride, (wrow + N) / kQuantBlock * w.scale_stride};
   auto weight_scales = [&](int kb) {
@@ -228,15 +230,15 @@ __global__ void __launch_bounds__(Cfg::kThreads, Cfg::kWaves) k_gemm_quant(const
     }
   };
 
-  // (block: the sums of the block at hand)
-  constexpr bool BLOCKS = FLOATS && EXACT, PARTS = FLOATS && !EXACT;
+  constexpr bool BLOCKS = FLOATS && EXACT && !GATED;   // a block's sums by themselves
   floatx16 acc[TW][TA], block[BLOCKS ? TW : 1][BLOCKS ? TA : 1];
   const floatx16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  float factor[2] = {0.f, 0.f}, part[2] = {1.f, 1.f};   // scales of the block before (BLOCKS) or what the sums are to be multiplied by (PARTS); parts of the block at hand
-  auto add_block = [&](int i, int j) {
+  // (FLOATS) what the sums are to be multiplied by, and the block's part that they are divided by; BLOCKS: what the sums of the block before are
+  float factor[2] = {1.f, 1.f}, part[2] = {1.f, 1.f};
+  auto rescale = [&](int i, int j) {
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
-      if constexpr (BLOCKS) acc[i][j][v] = __builtin_fmaf(block[i][j][v], factor[GATED ? i & 1 : 0], acc[i][j][v]);
+      if constexpr (BLOCKS) acc[i][j][v] = __builtin_fmaf(block[i][j][v], factor[0], acc[i][j][v]), block[i][j][v] = 0.f;
       else acc[i][j][v] *= factor[GATED ? i & 1 : 0];
     }
   };
@@ -265,32 +267,37 @@ __global__ void __launch_bounds__(Cfg::kThreads, Cfg::kWaves) k_gemm_quant(const
   // The products of a step, with what else it has to do dealt out between them; `begin`: it begins a block
   constexpr int PRODUCTS = TA * TW, FRAGS = H * (TA + TW), OWN = Cfg::ASK ? 0 : REQUESTS;   // (requests among the products)
   auto step = [&](int buf, bool begin, auto &&other, int others) {
-    Fragment16 cw[EXACT ? TW : 1], ca;
+    if constexpr (EXACT) {
+      bf16x8 cw[TW];
 #pragma unroll
-    for (int n = 0; n < H * PRODUCTS; ++n) {
-      const int h = n / PRODUCTS, j = n % PRODUCTS / TW, i = n % TW;
-      if constexpr (EXACT) {
-        if (n % PRODUCTS == 0) {
+      for (int n = 0; n < H * 4 * TA; ++n) {   // a quarter of half a block, of a row of sub-tiles
+        const int h = n / (4 * TA), k = n / TA % 4, j = n % TA;
+        if (j == 0) {
 #pragma unroll
-          for (int k = 0; k < TW; ++k) cw[k] = widen(fw[buf][h][k], FLOATS ? 1.f : two_to_byte(ws_now[GATED ? k & 1 : 0]));
+          for (int i = 0; i < TW; ++i) cw[i] = widen(fw[buf][h][i], k, BLOCKS ? 1.f : two_to_byte(ws_now[GATED ? i & 1 : 0]));
         }
-      }
-      if constexpr (FLOATS) {
-        if (begin && h == 0) {
-          add_block(i, j);
-          if constexpr (BLOCKS) block[i][j] = zero;
-        }
-      }
-      floatx16 &sum = BLOCKS ? block[BLOCKS ? i : 0][BLOCKS ? j : 0] : acc[i][j];
-      if constexpr (EXACT) {
-        if (i == 0) ca = widen(fa[buf][h][j], two_to_byte(sa[0][j] & 255));
+        const bf16x8 ca = widen(fa[buf][h][j], k, two_to_byte(sa[0][j] & 255));
+        bf16x8 cu = ca;   // (float scales may leave the rows other exponents for gate and up: next to never, but a branch here costs more than widening twice)
+        if constexpr (kApart == 2) cu = widen(fa[buf][h][j], k, two_to_byte(sa[1 % kApart][j] & 255));
 #pragma unroll
-        for (int k = 0; k < 4; ++k) sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cw[i].v[k], ca.v[k], sum, 0, 0, 0);
-      } else {
-        sum = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fw[buf][h][i], fa[buf][h][j], sum, 0, 0, 0, ws_now[GATED ? i & 1 : 0], 0, sa[PARTS && GATED ? i & 1 : 0][j]);
+        for (int i = 0; i < TW; ++i) {
+          if (FLOATS && begin && h == 0 && k == 0) rescale(i, j);
+          floatx16 &sum = BLOCKS ? block[BLOCKS ? i : 0][BLOCKS ? j : 0] : acc[i][j];
+          sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cw[i], i & 1 ? cu : ca, sum, 0, 0, 0);
+        }
+        for (int o = n * others / (H * TA * 4); o < (n + 1) * others / (H * TA * 4); ++o) other(o);
+        __builtin_amdgcn_sched_barrier(0);
       }
-      for (int k = n * others / (H * PRODUCTS); k < (n + 1) * others / (H * PRODUCTS); ++k) other(k);
-      __builtin_amdgcn_sched_barrier(0);
+    } else {
+#pragma unroll
+      for (int n = 0; n < H * PRODUCTS; ++n) {
+        const int h = n / PRODUCTS, j = n % PRODUCTS / TW, i = n % TW;
+        if (FLOATS && begin && h == 0) rescale(i, j);
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fw[buf][h][i], fa[buf][h][j], acc[i][j], 0, 0, 0, ws_now[GATED ? i & 1 : 0], 0,
+                                                                    sa[GATED ? i & 1 & (kApart - 1) : 0][j]);
+        for (int k = n * others / (H * PRODUCTS); k < (n + 1) * others / (H * PRODUCTS); ++k) other(k);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
   };
 
@@ -315,22 +322,23 @@ __global__ void __launch_bounds__(Cfg::kThreads, Cfg::kWaves) k_gemm_quant(const
       if constexpr (BLOCKS) block[i][j] = zero;
     }
   auto begin_block = [&](int kt) {   // scales of the block at hand, and the next one's requested
-    if constexpr (BLOCKS) factor[0] = __uint_as_float(ws_now[0]), factor[1] = __uint_as_float(ws_now[1]);
-    uint32_t less[2] = {0, 0};
+    int less[2] = {0, 0};
 #pragma unroll
     for (int i = 0; i < (GATED ? 2 : 1); ++i) {
-      if constexpr (PARTS) {
-        const ScaleParts p = scale_parts(ws_next[i]);
+      if constexpr (BLOCKS) {
+        factor[0] = kt > 0 ? __uint_as_float(ws_now[0]) : 0.f, ws_now[0] = ws_next[0];
+      } else if constexpr (FLOATS) {
+        const ScaleParts p = scale_parts<EXACT>(ws_next[i]);
         factor[i] = part[i] / p.part, part[i] = p.part, ws_now[i] = p.byte, less[i] = p.less;
       } else {
-        ws_now[i] = FLOATS ? ws_next[i] : ws_next[i] >> ws_byte[i] & 255;
+        ws_now[i] = ws_next[i] >> ws_byte[i] & 255;
       }
     }
 #pragma unroll
     for (int i = 0; i < TA; ++i) {
       const uint32_t x = sa_next[i] >> (8 * (kt & 3));
-      sa[0][i] = PARTS ? __builtin_elementwise_sub_sat(x & 255, less[0]) : x;
-      if constexpr (PARTS && GATED) sa[1][i] = __builtin_elementwise_sub_sat(x & 255, less[1]);
+      sa[0][i] = FLOATS && !BLOCKS ? max(static_cast<int>(x & 255) - less[0], 0) : x;
+      if constexpr (kApart == 2) sa[1][i] = max(static_cast<int>(x & 255) - less[1], 0);
     }
     weight_scales(min(kt + 1, nk - 1));
     __builtin_amdgcn_sched_barrier(0);
@@ -356,11 +364,11 @@ __global__ void __launch_bounds__(Cfg::kThreads, Cfg::kWaves) k_gemm_quant(const
     if (nk & 1) do_block(nk - 1, 0);
   }
   if constexpr (FLOATS) {
-    factor[0] = BLOCKS ? __uint_as_float(ws_now[0]) : part[0], factor[1] = BLOCKS ? __uint_as_float(ws_now[1]) : part[1];
+    factor[0] = BLOCKS ? __uint_as_float(ws_now[0]) : part[0], factor[1] = part[1];
 #pragma unroll
     for (int i = 0; i < TW; ++i)
 #pragma unroll
-      for (int j = 0; j < TA; ++j) add_block(i, j);
+      for (int j = 0; j < TA; ++j) rescale(i, j);
   }
   // ---- results: lane l has row l % 32 of a sub-tile and, of its 32 weight rows, 8 (v / 4) + 4 (l / 32) + v % 4
   unsigned char *stage = smem_raw;

@@ -87,15 +87,17 @@ __global__ void __launch_bounds__(64 * FewRows<MT>::kMostWaves) k_gemm_quant_few
       request(kb + S * waves, slot);
     }
     slot = slot + 1 == S ? 0 : slot + 1;
-    Fragment16 fw;
-    if constexpr (EXACT) fw = widen(cw, FLOATS ? 1.f : two_to_byte(sw));
+    bf16x8 fw[4];
+    if constexpr (EXACT) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) fw[k] = widen(cw, k, FLOATS ? 1.f : two_to_byte(sw));
+    }
 #pragma unroll
     for (int j = 0; j < MT; ++j) {
       floatx4 sum = FLOATS ? zero : acc[j];
       if constexpr (EXACT) {
-        const Fragment16 fa = widen(ca[j], two_to_byte(sa[j]));
 #pragma unroll
-        for (int k = 0; k < 4; ++k) sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw.v[k], fa.v[k], sum, 0, 0, 0);
+        for (int k = 0; k < 4; ++k) sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw[k], widen(ca[j], k, two_to_byte(sa[j])), sum, 0, 0, 0);
       } else {
         sum = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(cw, ca[j], sum, 0, 0, 0, FLOATS ? 127 : sw, 0, sa[j]);
       }

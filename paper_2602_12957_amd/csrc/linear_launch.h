@@ -135,7 +135,7 @@ int run_linear(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, 
   if (quant_tiles(M, N, 64, 64) <= kUnits) return launch_product<ProductTile<64, 64, 2, 2, 4, 2, true>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
   if (quant_tiles(M, N, 64, 128) <= kUnits) return launch_product<ProductTile<64, 128, 2, 2, 3, 2, true>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
   if constexpr (EXACT) {
-    // (the codes' bf16 forms take the registers of larger tiles with float scales: 4096 rows of 4096 to 4096 145 us in tiles of 64x128, 178 of 128x128)
+    // (a block's sums beside the sums take the registers of larger tiles with float scales: 4096 rows of 4096 to 4096 145 us in tiles of 64x128, 178 of 128x128)
     if constexpr (FLOATS) return launch_product<ProductTile<64, 128, 2, 2, 3, 1, true>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
     else return launch_product<ProductTile<128, 128, 2, 2, 2>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
   } else {
@@ -152,20 +152,18 @@ int run_linear(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, 
   }
 }
 
-// Gate and up: up to 64 rows with bf16 products of the codes (rows in 8 bits then differ from the definition's by fp32's roundings alone), in tiles of 32 rows
-// where those leave no second round: 16 rows of 1024 to 4096 8.1 us, in tiles of 64 rows 10.2, and 7.3 with 8-bit products; 64 rows 8.2 and 10.4.
-// More rows in tiles of 64, 128 and 256 by 128 columns of both.  us a call,
-// 1024 columns to 4096: 512 rows 8.5 / 10.4 / 19.0, 1024 15.5 / 12.2 / 19.5, 1856 28.0 / 21.7 / 20.5, 32768 430 / 339 / 293 (with float scales 333; tiles of
-// 256 rows in four waves 22.2 and 309)
+// Gate and up: bf16 products of the codes, so that rows in 8 bits differ from the definition's by fp32's roundings alone (8-bit products take 293 us where these take 447, and move
+// values across the borders between codes: errors of a feed-forward block 1.1 to 1.9 times those of the definition's roundings).  Tiles of 32, 64, 128 or 256 rows by
+// 128 columns of both, the smallest that leave no second round, 256 beyond; us a call, 1024 columns to 4096: 16 rows 8.1 / 10.2, 512 in tiles of 64 11.5,
+// 1024 of 64 / 128 / 256 20.9 / 18.1 / 26.0, 1856 38.5 / 32.4 / 30.0, 32768 622 / 519 / 447 (with float scales 520)
 template <bool FLOATS>
 int run_gated(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, int N, int nk, const RowsQuant &q) {
   bf16 *none = nullptr;
-  if (M <= 64 && quant_tiles(M, N, 32, 128) <= kUnits) return launch_product<ProductTile<32, 256, 1, 4, 4, 2, true>, true, FLOATS, true, bf16>(st, a, w, M, N, nk, none, 0, q);
-  if (M <= 64) return launch_product<ProductTile<64, 256, 1, 4, 3, 1, true>, true, FLOATS, true, bf16>(st, a, w, M, N, nk, none, 0, q);
-  if (quant_tiles(M, N, 64, 128) <= kUnits) return launch_product<ProductTile<64, 256, 1, 4, 3, 1, true>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
-  if (quant_tiles(M, N, 128, 128) <= kUnits) return launch_product<ProductTile<128, 256, 2, 2, 3, 1, true>, true, FLOATS, false, bf16>(st, a, w, M, N, nk, none, 0, q);
+  if (quant_tiles(M, N, 32, 128) <= kUnits) return launch_product<ProductTile<32, 256, 1, 4, 4, 2, true>, true, FLOATS, true, bf16>(st, a, w, M, N, nk, none, 0, q);
+  if (quant_tiles(M, N, 64, 128) <= kUnits) return launch_product<ProductTile<64, 256, 1, 4, 3, 1, true>, true, FLOATS, true, bf16>(st, a, w, M, N, nk, none, 0, q);
+  if (quant_tiles(M, N, 128, 128) <= kUnits) return launch_product<ProductTile<128, 256, 2, 4, 3>, true, FLOATS, true, bf16>(st, a, w, M, N, nk, none, 0, q);
   const int rest = last_rows(M, N, 128);
-  const int rc = launch_product<ProductTile<256, 256, 4, 2, 2>, true, FLOATS, false, bf16>(st, a, w, M - rest, N, nk, none, 0, q);
+  const int rc = launch_product<ProductTile<256, 256, 4, 2, 2>, true, FLOATS, true, bf16>(st, a, w, M - rest, N, nk, none, 0, q);
   if (rc != HSD_OK || rest == 0) return rc;
   return run_gated<FLOATS>(st, rows_from(a, M - rest), w, rest, N, nk, rows_from(q, M - rest));
 }
