@@ -16,10 +16,10 @@ struct WeightQuant {
   int64_t code_stride, scale_stride;
 };
 
-// N LDS-direct loads of 1 KB, N = 1, 2 or 4: lane l's 16 bytes of load j go to dst + 1024 j + 16 l; they come from base - 3072 + off[j] + 1024 j (an
+// N LDS-direct loads of 1 KB, N = 1, 2 or 4: lane l's 16 bytes of load j go to dst + 1024 j + 16 l; they come from base - 3 KB + off[j] + 1024 j (an
 // instruction's offset moves both addresses).  In asm: the compiler would otherwise wait for every load in flight before each LDS
 // read.  No register is written; the reads wait by quant_wait and a barrier.  m0 is put back as it was found.
-constexpr int kLoadBias = 3072;
+constexpr int kLoadBias = 3 * 1024;
 template <int N>
 __device__ __forceinline__ void lds_load(uint32_t dst, uint64_t b, const uint32_t *off) {
   static_assert(N == 1 || N == 2 || N == 4, "loads of a group");
@@ -37,8 +37,8 @@ __device__ __forceinline__ void lds_load(uint32_t dst, uint64_t b, const uint32_
   else
     asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"
                  "global_load_lds_dwordx4 %2, %6\n\tglobal_load_lds_dwordx4 %3, %6 offset:1024\n\t"
-                 "global_load_lds_dwordx4 %4, %6 offset:2048\n\tglobal_load_lds_dwordx4 %5, %6 offset:3072\n\t"
-                 "s_mov_b32 m0, %0" : "=&s"(m0) : "s"(dst), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(p) : "memory");
+                 "global_load_lds_dwordx4 %4, %6 offset:2048\n\tglobal_load_lds_dwordx4 %5, %6 offset:%7\n\t"
+                 "s_mov_b32 m0, %0" : "=&s"(m0) : "s"(dst), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(p), "n"(kLoadBias) : "memory");
 }
 // One of 256 bytes, 4 a lane
 __device__ __forceinline__ void lds_load_256(uint32_t dst, uint64_t p) {
@@ -131,9 +131,10 @@ __device__ __forceinline__ void lds_barrier() {
   asm volatile("" ::: "memory");
 }
 
-// Float scales: exact products for fp32 results have a block's own sums beside the sums, added times its scale. Elsewhere that would take the registers of half a tile
-// (32768 rows of 4096 to 1024 165 us, here 138; where tiles are small it is the faster and the more exact, 777 rows of 1000 to 1537 8.2 and 9.1): operands carry a scale's power of two, and the sums its rest, in +-[1, 2): they are kept divided by that of the block at hand, so multiplied by the one before
-// over the next from block to block.
+// Float scales: exact products for fp32 results have a block's own sums beside the sums, added times its scale (where tiles are small that is the faster and the
+// more exact: 777 rows of 1000 to 1537 8.3 us, otherwise 9.1).  With larger tiles it would take the registers of half a tile (32768 rows of 4096 to 1024 165 us, here 138):
+// operands carry a scale's power of two, and the sums its rest, in +-[1, 2): they are kept divided by that of the block at hand, so multiplied by the one before over the
+// next from block to block.
 //
 // GATED: gate and up rows of 128 output columns (BN = 256), silu(gate) * up to 8 bits; else out.  FLOATS: weight scales are floats.
 // EXACT: bf16 products of the codes instead of the 8-bit ones, by quarters of half a block (a quarter's operands are all that is in registers in 16 bits).  Grid: tiles.
