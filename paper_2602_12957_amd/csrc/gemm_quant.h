@@ -143,6 +143,7 @@ __global__ void __launch_bounds__(Cfg::kThreads, Cfg::kWaves) k_gemm_quant(const
                                                                           int64_t out_stride, const RowsQuant q) {
   constexpr int BM = Cfg::BM, BN = Cfg::BN, TA = Cfg::TA, TW = Cfg::TW, NW = Cfg::NW, S = Cfg::S, H = Cfg::H;
   constexpr int COLS = GATED ? BN / 2 : BN;
+  static_assert(!GATED || EXACT, "a value that becomes a code has no larger error than fp32's roundings");
   static_assert(!GATED || (COLS == kQuantBlock && TW % 2 == 0), "a workgroup has whole blocks of the rows that it rounds");
   static_assert(Cfg::out_bytes(GATED, sizeof(T)) <= Cfg::kLds, "results are staged in the operands' place");
   extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
@@ -294,8 +295,7 @@ __global__ void __launch_bounds__(Cfg::kThreads, Cfg::kWaves) k_gemm_quant(const
       for (int n = 0; n < H * PRODUCTS; ++n) {
         const int h = n / PRODUCTS, j = n % PRODUCTS / TW, i = n % TW;
         if (FLOATS && begin && h == 0) rescale(i, j);
-        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fw[buf][h][i], fa[buf][h][j], acc[i][j], 0, 0, 0, ws_now[GATED ? i & 1 : 0], 0,
-                                                                    sa[GATED ? i & 1 & (kApart - 1) : 0][j]);
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fw[buf][h][i], fa[buf][h][j], acc[i][j], 0, 0, 0, ws_now[0], 0, sa[0][j]);
         for (int k = n * others / (H * PRODUCTS); k < (n + 1) * others / (H * PRODUCTS); ++k) other(k);
         __builtin_amdgcn_sched_barrier(0);
       }
