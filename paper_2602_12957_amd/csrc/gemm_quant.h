@@ -104,7 +104,8 @@ __device__ __forceinline__ bf16x8 widen(const i32x8 &f, int k, float scale) {
 
 // A finite float scale as products take it: scale = part * 2^(byte - 127) * 2^-less, part in +-[1, 2).  `less` is to be taken from the rows' exponents, which
 // are at least -100: 0 but for scales below 2^-126; a scale of 0 takes everything from them, so that all products vanish and NaN stays.  EXACT: bytes within
-// 9 .. 245, so that a code times the power of two is a bf16 number; the rest is taken from the rows' too (what then leaves bf16's range there leaves fp32's in the product).
+// 9 .. 245, so that a code times the power of two is a bf16 number.  What is missing below is taken from the rows' exponents too; what is beyond goes into part, in +-[1, 2^10) then
+// (to the rows' it would make infinities of large codes, which times a code of 0 are NaN).  The sums are held divided by it: those below 2^-116 may lose bits to that.
 struct ScaleParts {
   float part;
   uint32_t byte;
@@ -118,8 +119,9 @@ __device__ __forceinline__ ScaleParts scale_parts(uint32_t u) {
   if (e != 0) p = {__uint_as_float(sign | 0x3f800000u | man), e, 0};
   else p = {__uint_as_float(sign | 0x3f800000u | (man << up & 0x7fffffu)), 0u, man ? static_cast<int>(up) - 1 : 255};
   if constexpr (EXACT) {
-    const int b = p.byte, c = min(max(b, 9), 245);
-    p.byte = c, p.less += c - b;
+    const int b = p.byte;
+    p.part = __uint_as_float(__float_as_uint(p.part) + (max(b - 245, 0) << 23));
+    p.byte = min(max(b, 9), 245), p.less += max(9 - b, 0);
   }
   return p;
 }
@@ -133,7 +135,7 @@ __device__ __forceinline__ void lds_barrier() {
 
 // Float scales: exact products for fp32 results have a block's own sums beside the sums, added times its scale (where tiles are small that is the faster and the
 // more exact: 777 rows of 1000 to 1537 8.3 us, otherwise 9.1).  With larger tiles it would take the registers of half a tile (32768 rows of 4096 to 1024 165 us, here 138):
-// operands carry a scale's power of two, and the sums its rest, in +-[1, 2): they are kept divided by that of the block at hand, so multiplied by the one before over the
+// operands carry a scale's power of two, and the sums its rest, as ScaleParts has them: they are kept divided by that of the block at hand, so multiplied by the one before over the
 // next from block to block.
 //
 // GATED: gate and up rows of 128 output columns (BN = 256), silu(gate) * up to 8 bits; else out.  FLOATS: weight scales are floats.

@@ -123,3 +123,46 @@ def check_product(got, rows8, w8):
     # taken together they are far nearer than that: cuts go either way, and a result's error is that of its rounding, at most half a step
     rms = lambda t: float(t.square().mean().sqrt())   # noqa: E731
     assert rms(off) <= h * rms(y) + (2.0 ** -13 if got.dtype == torch.bfloat16 else rows8.dim * U) * rms(mag) / max(1.0, rows8.dim) ** 0.5 + 2.0 ** -126
+
+
+def nearest_codes_values(y):
+    """The values that rows in 8 bits hold of y (64 bits, finite), and the step between codes at each."""
+    e = exponent(block_tops(y))
+    s = torch.exp2(e).repeat_interleave(BLOCK, 1)[:, :y.shape[1]]
+    step = torch.exp2(torch.floor(torch.log2((y.abs() / s).clamp(min=2.0 ** -6))) - 3) * s
+    return torch.round(y / step) * step, step
+
+
+def moved_codes(values, y, rms):
+    """How many of the values that rows in 8 bits hold are not y's (64 bits), and how many may be if y is known up to random errors of `rms`.
+
+    A value gets another code if a border between two codes lies within its error: with a probability of the error over the step, so rms / step on
+    average at most (a mean magnitude is no larger than its rms).  A block gets another scale if its largest value is that near to a power of two times 448; such values
+    have less than two of them a factor of e, and a scale changes 128 values at most.  Six standard deviations of such a count, and six more for small ones."""
+    want, step = nearest_codes_values(y)
+    moved = int((values != want).sum())
+    few = float((rms / step).clamp(max=1.0).sum())
+    tops = block_tops(y)
+    at = block_tops(torch.where(y.abs() >= tops.repeat_interleave(BLOCK, 1)[:, :y.shape[1]], rms, torch.zeros_like(rms)))
+    few += float((2.0 * BLOCK * at / tops.clamp(min=1e-300)).clamp(max=BLOCK).sum())
+    return moved, few + 6 * few ** 0.5 + 6
+
+
+def gate_and_up(rows8, w8):
+    """silu(gate) * up in 64 bits, how far a value may be off (worst), and the rms of the errors that fp32's roundings make.
+
+    The sums: products of codes are exact, dim additions and three roundings a block at most in fp32.  A rounding is off by 2^-24 of the sum so far at most, by a
+    root of 3 less in the rms; the sum so far is a random walk's, so that the additions together leave 2^-24 * sqrt(dim / 6) of the root of the summed squares.  |silu'| <= 1.1; silu
+    and its product round eight times at most, the exponential's argument |g| times 2^-24 twice, which counts for negative gates (for positive ones it is in what is added to 1); gates
+    below -87 count as ones of silu 0, whose silu is below 2^-119."""
+    y, _, err = product(rows8, w8)
+    f, k = w8.n_out // 2, rows8.dim
+    g, u = y.split(f, 1)
+    eg, eu = err[torch.float32].split(f, 1)
+    sq = (row_values(rows8.codes, rows8.scale, k).square() @ weight_values(w8.codes, w8.scale, k).square().T).sqrt()
+    rg, ru = (U * ((k + 3 * -(-k // BLOCK) + 8) / 6.0) ** 0.5 * sq).split(f, 1)
+    sig = torch.sigmoid(g)
+    want, slope = g * sig * u, (sig * (1 + g * (1 - sig))).abs()
+    own = (8 + 2 * (-g).clamp(min=0)) * U * want.abs() + torch.where(g < -80, 2.0 ** -119 * u.abs(), torch.zeros_like(u))
+    worst = (1.1 * eg * (u.abs() + eu) + (g * sig).abs() * eu) * 1.01 + own + 2.0 ** -126
+    return want, worst, ((slope * u * rg).square() + (g * sig * ru).square() + own.square()).sqrt()

@@ -1,0 +1,55 @@
+"""Gate and up by value: float scales of every kind."""
+
+import pytest
+import torch
+
+from linear8_testlib import BLOCK, check_product, check_rows, gate_and_up
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF, F32 = torch.bfloat16, torch.float32
+FORMS = [300, 700, 1500, 4000]      # rows that 4096 weight rows' gate and up take in tiles of 32, 64, 128 and 256
+
+
+def lib():
+    from paper_2602_12957_amd import linear8
+    return linear8
+
+
+def small_codes(n, dim, seed, size):
+    """e4m3 codes of normal values times `size`, padded to whole blocks with zeros."""
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    x = torch.nn.functional.pad(torch.randn((n, dim), generator=g, device=DEV) * size, (0, -dim % BLOCK))
+    return x.to(torch.float8_e4m3fn).view(torch.uint8)
+
+
+def float_scaled(rows, dim, t, cg, cu, size=1.0, f=2048):
+    """Rows whose block b has the power 2^t[b], and gate and up weights whose scales take it back but for 2^cg and 2^cu: +-[1, 2) * 2^(c - t[b])."""
+    L = lib()
+    a = L.Rows8(small_codes(rows, dim, rows, size), torch.tensor(([127 + e for e in t] + [127])[:4], dtype=torch.uint8, device=DEV).expand(rows, 4).contiguous(), dim)
+    g = torch.Generator().manual_seed(5)
+    s = 1 + torch.rand((2 * f // BLOCK, len(t)), generator=g, dtype=torch.float64)
+    s = torch.where(torch.rand(s.shape, generator=g) < 0.5, -s, s)
+    s[:f // BLOCK] *= torch.exp2(torch.tensor([float(cg - e) for e in t], dtype=torch.float64))
+    s[f // BLOCK:] *= torch.exp2(torch.tensor([float(cu - e) for e in t], dtype=torch.float64))
+    s = s.float()
+    assert bool(torch.isfinite(s).all())
+    return a, L.Weight8(small_codes(2 * f, dim, 3, size), s.to(DEV), dim)
+
+
+@pytest.mark.parametrize("rows", FORMS)
+@pytest.mark.parametrize("power", [118, 119, 123, 127])
+def test_gated_of_the_largest_values_times_nothing(rows, power):
+    """A block whose rows are as large as they can be and whose weights are codes of 0 with a large scale adds nothing, before and behind one that counts."""
+    L = lib()
+    a, w = float_scaled(rows, 384, [119, 0, 119], -4, 0)
+    for b in (0, 2):
+        w.codes[:, b * BLOCK:(b + 1) * BLOCK] = 0
+        w.scale[:, b] = torch.where(torch.arange(32, device=DEV) % 3 == 0, -1.9, 1.9) * 2.0 ** power
+    a.codes[:, :BLOCK], a.codes[:, 2 * BLOCK:] = 126, 254       # +-448
+    want, worst, _ = gate_and_up(a, w)
+    got = L.gated(a, w)
+    check_rows(got, want, worst)
+    assert bool((got.read(F32) != 0).double().mean() > 0.95)
+    for dtype in (BF, F32):
+        check_product(L.linear(a, w, dtype), a, w)
