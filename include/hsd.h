@@ -401,7 +401,7 @@ typedef struct hsd_rows_quant {
 
 /* Weights in 8 bits, [n_out, dim] row-major in blocks of 128 rows by 128 columns: codes as above, one scale a block, a byte as above
  * (HSD_SCALE_POW2: the matrix unit applies it) or any finite float (HSD_SCALE_FP32: value = code * scale; a block's sum of products before its scale has to be
- * finite in 32 bits: it is where the rows' magnitudes stay below 2^100). */
+ * finite in 32 bits: it is where the rows' magnitudes stay below 2^100).  An infinite scale or NaN leaves no finite result in its weight rows' columns. */
 enum { HSD_SCALE_FP32 = 0, HSD_SCALE_POW2 = 1 };
 typedef struct hsd_weight_quant {
   const void *codes;    /* dev [n_out][128 * ceil(dim / 128)], 16-byte aligned                                   */

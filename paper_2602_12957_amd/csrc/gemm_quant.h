@@ -106,6 +106,7 @@ __device__ __forceinline__ bf16x8 widen(const i32x8 &f, int k, float scale) {
 // are at least -100: 0 but for scales below 2^-126; a scale of 0 takes everything from them, so that all products vanish and NaN stays.  EXACT: bytes within
 // 9 .. 245, so that a code times the power of two is a bf16 number.  What is missing below is taken from the rows' exponents too; what is beyond goes into part, in +-[1, 2^10) then
 // (to the rows' it would make infinities of large codes, which times a code of 0 are NaN).  The sums are held divided by it: those below 2^-116 may lose bits to that.
+// A scale that is no number: the byte 255, which the matrix unit takes for NaN, and with EXACT, whose codes it does not scale, the part.
 struct ScaleParts {
   float part;
   uint32_t byte;
@@ -120,7 +121,7 @@ __device__ __forceinline__ ScaleParts scale_parts(uint32_t u) {
   else p = {__uint_as_float(sign | 0x3f800000u | (man << up & 0x7fffffu)), 0u, man ? static_cast<int>(up) - 1 : 255};
   if constexpr (EXACT) {
     const int b = p.byte;
-    p.part = __uint_as_float(__float_as_uint(p.part) + (max(b - 245, 0) << 23));
+    p.part = e == 255 ? NAN : __uint_as_float(__float_as_uint(p.part) + (max(b - 245, 0) << 23));
     p.byte = min(max(b, 9), 245), p.less += max(9 - b, 0);
   }
   return p;

@@ -52,7 +52,7 @@ def _held(name: str, t: torch.Tensor, rows: int, least: int, step: int, index: i
 
 class Rows8:
     """Rows of `dim` values in 8 bits.  codes: uint8 (or float8_e4m3fn) [rows, 128 * ceil(dim / 128)], zeros behind dim; scale: uint8 (or
-    float8_e8m0fnu) [rows, ceil(dim / 128) rounded up to a multiple of 4]; value = code * 2^(scale - 127)."""
+    float8_e8m0fnu) [rows, ceil(dim / 128) rounded up to a multiple of 4]; value = code * 2^(scale - 127), bytes 27 .. 246 (others have no meaning)."""
     __slots__ = ("_codes", "_scale", "_room", "dim", "rows", "index", "device", "c")
 
     def __init__(self, codes: torch.Tensor, scale: torch.Tensor, dim: int):
@@ -108,8 +108,8 @@ class Rows8:
 
 class Weight8:
     """A weight matrix [n_out, dim] in 8 bits, blocks of 128 rows by 128 columns.  codes: uint8 (or float8_e4m3fn) [n_out, 128 * ceil(dim / 128)],
-    zeros behind dim; scale: [ceil(n_out / 128), ceil(dim / 128)], uint8 or float8_e8m0fnu (value = code * 2^(scale - 127)) or float32
-    (value = code * scale)."""
+    zeros behind dim; scale: [ceil(n_out / 128), ceil(dim / 128)], uint8 or float8_e8m0fnu (value = code * 2^(scale - 127); bytes 27 .. 246, others have no
+    meaning) or float32 (value = code * scale; any finite number, others leave no finite result in their columns)."""
     __slots__ = ("codes", "scale", "dim", "n_out", "index", "c")
 
     def __init__(self, codes: torch.Tensor, scale: torch.Tensor, dim: int):

@@ -1,9 +1,10 @@
-"""Gate and up by value: float scales of every kind."""
+"""Gate and up by value: float scales of every kind, and those that are no numbers."""
+import math
 
 import pytest
 import torch
 
-from linear8_testlib import BLOCK, check_product, check_rows, gate_and_up
+from linear8_testlib import BLOCK, check_product, check_rows, gate_and_up, random_rows8, random_weight8
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -37,6 +38,22 @@ def float_scaled(rows, dim, t, cg, cu, size=1.0, f=2048):
     return a, L.Weight8(small_codes(2 * f, dim, 3, size), s.to(DEV), dim)
 
 
+# ------------------------------------------------------------------------------------------------------------ scales that are no numbers
+@pytest.mark.parametrize("rows", FORMS)
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_gated_with_a_scale_that_is_no_number(rows, bad):
+    """It shows in every value of its 128 columns, in any block of the sum and in the gate or the up projection, and nowhere else."""
+    L = lib()
+    a, w = float_scaled(rows, 512, [0, 3, -2, 1], -4, 0)
+    at = {1: 0, 4: 2, 7: 3}                                     # columns' block: block of the sum
+    for c, b in at.items():
+        w.scale[c + 16 * (c == 4), b] = bad
+    got = L.gated(a, w).read(F32)
+    nan = torch.isnan(got).reshape(rows, 16, BLOCK)
+    want = torch.tensor([c in at for c in range(16)], device=DEV)[None, :, None].expand_as(nan)
+    assert torch.equal(nan, want)
+
+
 @pytest.mark.parametrize("rows", FORMS)
 @pytest.mark.parametrize("power", [118, 119, 123, 127])
 def test_gated_of_the_largest_values_times_nothing(rows, power):
@@ -53,3 +70,18 @@ def test_gated_of_the_largest_values_times_nothing(rows, power):
     assert bool((got.read(F32) != 0).double().mean() > 0.95)
     for dtype in (BF, F32):
         check_product(L.linear(a, w, dtype), a, w)
+
+
+@pytest.mark.parametrize("rows,n_out", [(8, 512), (100, 512), (300, 512), (2100, 512), (1500, 1600), (5000, 4096)])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_linear_with_a_scale_that_is_no_number(rows, n_out, bad, dtype):
+    L = lib()
+    a, w = random_rows8(rows, 512, rows), random_weight8(n_out, 512, 3, F32)
+    fine = L.linear(a, w, dtype)
+    check_product(fine, a, w)
+    w.scale[1, 0], w.scale[3, 3] = bad, bad
+    got = L.linear(a, w, dtype)
+    odd = torch.zeros(n_out, dtype=torch.bool, device=DEV)
+    odd[128:256], odd[384:512] = True, True
+    assert not bool(torch.isfinite(got[:, odd]).any()) and torch.equal(got[:, ~odd], fine[:, ~odd])
