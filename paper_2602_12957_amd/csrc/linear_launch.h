@@ -38,6 +38,8 @@ WeightQuant weight_quant(const hsd_weight_quant *w) {
   return WeightQuant{static_cast<const uint8_t *>(w->codes), w->scale, w->code_stride, w->scale_stride};
 }
 
+RowsQuant rows_from(const RowsQuant &r, int64_t m) { return RowsQuant{r.codes + m * r.code_stride, r.scale + m * r.scale_stride, r.code_stride, r.scale_stride}; }
+
 template <typename TX, typename TR>
 int launch_norm(hipStream_t st, const NormRows &a, const void *x, const void *res, void *sum) {
   // (up to 1024 threads a row: launches of 2^31 threads at most)
@@ -87,9 +89,14 @@ int launch_product(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int
   static std::atomic<uint64_t> done{0};
   if (allow_lds(reinterpret_cast<const void *>(kern), Cfg::kLds, done) != hipSuccess) return HSD_EHIP;
   constexpr int COLS = GATED ? Cfg::BN / 2 : Cfg::BN;
-  const int64_t tiles = static_cast<int64_t>((M + Cfg::BM - 1) / Cfg::BM) * ((N + COLS - 1) / COLS);
-  if (tiles > INT32_MAX / Cfg::kThreads) return HSD_ERANGE;
-  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(tiles)), dim3(Cfg::kThreads), Cfg::kLds, st, a, w, M, N, nk, out, out_stride, q);
+  // (launches of 2^31 threads at most, by whole tiles of rows: 2^24 rows to 8192 gated take two)
+  const int tiles_n = (N + COLS - 1) / COLS, most = INT32_MAX / Cfg::kThreads / tiles_n * Cfg::BM;
+  for (int64_t first = 0; first < M; first += most) {
+    const int rows = static_cast<int>(std::min<int64_t>(most, M - first));
+    const unsigned tiles = static_cast<unsigned>((rows + Cfg::BM - 1) / Cfg::BM) * tiles_n;
+    hipLaunchKernelGGL(kern, dim3(tiles), dim3(Cfg::kThreads), Cfg::kLds, st, rows_from(a, first), w, rows, N, nk, GATED ? out : out + first * out_stride, out_stride,
+                       GATED ? rows_from(q, first) : q);
+  }
   HSD_LAUNCH_CHECK();
   return HSD_OK;
 }
@@ -115,7 +122,6 @@ int last_rows(int M, int N, int bn) {
   const int rest = M % 256;
   return rest > 0 && rest <= 64 && M > 256 && rounds(quant_tiles(M, N, 256, bn)) > rounds(quant_tiles(M - rest, N, 256, bn)) ? rest : 0;
 }
-RowsQuant rows_from(const RowsQuant &r, int64_t m) { return RowsQuant{r.codes + m * r.code_stride, r.scale + m * r.scale_stride, r.code_stride, r.scale_stride}; }
 
 // The form of a product goes by how many tiles it has: the smallest tiles that leave no second round over the chip (a compute unit works as fast on
 // one large tile as on a small one, until it has all that the matrix unit can do); us a call, by tiles of 64x64 / 64x128 / 128x128 / 128x128 two a
