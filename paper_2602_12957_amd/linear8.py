@@ -186,7 +186,8 @@ def _pair(rows: Rows8, w: Weight8):
 
 
 def linear(rows: Rows8, w: Weight8, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """rows * w^T, [rows, n_out] in bfloat16 or float32 (that of `out` if given), sums in 32 bits."""
+    """rows * w^T, [rows, n_out] in bfloat16 or float32 (that of `out` if given), sums in 32 bits.  For bfloat16 each eight neighbouring products lose what lies
+    13 bits below the largest of them (7 * 2^-13 of the products' magnitudes at most); where large products cancel, take float32."""
     _pair(rows, w)
     if out is None:
         if dtype not in _TYPES:

@@ -1,10 +1,10 @@
-"""Gate and up by value: float scales of every kind, and those that are no numbers."""
+"""Products in 8 bits by value: gate and up with float scales of every kind, scales that are no numbers, sums that cancel."""
 import math
 
 import pytest
 import torch
 
-from linear8_testlib import BLOCK, check_product, check_rows, gate_and_up, random_rows8, random_weight8
+from linear8_testlib import BLOCK, HALF, check_product, check_rows, gate_and_up, product, random_rows8, random_weight8
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -85,3 +85,37 @@ def test_linear_with_a_scale_that_is_no_number(rows, n_out, bad, dtype):
     odd = torch.zeros(n_out, dtype=torch.bool, device=DEV)
     odd[128:256], odd[384:512] = True, True
     assert not bool(torch.isfinite(got[:, odd]).any()) and torch.equal(got[:, ~odd], fine[:, ~odd])
+
+
+# ------------------------------------------------------------------------------------------------------------ sums that cancel
+@pytest.mark.parametrize("rows,n_out", [(5, 40), (60, 200), (300, 300), (1500, 1600), (2100, 2100)])
+@pytest.mark.parametrize("scale", [torch.uint8, F32])
+def test_sums_that_cancel(rows, n_out, scale):
+    """Two products of 448 * 448 that cancel beside one of 20, in one group of eight columns and in different ones, and in random places: fp32 results are
+    the sums, bf16 ones within 7 * 2^-13 of the magnitudes."""
+    L = lib()
+    a, w = random_rows8(rows, 256, 1), random_weight8(n_out, 256, 2, scale)
+    values = torch.zeros((2, 256), device=DEV)
+    values[:, 0], values[0, 1], values[1, 1], values[0, 2], values[1, 2] = 448.0, 448.0, -448.0, 20.0, 1.0
+    spread = torch.zeros((2, 256), device=DEV)
+    spread[:, 0], spread[0, 131], spread[1, 131], spread[0, 70], spread[1, 70] = 448.0, 448.0, -448.0, 20.0, 1.0
+    for v in (values, spread):
+        c = v.to(torch.float8_e4m3fn).view(torch.uint8)
+        a.codes.copy_(c[:1].expand(rows, 256)), w.codes.copy_(c[1:].expand(n_out, 256))
+        a.scale.fill_(127)
+        w.scale.fill_(1 if scale == F32 else 127)
+        assert bool((L.linear(a, w, F32) == 20.0).all())
+        got = L.linear(a, w, BF).double()
+        y, mag, err = product(a, w)
+        assert bool(((got - y).abs() <= err[BF] * (1 + HALF[BF]) + HALF[BF] * y.abs()).all())
+    # every row's other half is its first with the other sign, but for one product of each
+    g = torch.Generator(device=DEV).manual_seed(9)
+    c = torch.randint(1, 127, (rows, 128), generator=g, device=DEV).to(torch.uint8)
+    a.codes.copy_(torch.cat([c, c], 1))
+    c = torch.randint(1, 127, (n_out, 128), generator=g, device=DEV).to(torch.uint8)
+    w.codes.copy_(torch.cat([c, c | 128], 1))
+    w.codes[:, 200] = 0
+    for dtype in (BF, F32):
+        got = L.linear(a, w, dtype).double()
+        y, mag, err = product(a, w)
+        assert bool(((got - y).abs() <= err[dtype] * (1 + HALF[dtype]) + HALF[dtype] * y.abs()).all())
