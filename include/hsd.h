@@ -406,12 +406,12 @@ enum { HSD_SCALE_FP32 = 0, HSD_SCALE_POW2 = 1 };
 typedef struct hsd_weight_quant {
   const void *codes;    /* dev [n_out][128 * ceil(dim / 128)], 16-byte aligned                                   */
   const void *scale;    /* dev [ceil(n_out / 128)][ceil(dim / 128)] bytes or floats, aligned to them             */
-  int64_t code_stride;  /* bytes: a multiple of 16, whole blocks at least                                        */
+  int64_t code_stride;  /* bytes: a multiple of 16, whole blocks at least, 2^23 at most                          */
   int64_t scale_stride; /* elements from row to row of blocks, whole blocks at least                             */
   int32_t scale_type;   /* HSD_SCALE_FP32 or HSD_SCALE_POW2                                                      */
 } hsd_weight_quant;
 
-/* Sizes, here and below: dim (and d_ffn) up to 2^20, fewer than 2^24 rows and weight rows, else HSD_ERANGE; n_rows may be 0.  Rows of x, residual, sum and
+/* Sizes, here and below: dim (and d_ffn) up to 2^20, fewer than 2^24 rows and weight rows, code strides as above, else HSD_ERANGE; n_rows may be 0.  Rows of x, residual, sum and
  * out lie *_stride elements apart (dim of them at least) and are aligned to their elements; dtype (of x or out): HSD_BF16 or HSD_FP32.
  *
  * x [n_rows, dim] to 8 bits.  A block's byte is e + 127, e the least in -100 .. 119 with 448 * 2^e >= every finite magnitude
@@ -428,8 +428,8 @@ int hsd_quant_norm_rows(void *stream, int32_t n_rows, int32_t dim, int32_t dtype
 /* The values that rows in 8 bits stand for, to out: exact in both types. */
 int hsd_quant_read_rows(void *stream, int32_t n_rows, int32_t dim, const hsd_rows_quant *rows, int32_t dtype, void *out, int64_t out_stride);
 
-/* w [n_out, dim] to 8 bits in blocks of 128 by 128, once for a model: bytes as in hsd_quant_rows, or floats: the largest finite magnitude / 448, 1
- * where that is 0.  Writes out->codes and out->scale.  n_out beyond 65535 * 128: HSD_ERANGE. */
+/* w [n_out, dim] to 8 bits in blocks of 128 by 128, once for a model: bytes as in hsd_quant_rows, or floats: the largest finite magnitude / 448, 2^-126 at
+ * least (smaller ones would have fewer bits themselves), 1 where that magnitude is 0.  Writes out->codes and out->scale.  n_out beyond 65535 * 128: HSD_ERANGE. */
 int hsd_quant_weights(void *stream, int32_t n_out, int32_t dim, int32_t dtype, const void *w, int64_t w_stride, const hsd_weight_quant *out);
 
 /* out[m][n] = sum_k rows[m][k] * w[n][k], [n_rows, n_out] in dtype, of the values that both stand for.  Sums in fp32; products of codes are exact.  For

@@ -126,7 +126,7 @@ class Weight8:
 
     @classmethod
     def quantize(cls, w: torch.Tensor, scale: torch.dtype = torch.uint8) -> "Weight8":
-        """w [n_out, dim], bfloat16 or float32, to 8 bits.  scale: uint8 for powers of two (the faster ones), float32 for the largest magnitude / 448."""
+        """w [n_out, dim], bfloat16 or float32, to 8 bits.  scale: uint8 for powers of two (the faster ones), float32 for the largest magnitude / 448 (2^-126 at least)."""
         stride = _matrix("w", w)
         if w.shape[0] < 1 or scale not in (torch.uint8, torch.float32):
             raise ValueError(f"w must have rows, and scale be uint8 or float32; got {tuple(w.shape)} and {scale}")

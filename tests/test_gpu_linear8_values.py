@@ -1,10 +1,10 @@
-"""Products in 8 bits by value: gate and up with float scales of every kind, scales that are no numbers, sums that cancel."""
+"""Products in 8 bits by value: gate and up with float scales of every kind, scales that are no numbers, sums that cancel, weights of small magnitudes."""
 import math
 
 import pytest
 import torch
 
-from linear8_testlib import BLOCK, HALF, check_product, check_rows, gate_and_up, product, random_rows8, random_weight8
+from linear8_testlib import (BLOCK, HALF, U, check_product, check_rows, exponent, gate_and_up, product, random_rows8, random_weight8, weight_values)
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -119,3 +119,27 @@ def test_sums_that_cancel(rows, n_out, scale):
         got = L.linear(a, w, dtype).double()
         y, mag, err = product(a, w)
         assert bool(((got - y).abs() <= err[dtype] * (1 + HALF[dtype]) + HALF[dtype] * y.abs()).all())
+
+
+# ------------------------------------------------------------------------------------------------------------ weights of small magnitudes
+@pytest.mark.parametrize("power", [-60, -98, -101, -112, -117, -120, -126, -127, -130, -140, -149])
+@pytest.mark.parametrize("scale", [torch.uint8, F32])
+def test_weights_of_small_magnitudes(power, scale):
+    """A block's scale is its largest magnitude / 448, but no smaller than 2^-126, or the least power of two from 2^-100 on; codes are the nearest of the values over it."""
+    g = torch.Generator().manual_seed(power + 200)
+    w = torch.rand((256, 200), generator=g, dtype=torch.float64) * 2 - 1
+    w[3, 5], w[200, 199] = 1.0, -1.75
+    w = (w * 2.0 ** power).float()
+    w8 = lib().Weight8.quantize(w.to(DEV), scale)
+    w = w.double()
+    top = torch.nn.functional.pad(w.abs(), (0, 56)).reshape(2, BLOCK, 2, BLOCK).amax((1, 3))
+    got = w8.scale.cpu().double() if scale == F32 else torch.exp2(w8.scale.cpu().double() - 127)
+    if scale == F32:
+        want = torch.where(top > 0, (top / 448).clamp(min=2.0 ** -126), torch.ones_like(top))
+        assert bool(((got - want).abs() <= 2 * U * want).all())   # (one division)
+    else:
+        assert torch.equal(got, torch.exp2(exponent(top)))
+    v = weight_values(w8.codes.cpu(), w8.scale.cpu(), 200)
+    each = got.repeat_interleave(BLOCK, 0).repeat_interleave(BLOCK, 1)[:, :200]
+    step = torch.exp2(torch.floor(torch.log2((w.abs() / each).clamp(min=2.0 ** -6))) - 3) * each
+    assert bool(((v - w).abs() <= step / 2 * (1 + 4 * U) + 2 * U * w.abs()).all())
