@@ -440,7 +440,7 @@ int hsd_quant_linear(void *stream, int32_t n_rows, int32_t n_out, int32_t dim, c
                      void *out, int64_t out_stride);
 
 /* silu(gate) * up, gate = rows * w[0 .. d_ffn - 1]^T and up = rows * w[d_ffn .. 2 d_ffn - 1]^T in fp32, to 8 bits as hsd_quant_rows:
- * out is [n_rows, d_ffn], d_ffn a multiple of 128. */
+ * out is [n_rows, d_ffn], d_ffn a multiple of 128.  Products of the codes are exact here.  Gates below -87 may count as ones whose silu is 0 (it is below 2^-119). */
 int hsd_quant_gated(void *stream, int32_t n_rows, int32_t d_ffn, int32_t dim, const hsd_rows_quant *rows, const hsd_weight_quant *w,
                     const hsd_rows_quant *out);
 

@@ -1,10 +1,12 @@
-"""Products in 8 bits by value: gate and up with float scales of every kind, scales that are no numbers, sums that cancel, weights of small magnitudes."""
+"""Products in 8 bits by value: codes of gate and up that are the definition's, float scales of every kind, scales that are no numbers, sums that cancel,
+weights of small magnitudes."""
 import math
 
 import pytest
 import torch
 
-from linear8_testlib import (BLOCK, HALF, U, check_product, check_rows, exponent, gate_and_up, product, random_rows8, random_weight8, weight_values)
+from linear8_testlib import (BLOCK, HALF, U, check_product, check_rows, exponent, gate_and_up, moved_codes, product, random_rows, random_rows8,
+                             random_weight8, weight_values)
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -15,6 +17,21 @@ FORMS = [300, 700, 1500, 4000]      # rows that 4096 weight rows' gate and up ta
 def lib():
     from paper_2602_12957_amd import linear8
     return linear8
+
+
+@pytest.mark.parametrize("rows", FORMS)
+@pytest.mark.parametrize("dim", [1024, 4096])
+@pytest.mark.parametrize("scale", [torch.uint8, F32])
+def test_gated_codes_are_the_definition_s(rows, dim, scale):
+    """Other codes than those of the sums in 64 bits are as few as fp32's roundings make them: the 8-bit products' cut (1.5e-5 of a sum) would make many more."""
+    L = lib()
+    a = L.quantize_rows(random_rows(rows, dim, rows + dim, spread=0.5))
+    w = L.Weight8.quantize(random_rows(4096, dim, 7, F32, spread=0.3) / dim ** 0.5, scale)
+    want, worst, rms = gate_and_up(a, w)
+    got = L.gated(a, w)
+    check_rows(got, want, worst)
+    moved, most = moved_codes(got.read(F32).double(), want, rms)
+    assert moved <= most, (moved, most)
 
 
 def small_codes(n, dim, seed, size):
@@ -38,20 +55,61 @@ def float_scaled(rows, dim, t, cg, cu, size=1.0, f=2048):
     return a, L.Weight8(small_codes(2 * f, dim, 3, size), s.to(DEV), dim)
 
 
-# ------------------------------------------------------------------------------------------------------------ scales that are no numbers
+SCALES = {   # powers of the rows' four blocks, of the gate's and of the up projection's scales beside them, size of the codes
+    "signs": ([0, 3, -2, 1], -4, 0, 1.0),
+    "up_subnormal": ([100, 119, 90, 110], -4, -25, 1.0),
+    "gate_subnormal": ([119, 118, 117, 119], -9, 40, 1.0),
+    "both_subnormal": ([119, 119, 118, 119], -12, -20, 1.0),
+    "up_large": ([-100, -90, -95, -100], -4, 26, 1.0),
+    "gate_large": ([-100, -99, -100, -98], 24, 2, 2.0 ** -5),
+    "from_block_to_block": ([-100, 119, 0, -60], -4, 5, 1.0),
+}
+
+
 @pytest.mark.parametrize("rows", FORMS)
-@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
-def test_gated_with_a_scale_that_is_no_number(rows, bad):
-    """It shows in every value of its 128 columns, in any block of the sum and in the gate or the up projection, and nowhere else."""
+@pytest.mark.parametrize("kind", list(SCALES))
+@pytest.mark.parametrize("dim", [512, 460])
+def test_gated_with_float_scales(rows, kind, dim):
+    """Scales of both signs, subnormal, below 2^-118 and above 2^118 ones, gate and up far apart: every value that is not lost to its block's scale."""
     L = lib()
-    a, w = float_scaled(rows, 512, [0, 3, -2, 1], -4, 0)
-    at = {1: 0, 4: 2, 7: 3}                                     # columns' block: block of the sum
-    for c, b in at.items():
-        w.scale[c + 16 * (c == 4), b] = bad
-    got = L.gated(a, w).read(F32)
-    nan = torch.isnan(got).reshape(rows, 16, BLOCK)
-    want = torch.tensor([c in at for c in range(16)], device=DEV)[None, :, None].expand_as(nan)
-    assert torch.equal(nan, want)
+    a, w = float_scaled(rows, dim, *SCALES[kind])
+    want, worst, _ = gate_and_up(a, w)
+    got = L.gated(a, w)
+    check_rows(got, want, worst)
+    v = got.read(F32).double()
+    assert float((v - want).norm() / want.norm()) < 0.04        # (2.65 % is what codes round)
+    assert float((v == 0).double().mean()) < (0.7 if kind == "gate_large" else 0.05)   # (there, gates far below 0 have a silu of 0)
+    assert torch.equal(L.gated(a, w).codes, got.codes)
+
+
+@pytest.mark.parametrize("rows", FORMS)
+def test_gated_with_float_scales_that_are_zero_in_some_blocks(rows):
+    L = lib()
+    a, w = float_scaled(rows, 512, [0, 20, -3, 1], -4, 3)
+    w.scale[:16, 1], w.scale[16:, 2] = 0, 0                     # of the gate, of the up projection
+    w.scale[5], w.scale[16 + 9] = 0, 0                          # columns of nothing
+    want, worst, _ = gate_and_up(a, w)
+    got = L.gated(a, w)
+    check_rows(got, want, worst)
+    zero = (want == 0).reshape(rows, 16, BLOCK).all(-1)
+    assert torch.equal(zero, torch.tensor([i in (5, 9) for i in range(16)], device=DEV).expand(rows, 16))
+
+
+@pytest.mark.parametrize("rows", FORMS)
+def test_gated_with_the_smallest_codes_at_the_smallest_scales(rows):
+    """Codes of 2^-9 times scales of 2^-118, 2^-126 and less: no product of theirs is lost to the operands' type."""
+    L = lib()
+    for power in (-118, -119, -126, -140):
+        a = L.Rows8(torch.full((rows, 128), 1, dtype=torch.uint8, device=DEV), torch.full((rows, 4), 246, dtype=torch.uint8, device=DEV), 128)
+        codes = torch.full((4096, 128), 1, dtype=torch.uint8, device=DEV)
+        codes[:, 64:] = 0
+        codes[:2048, 3] = 9                                     # (a normal code: 2^-9 * 9)
+        s = torch.tensor([[1.5 * 2.0 ** power]] * 16 + [[2.0 ** power]] * 16, dtype=torch.float64).float().to(DEV)
+        w = L.Weight8(codes, s, 128)
+        want, worst, _ = gate_and_up(a, w)
+        got = L.gated(a, w)
+        check_rows(got, want, worst)
+        assert bool((got.read(F32) > 0).all())
 
 
 @pytest.mark.parametrize("rows", FORMS)
@@ -70,6 +128,37 @@ def test_gated_of_the_largest_values_times_nothing(rows, power):
     assert bool((got.read(F32) != 0).double().mean() > 0.95)
     for dtype in (BF, F32):
         check_product(L.linear(a, w, dtype), a, w)
+
+
+@pytest.mark.parametrize("rows", [6, 70, 300, 700, 1500, 4000])
+def test_gated_of_large_values_zeros_and_nan(rows):
+    """Gates far out on either side, a row of zeros, NaN in one row and in one column, within what exact products leave."""
+    L = lib()
+    f = 256 if rows < 512 else 2048
+    x = random_rows(rows, 256, 3, F32, spread=0.0)
+    x[0] *= 1e4
+    x[1] = 0
+    a, w = L.quantize_rows(x), L.Weight8.quantize(random_rows(2 * f, 256, 4, F32, spread=0.0))
+    a.codes[2, 17], w.codes[f + 100, 5] = 127, 127
+    want, worst, _ = gate_and_up(a, w)
+    assert bool(torch.isnan(want[2]).all()) and bool(torch.isnan(want[:, 100]).all()) and int(torch.isnan(want).sum()) == f + rows - 1
+    check_rows(L.gated(a, w), want, worst)
+
+
+# ------------------------------------------------------------------------------------------------------------ scales that are no numbers
+@pytest.mark.parametrize("rows", FORMS)
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_gated_with_a_scale_that_is_no_number(rows, bad):
+    """It shows in every value of its 128 columns, in any block of the sum and in the gate or the up projection, and nowhere else."""
+    L = lib()
+    a, w = float_scaled(rows, 512, [0, 3, -2, 1], -4, 0)
+    at = {1: 0, 4: 2, 7: 3}                                     # columns' block: block of the sum
+    for c, b in at.items():
+        w.scale[c + 16 * (c == 4), b] = bad
+    got = L.gated(a, w).read(F32)
+    nan = torch.isnan(got).reshape(rows, 16, BLOCK)
+    want = torch.tensor([c in at for c in range(16)], device=DEV)[None, :, None].expand_as(nan)
+    assert torch.equal(nan, want)
 
 
 @pytest.mark.parametrize("rows,n_out", [(8, 512), (100, 512), (300, 512), (2100, 512), (1500, 1600), (5000, 4096)])
