@@ -125,11 +125,13 @@ int last_rows(int M, int N, int bn) {
 
 // The form of a product goes by how many tiles it has: the smallest tiles that leave no second round over the chip (a compute unit works as fast on
 // one large tile as on a small one, until it has all that the matrix unit can do); us a call, by tiles of 64x64 / 64x128 / 128x128 / 128x128 two a
-// unit / 256x256, 1024 columns to 1024, 4096 and 16384 rows of weights:
-//   200 rows to 4096  4.7 /  5.5 /  6.8                   512 to 4096   7.1 /  5.9 /  7.3 /  8.8 / 18.1     1024 to 4096   12.1 /  9.0 /  8.3 /  9.5 / 18.6
-//   2048 to 4096     20.9 / 15.4 / 14.4 / 13.4 / 20.0     4096 to 4096 38.4 / 28.1 / 26.4 / 23.3 / 22.0     4096 to 16384 184.5 / 138.7 / 138.5 / 110.7 / 81.4
+// unit / 256x256, 1024 columns to 4096 and 16384 rows of weights:
+//   200 rows to 4096  4.7 /  5.5 /  6.9 /  8.4 / 15.5     512 to 4096   7.1 /  6.0 /  7.4 /  8.8 / 15.9     1024 to 4096   12.3 /  9.4 /  8.7 /  9.8 / 16.5
+//   2048 to 4096     20.6 / 15.9 / 15.4 / 13.8 / 17.8     4096 to 4096 38.1 / 29.5 / 28.1 / 24.0 / 21.8     4096 to 16384 176.5 / 130.4 / 139.5 / 109.6 / 82.8
 // Few rows: a split of K over waves (k_gemm_quant_few), where that makes enough workgroups but not too many, each of which reads all rows: 64 rows of 4096 to
-// 1024 6.9 where tiles take 8.6, to 4096 8.3 / 8.7; 16 of 8192 to 8192 17.1 / 20.1, of 4096 to 16384 21.0 / 16.8.
+// 1024 6.7 where tiles take 8.6, to 4096 8.2 / 8.7; 16 of 8192 to 8192 17.1 / 20.0, of 4096 to 16384 20.8 / 16.8.
+// The count of tiles does not see that few rows leave most of a large one empty: beyond 32768 columns 64x128 would be the better ones for them (1 row of 1024 to
+// 131072 in 256x256 37.4, in 64x128 26.3; 64 rows 41.1 / 30.7).
 template <bool FLOATS, bool EXACT, typename T>
 int run_linear(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, int N, int nk, T *out, int64_t out_stride) {
   const RowsQuant none{};
@@ -141,7 +143,8 @@ int run_linear(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, 
   if (quant_tiles(M, N, 64, 64) <= kUnits) return launch_product<ProductTile<64, 64, 2, 2, 4, 2, true>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
   if (quant_tiles(M, N, 64, 128) <= kUnits) return launch_product<ProductTile<64, 128, 2, 2, 3, 2, true>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
   if constexpr (EXACT) {
-    // (a block's sums beside the sums take the registers of larger tiles with float scales: 4096 rows of 4096 to 4096 145 us in tiles of 64x128, 178 of 128x128)
+    // (a block's sums beside the sums take the registers of larger tiles with float scales: 4096 rows of 4096 to 4096 143 us in tiles of 64x128, 159 of
+    // 128x128, of 1024 47.0 / 46.6; with scales in bytes 136 / 121)
     if constexpr (FLOATS) return launch_product<ProductTile<64, 128, 2, 2, 3, 1, true>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
     else return launch_product<ProductTile<128, 128, 2, 2, 2>, false, FLOATS, EXACT, T>(st, a, w, M, N, nk, out, out_stride, none);
   } else {
@@ -158,10 +161,10 @@ int run_linear(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, 
   }
 }
 
-// Gate and up: bf16 products of the codes, so that rows in 8 bits differ from the definition's by fp32's roundings alone (8-bit products take 293 us where these take 447, and move
+// Gate and up: bf16 products of the codes, so that rows in 8 bits differ from the definition's by fp32's roundings alone (8-bit products took 293 us where these take 458, and move
 // values across the borders between codes: errors of a feed-forward block 1.1 to 1.9 times those of the definition's roundings).  Tiles of 32, 64, 128 or 256 rows by
-// 128 columns of both, the smallest that leave no second round, 256 beyond; us a call, 1024 columns to 4096: 16 rows 8.1 / 10.2, 512 in tiles of 64 11.5,
-// 1024 of 64 / 128 / 256 20.9 / 18.1 / 26.0, 1856 38.5 / 32.4 / 30.0, 32768 622 / 519 / 447 (with float scales 520)
+// 128 columns of both, the smallest that leave no second round, 256 beyond; us a call, 1024 columns to 4096: 16 rows of 32 / 64 8.2 / 10.2, 512 16.9 / 12.5,
+// 1024 of 64 / 128 / 256 21.9 / 19.0 / 25.9, 1856 40.2 / 33.3 / 30.9, 32768 636 / 537 / 458 (with float scales 520 to 541)
 template <bool FLOATS>
 int run_gated(hipStream_t st, const RowsQuant &a, const WeightQuant &w, int M, int N, int nk, const RowsQuant &q) {
   bf16 *none = nullptr;
