@@ -232,3 +232,17 @@ def test_weights_of_small_magnitudes(power, scale):
     each = got.repeat_interleave(BLOCK, 0).repeat_interleave(BLOCK, 1)[:, :200]
     step = torch.exp2(torch.floor(torch.log2((w.abs() / each).clamp(min=2.0 ** -6))) - 3) * each
     assert bool(((v - w).abs() <= step / 2 * (1 + 4 * U) + 2 * U * w.abs()).all())
+
+
+# ------------------------------------------------------------------------------------------------------------ one tensor for all
+@pytest.mark.parametrize("rows,dim", [(3, 200), (700, 1000), (2000, 1024), (40, 4096), (600, 8192), (2, 20000)])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_norm_rows_of_a_tensor_added_to_itself(rows, dim, dtype):
+    """x, the residual and the place of their sum are the same tensor."""
+    x = random_rows(rows, dim, rows + dim, dtype)
+    h = 2 * x.double()
+    eps = 2.0 ** -16
+    r, total = lib().norm_rows(x, None, eps, residual=x, out=x)
+    assert total is x and torch.equal(x.double(), h)   # (twice a value is exact)
+    y = h / torch.sqrt(h.square().mean(-1, keepdim=True) + eps)
+    check_rows(r, y, (dim + 60) * 2.0 ** -53 * y.abs() + 2.0 ** -149)
